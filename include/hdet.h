@@ -21,6 +21,10 @@
  *   hdet_converge_static   allocation-free variant of hdet_converge
  *   hdet_plan_tiles        host-only view of the work plan (tests, tools)
  *   hdet_selftest_bounded_wait   makes a kernel's bounded wait run out, to show the timeout status
+ * and where the replicas' models meet their vocabulary (no handle needed):
+ *   hdet_embed / hdet_embed_grad   embedding lookup with scaling, and the table's gradient
+ *   hdet_token_loss                softmax cross entropy against the table, one mean per replica (the losses that
+ *                                  hdet_step_device reads), with the gradients of hidden states and table
  *
  * Conventions
  *   - Every tensor pointer is a DEVICE pointer owned by the caller; it must stay
@@ -72,7 +76,8 @@ typedef enum {
 } hdet_status;
 
 enum { HDET_OPT_SGD = 0, HDET_OPT_ADAMW = 1 };
-enum { HDET_DTYPE_F32 = 0, HDET_DTYPE_BF16 = 1, HDET_DTYPE_F64 = 2 /* losses only */ };
+enum { HDET_DTYPE_F32 = 0, HDET_DTYPE_BF16 = 1, HDET_DTYPE_F64 = 2 /* losses only */,
+       HDET_DTYPE_I32 = 3, HDET_DTYPE_I64 = 4 /* tokens and targets only */ };
 enum { HDET_GRAD_AS_GIVEN = 0, HDET_GRAD_REPLICA_MEAN = 1 };
 enum { HDET_SCHED_CONSTANT = 0, HDET_SCHED_ONECYCLE_COS = 1, HDET_SCHED_ONECYCLE_LINEAR = 2 };
 
@@ -419,8 +424,69 @@ HDET_API int hdet_destroy(hdet_handle h);
 HDET_API int hdet_converge_static(const hdet_tensor* tensors, int64_t n_tensors, int32_t n_replicas,
                                   int32_t device, void* stream);
 
+/* ---------------------------------------------------------------------------------------------------------------
+ * The vocabulary ends of the replicas' models.  Algorithm 1 takes the losses L_r and the gradients g_r as given; for a
+ * decoder with a tied table both come from the table: rows of it go in, and the loss is taken against it.  These calls
+ * work on all N replicas at once, read the replicas' tables where the update left them (hdet_tensor.param with its
+ * param_stride, or the one averaged copy param_bf16 with stride 0), write the table's gradient where the update will
+ * read it (hdet_tensor.grad with its grad_stride) and the losses where hdet_step_device reads them.
+ * (Section 4.1's training setting; the paper leaves the model itself to its framework.)
+ *
+ * No handle is needed.  All pointers are DEVICE pointers on `device`; strides are in elements; with n_replicas == 1 the
+ * replica strides are not looked at.  The calls are asynchronous on `stream`, allocate nothing and copy nothing, so
+ * they can be captured into a graph.  A workspace belongs to the caller, must be 256-byte aligned, and holds nothing
+ * from one call to the next; calls that share one must be ordered on the device (this holds for two captured graphs
+ * that share one too).  Errors have their text in hdet_last_error(NULL).
+ *
+ * A token or target outside 0 .. vocab - 1 (any negative number, for instance) is PADDING: it has no row, no loss and
+ * no gradient, and what hidden states or row gradients hold at its place (NaN included) reaches no output.
+ */
+#define HDET_MAX_TOKENS (1 << 24) /* tokens per replica */
+#define HDET_MAX_VOCAB (1 << 24)
+#define HDET_MAX_WIDTH (1 << 16)
+
+typedef struct {
+  const void* tokens;    /* [N] x n_tokens, token_dtype                                                        */
+  void* rows;            /* [N] x n_tokens x width: written by hdet_embed, read by hdet_embed_grad             */
+  void* table;           /* [N] x vocab x width: read by hdet_embed, written by hdet_embed_grad                */
+  int64_t n_tokens;      /* tokens per replica, 0 .. HDET_MAX_TOKENS                                           */
+  int64_t vocab, width;  /* rows of the table and elements per row, >= 1                                       */
+  int64_t token_stride;  /* between replicas; 0 = one batch of tokens for all                                  */
+  int64_t rows_stride, rows_row;   /* between replicas and between consecutive tokens; hdet_embed_grad accepts
+                                      rows_stride 0 (one gradient for all replicas)                            */
+  int64_t table_stride, table_row; /* between replicas and between rows; hdet_embed accepts table_stride 0 (one
+                                      table for all replicas)                                                  */
+  double scale;
+  int32_t n_replicas;    /* 1 .. HDET_MAX_REPLICAS                                                             */
+  int32_t token_dtype;   /* HDET_DTYPE_I32 or HDET_DTYPE_I64                                                   */
+  int32_t rows_dtype, table_dtype; /* HDET_DTYPE_F32 or HDET_DTYPE_BF16 each                                   */
+  int32_t device;        /* CUDA device ordinal                                                                */
+  int32_t reserved;      /* set to 0                                                                           */
+} hdet_embedding;
+
+/*
+ * hdet_embed -- rows[r, t, :] = scale * table[r, tokens[r, t], :], computed in fp32 and rounded once; padding gives
+ * zeros.  `rows` must not overlap the table or the tokens.
+ * Errors: INVALID_ARG (NULL, sizes, strides or dtypes out of range), ALIGN (pointer not aligned to its element type), CUDA.
+ */
+HDET_API int hdet_embed(const hdet_embedding* d, void* stream);
+
+/*
+ * hdet_embed_grad -- the gradient of hdet_embed with respect to the table:
+ *   table[r, v, :] = (accumulate ? table[r, v, :] : 0) + scale * sum over t with tokens[r, t] = v of rows[r, t, :].
+ * With accumulate == 0 every row of the table is written (zeros where no token points); with accumulate != 0 rows
+ * without a token are neither read nor written, so that the gradient joins the one hdet_token_loss left there.
+ * The tokens are sorted (stably) and every row is summed in the order of t in fp32 by one owner and rounded once: no
+ * atomics, the same bits on every run.
+ * hdet_embed_grad_workspace gives the bytes that the call needs; it looks at sizes, strides and dtypes alone.
+ * Errors: as hdet_embed, plus INVALID_ARG (workspace NULL or too small) and ALIGN (workspace).
+ */
+HDET_API int hdet_embed_grad_workspace(const hdet_embedding* d, int64_t* bytes);
+HDET_API int hdet_embed_grad(const hdet_embedding* d, int32_t accumulate, void* workspace, int64_t workspace_bytes,
+                             void* stream);
+
 /* hdet_last_error -- text of the last failure on h (when h is NULL: of the last failed call
- * that has no handle, hdet_create or hdet_converge_static, on this thread).  The pointer stays valid until the next call on that handle. */
+ * that has no handle, hdet_create, hdet_converge_static or a call of the vocabulary ends, on this thread).  The pointer stays valid until the next call on that handle. */
 HDET_API const char* hdet_last_error(hdet_handle h);
 
 /*

@@ -22,7 +22,7 @@ HDET_ERR_NONFINITE = 6
 HDET_ERR_TIMEOUT = 7
 
 HDET_OPT_SGD, HDET_OPT_ADAMW = 0, 1
-HDET_DTYPE_F32, HDET_DTYPE_BF16, HDET_DTYPE_F64 = 0, 1, 2
+HDET_DTYPE_F32, HDET_DTYPE_BF16, HDET_DTYPE_F64, HDET_DTYPE_I32, HDET_DTYPE_I64 = 0, 1, 2, 3, 4
 HDET_GRAD_AS_GIVEN, HDET_GRAD_REPLICA_MEAN = 0, 1
 HDET_SCHED_CONSTANT, HDET_SCHED_ONECYCLE_COS, HDET_SCHED_ONECYCLE_LINEAR = 0, 1, 2
 
@@ -62,6 +62,16 @@ class hdet_schedule(C.Structure):
         ("pct_start", C.c_double), ("div_factor", C.c_double), ("final_div_factor", C.c_double),
         ("warmup_steps", C.c_int64), ("beta", C.c_double), ("sigma", C.c_double), ("lambda_", C.c_double),
         ("f_div", C.c_double), ("f_final", C.c_double), ("auto_wd", C.c_int32), ("reserved", C.c_int32),
+    ]
+
+
+class hdet_embedding(C.Structure):
+    _fields_ = [
+        ("tokens", C.c_void_p), ("rows", C.c_void_p), ("table", C.c_void_p),
+        ("n_tokens", C.c_int64), ("vocab", C.c_int64), ("width", C.c_int64), ("token_stride", C.c_int64),
+        ("rows_stride", C.c_int64), ("rows_row", C.c_int64), ("table_stride", C.c_int64), ("table_row", C.c_int64),
+        ("scale", C.c_double), ("n_replicas", C.c_int32), ("token_dtype", C.c_int32), ("rows_dtype", C.c_int32),
+        ("table_dtype", C.c_int32), ("device", C.c_int32), ("reserved", C.c_int32),
     ]
 
 
@@ -124,6 +134,12 @@ def _load() -> C.CDLL:
     lib.hdet_plan_tiles.restype = C.c_int
     lib.hdet_selftest_bounded_wait.argtypes = [H, C.c_void_p]
     lib.hdet_selftest_bounded_wait.restype = C.c_int
+    lib.hdet_embed.argtypes = [C.POINTER(hdet_embedding), C.c_void_p]
+    lib.hdet_embed.restype = C.c_int
+    lib.hdet_embed_grad_workspace.argtypes = [C.POINTER(hdet_embedding), C.POINTER(C.c_int64)]
+    lib.hdet_embed_grad_workspace.restype = C.c_int
+    lib.hdet_embed_grad.argtypes = [C.POINTER(hdet_embedding), C.c_int32, C.c_void_p, C.c_int64, C.c_void_p]
+    lib.hdet_embed_grad.restype = C.c_int
     for f in ("hdet_create", "hdet_set_schedule", "hdet_step", "hdet_converge", "hdet_autolr_update",
               "hdet_get_state", "hdet_set_state", "hdet_destroy"):
         getattr(lib, f).restype = C.c_int
@@ -300,6 +316,92 @@ def hdet_converge_static(tensors: Sequence[hdet_tensor], n_replicas: int, device
     """
     arr = (hdet_tensor * len(tensors))(*tensors) if tensors else None
     _check(_lib.hdet_converge_static(arr, len(tensors), n_replicas, device, C.c_void_p(stream)), None)
+
+
+HDET_MAX_TOKENS = 1 << 24
+HDET_MAX_VOCAB = 1 << 24
+HDET_MAX_WIDTH = 1 << 16
+_dtype_codes = {}
+
+
+def _code(tensor) -> int:
+    """HDET_DTYPE_* of a torch tensor."""
+    if not _dtype_codes:
+        import torch
+        _dtype_codes.update({torch.float32: HDET_DTYPE_F32, torch.bfloat16: HDET_DTYPE_BF16, torch.float64: HDET_DTYPE_F64,
+                             torch.int32: HDET_DTYPE_I32, torch.int64: HDET_DTYPE_I64})
+    code = _dtype_codes.get(tensor.dtype)
+    if code is None:
+        raise ValueError(f"dtype {tensor.dtype} is not supported")
+    return code
+
+
+def _one_device(*tensors) -> int:
+    """Ordinal of the CUDA device that all tensors are on."""
+    device = tensors[0].device
+    for t in tensors:
+        if not t.is_cuda or t.device != device:
+            raise ValueError("all tensors must be on one CUDA device")
+    return device.index
+
+
+def _replica_stride(tensor, dims: int, n: int, what: str) -> int:
+    """Replica stride of [N, ...] (``dims`` + 1 axes), 0 for one copy without that axis; the last axis must be contiguous."""
+    shape, stride = tensor.shape, tensor.stride()
+    if shape[-1] > 1 and stride[-1] != 1:
+        raise ValueError(f"{what}: the last axis must be contiguous")
+    if len(shape) == dims:
+        return 0
+    if len(shape) != dims + 1 or shape[0] != n:
+        raise ValueError(f"{what}: expected {dims} axes, or {dims + 1} with {n} replicas first")
+    return stride[0]
+
+
+def _row_stride(tensor, width: int) -> int:
+    return tensor.stride(-2) if tensor.shape[-2] > 1 else width
+
+
+def _embedding(tokens, rows, table, n: int, scale: float) -> hdet_embedding:
+    T, D, V = rows.shape[-2], rows.shape[-1], table.shape[-2]
+    if tokens.shape[-1] != T or table.shape[-1] != D:
+        raise ValueError("tokens, rows and table disagree on the number of tokens or the width")
+    return hdet_embedding(
+        tokens.data_ptr(), rows.data_ptr(), table.data_ptr(), T, V, D, _replica_stride(tokens, 1, n, "tokens"),
+        _replica_stride(rows, 2, n, "rows"), _row_stride(rows, D), _replica_stride(table, 2, n, "table"),
+        _row_stride(table, D), scale, n, _code(tokens), _code(rows), _code(table), _one_device(tokens, rows, table), 0)
+
+
+def hdet_embed(tokens, table, out, scale: float = 1.0, stream: int = 0) -> None:
+    """out[r, t] = scale * table[r, tokens[r, t]] for CUDA tensors tokens [N, T] or [T] (int32 or int64), table [N, V, D] or
+    [V, D] (one for all replicas) and out [N, T, D], float32 or bfloat16 each.  Tokens outside 0 .. V-1 give zeros."""
+    if out.dim() != 3:
+        raise ValueError("out must be [N, T, D]")
+    d = _embedding(tokens, out, table, out.shape[0], scale)
+    _check(_lib.hdet_embed(C.byref(d), stream), None)
+
+
+def hdet_embed_grad_workspace(tokens, d_out, d_table) -> int:
+    """Bytes of workspace that hdet_embed_grad needs for these tensors."""
+    d = _embedding(tokens, d_out, d_table, d_table.shape[0], 1.0)
+    need = C.c_int64(0)
+    _check(_lib.hdet_embed_grad_workspace(C.byref(d), C.byref(need)), None)
+    return int(need.value)
+
+
+def hdet_embed_grad(tokens, d_out, d_table, workspace, scale: float = 1.0, accumulate: bool = False, stream: int = 0) -> None:
+    """Gradient of hdet_embed: d_table [N, V, D] (+)= scale * the sums of d_out's rows ([N, T, D], or [T, D] for all replicas)
+    by token.  ``workspace`` is a contiguous CUDA tensor of at least hdet_embed_grad_workspace bytes."""
+    if d_table.dim() != 3:
+        raise ValueError("d_table must be [N, V, D]")
+    d = _embedding(tokens, d_out, d_table, d_table.shape[0], scale)
+    ptr, size = _workspace(workspace, d.device)
+    _check(_lib.hdet_embed_grad(C.byref(d), 1 if accumulate else 0, ptr, size, stream), None)
+
+
+def _workspace(workspace, device: int):
+    if not workspace.is_cuda or workspace.device.index != device or not workspace.is_contiguous():
+        raise ValueError("the workspace must be a contiguous tensor on the inputs' CUDA device")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 def hdet_autolr_update(h, round_losses: Optional[Sequence[float]] = None, stream: int = 0) -> None:

@@ -1,0 +1,554 @@
+// Embedding lookup with scaling, and its gradient by sorted tokens (contract: include/hdet.h).
+//
+//   lookup    rows[r,t,:] = scale * table[r, tok[r,t], :]
+//   gradient  table[r,v,:] (+)= scale * sum over t with tok[r,t] = v of rows[r,t,:]
+//
+// Both are bound by HBM.  The gradient is a sum over tokens that share a row.  Atomics would add them in an order
+// that changes from run to run, so the tokens are sorted first (stable: equal tokens stay in the order of t) and every
+// row is summed in that order in fp32 by one owner, then rounded once.
+#include <cuda_bf16.h>
+
+#include <cstdio>
+
+#include "hdet_internal.h"
+#include "../../include/hdet.h"
+
+namespace {
+
+constexpr int kChunkSmall = 1024;   // tokens ranked against one another at once when there are many
+constexpr int kChunkLarge = 2048;   // ... when all of them fit: one launch less, twice the comparisons per token
+constexpr int kMergeRuns = 16;      // sorted runs merged per level
+constexpr int kEntries = 32;        // sorted entries per warp in the gradient kernel: one per lane
+
+__host__ __device__ constexpr int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Token t of replica r as a row index; anything outside 0 .. vocab-1 becomes vocab, "no row".
+__device__ __forceinline__ int row_of(const void* tokens, bool wide, int64_t at, int vocab) {
+  if (wide) {
+    const long long v = static_cast<const long long*>(tokens)[at];
+    return v >= 0 && v < vocab ? (int)v : vocab;
+  }
+  const int v = static_cast<const int*>(tokens)[at];
+  return v >= 0 && v < vocab ? v : vocab;
+}
+
+// VEC consecutive elements of type T, moved in accesses of at most 16 bytes; VEC * sizeof(T) bytes aligned (16 at most).
+template <typename T, int VEC>
+struct Pack {
+  static constexpr int kBytes = VEC * (int)sizeof(T);
+  static constexpr int kAlign = kBytes < 16 ? kBytes : 16;
+  struct alignas(kAlign) Raw { T v[VEC]; };
+  Raw raw;
+  __device__ __forceinline__ void load(const T* p) { raw = *reinterpret_cast<const Raw*>(p); }
+  __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<Raw*>(p) = raw; }
+  __device__ __forceinline__ float get(int i) const {
+    if constexpr (sizeof(T) == 4) return raw.v[i]; else return __bfloat162float(raw.v[i]);
+  }
+  __device__ __forceinline__ void set(int i, float x) {
+    if constexpr (sizeof(T) == 4) raw.v[i] = x; else raw.v[i] = __float2bfloat16_rn(x);
+  }
+};
+
+struct EmbedParams {
+  const void* tokens;
+  void* rows;
+  void* table;
+  int64_t token_stride, rows_stride, rows_row, table_stride, table_row;
+  int64_t n_tokens, width;
+  int vocab, n_replicas;
+  bool wide;
+  float scale;
+};
+
+// ------------------------------------------------------------------------------------------------ lookup
+// A block covers blockDim.y rows times kRowsPerThread, and blockDim.x vectors of each; every thread reads its
+// kRowsPerThread token ids, then has that many independent row loads in flight.
+constexpr int kRowsPerThread = 4;
+
+template <typename TableT, typename RowT, int VEC>
+__global__ void __launch_bounds__(256) lookup_kernel(const EmbedParams p) {
+  const int64_t base = (int64_t)blockIdx.x * (blockDim.y * kRowsPerThread) + threadIdx.y;
+  const int r = blockIdx.y;
+  const TableT* table = static_cast<const TableT*>(p.table) + r * p.table_stride;
+  RowT* rows = static_cast<RowT*>(p.rows) + r * p.rows_stride;
+  int id[kRowsPerThread];
+#pragma unroll
+  for (int k = 0; k < kRowsPerThread; ++k) {
+    const int64_t t = base + (int64_t)k * blockDim.y;
+    id[k] = t < p.n_tokens ? row_of(p.tokens, p.wide, r * p.token_stride + t, p.vocab) : -1;
+  }
+  for (int64_t c = (int64_t)threadIdx.x * VEC; c < p.width; c += (int64_t)blockDim.x * VEC) {
+    Pack<TableT, VEC> x[kRowsPerThread];
+#pragma unroll
+    for (int k = 0; k < kRowsPerThread; ++k)
+      if (id[k] >= 0 && id[k] < p.vocab) x[k].load(table + id[k] * p.table_row + c);
+#pragma unroll
+    for (int k = 0; k < kRowsPerThread; ++k) {
+      if (id[k] < 0) continue;
+      const bool some = id[k] < p.vocab;
+      Pack<RowT, VEC> y;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) y.set(i, some ? x[k].get(i) * p.scale : 0.0f);
+      y.store(rows + (base + (int64_t)k * blockDim.y) * p.rows_row + c);
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ sorting
+// Rank of every token among its chunk's by comparing it with all of them: no passes, no atomics, one launch.  With
+// 1024 tokens a chunk that is 2 instructions x 1024 per token, spread over chunk / 256 blocks a chunk.
+// Equal tokens keep their order: tokens before this one count when <=, tokens behind it when <.
+__global__ void __launch_bounds__(256) rank_chunks_kernel(const EmbedParams p, int chunk, int* __restrict__ key_out,
+                                                          int* __restrict__ pos_out) {
+  extern __shared__ int4 s_tok4[];
+  int* s_tok = reinterpret_cast<int*>(s_tok4);
+  const int r = blockIdx.y;
+  const int parts = chunk / 256;
+  const int64_t c0 = (int64_t)(blockIdx.x / parts) * chunk;
+  const int n = (int)(p.n_tokens - c0 < chunk ? p.n_tokens - c0 : chunk);
+  const int mine = (blockIdx.x % parts) * 256 + threadIdx.x;
+  if ((int)(blockIdx.x % parts) * 256 >= n) return;
+  const int n4 = (n + 3) & ~3;
+  // entries behind the end compare as larger than every row and than "no row"
+  for (int i = threadIdx.x; i < n4; i += 256)
+    s_tok[i] = i < n ? row_of(p.tokens, p.wide, r * p.token_stride + c0 + i, p.vocab) : 0x7fffffff;
+  __syncthreads();
+  if (mine >= n) return;
+  const int key = s_tok[mine];
+  const int warp0 = mine & ~31;                 // the warp's own 32 tokens are compared one by one
+  const int warp1 = warp0 + 32 < n4 ? warp0 + 32 : n4;
+  int rank = 0;
+#pragma unroll 4
+  for (int j = 0; j < warp0 / 4; ++j) {
+    const int4 o = s_tok4[j];
+    rank += (o.x <= key) + (o.y <= key) + (o.z <= key) + (o.w <= key);
+  }
+  for (int j = warp0; j < warp1; ++j) rank += j < mine ? s_tok[j] <= key : s_tok[j] < key;
+#pragma unroll 4
+  for (int j = warp1 / 4; j < n4 / 4; ++j) {
+    const int4 o = s_tok4[j];
+    rank += (o.x < key) + (o.y < key) + (o.z < key) + (o.w < key);
+  }
+  const int64_t at = r * p.n_tokens + c0 + rank;
+  key_out[at] = key;
+  pos_out[at] = (int)(c0 + mine);
+}
+
+// Entries of run[0 .. n) that come before `key`: those < key, or <= key.
+__device__ __forceinline__ int64_t count_before(const int* __restrict__ run, int64_t n, int key, bool or_equal) {
+  int64_t lo = 0, hi = n;
+  while (lo < hi) {
+    const int64_t mid = (lo + hi) >> 1;
+    const int o = run[mid];
+    if (o < key || (or_equal && o == key)) lo = mid + 1; else hi = mid;
+  }
+  return lo;
+}
+
+// Merges groups of kMergeRuns sorted runs of `run` entries: an entry's place in its group is its place in its own run
+// plus, for every other run, the entries there that come before it.
+__global__ void __launch_bounds__(256) merge_runs_kernel(int64_t n, int64_t run, const int* __restrict__ key_in,
+                                                         const int* __restrict__ pos_in, int* __restrict__ key_out,
+                                                         int* __restrict__ pos_out) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  const int64_t base = (int64_t)blockIdx.y * n;
+  const int* keys = key_in + base;
+  const int key = keys[i];
+  const int64_t own = i / run, first = own / kMergeRuns * kMergeRuns;
+  int64_t at = first * run + (i - own * run);
+  for (int64_t q = first; q < first + kMergeRuns && q * run < n; ++q) {
+    if (q == own) continue;
+    const int64_t len = n - q * run < run ? n - q * run : run;
+    at += count_before(keys + q * run, len, key, q < own);
+  }
+  key_out[base + at] = key;
+  pos_out[base + at] = pos_in[base + i];
+}
+
+// ------------------------------------------------------------------------------------------------ gradient
+struct GradParams {
+  EmbedParams e;
+  const int* keys;       // [replicas or 1][n_tokens], sorted; vocab = no row
+  const int* pos;        // the token behind each key
+  int64_t sorted_stride; // n_tokens, or 0 when all replicas share one batch of tokens
+  float* partial;        // [replicas][blocks][2][width]
+  int64_t n_blocks;      // entry blocks per replica
+  int64_t n_col;         // column chunks of 32 * VEC
+  int64_t grad_units;    // n_blocks * n_col
+  int64_t zero_units;    // 32-row groups of the table to look at for rows without a token (0 when accumulating)
+  bool accumulate;
+};
+
+template <typename TableT, int VEC>
+__device__ __forceinline__ void write_row(const GradParams& p, int r, int key, int64_t c, const float (&acc)[VEC]) {
+  TableT* to = static_cast<TableT*>(p.e.table) + r * p.e.table_stride + key * p.e.table_row + c;
+  Pack<TableT, VEC> y;
+  if (p.accumulate) {
+    y.load(to);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) y.set(i, fmaf(acc[i], p.e.scale, y.get(i)));
+  } else {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) y.set(i, acc[i] * p.e.scale);
+  }
+  y.store(to);
+}
+
+// One warp: 32 consecutive sorted entries (one per lane) and 32 * VEC columns.  A run of equal keys that lies inside
+// the 32 entries is finished here; the piece of a run that came from the block before goes to partial slot 0, the piece
+// of a run that starts here and goes on into the next block to slot 1, and join_kernel adds those in order.
+// Warps behind those write zeros to the table rows that have no token.
+template <typename RowT, typename TableT, int VEC>
+__global__ void __launch_bounds__(256) grad_kernel(const GradParams p) {
+  const int r = blockIdx.y, lane = threadIdx.x & 31;
+  const int64_t unit = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int64_t n = p.e.n_tokens;
+  const int* keys = p.keys + r * p.sorted_stride;
+  if (unit >= p.grad_units) {
+    const int64_t row0 = (unit - p.grad_units) * 32;
+    if (unit - p.grad_units >= p.zero_units) return;
+    bool empty = false;
+    if (row0 + lane < p.e.vocab) {
+      const int64_t at = count_before(keys, n, (int)(row0 + lane), false);
+      empty = at >= n || keys[at] != row0 + lane;
+    }
+    unsigned todo = __ballot_sync(0xffffffffu, empty);
+    Pack<TableT, VEC> zero;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) zero.set(i, 0.0f);
+    TableT* table = static_cast<TableT*>(p.e.table) + r * p.e.table_stride;
+    for (; todo; todo &= todo - 1) {
+      TableT* row = table + (row0 + __ffs(todo) - 1) * p.e.table_row;
+      for (int64_t c = (int64_t)lane * VEC; c < p.e.width; c += 32 * VEC) zero.store(row + c);
+    }
+    return;
+  }
+  const int64_t block = unit / p.n_col;
+  const int64_t c = (unit % p.n_col) * (32 * VEC) + (int64_t)lane * VEC;
+  const bool on = c < p.e.width;
+  const int64_t i0 = block * kEntries;
+  const int* pos = p.pos + r * p.sorted_stride;
+  const int my_key = i0 + lane < n ? keys[i0 + lane] : p.e.vocab;
+  const int my_pos = i0 + lane < n ? pos[i0 + lane] : 0;
+  const int before = i0 > 0 ? keys[i0 - 1] : -1;
+  const int after = i0 + kEntries < n ? keys[i0 + kEntries] : p.e.vocab;
+  const int count = __popc(__ballot_sync(0xffffffffu, my_key < p.e.vocab));   // sorted: the entries with a row come first
+  const RowT* rows = static_cast<const RowT*>(p.e.rows) + r * p.e.rows_stride;
+  float* partial = p.partial + ((int64_t)r * p.n_blocks + block) * 2 * p.e.width;
+  float acc[VEC];
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) acc[i] = 0.0f;
+  bool from_before = false;
+  constexpr int kAhead = 8;
+  for (int e0 = 0; e0 < count; e0 += kAhead) {
+    Pack<RowT, VEC> x[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int ps = __shfl_sync(0xffffffffu, my_pos, (e0 + k) & 31);
+      if (e0 + k < count && on) x[k].load(rows + ps * p.e.rows_row + c);
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int e = e0 + k;
+      if (e >= count) break;
+      const int key = __shfl_sync(0xffffffffu, my_key, e);
+      const int next = e + 1 < kEntries ? __shfl_sync(0xffffffffu, my_key, (e + 1) & 31) : after;
+      if (e == 0) from_before = key == before;
+      if (on) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) acc[i] += x[k].get(i);
+      }
+      if (next == key && e + 1 < kEntries) continue;
+      // the run's piece in this block ends here
+      const bool goes_on = e + 1 == kEntries && next == key;
+      if (on) {
+        if (from_before || goes_on) {
+          float* to = partial + (from_before ? 0 : p.e.width) + c;
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) to[i] = acc[i];
+        } else {
+          write_row<TableT, VEC>(p, r, key, c, acc);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) acc[i] = 0.0f;
+      from_before = false;
+    }
+  }
+}
+
+// One block per entry block and column chunk in which a run starts that goes on behind it: its pieces are added in
+// order.  The eight warps take consecutive stretches of a long run and their sums are added in order too, so the result
+// does not depend on timing.
+template <typename TableT, int VEC>
+__global__ void __launch_bounds__(256) join_kernel(const GradParams p) {
+  __shared__ float s_sum[8][32 * VEC];
+  const int r = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t block = blockIdx.x / p.n_col;
+  const int64_t c = (blockIdx.x % p.n_col) * (32 * VEC) + (int64_t)lane * VEC;
+  const int64_t n = p.e.n_tokens, last = block * kEntries + kEntries - 1;
+  const int* keys = p.keys + r * p.sorted_stride;
+  if (last + 1 >= n) return;
+  const int key = keys[last];
+  if (key >= p.e.vocab || keys[last + 1] != key) return;
+  const int64_t i0 = block * kEntries;
+  if (keys[i0] == key && i0 > 0 && keys[i0 - 1] == key) return;       // the run started in an earlier block
+  const int64_t end = last + 1 + count_before(keys + last + 1, n - last - 1, key, true);   // behind the run's last entry
+  const int64_t n_more = (end - 1) / kEntries - block;                // blocks that the run goes on into
+  const float* base = p.partial + ((int64_t)r * p.n_blocks + block) * 2 * p.e.width;
+  const bool on = c < p.e.width;
+  float acc[VEC];
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) acc[i] = 0.0f;
+  // piece 0 is slot 1 of this block, piece j > 0 slot 0 of block + j
+  const int64_t pieces = n_more + 1, each = div_up(pieces, 8);
+  const int64_t from = warp * each, to = from + each < pieces ? from + each : pieces;
+  if (on) {
+#pragma unroll 4
+    for (int64_t j = from; j < to; ++j) {
+      const float* x = base + (j == 0 ? p.e.width : j * 2 * p.e.width) + c;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) acc[i] += x[i];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) s_sum[warp][i * 32 + lane] = acc[i];
+  __syncthreads();
+  if (warp != 0 || !on) return;
+  for (int w = 1; w < 8; ++w)
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) acc[i] += s_sum[w][i * 32 + lane];
+  write_row<TableT, VEC>(p, r, key, c, acc);
+}
+
+// ------------------------------------------------------------------------------------------------ host side
+int fail(int code, const char* who, const char* what) {
+  char msg[240];
+  snprintf(msg, sizeof msg, "%s: %s", who, what);
+  hdet::set_handleless_error(msg);
+  return code;
+}
+
+int elem_size(int dtype) { return dtype == HDET_DTYPE_BF16 ? 2 : 4; }
+
+// Checks shared by the three entry points.
+int check(const char* who, const hdet_embedding* d) {
+  if (!d) return fail(HDET_ERR_INVALID_ARG, who, "the descriptor is NULL");
+  if (d->n_replicas < 1 || d->n_replicas > HDET_MAX_REPLICAS)
+    return fail(HDET_ERR_INVALID_ARG, who, "n_replicas must be in 1..32");
+  if (d->n_tokens < 0 || d->n_tokens > HDET_MAX_TOKENS || d->vocab < 1 || d->vocab > HDET_MAX_VOCAB || d->width < 1 ||
+      d->width > HDET_MAX_WIDTH)
+    return fail(HDET_ERR_INVALID_ARG, who, "n_tokens, vocab or width out of range");
+  if (d->token_dtype != HDET_DTYPE_I32 && d->token_dtype != HDET_DTYPE_I64)
+    return fail(HDET_ERR_INVALID_ARG, who, "token_dtype must be HDET_DTYPE_I32 or HDET_DTYPE_I64");
+  if ((d->table_dtype != HDET_DTYPE_F32 && d->table_dtype != HDET_DTYPE_BF16) ||
+      (d->rows_dtype != HDET_DTYPE_F32 && d->rows_dtype != HDET_DTYPE_BF16))
+    return fail(HDET_ERR_INVALID_ARG, who, "table_dtype and rows_dtype must be HDET_DTYPE_F32 or HDET_DTYPE_BF16");
+  if (d->device < 0) return fail(HDET_ERR_INVALID_ARG, who, "device must be >= 0");
+  if (!(d->scale == d->scale) || d->scale - d->scale != 0.0) return fail(HDET_ERR_INVALID_ARG, who, "scale must be finite");
+  if (d->table_row < d->width || d->rows_row < d->width)
+    return fail(HDET_ERR_INVALID_ARG, who, "a row stride is smaller than width");
+  return HDET_OK;
+}
+
+// Checks of the pointers, and of strides that the call will write through.
+int check_pointers(const char* who, const hdet_embedding* d, bool writes_table) {
+  if (!d->table || (d->n_tokens > 0 && (!d->tokens || !d->rows)))
+    return fail(HDET_ERR_INVALID_ARG, who, "a pointer is NULL");
+  const int64_t table_len = (d->vocab - 1) * d->table_row + d->width;
+  const int64_t rows_len = d->n_tokens > 0 ? (d->n_tokens - 1) * d->rows_row + d->width : 0;
+  if (d->table_stride < 0 || d->rows_stride < 0 || d->token_stride < 0)
+    return fail(HDET_ERR_INVALID_ARG, who, "negative stride");
+  if (d->n_replicas > 1) {
+    if (d->table_stride < table_len && (writes_table || d->table_stride != 0))
+      return fail(HDET_ERR_INVALID_ARG, who, "table_stride is smaller than one table");
+    if (d->rows_stride < rows_len && (!writes_table || d->rows_stride != 0))
+      return fail(HDET_ERR_INVALID_ARG, who, "rows_stride is smaller than one replica's rows");
+    if (d->token_stride < d->n_tokens && d->token_stride != 0)
+      return fail(HDET_ERR_INVALID_ARG, who, "token_stride is smaller than n_tokens");
+  }
+  const uintptr_t a = reinterpret_cast<uintptr_t>(d->tokens) % (d->token_dtype == HDET_DTYPE_I64 ? 8 : 4);
+  const uintptr_t b = reinterpret_cast<uintptr_t>(d->table) % elem_size(d->table_dtype);
+  const uintptr_t c = reinterpret_cast<uintptr_t>(d->rows) % elem_size(d->rows_dtype);
+  if (a || b || c) return fail(HDET_ERR_ALIGN, who, "a pointer is not aligned to its element type");
+  return HDET_OK;
+}
+
+EmbedParams params_of(const hdet_embedding* d) {
+  EmbedParams p{};
+  p.tokens = d->tokens; p.rows = d->rows; p.table = d->table;
+  const bool many = d->n_replicas > 1;
+  p.token_stride = many ? d->token_stride : 0;
+  p.rows_stride = many ? d->rows_stride : 0;
+  p.table_stride = many ? d->table_stride : 0;
+  p.rows_row = d->rows_row; p.table_row = d->table_row;
+  p.n_tokens = d->n_tokens; p.width = d->width; p.vocab = (int)d->vocab; p.n_replicas = d->n_replicas;
+  p.wide = d->token_dtype == HDET_DTYPE_I64;
+  p.scale = (float)d->scale;
+  return p;
+}
+
+// Elements per access: the largest of 8, 4, 2, 1 that divides the width and every stride and keeps each access inside
+// one aligned 16-byte unit (or whole units) on both sides.
+int vector_of(const hdet_embedding* d) {
+  const bool many = d->n_replicas > 1;
+  for (int v = 8; v > 1; v /= 2) {
+    if (d->width % v || d->rows_row % v || d->table_row % v) continue;
+    if (many && (d->rows_stride % v || d->table_stride % v)) continue;
+    const int rb = v * elem_size(d->rows_dtype), tb = v * elem_size(d->table_dtype);
+    if (reinterpret_cast<uintptr_t>(d->rows) % (rb < 16 ? rb : 16)) continue;
+    if (reinterpret_cast<uintptr_t>(d->table) % (tb < 16 ? tb : 16)) continue;
+    return v;
+  }
+  return 1;
+}
+
+// Sets the descriptor's device for the scope of one call and restores the caller's.
+struct DeviceScope {
+  int prev = -1;
+  bool switched = false;
+  cudaError_t err = cudaSuccess;
+  explicit DeviceScope(int dev) {
+    err = cudaGetDevice(&prev);
+    if (err == cudaSuccess && prev != dev) {
+      err = cudaSetDevice(dev);
+      switched = err == cudaSuccess;
+    }
+  }
+  ~DeviceScope() { if (switched) cudaSetDevice(prev); }
+};
+
+int fail_cuda(const char* who, cudaError_t e) { return fail(HDET_ERR_CUDA, who, cudaGetErrorString(e)); }
+
+template <typename TableT, typename RowT, int VEC>
+void launch_lookup(const EmbedParams& p, cudaStream_t st) {
+  int x = 1;
+  while (x < 256 && (int64_t)x * VEC < p.width) x *= 2;
+  const dim3 block(x, 256 / x);
+  const dim3 grid((unsigned)div_up(p.n_tokens, (int64_t)block.y * kRowsPerThread), p.n_replicas);
+  lookup_kernel<TableT, RowT, VEC><<<grid, block, 0, st>>>(p);
+}
+
+template <typename RowT, typename TableT, int VEC>
+void launch_grad(GradParams p, cudaStream_t st) {
+  p.n_blocks = div_up(p.e.n_tokens, kEntries);
+  p.n_col = div_up(p.e.width, 32 * VEC);
+  p.grad_units = p.n_blocks * p.n_col;
+  p.zero_units = p.accumulate ? 0 : div_up(p.e.vocab, 32);
+  const int64_t units = p.grad_units + p.zero_units;
+  if (units > 0) grad_kernel<RowT, TableT, VEC><<<dim3((unsigned)div_up(units, 8), p.e.n_replicas), 256, 0, st>>>(p);
+  if (p.n_blocks > 1)
+    join_kernel<TableT, VEC><<<dim3((unsigned)((p.n_blocks - 1) * p.n_col), p.e.n_replicas), 256, 0, st>>>(p);
+}
+
+// Calls f.template operator()<A, B, VEC>() for the element types and the vector width.
+template <typename A, typename B, typename F>
+void with_vector(int vec, F&& f) {
+  if (vec == 8) f.template operator()<A, B, 8>();
+  else if (vec == 4) f.template operator()<A, B, 4>();
+  else if (vec == 2) f.template operator()<A, B, 2>();
+  else f.template operator()<A, B, 1>();
+}
+
+template <typename F>
+void with_types(int a, int b, int vec, F&& f) {
+  if (a == HDET_DTYPE_F32 && b == HDET_DTYPE_F32) with_vector<float, float>(vec, f);
+  else if (a == HDET_DTYPE_F32) with_vector<float, __nv_bfloat16>(vec, f);
+  else if (b == HDET_DTYPE_F32) with_vector<__nv_bfloat16, float>(vec, f);
+  else with_vector<__nv_bfloat16, __nv_bfloat16>(vec, f);
+}
+
+struct LookupLauncher {
+  const EmbedParams& p;
+  cudaStream_t st;
+  template <typename TableT, typename RowT, int VEC> void operator()() { launch_lookup<TableT, RowT, VEC>(p, st); }
+};
+
+struct GradLauncher {
+  const GradParams& p;
+  cudaStream_t st;
+  template <typename RowT, typename TableT, int VEC> void operator()() { launch_grad<RowT, TableT, VEC>(p, st); }
+};
+
+// Workspace of the gradient: two copies of the sorted keys and positions, then the partial sums.
+struct GradLayout {
+  int64_t list_bytes;     // one array of one entry per sorted token
+  int64_t partial_off, total;
+  int sorted_replicas;
+};
+
+GradLayout layout_of(const hdet_embedding* d) {
+  GradLayout l{};
+  const auto up = [](int64_t x) { return div_up(x, 256) * 256; };
+  l.sorted_replicas = d->n_replicas > 1 && d->token_stride != 0 ? d->n_replicas : 1;
+  l.list_bytes = up(4 * d->n_tokens * l.sorted_replicas);
+  l.partial_off = 4 * l.list_bytes;
+  l.total = l.partial_off + up(4 * 2 * d->width * div_up(d->n_tokens, kEntries) * d->n_replicas);
+  if (l.total < 256) l.total = 256;
+  return l;
+}
+
+}  // namespace
+
+extern "C" HDET_API int hdet_embed(const hdet_embedding* d, void* stream) {
+  hdet::TraceRange trace("hdet_embed");
+  if (const int rc = check("hdet_embed", d)) return rc;
+  if (const int rc = check_pointers("hdet_embed", d, false)) return rc;
+  if (d->n_tokens == 0) return HDET_OK;
+  DeviceScope scope(d->device);
+  if (scope.err != cudaSuccess) return fail_cuda("hdet_embed", scope.err);
+  const EmbedParams p = params_of(d);
+  with_types(d->table_dtype, d->rows_dtype, vector_of(d), LookupLauncher{p, static_cast<cudaStream_t>(stream)});
+  const cudaError_t e = cudaGetLastError();
+  return e == cudaSuccess ? HDET_OK : fail_cuda("hdet_embed", e);
+}
+
+extern "C" HDET_API int hdet_embed_grad_workspace(const hdet_embedding* d, int64_t* bytes) {
+  if (!bytes) return fail(HDET_ERR_INVALID_ARG, "hdet_embed_grad_workspace", "bytes is NULL");
+  *bytes = 0;
+  if (const int rc = check("hdet_embed_grad_workspace", d)) return rc;
+  *bytes = layout_of(d).total;
+  return HDET_OK;
+}
+
+extern "C" HDET_API int hdet_embed_grad(const hdet_embedding* d, int32_t accumulate, void* workspace,
+                                        int64_t workspace_bytes, void* stream) {
+  hdet::TraceRange trace("hdet_embed_grad");
+  if (const int rc = check("hdet_embed_grad", d)) return rc;
+  if (const int rc = check_pointers("hdet_embed_grad", d, true)) return rc;
+  const GradLayout l = layout_of(d);
+  if (!workspace || workspace_bytes < l.total)
+    return fail(HDET_ERR_INVALID_ARG, "hdet_embed_grad", "the workspace is NULL or smaller than hdet_embed_grad_workspace says");
+  if (reinterpret_cast<uintptr_t>(workspace) % 256)
+    return fail(HDET_ERR_ALIGN, "hdet_embed_grad", "the workspace is not 256-byte aligned");
+  DeviceScope scope(d->device);
+  if (scope.err != cudaSuccess) return fail_cuda("hdet_embed_grad", scope.err);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  char* ws = static_cast<char*>(workspace);
+  int *key[2], *pos[2];
+  for (int k = 0; k < 2; ++k) {
+    key[k] = reinterpret_cast<int*>(ws + k * l.list_bytes);
+    pos[k] = reinterpret_cast<int*>(ws + (2 + k) * l.list_bytes);
+  }
+  const EmbedParams e = params_of(d);
+  int now = 0;
+  if (d->n_tokens > 0) {
+    const int chunk = d->n_tokens > kChunkSmall && d->n_tokens <= kChunkLarge ? kChunkLarge : kChunkSmall;
+    const dim3 grid((unsigned)(div_up(d->n_tokens, chunk) * (chunk / 256)), l.sorted_replicas);
+    rank_chunks_kernel<<<grid, 256, chunk * 4, st>>>(e, chunk, key[0], pos[0]);
+    for (int64_t run = chunk; run < d->n_tokens; run *= kMergeRuns, now ^= 1)
+      merge_runs_kernel<<<dim3((unsigned)div_up(d->n_tokens, 256), l.sorted_replicas), 256, 0, st>>>(
+          d->n_tokens, run, key[now], pos[now], key[now ^ 1], pos[now ^ 1]);
+  }
+  GradParams p{};
+  p.e = e;
+  p.keys = key[now];
+  p.pos = pos[now];
+  p.sorted_stride = l.sorted_replicas > 1 ? d->n_tokens : 0;
+  p.partial = reinterpret_cast<float*>(ws + l.partial_off);
+  p.accumulate = accumulate != 0;
+  with_types(d->rows_dtype, d->table_dtype, vector_of(d), GradLauncher{p, st});
+  const cudaError_t err = cudaGetLastError();
+  return err == cudaSuccess ? HDET_OK : fail_cuda("hdet_embed_grad", err);
+}
