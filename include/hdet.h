@@ -485,6 +485,53 @@ HDET_API int hdet_embed_grad_workspace(const hdet_embedding* d, int64_t* bytes);
 HDET_API int hdet_embed_grad(const hdet_embedding* d, int32_t accumulate, void* workspace, int64_t workspace_bytes,
                              void* stream);
 
+typedef struct {
+  const void* hidden;    /* bf16 [N] x n_tokens x width: what the model's last layer gives                     */
+  const void* weight;    /* bf16 [N] x vocab x width: the table; stride 0 = one for all replicas (param_bf16)  */
+  const void* targets;   /* [N] x n_tokens, target_dtype                                                       */
+  void* loss;            /* [N], loss_dtype: the replica's mean over its counted targets (0 if it has none)    */
+  void* token_loss;      /* fp32 [N] x n_tokens, or NULL: the tokens' own losses (0 at padding)                */
+  void* d_hidden;        /* [N] x n_tokens x width, d_hidden_dtype, or NULL (rows of padding get zeros)        */
+  void* d_weight;        /* [N] x vocab x width, d_weight_dtype, or NULL                                       */
+  int64_t n_tokens;      /* tokens per replica, 0 .. HDET_MAX_TOKENS                                           */
+  int64_t vocab, width;
+  int64_t hidden_stride, hidden_row;     /* between replicas (0 = the same for all) and between tokens         */
+  int64_t weight_stride, weight_row;
+  int64_t target_stride, token_loss_stride;
+  int64_t d_hidden_stride, d_hidden_row;
+  int64_t d_weight_stride, d_weight_row;
+  double grad_scale;     /* the gradients are those of grad_scale x loss (a loss scale; 1 otherwise)           */
+  int64_t piece_bytes;   /* workspace for the softmax's gradient, the largest part; 0 = 512 MB.  Smaller pieces
+                            mean more launches, at least one tile of 256 rows of the table x n_tokens          */
+  int32_t n_replicas;
+  int32_t hidden_dtype, weight_dtype;    /* HDET_DTYPE_BF16                                                    */
+  int32_t target_dtype;  /* HDET_DTYPE_I32 or HDET_DTYPE_I64                                                   */
+  int32_t loss_dtype;    /* HDET_DTYPE_F32 or HDET_DTYPE_F64                                                   */
+  int32_t d_hidden_dtype, d_weight_dtype; /* HDET_DTYPE_F32 or HDET_DTYPE_BF16                                 */
+  int32_t accumulate;    /* != 0: d_weight is added to what is there                                           */
+  int32_t device;
+  int32_t reserved;      /* set to 0                                                                           */
+} hdet_token_loss_args;
+
+/*
+ * hdet_token_loss -- softmax cross entropy of every replica's hidden states against its table, with the gradients that
+ * are asked for (d_hidden, d_weight, both or neither), in one call and without keeping the n_tokens x vocab logits:
+ *   z = hidden[r,t] . weight[r,v],  lse = log sum_v exp z,  token_loss[r,t] = lse - z_target,
+ *   loss[r] = mean of token_loss[r,t] over the counted targets,
+ *   d_hidden, d_weight = grad_scale x the gradients of loss[r].
+ * The logits are formed on the tensor cores (bf16 products, fp32 sums) tile by tile, twice when gradients are asked for;
+ * losses and softmax are fp32, means fp64.  The softmax's gradient is a bf16 operand of the two products behind it, a
+ * pair of bf16 numbers for fp32 gradients (then they cost twice the products).  The same inputs give the same bits.
+ * Work goes with the counted targets: padding is left out of the products.
+ * If a bounded wait inside a kernel runs out, every loss is set to NaN.
+ * hdet_token_loss_workspace gives the bytes that the call needs; it looks at sizes, strides, dtypes, piece_bytes, the
+ * table's address (its alignment) and at which gradients are asked for.
+ * Errors: INVALID_ARG (NULL, sizes, strides or dtypes out of range, workspace NULL or too small), ALIGN, UNSUPPORTED
+ * (hidden states or table not bf16; too many tiles), CUDA.
+ */
+HDET_API int hdet_token_loss_workspace(const hdet_token_loss_args* d, int64_t* bytes);
+HDET_API int hdet_token_loss(const hdet_token_loss_args* d, void* workspace, int64_t workspace_bytes, void* stream);
+
 /* hdet_last_error -- text of the last failure on h (when h is NULL: of the last failed call
  * that has no handle, hdet_create, hdet_converge_static or a call of the vocabulary ends, on this thread).  The pointer stays valid until the next call on that handle. */
 HDET_API const char* hdet_last_error(hdet_handle h);

@@ -75,6 +75,20 @@ class hdet_embedding(C.Structure):
     ]
 
 
+class hdet_token_loss_args(C.Structure):
+    _fields_ = [
+        ("hidden", C.c_void_p), ("weight", C.c_void_p), ("targets", C.c_void_p), ("loss", C.c_void_p),
+        ("token_loss", C.c_void_p), ("d_hidden", C.c_void_p), ("d_weight", C.c_void_p),
+        ("n_tokens", C.c_int64), ("vocab", C.c_int64), ("width", C.c_int64),
+        ("hidden_stride", C.c_int64), ("hidden_row", C.c_int64), ("weight_stride", C.c_int64), ("weight_row", C.c_int64),
+        ("target_stride", C.c_int64), ("token_loss_stride", C.c_int64), ("d_hidden_stride", C.c_int64),
+        ("d_hidden_row", C.c_int64), ("d_weight_stride", C.c_int64), ("d_weight_row", C.c_int64),
+        ("grad_scale", C.c_double), ("piece_bytes", C.c_int64), ("n_replicas", C.c_int32), ("hidden_dtype", C.c_int32),
+        ("weight_dtype", C.c_int32), ("target_dtype", C.c_int32), ("loss_dtype", C.c_int32), ("d_hidden_dtype", C.c_int32),
+        ("d_weight_dtype", C.c_int32), ("accumulate", C.c_int32), ("device", C.c_int32), ("reserved", C.c_int32),
+    ]
+
+
 _GD = C.c_double * HDET_MAX_GROUPS
 _ND = C.c_double * HDET_MAX_REPLICAS
 _GND = (C.c_double * HDET_MAX_REPLICAS) * HDET_MAX_GROUPS
@@ -140,6 +154,10 @@ def _load() -> C.CDLL:
     lib.hdet_embed_grad_workspace.restype = C.c_int
     lib.hdet_embed_grad.argtypes = [C.POINTER(hdet_embedding), C.c_int32, C.c_void_p, C.c_int64, C.c_void_p]
     lib.hdet_embed_grad.restype = C.c_int
+    lib.hdet_token_loss_workspace.argtypes = [C.POINTER(hdet_token_loss_args), C.POINTER(C.c_int64)]
+    lib.hdet_token_loss_workspace.restype = C.c_int
+    lib.hdet_token_loss.argtypes = [C.POINTER(hdet_token_loss_args), C.c_void_p, C.c_int64, C.c_void_p]
+    lib.hdet_token_loss.restype = C.c_int
     for f in ("hdet_create", "hdet_set_schedule", "hdet_step", "hdet_converge", "hdet_autolr_update",
               "hdet_get_state", "hdet_set_state", "hdet_destroy"):
         getattr(lib, f).restype = C.c_int
@@ -396,6 +414,67 @@ def hdet_embed_grad(tokens, d_out, d_table, workspace, scale: float = 1.0, accum
     d = _embedding(tokens, d_out, d_table, d_table.shape[0], scale)
     ptr, size = _workspace(workspace, d.device)
     _check(_lib.hdet_embed_grad(C.byref(d), 1 if accumulate else 0, ptr, size, stream), None)
+
+
+def _token_loss_args(hidden, weight, targets, loss, token_loss, d_hidden, d_weight, n, grad_scale, accumulate, piece_bytes):
+    T, D, V = hidden.shape[-2], hidden.shape[-1], weight.shape[-2]
+    if targets.shape[-1] != T or weight.shape[-1] != D:
+        raise ValueError("hidden, weight and targets disagree on the number of tokens or the width")
+    given = [t for t in (hidden, weight, targets, loss, token_loss, d_hidden, d_weight) if t is not None]
+    a = hdet_token_loss_args(
+        hidden.data_ptr(), weight.data_ptr(), targets.data_ptr(), None, None, None, None, T, V, D,
+        _replica_stride(hidden, 2, n, "hidden"), _row_stride(hidden, D), _replica_stride(weight, 2, n, "weight"),
+        _row_stride(weight, D), _replica_stride(targets, 1, n, "targets"), 0, 0, D, 0, D, grad_scale, piece_bytes, n,
+        _code(hidden), _code(weight), _code(targets), HDET_DTYPE_F32, HDET_DTYPE_F32, HDET_DTYPE_F32, 1 if accumulate else 0,
+        _one_device(*given), 0)
+    if loss is not None:
+        if loss.shape != (n,) or not loss.is_contiguous():
+            raise ValueError("loss must be a contiguous [N]")
+        a.loss, a.loss_dtype = loss.data_ptr(), _code(loss)
+    if token_loss is not None:
+        if token_loss.shape != (n, T) or _code(token_loss) != HDET_DTYPE_F32:
+            raise ValueError("token_loss must be float32 [N, T]")
+        a.token_loss, a.token_loss_stride = token_loss.data_ptr(), _replica_stride(token_loss, 1, n, "token_loss")
+    if d_hidden is not None:
+        if d_hidden.shape != (n, T, D):
+            raise ValueError("d_hidden must be [N, T, D]")
+        a.d_hidden, a.d_hidden_dtype = d_hidden.data_ptr(), _code(d_hidden)
+        a.d_hidden_stride, a.d_hidden_row = _replica_stride(d_hidden, 2, n, "d_hidden"), _row_stride(d_hidden, D)
+    if d_weight is not None:
+        if d_weight.shape != (n, V, D):
+            raise ValueError("d_weight must be [N, V, D]")
+        a.d_weight, a.d_weight_dtype = d_weight.data_ptr(), _code(d_weight)
+        a.d_weight_stride, a.d_weight_row = _replica_stride(d_weight, 2, n, "d_weight"), _row_stride(d_weight, D)
+    return a
+
+
+def _replicas(*tensors) -> int:
+    """N, from the first of (tensor, axes of one replica) that has a replica axis; 1 when none has."""
+    for t, dims in tensors:
+        if t is not None and t.dim() == dims + 1:
+            return t.shape[0]
+    return 1
+
+
+def hdet_token_loss_workspace(hidden, weight, targets, d_hidden=None, d_weight=None, piece_bytes: int = 0) -> int:
+    """Bytes of workspace that hdet_token_loss needs for these tensors and gradients."""
+    n = _replicas((hidden, 2), (weight, 2), (targets, 1), (d_hidden, 2), (d_weight, 2))
+    a = _token_loss_args(hidden, weight, targets, None, None, d_hidden, d_weight, n, 1.0, False, piece_bytes)
+    need = C.c_int64(0)
+    _check(_lib.hdet_token_loss_workspace(C.byref(a), C.byref(need)), None)
+    return int(need.value)
+
+
+def hdet_token_loss(hidden, weight, targets, loss, workspace, token_loss=None, d_hidden=None, d_weight=None,
+                    grad_scale: float = 1.0, accumulate: bool = False, piece_bytes: int = 0, stream: int = 0) -> None:
+    """Softmax cross entropy of hidden [N, T, D] against the table weight [N, V, D] (or [V, D] for all replicas), both bf16,
+    with targets [N, T] (or [T]; int32 or int64; outside 0 .. V-1: padding).  Writes the replicas' means to ``loss`` [N]
+    (float32 or float64, as hdet_step_device reads them) and, where given, ``token_loss`` [N, T] and the gradients
+    ``d_hidden`` [N, T, D] and ``d_weight`` [N, V, D] (float32 or bfloat16; ``accumulate`` adds d_weight to what is there)."""
+    a = _token_loss_args(hidden, weight, targets, loss, token_loss, d_hidden, d_weight, loss.shape[0], grad_scale, accumulate,
+                         piece_bytes)
+    ptr, size = _workspace(workspace, a.device)
+    _check(_lib.hdet_token_loss(C.byref(a), ptr, size, stream), None)
 
 
 def _workspace(workspace, device: int):

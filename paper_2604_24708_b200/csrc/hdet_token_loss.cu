@@ -1,0 +1,1032 @@
+// Softmax cross entropy of hidden states against a large table, and its gradients, without keeping the logits (contract:
+// include/hdet.h).  For each replica, with H the hidden states of its counted tokens, W its table, y the targets:
+//
+//   Z = H W^T,  lse_t = log sum_v exp Z_tv,  l_t = lse_t - Z_{t,y_t},  loss = mean of l_t
+//   P = exp(Z - lse),  G = P - onehot(y),  dH = (c) G W,  dW = (c) G^T H,  c = grad_scale / counted tokens
+//
+// Three products of T x V x D, plus one more because Z is formed twice: once for lse, once for G, which needs it.
+//
+//   pack      counted tokens move together (padding drops out: no work, and nothing it holds reaches a product)
+//   stats     Z tile by tile on the tensor cores; the epilogue keeps, of each tile's row, its maximum and sum of exp
+//   join      those over the vocabulary: lse, the token's loss, the replica's mean
+//   probs     Z again, for a piece of the vocabulary; the epilogue writes G as bf16 into the workspace
+//   grads     both products with G in one launch; after the last piece, dH's partial sums are joined
+//
+// A piece is as much of G as the workspace holds: as many whole replicas as fit, else a part of one replica's vocabulary.
+//
+// G is the operand of a bf16 product, so it is rounded to bf16, unscaled: the -1 of the target is then exact where the
+// target is unlikely.  Its relative error, 2^-9 a value, is that of a bf16 gradient's own rounding.  For fp32 gradients
+// that would be too coarse: G is written as a pair, G = hi + lo with both bf16 (2^-17), and the products run over both.
+#include <cuda_bf16.h>
+
+#include <cmath>
+#include <cstdio>
+#include <mutex>
+
+#include "../../include/hdet.h"
+#include "hdet_internal.h"
+#include "hdet_umma.cuh"
+
+namespace {
+
+using namespace hdet::umma;
+namespace bulk = hdet::bulk;
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kStages = 3;
+constexpr int kStageBytes = 2 * kOperandBytes;
+// warp 0 copies, warp 1 issues the products, warps 2 - 5 read the accumulator, one quarter of its lanes each
+constexpr int kGemmThreads = 192;
+constexpr int kGemmSmem = kStages * kStageBytes + 1024 + 256;
+constexpr long long kDrainLimitCycles = 200000000ll;
+
+__host__ __device__ constexpr int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+__host__ __device__ constexpr int64_t round_up(int64_t a, int64_t b) { return div_up(a, b) * b; }
+
+enum Phase { kStats, kProbs, kGrads };
+
+struct Control {            // first bytes of the workspace; zeroed by pack_kernel
+  unsigned status;          // a bounded wait ran out
+  unsigned done[HDET_MAX_REPLICAS];   // blocks of join_kernel that have finished
+};
+
+struct Out {                // a gradient
+  void* p;
+  int64_t stride, row;
+  int f32, accumulate, vec; // vec: rows start on 16-byte boundaries
+};
+
+struct LossParams {
+  CUtensorMap hidden, weight, grad_hi, grad_lo;
+  // problem
+  int n_replicas, vocab, width, n_tokens;
+  int rows_pad;             // rows per replica of everything packed
+  bool weight_shared;
+  double grad_scale;
+  // packed inputs and per-row values [replica][rows_pad]
+  const int* count;
+  const int* target;
+  const int* token_of;
+  float* z_target;
+  float* lse2;              // lse in units of log 2
+  float2* part;             // [replica][column tiles][rows_pad]: maximum, sum of exp
+  // piece of the vocabulary
+  int r0, n_r;              // replicas of this launch
+  int v0, v_len, v_pitch;   // first row of the table, rows, pitch of G
+  __nv_bfloat16 *g_hi, *g_lo;
+  // gradients
+  int m_tiles, n_tiles;     // stats, probs: tiles of tokens, of the vocabulary
+  int h_tiles_m, h_tiles_n, h_splits, h_len, h_jobs;   // dH: tiles, parts of the sum over the vocabulary, 64-steps a part
+  int w_tiles_m, w_tiles_n;                            // dW
+  bool h_two, w_two;        // product over hi and lo
+  bool h_slabs, h_add;      // dH goes to fp32 partial sums; added to what an earlier piece left
+  float* slabs;             // [split][replica of the launch][rows_pad][width]
+  Out d_hidden, d_weight;
+  void* loss;
+  int loss_f64;
+  Control* control;
+};
+
+__device__ __forceinline__ void poison_loss(const LossParams& p) {
+  for (int r = 0; r < p.n_replicas; ++r) {
+    if (p.loss_f64) static_cast<double*>(p.loss)[r] = NAN; else static_cast<float*>(p.loss)[r] = NAN;
+  }
+}
+
+// What one CTA (or pair) computes: rows m0.., columns n0.. of a product over k_blocks steps of 64.
+struct Job {
+  const CUtensorMap *a, *a2, *b;
+  bool a_mn, b_mn;          // MN-major operands
+  int k_half;               // steps of one pass over the sum (two passes: first with a, then with a2)
+  int k_blocks;
+  int a_row, a_k, a_z, b_row, b_k, b_z;   // where the operands start
+  int r, m0, n0, split;
+  bool is_dw;
+};
+
+template <int CTAS, int PHASE>
+__device__ __forceinline__ bool find_job(const LossParams& p, int tile, Job& j) {
+  constexpr int kTile = 128 * CTAS;
+  if constexpr (PHASE != kGrads) {
+    // tokens fastest: the tiles that run at the same time share rows of the table, and the hidden states stay in L2
+    const int per_r = p.m_tiles * p.n_tiles;
+    const int g = tile / per_r, rest = tile % per_r;
+    j.r = p.r0 + g;
+    j.m0 = rest % p.m_tiles * kTile;
+    j.n0 = rest / p.m_tiles * kTile;
+    if (j.m0 >= p.count[j.r]) return false;
+    j.a = &p.hidden; j.b = &p.weight; j.a2 = nullptr;
+    j.a_mn = j.b_mn = false;
+    j.a_row = j.m0; j.a_k = 0; j.a_z = j.r;
+    j.b_row = p.v0 + j.n0; j.b_k = 0; j.b_z = p.weight_shared ? 0 : j.r;
+    j.k_half = j.k_blocks = (p.width + kBlockK - 1) / kBlockK;
+    j.split = 0; j.is_dw = false;
+    return true;
+  } else {
+    // dH first: its sums are the longest, so the short dW tiles fill the machine's end
+    if (tile < p.h_jobs) {
+      const int per_split = p.n_r * p.h_tiles_m * p.h_tiles_n;
+      const int rest = tile % per_split, g = rest / (p.h_tiles_m * p.h_tiles_n), mn = rest % (p.h_tiles_m * p.h_tiles_n);
+      j.split = tile / per_split;
+      j.r = p.r0 + g;
+      j.m0 = mn / p.h_tiles_n * kTile;
+      j.n0 = mn % p.h_tiles_n * kTile;
+      if (j.m0 >= p.count[j.r]) return false;
+      const int all = (p.v_len + kBlockK - 1) / kBlockK;
+      const int from = min(j.split * p.h_len, all), to = min(from + p.h_len, all);
+      j.k_half = to - from;
+      j.k_blocks = j.k_half * (p.h_two ? 2 : 1);
+      j.a = &p.grad_hi; j.a2 = &p.grad_lo; j.b = &p.weight;
+      j.a_mn = false; j.b_mn = true;
+      j.a_row = j.m0; j.a_k = from * kBlockK; j.a_z = g;
+      j.b_row = j.n0; j.b_k = p.v0 + from * kBlockK; j.b_z = p.weight_shared ? 0 : j.r;
+      j.is_dw = false;
+      return true;
+    }
+    const int t = tile - p.h_jobs;
+    const int g = t / (p.w_tiles_m * p.w_tiles_n), mn = t % (p.w_tiles_m * p.w_tiles_n);
+    j.split = 0;
+    j.r = p.r0 + g;
+    j.m0 = mn / p.w_tiles_n * kTile;
+    j.n0 = mn % p.w_tiles_n * kTile;
+    j.k_half = (p.count[j.r] + kBlockK - 1) / kBlockK;
+    j.k_blocks = j.k_half * (p.w_two ? 2 : 1);
+    j.a = &p.grad_hi; j.a2 = &p.grad_lo; j.b = &p.hidden;
+    j.a_mn = j.b_mn = true;
+    j.a_row = j.m0; j.a_k = 0; j.a_z = g;
+    j.b_row = j.n0; j.b_k = 0; j.b_z = j.r;
+    j.is_dw = true;
+    return true;
+  }
+}
+
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// Writes up to 32 consecutive values of one row of a gradient.
+__device__ __forceinline__ void write_values(const Out& o, int64_t at, const float (&x)[32], int n) {
+  if (o.f32) {
+    float* to = static_cast<float*>(o.p) + at;
+    if (n == 32 && o.vec) {
+#pragma unroll
+      for (int i = 0; i < 32; i += 4) {
+        float4 v = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+        if (o.accumulate) {
+          const float4 old = *reinterpret_cast<const float4*>(to + i);
+          v.x += old.x; v.y += old.y; v.z += old.z; v.w += old.w;
+        }
+        *reinterpret_cast<float4*>(to + i) = v;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (i < n) to[i] = o.accumulate ? to[i] + x[i] : x[i];
+    }
+  } else {
+    __nv_bfloat16* to = static_cast<__nv_bfloat16*>(o.p) + at;
+    if (n == 32 && o.vec) {
+#pragma unroll
+      for (int i = 0; i < 32; i += 8) {
+        float y[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) y[k] = x[i + k];
+        if (o.accumulate) {
+          const uint4 old = *reinterpret_cast<const uint4*>(to + i);
+          const uint32_t w[4] = {old.x, old.y, old.z, old.w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            y[2 * k] += __uint_as_float(w[k] << 16);
+            y[2 * k + 1] += __uint_as_float(w[k] & 0xffff0000u);
+          }
+        }
+        *reinterpret_cast<uint4*>(to + i) =
+            make_uint4(bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3]), bf16_pair(y[4], y[5]), bf16_pair(y[6], y[7]));
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (i < n) to[i] = __float2bfloat16_rn(o.accumulate ? __bfloat162float(to[i]) + x[i] : x[i]);
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ epilogues
+// One thread per row of the tile; the accumulator's columns pass through registers 32 at a time.
+
+template <int CTAS>
+__device__ __forceinline__ void stats_epilogue(const LossParams& p, const Job& j, uint32_t tmem, int row) {
+  constexpr int kCols = 128 * CTAS;
+  const int64_t at = (int64_t)j.r * p.rows_pad + row;
+  const int target = p.target[at];                 // -1 behind the counted tokens
+  float top = -INFINITY, sum = 0.0f, picked = 0.0f;
+#pragma unroll 1
+  for (int c = 0; c < kCols; c += 32) {
+    float x[32];
+    tmem_load32(tmem + c, x);
+    tmem_load_wait(x);
+    const int v = j.n0 + c;                        // v0 is 0 here
+    if (v + 32 > p.vocab) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (v + i >= p.vocab) x[i] = -INFINITY;
+    }
+    if ((unsigned)(target - v) < 32u) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (v + i == target) picked = x[i];
+    }
+    float here = x[0];
+#pragma unroll
+    for (int i = 1; i < 32; ++i) here = fmaxf(here, x[i]);
+    const float now = fmaxf(top, here);
+    const float shift = now == -INFINITY ? 0.0f : now * kLog2e;    // nothing finite yet: exp of -inf, not of NaN
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) s += exp2_fast(fmaf(x[i], kLog2e, -shift));
+    sum = fmaf(sum, exp2_fast(fmaf(top, kLog2e, -shift)), s);
+    top = now;
+  }
+  const int n_tile = j.n0 / kCols;
+  p.part[((int64_t)j.r * p.n_tiles + n_tile) * p.rows_pad + row] = make_float2(top, sum);
+  if (target >= j.n0 && target < j.n0 + kCols) p.z_target[at] = picked;
+}
+
+template <int CTAS>
+__device__ __forceinline__ void probs_epilogue(const LossParams& p, const Job& j, uint32_t tmem, int row) {
+  constexpr int kCols = 128 * CTAS;
+  const int64_t at = (int64_t)j.r * p.rows_pad + row;
+  const bool counted = row < p.count[j.r];
+  const int target = counted ? p.target[at] - p.v0 : -1;
+  const float lse2 = counted ? p.lse2[at] : INFINITY;
+  const int64_t to = ((int64_t)(j.r - p.r0) * p.rows_pad + row) * p.v_pitch + j.n0;
+#pragma unroll 1
+  for (int c = 0; c < kCols; c += 32) {
+    float x[32];
+    tmem_load32(tmem + c, x);
+    tmem_load_wait(x);
+    const int v = j.n0 + c;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) x[i] = exp2_fast(fmaf(x[i], kLog2e, -lse2));
+    if ((unsigned)(target - v) < 32u) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (v + i == target) x[i] -= 1.0f;
+    }
+    if (!counted || v + 32 > p.v_len) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (!counted || v + i >= p.v_len) x[i] = 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < 32; i += 8) {
+      uint32_t w[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) w[k] = bf16_pair(x[i + 2 * k], x[i + 2 * k + 1]);
+      *reinterpret_cast<uint4*>(p.g_hi + to + c + i) = make_uint4(w[0], w[1], w[2], w[3]);
+      if (p.g_lo) {
+        uint32_t l[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          l[k] = bf16_pair(x[i + 2 * k] - __uint_as_float(w[k] << 16),
+                           x[i + 2 * k + 1] - __uint_as_float(w[k] & 0xffff0000u));
+        *reinterpret_cast<uint4*>(p.g_lo + to + c + i) = make_uint4(l[0], l[1], l[2], l[3]);
+      }
+    }
+  }
+}
+
+template <int CTAS>
+__device__ __forceinline__ void grads_epilogue(const LossParams& p, const Job& j, uint32_t tmem, int row) {
+  constexpr int kCols = 128 * CTAS;
+  const int count = p.count[j.r];
+  Out o;
+  int64_t base;
+  float scale = (float)(p.grad_scale / (double)(count > 0 ? count : 1));
+  bool on;
+  if (j.is_dw) {
+    o = p.d_weight;
+    on = row < p.v_len;
+    base = j.r * o.stride + (int64_t)(p.v0 + row) * o.row;
+  } else if (p.h_slabs) {
+    o.p = p.slabs; o.f32 = 1; o.accumulate = p.h_add; o.vec = p.width % 4 == 0;
+    on = row < count;
+    base = (((int64_t)j.split * p.n_r + (j.r - p.r0)) * p.rows_pad + row) * p.width;
+    scale = 1.0f;
+  } else {
+    o = p.d_hidden;
+    on = row < count;
+    base = on ? j.r * o.stride + (int64_t)p.token_of[(int64_t)j.r * p.rows_pad + row] * o.row : 0;
+  }
+#pragma unroll 1
+  for (int c = 0; c < kCols; c += 32) {
+    if (j.n0 + c >= p.width) break;
+    float x[32];
+    if (j.k_blocks > 0) {
+      tmem_load32(tmem + c, x);
+      tmem_load_wait(x);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) x[i] = 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < 32; ++i) x[i] *= scale;
+    if (on) write_values(o, base + j.n0 + c, x, min(32, p.width - j.n0 - c));
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ product
+// One tile of (128 * CTAS) x (128 * CTAS) per CTA or pair, two CTAs a SM: while one reads its accumulator out, the other
+// keeps the tensor cores busy, and the hardware hands out tiles as SMs free up, whatever their lengths.
+template <int CTAS, int PHASE>
+__global__ void __launch_bounds__(kGemmThreads, 2) gemm_kernel(const __grid_constant__ LossParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ int s_failed, s_issued;
+  Job j;
+  if (!find_job<CTAS, PHASE>(p, blockIdx.x / CTAS, j)) return;   // the same for both CTAs of a pair
+  const uint32_t smem = (bulk::smem_addr(smem_raw) + 1023u) & ~1023u;
+  const uint32_t bars = smem + kStages * kStageBytes;
+  const auto full = [&](int s) { return bars + 8 * s; };
+  const auto empty = [&](int s) { return bars + 8 * (kStages + s); };
+  const uint32_t acc_full = bars + 8 * (2 * kStages), tmem_at = acc_full + 8;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = CTAS == 1 ? 0 : cluster_rank();
+
+  if (threadIdx.x == 0) {
+    s_failed = 0;
+    s_issued = 0;
+    for (int s = 0; s < kStages; ++s) {
+      bulk::barrier_init(full(s), 1);
+      bulk::barrier_init(empty(s), 1);
+    }
+    bulk::barrier_init(acc_full, 1);
+    bulk::barrier_init_fence();
+    prefetch_map(j.a);
+    prefetch_map(j.b);
+  }
+  if (warp == 1) tmem_alloc<CTAS>(tmem_at, 128 * CTAS);
+  fence_before_sync();
+  __syncthreads();
+  if constexpr (CTAS == 2) cluster_sync();       // the peer's barriers exist before anything arrives there
+  fence_after_sync();
+  uint32_t tmem;
+  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tmem) : "r"(tmem_at));
+
+  const int n_k = j.k_blocks;
+  if (warp == 0) {
+    if (lane == 0) {
+      const int a_row = j.a_row + 128 * (int)rank, b_row = j.b_row + 128 * (int)rank;
+      for (int kb = 0; kb < n_k; ++kb) {
+        const int s = kb % kStages;
+        if (kb >= kStages && !bulk::barrier_wait(empty(s), (kb / kStages - 1) & 1)) {
+          s_failed = 1;
+          break;
+        }
+        if (rank == 0) bulk::barrier_expect(full(s), CTAS * kStageBytes);
+        const uint32_t bar = CTAS == 1 ? full(s) : in_leader(full(s));
+        const uint32_t dst = smem + s * kStageBytes;
+        const bool second = kb >= j.k_half;
+        const int k = (second ? kb - j.k_half : kb) * kBlockK;
+        const CUtensorMap* a = second ? j.a2 : j.a;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          if (j.a_mn) load_box<CTAS>(dst + i * kBoxBytes, a, a_row + 64 * i, j.a_k + k, j.a_z, bar);
+          else load_box<CTAS>(dst + i * kBoxBytes, a, j.a_k + k, a_row + 64 * i, j.a_z, bar);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          if (j.b_mn) load_box<CTAS>(dst + kOperandBytes + i * kBoxBytes, j.b, b_row + 64 * i, j.b_k + k, j.b_z, bar);
+          else load_box<CTAS>(dst + kOperandBytes + i * kBoxBytes, j.b, j.b_k + k, b_row + 64 * i, j.b_z, bar);
+        }
+        s_issued = kb + 1;
+      }
+      // the products have read the last stages: every arrival that was sent to this CTA's barriers is in
+      for (int kb = n_k > kStages ? n_k - kStages : 0; kb < n_k && s_issued == n_k; ++kb)
+        if (!bulk::barrier_wait(empty(kb % kStages), (kb / kStages) & 1)) {
+          s_failed = 1;
+          break;
+        }
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && rank == 0 && n_k > 0) {
+      const uint32_t idesc = instruction_desc<CTAS>(j.a_mn, j.b_mn);
+      const uint32_t a_step = k_step_bytes(j.a_mn), b_step = k_step_bytes(j.b_mn);
+      for (int kb = 0; kb < n_k; ++kb) {
+        const int s = kb % kStages;
+        if (!bulk::barrier_wait(full(s), (kb / kStages) & 1)) {
+          s_failed = 1;
+          break;
+        }
+        fence_after_sync();
+        const uint32_t a = smem + s * kStageBytes, b = a + kOperandBytes;
+#pragma unroll
+        for (int k = 0; k < kBlockK / 16; ++k)
+          mma<CTAS>(tmem, operand_desc(a + k * a_step, j.a_mn), operand_desc(b + k * b_step, j.b_mn), idesc, kb > 0 || k > 0);
+        commit<CTAS>(empty(s));
+      }
+      commit<CTAS>(acc_full);
+    }
+  } else {
+    bool ok = true;
+    if (n_k > 0) ok = bulk::barrier_wait(acc_full, 0, 2 * bulk::kWaitLimitCycles);
+    ok = __all_sync(0xffffffffu, ok);
+    fence_after_sync();
+    if (!ok) {
+      s_failed = 1;
+    } else {
+      const int quarter = warp & 3;
+      const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
+      const int row = j.m0 + 128 * (int)rank + quarter * 32 + lane;
+      if constexpr (PHASE == kStats) stats_epilogue<CTAS>(p, j, lanes, row);
+      else if constexpr (PHASE == kProbs) probs_epilogue<CTAS>(p, j, lanes, row);
+      else grads_epilogue<CTAS>(p, j, lanes, row);
+    }
+  }
+  __syncwarp();
+  fence_before_sync();
+  __syncthreads();
+  if (s_failed && threadIdx.x == 0) {
+    atomicExch(&p.control->status, 1u);
+    poison_loss(p);
+    // copies still on their way may write this CTA's shared memory: a bounded wait for each (the leader sees both CTAs')
+    if (rank == 0)
+      for (int kb = max(0, s_issued - kStages); kb < s_issued; ++kb)
+        bulk::barrier_wait(full(kb % kStages), (kb / kStages) & 1, kDrainLimitCycles);
+  }
+  if constexpr (CTAS == 2) cluster_sync();       // neither CTA leaves while the other's products may read it
+  fence_after_sync();
+  if (warp == 1) tmem_free<CTAS>(tmem, 128 * CTAS);
+}
+
+// ------------------------------------------------------------------------------------------------ packing
+struct PackParams {
+  const __nv_bfloat16* hidden;
+  int64_t hidden_stride, hidden_row;
+  const void* targets;
+  int64_t target_stride;
+  bool wide, hidden_vec, d_hidden_vec;
+  int n_tokens, vocab, width, rows_pad, row_tile, packed_row;
+  __nv_bfloat16* packed;
+  int *count, *target, *token_of;
+  float* token_loss;
+  int64_t token_loss_stride;
+  Out d_hidden;             // p NULL: none
+  Control* control;
+};
+
+constexpr int kPackRows = 32;
+
+// Moves the hidden states of counted tokens together, 32 tokens a block.  Every block counts the targets before its own
+// (and all of them) itself: that is 4 bytes a token from L2 instead of a launch of its own for the offsets.
+__global__ void __launch_bounds__(256) pack_kernel(const PackParams p) {
+  __shared__ int s_before[8], s_all[8], s_to[kPackRows];
+  const int r = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int t0 = blockIdx.x * kPackRows;
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    p.control->done[r] = 0;
+    if (r == 0) p.control->status = 0;
+  }
+  const auto target_of = [&](int t) -> int {
+    const int64_t at = r * p.target_stride + t;
+    if (p.wide) {
+      const long long v = static_cast<const long long*>(p.targets)[at];
+      return v >= 0 && v < p.vocab ? (int)v : -1;
+    }
+    const int v = static_cast<const int*>(p.targets)[at];
+    return v >= 0 && v < p.vocab ? v : -1;
+  };
+  int before = 0, all = 0;
+  for (int t = threadIdx.x; t < p.n_tokens; t += 256) {
+    const int one = target_of(t) >= 0;
+    all += one;
+    before += t < t0 ? one : 0;
+  }
+  before = __reduce_add_sync(0xffffffffu, before);
+  all = __reduce_add_sync(0xffffffffu, all);
+  if (lane == 0) { s_before[warp] = before; s_all[warp] = all; }
+  __syncthreads();
+  before = all = 0;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) { before += s_before[w]; all += s_all[w]; }
+  const int64_t base = (int64_t)r * p.rows_pad;
+  if (warp == 0) {
+    const int t = t0 + lane;
+    const int y = t < p.n_tokens ? target_of(t) : -1;
+    const unsigned counted = __ballot_sync(0xffffffffu, y >= 0);
+    const int to = y >= 0 ? before + __popc(counted & ((1u << lane) - 1)) : -1;
+    s_to[lane] = to;
+    if (to >= 0) {
+      p.target[base + to] = y;
+      p.token_of[base + to] = t;
+    } else if (t < p.n_tokens && p.token_loss) {
+      p.token_loss[r * p.token_loss_stride + t] = 0.0f;
+    }
+    if (blockIdx.x == 0 && lane == 0) p.count[r] = all;
+  }
+  __syncthreads();
+  for (int i = warp; i < kPackRows && t0 + i < p.n_tokens; i += 8) {
+    const int to = s_to[i];
+    const int64_t t = t0 + i;
+    if (to >= 0) {
+      const __nv_bfloat16* from = p.hidden + r * p.hidden_stride + t * p.hidden_row;
+      __nv_bfloat16* dst = p.packed + (base + to) * p.packed_row;
+      if (p.hidden_vec) {
+        for (int c = lane * 8; c < p.width; c += 256)
+          *reinterpret_cast<uint4*>(dst + c) = *reinterpret_cast<const uint4*>(from + c);
+      } else {
+        for (int c = lane; c < p.width; c += 32) dst[c] = from[c];
+      }
+    } else if (p.d_hidden.p) {
+      const int64_t at = r * p.d_hidden.stride + t * p.d_hidden.row;
+      const int size = p.d_hidden.f32 ? 4 : 2;
+      char* dst = static_cast<char*>(p.d_hidden.p) + at * size;
+      if (p.d_hidden_vec) {
+        for (int b = lane * 16; b < p.width * size; b += 512) *reinterpret_cast<uint4*>(dst + b) = make_uint4(0, 0, 0, 0);
+      } else {
+        for (int c = lane; c < p.width; c += 32) {
+          if (p.d_hidden.f32) reinterpret_cast<float*>(dst)[c] = 0.0f;
+          else reinterpret_cast<__nv_bfloat16*>(dst)[c] = __float2bfloat16_rn(0.0f);
+        }
+      }
+    }
+  }
+  // rows behind the last counted token, up to the tile's end: zeros, since a product sums over them
+  const int end = min(p.rows_pad, (all + p.row_tile - 1) / p.row_tile * p.row_tile);
+  for (int row = all + (int)blockIdx.x * 8 + warp; row < end; row += (int)gridDim.x * 8) {
+    if (lane == 0) { p.target[base + row] = -1; p.token_of[base + row] = 0; }
+    __nv_bfloat16* dst = p.packed + (base + row) * p.packed_row;
+    for (int c = lane * 8; c < p.packed_row; c += 256) *reinterpret_cast<uint4*>(dst + c) = make_uint4(0, 0, 0, 0);
+  }
+}
+
+// A table whose rows cannot be copied as boxes (odd width, stride or address) is laid out once in the workspace.
+__global__ void __launch_bounds__(256) pack_table_kernel(const __nv_bfloat16* table, int64_t stride, int64_t row, int vocab,
+                                                         int width, int packed_row, __nv_bfloat16* packed) {
+  const int v = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (v >= vocab) return;
+  const __nv_bfloat16* from = table + blockIdx.y * stride + v * row;
+  __nv_bfloat16* to = packed + ((int64_t)blockIdx.y * vocab + v) * packed_row;
+  for (int c = lane; c < width; c += 32) to[c] = from[c];
+}
+
+// ------------------------------------------------------------------------------------------------ joining
+struct JoinParams {
+  const int *count, *token_of;
+  const float2* part;
+  const float* z_target;
+  float* lse2;
+  float* token_loss;
+  int64_t token_loss_stride;
+  double* block_sum;        // [replica][blocks]
+  int rows_pad, n_tiles;
+  void* loss;
+  int loss_f64;
+  Control* control;
+};
+
+// 32 rows a block, the column tiles of a row spread over 32 threads: lse = max + log sum exp over the tiles, in their
+// order within a thread and the threads' order after that.  The last block of a replica adds the blocks' sums (fp64, in
+// their order) and writes the mean.
+__global__ void __launch_bounds__(1024) join_kernel(const JoinParams p) {
+  __shared__ float2 s_part[32][33];
+  const int r = blockIdx.y, x = threadIdx.x, y = threadIdx.y;
+  const int row = blockIdx.x * 32 + x, count = p.count[r];
+  float top = -INFINITY, sum = 0.0f;
+  const auto add = [&](float2 o) {
+    const float now = fmaxf(top, o.x);
+    const float shift = now == -INFINITY ? 0.0f : now;
+    sum = sum * exp2_fast((top - shift) * kLog2e) + o.y * exp2_fast((o.x - shift) * kLog2e);
+    top = now;
+  };
+  if (row < count) {
+    const float2* part = p.part + (int64_t)r * p.n_tiles * p.rows_pad + row;
+    for (int n = y; n < p.n_tiles; n += 32) add(part[(int64_t)n * p.rows_pad]);
+  }
+  s_part[y][x] = make_float2(top, sum);
+  __syncthreads();
+  if (y != 0) return;
+  double loss = 0.0;
+  if (row < count) {
+    for (int k = 1; k < 32; ++k) add(s_part[k][x]);
+    const int64_t at = (int64_t)r * p.rows_pad + row;
+    const float lse = top + logf(sum);
+    p.lse2[at] = fmaf(top, kLog2e, log2f(sum));
+    const float l = lse - p.z_target[at];
+    if (p.token_loss) p.token_loss[r * p.token_loss_stride + p.token_of[at]] = l;
+    loss = l;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, o);
+  unsigned before = 0;
+  if (x == 0) {
+    p.block_sum[(int64_t)r * gridDim.x + blockIdx.x] = loss;
+    __threadfence();
+    before = atomicAdd(&p.control->done[r], 1u);
+  }
+  before = __shfl_sync(0xffffffffu, before, 0);
+  if (before != gridDim.x - 1) return;
+  __threadfence();
+  double total = 0.0;
+  for (int b = x; b < (int)gridDim.x; b += 32) total += __ldcg(p.block_sum + (int64_t)r * gridDim.x + b);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+  if (x == 0) {
+    double mean = count > 0 ? total / (double)count : 0.0;
+    if (__ldcg(&p.control->status)) mean = NAN;
+    if (p.loss_f64) static_cast<double*>(p.loss)[r] = mean; else static_cast<float*>(p.loss)[r] = (float)mean;
+  }
+}
+
+// dH: adds the partial sums over the vocabulary in their order, scales, rounds once and puts rows back at their tokens.
+__global__ void __launch_bounds__(256) join_hidden_kernel(const __grid_constant__ LossParams p) {
+  const int g = blockIdx.y, r = p.r0 + g, row = blockIdx.x;
+  const int count = p.count[r];
+  if (row >= count) return;
+  const float scale = (float)(p.grad_scale / (double)count);
+  const Out o = p.d_hidden;
+  const int64_t to = r * o.stride + (int64_t)p.token_of[(int64_t)r * p.rows_pad + row] * o.row;
+  for (int c = threadIdx.x; c < p.width; c += 256) {
+    float sum = 0.0f;
+    for (int s = 0; s < p.h_splits; ++s) sum += p.slabs[(((int64_t)s * p.n_r + g) * p.rows_pad + row) * p.width + c];
+    sum *= scale;
+    if (o.f32) static_cast<float*>(o.p)[to + c] = sum;
+    else static_cast<__nv_bfloat16*>(o.p)[to + c] = __float2bfloat16_rn(sum);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ host side
+int fail(int code, const char* who, const char* what) {
+  char msg[240];
+  snprintf(msg, sizeof msg, "%s: %s", who, what);
+  hdet::set_handleless_error(msg);
+  return code;
+}
+
+int fail_cuda(const char* who, cudaError_t e) { return fail(HDET_ERR_CUDA, who, cudaGetErrorString(e)); }
+
+bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+int elem_size(int dtype) { return dtype == HDET_DTYPE_BF16 ? 2 : 4; }
+bool is_float(int dtype) { return dtype == HDET_DTYPE_F32 || dtype == HDET_DTYPE_BF16; }
+
+int check(const char* who, const hdet_token_loss_args* d) {
+  if (!d) return fail(HDET_ERR_INVALID_ARG, who, "the descriptor is NULL");
+  if (d->n_replicas < 1 || d->n_replicas > HDET_MAX_REPLICAS)
+    return fail(HDET_ERR_INVALID_ARG, who, "n_replicas must be in 1..32");
+  if (d->n_tokens < 0 || d->n_tokens > HDET_MAX_TOKENS || d->vocab < 1 || d->vocab > HDET_MAX_VOCAB || d->width < 1 ||
+      d->width > HDET_MAX_WIDTH)
+    return fail(HDET_ERR_INVALID_ARG, who, "n_tokens, vocab or width out of range");
+  if (d->target_dtype != HDET_DTYPE_I32 && d->target_dtype != HDET_DTYPE_I64)
+    return fail(HDET_ERR_INVALID_ARG, who, "target_dtype must be HDET_DTYPE_I32 or HDET_DTYPE_I64");
+  if (d->loss_dtype != HDET_DTYPE_F32 && d->loss_dtype != HDET_DTYPE_F64)
+    return fail(HDET_ERR_INVALID_ARG, who, "loss_dtype must be HDET_DTYPE_F32 or HDET_DTYPE_F64");
+  if (d->hidden_dtype != HDET_DTYPE_BF16 || d->weight_dtype != HDET_DTYPE_BF16) {
+    if (!is_float(d->hidden_dtype) || !is_float(d->weight_dtype))
+      return fail(HDET_ERR_INVALID_ARG, who, "hidden_dtype and weight_dtype must be HDET_DTYPE_*");
+    return fail(HDET_ERR_UNSUPPORTED, who, "hidden states and table must be HDET_DTYPE_BF16 (hdet_tensor.param_bf16, or a bf16 copy)");
+  }
+  if ((d->d_hidden && !is_float(d->d_hidden_dtype)) || (d->d_weight && !is_float(d->d_weight_dtype)))
+    return fail(HDET_ERR_INVALID_ARG, who, "the gradients' dtypes must be HDET_DTYPE_F32 or HDET_DTYPE_BF16");
+  if (d->device < 0) return fail(HDET_ERR_INVALID_ARG, who, "device must be >= 0");
+  if (!std::isfinite(d->grad_scale)) return fail(HDET_ERR_INVALID_ARG, who, "grad_scale must be finite");
+  if (d->piece_bytes < 0) return fail(HDET_ERR_INVALID_ARG, who, "piece_bytes must be >= 0");
+  if (d->hidden_row < d->width || d->weight_row < d->width || (d->d_hidden && d->d_hidden_row < d->width) ||
+      (d->d_weight && d->d_weight_row < d->width))
+    return fail(HDET_ERR_INVALID_ARG, who, "a row stride is smaller than width");
+  const int64_t strides[] = {d->hidden_stride, d->weight_stride, d->target_stride, d->token_loss_stride, d->d_hidden_stride,
+                             d->d_weight_stride};
+  for (const int64_t s : strides)
+    if (s < 0) return fail(HDET_ERR_INVALID_ARG, who, "negative stride");
+  return HDET_OK;
+}
+
+int check_pointers(const char* who, const hdet_token_loss_args* d) {
+  if (!d->weight || !d->loss || (d->n_tokens > 0 && (!d->hidden || !d->targets)))
+    return fail(HDET_ERR_INVALID_ARG, who, "a pointer is NULL");
+  const auto span = [&](int64_t rows, int64_t row) { return rows > 0 ? (rows - 1) * row + d->width : 0; };
+  if (d->n_replicas > 1) {
+    if ((d->hidden_stride && d->hidden_stride < span(d->n_tokens, d->hidden_row)) ||
+        (d->weight_stride && d->weight_stride < span(d->vocab, d->weight_row)) ||
+        (d->target_stride && d->target_stride < d->n_tokens) ||
+        (d->token_loss && d->token_loss_stride < d->n_tokens) ||
+        (d->d_hidden && d->d_hidden_stride < span(d->n_tokens, d->d_hidden_row)) ||
+        (d->d_weight && d->d_weight_stride < span(d->vocab, d->d_weight_row)))
+      return fail(HDET_ERR_INVALID_ARG, who, "a replica stride is smaller than one replica");
+  }
+  if (!aligned(d->hidden, 2) || !aligned(d->weight, 2) || !aligned(d->targets, d->target_dtype == HDET_DTYPE_I64 ? 8 : 4) ||
+      !aligned(d->loss, d->loss_dtype == HDET_DTYPE_F64 ? 8 : 4) || !aligned(d->token_loss, 4) ||
+      (d->d_hidden && !aligned(d->d_hidden, elem_size(d->d_hidden_dtype))) ||
+      (d->d_weight && !aligned(d->d_weight, elem_size(d->d_weight_dtype))))
+    return fail(HDET_ERR_ALIGN, who, "a pointer is not aligned to its element type");
+  return HDET_OK;
+}
+
+// Whether the table's boxes can be copied from where it is.
+bool table_fits(const hdet_token_loss_args* d) {
+  const bool many = d->n_replicas > 1;
+  return aligned(d->weight, 16) && d->weight_row % 8 == 0 && (!many || d->weight_stride % 8 == 0);
+}
+
+constexpr int64_t kDefaultPieceBytes = 512ll << 20;
+constexpr int kSlots = 148;      // tiles of a pair that run at once: two for each of 74 pairs of SMs
+
+// Sizes, launches and the workspace's layout; host arithmetic only, the same for the size query and the call.
+struct Plan {
+  int ctas, tile;
+  int64_t rows_pad, packed_row, m_tiles, n_tiles, join_blocks;
+  bool grads, two, h_two, w_two;
+  int64_t group;                  // replicas per launch
+  int64_t piece;                  // rows of the table per launch (a multiple of the tile)
+  int64_t n_pieces, h_len, h_splits;
+  bool h_slabs;
+  bool pack_table;
+  int64_t off_count, off_target, off_token, off_z, off_lse, off_part, off_sum, off_hidden, off_table, off_hi, off_lo,
+      off_slabs, total;
+};
+
+Plan plan_of(const hdet_token_loss_args* d) {
+  Plan q{};
+  const int64_t R = d->n_replicas, T = d->n_tokens, V = d->vocab, D = d->width;
+  q.ctas = T > 128 ? 2 : 1;
+  q.tile = 128 * q.ctas;
+  q.rows_pad = round_up(T > 0 ? T : 1, q.tile);
+  q.packed_row = round_up(D, 8);
+  q.m_tiles = q.rows_pad / q.tile;
+  q.n_tiles = div_up(V, q.tile);
+  q.join_blocks = q.rows_pad / 32;
+  q.grads = d->d_hidden || d->d_weight;
+  q.h_two = d->d_hidden && d->d_hidden_dtype == HDET_DTYPE_F32;
+  q.w_two = d->d_weight && d->d_weight_dtype == HDET_DTYPE_F32;
+  q.two = q.h_two || q.w_two;
+  q.pack_table = !table_fits(d);
+  if (q.grads) {
+    const int64_t budget = d->piece_bytes ? d->piece_bytes : kDefaultPieceBytes;
+    const int64_t v_all = q.n_tiles * q.tile, per_row = q.rows_pad * 2 * (q.two ? 2 : 1);
+    const int64_t fit = budget / (per_row * v_all);
+    if (fit >= 1) {
+      const int64_t groups = div_up(R, fit);
+      q.group = div_up(R, groups);
+      q.piece = v_all;
+    } else {
+      q.group = 1;
+      int64_t tiles = budget / (per_row * q.tile);
+      if (tiles < 1) tiles = 1;
+      tiles = div_up(q.n_tiles, div_up(q.n_tiles, tiles));       // equal pieces
+      q.piece = tiles * q.tile;
+    }
+    q.n_pieces = div_up(v_all, q.piece);
+    if (d->d_hidden) {
+      // dH's sums run over the piece, dW's over the tokens.  dH is split so that its tiles are not longer than an equal
+      // share of the launch's work: otherwise a few of them would run on alone.
+      const int64_t all = div_up(q.piece, kBlockK), h_tiles = q.group * q.m_tiles * div_up(D, q.tile);
+      const int64_t w_tiles = d->d_weight ? q.group * (q.piece / q.tile) * div_up(D, q.tile) : 0;
+      const int64_t work = h_tiles * all * (q.h_two ? 2 : 1) + w_tiles * div_up(T, kBlockK) * (q.w_two ? 2 : 1);
+      int64_t share = work / (kSlots * (3 - q.ctas)) / (q.h_two ? 2 : 1);
+      if (share < 16) share = 16;
+      q.h_len = div_up(all, div_up(all, share));
+      q.h_splits = div_up(all, q.h_len);
+      q.h_slabs = q.h_splits > 1 || q.n_pieces > 1;
+    }
+  }
+  int64_t at = round_up(sizeof(Control), 256);
+  const auto take = [&](int64_t bytes) { const int64_t o = at; at = round_up(at + bytes, 256); return o; };
+  q.off_count = take(4 * R);
+  q.off_target = take(4 * R * q.rows_pad);
+  q.off_token = take(4 * R * q.rows_pad);
+  q.off_z = take(4 * R * q.rows_pad);
+  q.off_lse = take(4 * R * q.rows_pad);
+  q.off_part = take(8 * R * q.n_tiles * q.rows_pad);
+  q.off_sum = take(8 * R * q.join_blocks);
+  q.off_hidden = take(2 * R * q.rows_pad * q.packed_row);
+  if (q.pack_table) q.off_table = take(2 * (d->n_replicas > 1 && d->weight_stride ? R : 1) * V * q.packed_row);
+  if (q.grads) {
+    q.off_hi = take(2 * q.group * q.rows_pad * q.piece);
+    if (q.two) q.off_lo = take(2 * q.group * q.rows_pad * q.piece);
+    if (q.h_slabs) q.off_slabs = take(4 * q.h_splits * q.group * q.rows_pad * D);
+  }
+  q.total = at;
+  return q;
+}
+
+struct DeviceScope {
+  int prev = -1;
+  bool switched = false;
+  cudaError_t err = cudaSuccess;
+  explicit DeviceScope(int dev) {
+    err = cudaGetDevice(&prev);
+    if (err == cudaSuccess && prev != dev) {
+      err = cudaSetDevice(dev);
+      switched = err == cudaSuccess;
+    }
+  }
+  ~DeviceScope() { if (switched) cudaSetDevice(prev); }
+};
+
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+constexpr int kMaxDevices = 64;
+std::mutex g_mutex;
+EncodeTiled g_encode = nullptr;
+bool g_ready[kMaxDevices];
+
+// Once per process: the driver's tensor-map encoder.  Once per device: the kernels' shared-memory sizes.
+cudaError_t prepare(int device) {
+  std::lock_guard<std::mutex> lock(g_mutex);
+  if (!g_encode) {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found);
+    if (e != cudaSuccess) return e;
+    if (found != cudaDriverEntryPointSuccess || !f) return cudaErrorNotSupported;
+    g_encode = reinterpret_cast<EncodeTiled>(f);
+  }
+  if (device < kMaxDevices && g_ready[device]) return cudaSuccess;
+  const void* kernels[] = {(const void*)gemm_kernel<1, kStats>, (const void*)gemm_kernel<1, kProbs>, (const void*)gemm_kernel<1, kGrads>,
+                           (const void*)gemm_kernel<2, kStats>, (const void*)gemm_kernel<2, kProbs>, (const void*)gemm_kernel<2, kGrads>};
+  for (const void* k : kernels) {
+    const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmem);
+    if (e != cudaSuccess) return e;
+  }
+  if (device < kMaxDevices) g_ready[device] = true;
+  return cudaSuccess;
+}
+
+// [z][y][x] bf16, x contiguous, copied in boxes of 64 x 64; what lies outside reads as zero.
+bool encode(CUtensorMap* map, const void* base, int64_t x, int64_t y, int64_t z, int64_t y_stride, int64_t z_stride) {
+  const cuuint64_t dims[3] = {(cuuint64_t)x, (cuuint64_t)y, (cuuint64_t)z};
+  const cuuint64_t strides[2] = {(cuuint64_t)y_stride * 2, (cuuint64_t)z_stride * 2};
+  const cuuint32_t box[3] = {64, 64, 1}, step[3] = {1, 1, 1};
+  return g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, step,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int PHASE>
+cudaError_t launch_gemm(const LossParams& p, int ctas, int64_t tiles, cudaStream_t st) {
+  if (tiles == 0) return cudaSuccess;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(tiles * ctas));
+  cfg.blockDim = dim3(kGemmThreads);
+  cfg.dynamicSmemBytes = kGemmSmem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = ctas;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return ctas == 1 ? cudaLaunchKernelEx(&cfg, gemm_kernel<1, PHASE>, p) : cudaLaunchKernelEx(&cfg, gemm_kernel<2, PHASE>, p);
+}
+
+Out out_of(void* p, int dtype, int64_t stride, int64_t row, bool many, bool accumulate) {
+  Out o{};
+  o.p = p;
+  o.f32 = dtype == HDET_DTYPE_F32;
+  o.stride = many ? stride : 0;
+  o.row = row;
+  o.accumulate = accumulate;
+  const int per16 = 16 / elem_size(dtype);
+  o.vec = aligned(p, 16) && row % per16 == 0 && o.stride % per16 == 0;
+  return o;
+}
+
+}  // namespace
+
+extern "C" HDET_API int hdet_token_loss_workspace(const hdet_token_loss_args* d, int64_t* bytes) {
+  const char* who = "hdet_token_loss_workspace";
+  if (!bytes) return fail(HDET_ERR_INVALID_ARG, who, "bytes is NULL");
+  *bytes = 0;
+  if (const int rc = check(who, d)) return rc;
+  *bytes = plan_of(d).total;
+  return HDET_OK;
+}
+
+extern "C" HDET_API int hdet_token_loss(const hdet_token_loss_args* d, void* workspace, int64_t workspace_bytes, void* stream) {
+  const char* who = "hdet_token_loss";
+  hdet::TraceRange trace(who);
+  if (const int rc = check(who, d)) return rc;
+  if (const int rc = check_pointers(who, d)) return rc;
+  const Plan q = plan_of(d);
+  if (!workspace || workspace_bytes < q.total)
+    return fail(HDET_ERR_INVALID_ARG, who, "the workspace is NULL or smaller than hdet_token_loss_workspace says");
+  if (!aligned(workspace, 256)) return fail(HDET_ERR_ALIGN, who, "the workspace is not 256-byte aligned");
+  if (q.m_tiles * q.n_tiles * d->n_replicas * q.ctas > INT32_MAX || q.rows_pad * q.packed_row * 2 >= (1ll << 40) ||
+      d->weight_row * d->vocab * 2 >= (1ll << 40) || d->weight_stride * 2 >= (1ll << 40))
+    return fail(HDET_ERR_UNSUPPORTED, who, "too many tiles, or a stride of 2^40 bytes or more");
+  DeviceScope scope(d->device);
+  if (scope.err != cudaSuccess) return fail_cuda(who, scope.err);
+  cudaError_t e = prepare(d->device);
+  if (e != cudaSuccess) return fail_cuda(who, e);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  char* ws = static_cast<char*>(workspace);
+  const bool many = d->n_replicas > 1;
+  const bool shared_table = !many || d->weight_stride == 0;
+
+  LossParams p{};
+  p.n_replicas = d->n_replicas;
+  p.vocab = (int)d->vocab; p.width = (int)d->width; p.n_tokens = (int)d->n_tokens; p.rows_pad = (int)q.rows_pad;
+  p.weight_shared = shared_table;
+  p.grad_scale = d->grad_scale;
+  p.count = reinterpret_cast<int*>(ws + q.off_count);
+  p.target = reinterpret_cast<int*>(ws + q.off_target);
+  p.token_of = reinterpret_cast<int*>(ws + q.off_token);
+  p.z_target = reinterpret_cast<float*>(ws + q.off_z);
+  p.lse2 = reinterpret_cast<float*>(ws + q.off_lse);
+  p.part = reinterpret_cast<float2*>(ws + q.off_part);
+  p.loss = d->loss;
+  p.loss_f64 = d->loss_dtype == HDET_DTYPE_F64;
+  p.control = reinterpret_cast<Control*>(ws);
+  if (d->d_hidden) p.d_hidden = out_of(d->d_hidden, d->d_hidden_dtype, d->d_hidden_stride, d->d_hidden_row, many, false);
+  if (d->d_weight) p.d_weight = out_of(d->d_weight, d->d_weight_dtype, d->d_weight_stride, d->d_weight_row, many, d->accumulate != 0);
+
+  // packing
+  PackParams k{};
+  k.hidden = static_cast<const __nv_bfloat16*>(d->hidden);
+  k.hidden_stride = many ? d->hidden_stride : 0;
+  k.hidden_row = d->hidden_row;
+  k.targets = d->targets;
+  k.target_stride = many ? d->target_stride : 0;
+  k.wide = d->target_dtype == HDET_DTYPE_I64;
+  k.hidden_vec = aligned(d->hidden, 16) && d->hidden_row % 8 == 0 && k.hidden_stride % 8 == 0 && d->width % 8 == 0;
+  k.d_hidden = p.d_hidden;
+  k.d_hidden_vec = p.d_hidden.vec && d->width % 8 == 0;
+  k.n_tokens = p.n_tokens; k.vocab = p.vocab; k.width = p.width; k.rows_pad = p.rows_pad; k.row_tile = q.tile;
+  k.packed_row = (int)q.packed_row;
+  k.packed = reinterpret_cast<__nv_bfloat16*>(ws + q.off_hidden);
+  k.count = const_cast<int*>(p.count);
+  k.target = const_cast<int*>(p.target);
+  k.token_of = const_cast<int*>(p.token_of);
+  k.token_loss = static_cast<float*>(d->token_loss);
+  k.token_loss_stride = many ? d->token_loss_stride : 0;
+  k.control = p.control;
+  const unsigned pack_blocks = (unsigned)(d->n_tokens > 0 ? div_up(d->n_tokens, kPackRows) : 1);
+  pack_kernel<<<dim3(pack_blocks, d->n_replicas), 256, 0, st>>>(k);
+
+  const __nv_bfloat16* table = static_cast<const __nv_bfloat16*>(d->weight);
+  int64_t table_row = d->weight_row, table_stride = shared_table ? d->weight_row * d->vocab : d->weight_stride;
+  const int tables = shared_table ? 1 : d->n_replicas;
+  if (q.pack_table) {
+    __nv_bfloat16* packed = reinterpret_cast<__nv_bfloat16*>(ws + q.off_table);
+    pack_table_kernel<<<dim3((unsigned)div_up(d->vocab, 8), tables), 256, 0, st>>>(table, shared_table ? 0 : d->weight_stride,
+                                                                                table_row, p.vocab, p.width, k.packed_row, packed);
+    table = packed;
+    table_row = q.packed_row;
+    table_stride = q.packed_row * d->vocab;
+  }
+  bool maps = encode(&p.hidden, k.packed, d->width, q.rows_pad, d->n_replicas, q.packed_row, q.rows_pad * q.packed_row) &&
+              encode(&p.weight, table, d->width, d->vocab, tables, table_row, table_stride);
+  if (maps && q.grads) {
+    p.g_hi = reinterpret_cast<__nv_bfloat16*>(ws + q.off_hi);
+    p.g_lo = q.two ? reinterpret_cast<__nv_bfloat16*>(ws + q.off_lo) : nullptr;
+    maps = encode(&p.grad_hi, p.g_hi, q.piece, q.rows_pad, q.group, q.piece, q.rows_pad * q.piece) &&
+           (!q.two || encode(&p.grad_lo, p.g_lo, q.piece, q.rows_pad, q.group, q.piece, q.rows_pad * q.piece));
+  }
+  if (!maps) return fail(HDET_ERR_CUDA, who, "the driver refused a tensor map");
+
+  // the loss
+  p.r0 = 0; p.n_r = d->n_replicas;
+  p.v0 = 0; p.v_len = p.vocab;
+  p.m_tiles = (int)q.m_tiles; p.n_tiles = (int)q.n_tiles;
+  e = cudaGetLastError();
+  if (e == cudaSuccess && d->n_tokens > 0) e = launch_gemm<kStats>(p, q.ctas, q.m_tiles * q.n_tiles * d->n_replicas, st);
+  if (e != cudaSuccess) return fail_cuda(who, e);
+  JoinParams f{};
+  f.count = p.count; f.token_of = p.token_of; f.part = p.part; f.z_target = p.z_target; f.lse2 = p.lse2;
+  f.token_loss = k.token_loss; f.token_loss_stride = k.token_loss_stride;
+  f.block_sum = reinterpret_cast<double*>(ws + q.off_sum);
+  f.rows_pad = p.rows_pad; f.n_tiles = p.n_tiles;
+  f.loss = d->loss; f.loss_f64 = p.loss_f64; f.control = p.control;
+  join_kernel<<<dim3((unsigned)q.join_blocks, d->n_replicas), dim3(32, 32), 0, st>>>(f);
+
+  // the gradients, piece by piece
+  if (q.grads) {
+    p.slabs = reinterpret_cast<float*>(ws + q.off_slabs);
+    p.v_pitch = (int)q.piece;
+    p.h_two = q.h_two; p.w_two = q.w_two;
+    p.h_slabs = q.h_slabs;
+    p.h_splits = (int)q.h_splits; p.h_len = (int)q.h_len;
+    p.h_tiles_m = (int)q.m_tiles; p.h_tiles_n = p.w_tiles_n = (int)div_up(d->width, q.tile);
+    for (int64_t r0 = 0; r0 < d->n_replicas; r0 += q.group) {
+      p.r0 = (int)r0;
+      p.n_r = (int)(d->n_replicas - r0 < q.group ? d->n_replicas - r0 : q.group);
+      for (int64_t piece = 0; piece < q.n_pieces; ++piece) {
+        p.v0 = (int)(piece * q.piece);
+        p.v_len = (int)(d->vocab - p.v0 < q.piece ? d->vocab - p.v0 : q.piece);
+        p.n_tiles = (int)div_up(p.v_len, q.tile);
+        p.w_tiles_m = d->d_weight ? p.n_tiles : 0;
+        p.h_jobs = d->d_hidden && d->n_tokens > 0 ? p.h_splits * p.n_r * p.h_tiles_m * p.h_tiles_n : 0;
+        p.h_add = piece > 0;
+        if (d->n_tokens > 0) e = launch_gemm<kProbs>(p, q.ctas, (int64_t)p.n_r * p.m_tiles * p.n_tiles, st);
+        if (e == cudaSuccess)
+          e = launch_gemm<kGrads>(p, q.ctas, p.h_jobs + (int64_t)p.n_r * p.w_tiles_m * p.w_tiles_n, st);
+        if (e != cudaSuccess) return fail_cuda(who, e);
+      }
+      if (d->d_hidden && d->n_tokens > 0 && q.h_slabs)
+        join_hidden_kernel<<<dim3((unsigned)q.rows_pad, p.n_r), 256, 0, st>>>(p);
+    }
+  }
+  e = cudaGetLastError();
+  return e == cudaSuccess ? HDET_OK : fail_cuda(who, e);
+}
