@@ -40,6 +40,44 @@ __device__ __forceinline__ uint32_t in_leader(uint32_t smem) {
   return r;
 }
 
+// Shared address of the same variable in the cluster's CTA `rank`.
+__device__ __forceinline__ uint32_t in_cta(uint32_t smem, uint32_t rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem), "r"(rank));
+  return r;
+}
+
+// A store to, and an arrival at, shared memory of any CTA of the cluster (addresses from in_cta); the arrival releases what
+// this thread wrote before it to threads that wait with wait_cluster.
+__device__ __forceinline__ void store_cluster(uint32_t at, int value) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(value) : "memory");
+}
+
+__device__ __forceinline__ void arrive_cluster(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+__device__ __forceinline__ bool try_wait_cluster(uint32_t bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile(
+      "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+      : "=r"(done)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return done != 0;
+}
+
+// bulk::barrier_wait for arrivals from anywhere in the cluster; as bounded as that.
+__device__ __forceinline__ bool wait_cluster(uint32_t bar, uint32_t parity, long long limit_cycles = bulk::kWaitLimitCycles) {
+  if (try_wait_cluster(bar, parity)) return true;
+  const long long start = clock64();
+  for (;;) {
+    for (int i = 0; i < 32; ++i)
+      if (try_wait_cluster(bar, parity)) return true;
+    if (clock64() - start > limit_cycles) return false;
+  }
+}
+
 // One 64 x 64 box into this CTA's shared memory; completion counted in bytes on `bar` (in the leader's CTA for a pair).
 // Coordinates: x in elements along the contiguous axis (a multiple of 64 here, so 16-byte aligned), y, z.
 template <int CTAS>
