@@ -18,6 +18,7 @@
 // target is unlikely.  Its relative error, 2^-9 a value, is that of a bf16 gradient's own rounding.  For fp32 gradients
 // that would be too coarse: G is written as a pair, G = hi + lo with both bf16 (2^-17), and the products run over both.
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 
 #include <climits>
 #include <cmath>
@@ -46,7 +47,7 @@ constexpr long long kDrainLimitCycles = 200000000ll;
 __host__ __device__ constexpr int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 __host__ __device__ constexpr int64_t round_up(int64_t a, int64_t b) { return div_up(a, b) * b; }
 
-enum Phase { kStats, kProbs, kGrads };
+enum Phase { kStats, kNumerators, kProbs, kGrads };
 
 struct Control {            // first bytes of the workspace; zeroed by pack_kernel
   unsigned status;          // a bounded wait ran out
@@ -73,7 +74,8 @@ struct LossParams {
   const int* token_of;
   float* z_target;
   float* lse2;              // lse in units of log 2
-  float2* part;             // [replica][halves of column tiles][rows_pad]: maximum, sum of exp
+  float2* part;             // [replica][rows_pad][halves of column tiles]: maximum, sum of exp
+  float* row_loss;          // [replica][rows_pad]
   // piece of the vocabulary
   int r0, n_r;              // replicas of this launch
   int v0, v_len, v_pitch;   // first row of the table, rows, pitch of G
@@ -86,6 +88,8 @@ struct LossParams {
   bool h_slabs, h_add;      // dH goes to fp32 partial sums; added to what an earlier piece left
   float* slabs;             // [split][replica of the launch][rows_pad][width]
   Out d_hidden, d_weight;
+  float* token_loss;
+  int64_t token_loss_stride;
   void* loss;
   int loss_f64;
   Control* control;
@@ -168,6 +172,11 @@ __device__ __forceinline__ bool find_job(const LossParams& p, const int* counts,
 
 __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+__device__ __forceinline__ uint32_t f16_pair(float lo, float hi) {
+  const __half2 v = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
@@ -271,6 +280,47 @@ __device__ __forceinline__ void load_columns(uint32_t tmem, float (&x)[2][32]) {
   tmem_load_wait(x[1]);
 }
 
+__device__ __forceinline__ float largest(const float (&x)[2][32]) {
+  float top[4] = {x[0][0], x[0][1], x[1][0], x[1][1]};
+#pragma unroll
+  for (int i = 2; i < 32; i += 2) {
+    top[0] = fmaxf(top[0], x[0][i]); top[1] = fmaxf(top[1], x[0][i + 1]);
+    top[2] = fmaxf(top[2], x[1][i]); top[3] = fmaxf(top[3], x[1][i + 1]);
+  }
+  return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+}
+
+// Columns at or behind the vocabulary's end become -inf (nothing of theirs is left in exp).
+__device__ __forceinline__ void cut_columns(float (&x)[2][32], int v, int vocab) {
+  if (v + 64 <= vocab) return;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) {
+    if (v + i >= vocab) x[0][i] = -INFINITY;
+    if (v + 32 + i >= vocab) x[1][i] = -INFINITY;
+  }
+}
+
+__device__ __forceinline__ void pick_column(const float (&x)[2][32], int v, int target, float& picked) {
+  if ((unsigned)(target - v) >= 64u) return;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) {
+    if (v + i == target) picked = x[0][i];
+    if (v + 32 + i == target) picked = x[1][i];
+  }
+}
+
+// exp(x - shift) in place, `shift` in units of log 2; returns the sum.
+__device__ __forceinline__ float exponentials(float (&x)[2][32], float shift) {
+  float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int i = 0; i < 32; i += 2) {
+    x[0][i] = exp2_fast(fmaf(x[0][i], kLog2e, -shift)); x[0][i + 1] = exp2_fast(fmaf(x[0][i + 1], kLog2e, -shift));
+    x[1][i] = exp2_fast(fmaf(x[1][i], kLog2e, -shift)); x[1][i + 1] = exp2_fast(fmaf(x[1][i + 1], kLog2e, -shift));
+    s[0] += x[0][i]; s[1] += x[0][i + 1]; s[2] += x[1][i]; s[3] += x[1][i + 1];
+  }
+  return (s[0] + s[1]) + (s[2] + s[3]);
+}
+
 // `tmem`: the reader's lanes, at the first column of its half; `half`: that column within the tile.
 template <int CTAS>
 __device__ __forceinline__ void stats_epilogue(const LossParams& p, const Job& j, uint32_t tmem, int row, int half) {
@@ -283,38 +333,56 @@ __device__ __forceinline__ void stats_epilogue(const LossParams& p, const Job& j
   for (int c = 0; c < kCols; c += 64) {
     float x[2][32];
     load_columns(tmem + c, x);
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int v = v0 + c + 32 * h;
-      if (v + 32 > p.vocab) {
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-          if (v + i >= p.vocab) x[h][i] = -INFINITY;
-      }
-      if ((unsigned)(target - v) < 32u) {
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-          if (v + i == target) picked = x[h][i];
-      }
-    }
-    float here[4] = {x[0][0], x[0][1], x[1][0], x[1][1]};
-#pragma unroll
-    for (int i = 2; i < 32; i += 2) {
-      here[0] = fmaxf(here[0], x[0][i]); here[1] = fmaxf(here[1], x[0][i + 1]);
-      here[2] = fmaxf(here[2], x[1][i]); here[3] = fmaxf(here[3], x[1][i + 1]);
-    }
-    const float now = fmaxf(top, fmaxf(fmaxf(here[0], here[1]), fmaxf(here[2], here[3])));
+    cut_columns(x, v0 + c, p.vocab);
+    pick_column(x, v0 + c, target, picked);
+    const float now = fmaxf(top, largest(x));
     const float shift = now == -INFINITY ? 0.0f : now * kLog2e;    // nothing finite yet: exp of -inf, not of NaN
-    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int i = 0; i < 32; i += 2) {
-      s[0] += exp2_fast(fmaf(x[0][i], kLog2e, -shift)); s[1] += exp2_fast(fmaf(x[0][i + 1], kLog2e, -shift));
-      s[2] += exp2_fast(fmaf(x[1][i], kLog2e, -shift)); s[3] += exp2_fast(fmaf(x[1][i + 1], kLog2e, -shift));
-    }
-    sum = fmaf(sum, exp2_fast(fmaf(top, kLog2e, -shift)), (s[0] + s[1]) + (s[2] + s[3]));
+    const float s = exponentials(x, shift);
+    sum = fmaf(sum, exp2_fast(fmaf(top, kLog2e, -shift)), s);
     top = now;
   }
-  p.part[((int64_t)j.r * p.n_tiles * 2 + v0 / kCols) * p.rows_pad + row] = make_float2(top, sum);
+  p.part[at * 2 * p.n_tiles + v0 / kCols] = make_float2(top, sum);
+  if (target >= v0 && target < v0 + kCols) p.z_target[at] = picked;
+}
+
+// The same, and the numerators exp(z - maximum of the half tile's row) go to the workspace, where scale_kernel turns them
+// into G.  They are fp16: between 0 and 1 it is off by 2^-12 of the value, or 2^-25 below 2^-14, less than the rounding of
+// G to bf16 that follows.  The sum is taken before that rounding.  The columns are read twice, once for the maximum.
+template <int CTAS>
+__device__ __forceinline__ void numerators_epilogue(const LossParams& p, const Job& j, uint32_t tmem, int row, int half,
+                                                    uint32_t staging, int lane) {
+  constexpr int kCols = 64 * CTAS;
+  const int64_t at = (int64_t)j.r * p.rows_pad + row;
+  const int target = p.target[at];
+  const int v0 = j.n0 + half;
+  float top = -INFINITY, sum = 0.0f, picked = 0.0f;
+#pragma unroll 1
+  for (int c = 0; c < kCols; c += 64) {
+    float x[2][32];
+    load_columns(tmem + c, x);
+    cut_columns(x, v0 + c, p.vocab);
+    pick_column(x, v0 + c, target, picked);
+    top = fmaxf(top, largest(x));
+  }
+  const float shift = top == -INFINITY ? 0.0f : top * kLog2e;
+  Rows rows;
+  rows.base = reinterpret_cast<char*>(p.g_hi);
+  rows.offset = (((int64_t)(j.r - p.r0) * p.rows_pad + row) * p.v_pitch + v0) * 2;
+  rows.on = 0xffffffffu;
+#pragma unroll 1
+  for (int c = 0; c < kCols; c += 64) {
+    float x[2][32];
+    load_columns(tmem + c, x);
+    cut_columns(x, v0 + c, p.vocab);
+    sum += exponentials(x, shift);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float* y = &x[k / 4][8 * (k % 4)];
+      stage(staging, lane, k, make_uint4(f16_pair(y[0], y[1]), f16_pair(y[2], y[3]), f16_pair(y[4], y[5]), f16_pair(y[6], y[7])));
+    }
+    write_staged(rows, staging, lane, 2 * c, 2 * kCols);
+  }
+  p.part[at * 2 * p.n_tiles + v0 / kCols] = make_float2(top, sum);
   if (target >= v0 && target < v0 + kCols) p.z_target[at] = picked;
 }
 
@@ -624,6 +692,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
       const uint32_t at = tmem + b * 128 * CTAS + half + ((uint32_t)(quarter * 32) << 16);
       const int row = j.m0 + 128 * (int)rank + quarter * 32 + lane;
       if constexpr (PHASE == kStats) stats_epilogue<CTAS>(p, j, at, row, half);
+      else if constexpr (PHASE == kNumerators) numerators_epilogue<CTAS>(p, j, at, row, half, staging, lane);
       else if constexpr (PHASE == kProbs) probs_epilogue<CTAS>(p, j, at, row, half, sh.count[j.r], staging, lane);
       else grads_epilogue<CTAS>(p, j, at, row, half, sh.count[j.r], staging, lane);
       if (j.k_blocks > 0) {
@@ -762,71 +831,131 @@ __global__ void __launch_bounds__(256) pack_table_kernel(const __nv_bfloat16* ta
 }
 
 // ------------------------------------------------------------------------------------------------ joining
-struct JoinParams {
-  const int *count, *token_of;
-  const float2* part;
-  const float* z_target;
-  float* lse2;
-  float* token_loss;
-  int64_t token_loss_stride;
-  double* block_sum;        // [replica][blocks]
-  int rows_pad, n_tiles;
-  void* loss;
-  int loss_f64;
-  Control* control;
-};
-
-// 32 rows a block, the column tiles of a row spread over 32 threads: lse = max + log sum exp over the tiles, in their
-// order within a thread and the threads' order after that.  The last block of a replica adds the blocks' sums (fp64, in
-// their order) and writes the mean.
-__global__ void __launch_bounds__(1024) join_kernel(const JoinParams p) {
-  __shared__ float2 s_part[32][33];
-  const int r = blockIdx.y, x = threadIdx.x, y = threadIdx.y;
-  const int row = blockIdx.x * 32 + x, count = p.count[r];
-  float top = -INFINITY, sum = 0.0f;
-  const auto add = [&](float2 o) {
+struct Lse {
+  float top, sum;           // sum of exp(z - top)
+  __device__ __forceinline__ void add(float2 o) {
     const float now = fmaxf(top, o.x);
     const float shift = now == -INFINITY ? 0.0f : now;
     sum = sum * exp2_fast((top - shift) * kLog2e) + o.y * exp2_fast((o.x - shift) * kLog2e);
     top = now;
-  };
-  if (row < count) {
-    const float2* part = p.part + (int64_t)r * p.n_tiles * p.rows_pad + row;
-    for (int n = y; n < p.n_tiles; n += 32) add(part[(int64_t)n * p.rows_pad]);
   }
-  s_part[y][x] = make_float2(top, sum);
+  __device__ __forceinline__ void add_warp() {     // over a warp's lanes, in a fixed order
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) add(make_float2(__shfl_xor_sync(0xffffffffu, top, o), __shfl_xor_sync(0xffffffffu, sum, o)));
+  }
+  __device__ __forceinline__ float lse2() const { return fmaf(top, kLog2e, log2f(sum)); }
+};
+
+// A row's loss, where it belongs.
+__device__ __forceinline__ void write_row(const LossParams& p, int r, int row, const Lse& l) {
+  const int64_t at = (int64_t)r * p.rows_pad + row;
+  const float loss = l.top + logf(l.sum) - p.z_target[at];
+  p.row_loss[at] = loss;
+  if (p.token_loss) p.token_loss[r * p.token_loss_stride + p.token_of[at]] = loss;
+}
+
+// After a block has written its rows' losses: the last of a replica's `blocks` adds them up (fp64, in a fixed order) and
+// writes the mean.  256 threads.
+__device__ __forceinline__ void finish_block(const LossParams& p, int r, unsigned blocks) {
+  __shared__ bool s_last;
+  __shared__ double s_sum[8];
   __syncthreads();
-  if (y != 0) return;
-  double loss = 0.0;
-  if (row < count) {
-    for (int k = 1; k < 32; ++k) add(s_part[k][x]);
-    const int64_t at = (int64_t)r * p.rows_pad + row;
-    const float lse = top + logf(sum);
-    p.lse2[at] = fmaf(top, kLog2e, log2f(sum));
-    const float l = lse - p.z_target[at];
-    if (p.token_loss) p.token_loss[r * p.token_loss_stride + p.token_of[at]] = l;
-    loss = l;
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, o);
-  unsigned before = 0;
-  if (x == 0) {
-    p.block_sum[(int64_t)r * gridDim.x + blockIdx.x] = loss;
+  if (threadIdx.x == 0) {
     __threadfence();
-    before = atomicAdd(&p.control->done[r], 1u);
+    s_last = atomicAdd(&p.control->done[r], 1u) == blocks - 1;
   }
-  before = __shfl_sync(0xffffffffu, before, 0);
-  if (before != gridDim.x - 1) return;
+  __syncthreads();
+  if (!s_last) return;
   __threadfence();
-  double total = 0.0;
-  for (int b = x; b < (int)gridDim.x; b += 32) total += __ldcg(p.block_sum + (int64_t)r * gridDim.x + b);
+  const int count = p.count[r];
+  double sum = 0.0;
+  for (int row = threadIdx.x; row < count; row += 256) sum += (double)__ldcg(p.row_loss + (int64_t)r * p.rows_pad + row);
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-  if (x == 0) {
-    double mean = count > 0 ? total / (double)count : 0.0;
-    if (__ldcg(&p.control->status)) mean = NAN;
-    if (p.loss_f64) static_cast<double*>(p.loss)[r] = mean; else static_cast<float*>(p.loss)[r] = (float)mean;
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = sum;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  for (int w = 1; w < 8; ++w) sum += s_sum[w];
+  double mean = count > 0 ? sum / (double)count : 0.0;
+  if (__ldcg(&p.control->status)) mean = NAN;
+  if (p.loss_f64) static_cast<double*>(p.loss)[r] = mean; else static_cast<float*>(p.loss)[r] = (float)mean;
+}
+
+// lse and loss of a row from its parts, one warp a row.
+__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ LossParams p) {
+  const int r = blockIdx.y, row = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (row < p.count[r]) {
+    const int64_t at = (int64_t)r * p.rows_pad + row;
+    const int n = 2 * p.n_tiles;
+    const float2* part = p.part + at * n;
+    Lse l{-INFINITY, 0.0f};
+#pragma unroll 4
+    for (int i = lane; i < n; i += 32) l.add(part[i]);
+    l.add_warp();
+    if (lane == 0) {
+      p.lse2[at] = l.lse2();
+      write_row(p, r, row, l);
+    }
   }
+  finish_block(p, r, gridDim.x);
+}
+
+// One block a row: lse and loss as above, then the row's numerators become G in place: exp(z - m) exp(m - lse), bf16.  The
+// target's own value comes from its fp32 logit: where it is likely, p - 1 is small and no rounding of p may reach it.
+// Rows behind the counted ones, up to the next 64, become zeros, since dW's sums run over them.
+template <int CTAS>
+__global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ LossParams p) {
+  constexpr int kCols = 64 * CTAS;
+  extern __shared__ float s_factor[];              // per half tile: exp(m - lse)
+  __shared__ Lse s_lse[8];
+  const int g = blockIdx.y, r = p.r0 + g, row = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int count = p.count[r], n = 2 * p.n_tiles;
+  uint4* values = reinterpret_cast<uint4*>(p.g_hi + ((int64_t)g * p.rows_pad + row) * p.v_pitch);
+  const int vectors = p.n_tiles * 2 * kCols / 8;
+  if (row < count) {
+    const int64_t at = (int64_t)r * p.rows_pad + row;
+    const float2* part = p.part + at * n;
+    Lse l{-INFINITY, 0.0f};
+    for (int i = threadIdx.x; i < n; i += 256) {
+      const float2 o = part[i];
+      s_factor[i] = o.x;
+      l.add(o);
+    }
+    l.add_warp();
+    if (lane == 0) s_lse[warp] = l;
+    __syncthreads();
+    l = s_lse[0];
+#pragma unroll
+    for (int w = 1; w < 8; ++w) l.add(make_float2(s_lse[w].top, s_lse[w].sum));
+    const float lse2 = l.lse2();
+    for (int i = threadIdx.x; i < n; i += 256) s_factor[i] = exp2_fast(fmaf(s_factor[i], kLog2e, -lse2));
+    if (threadIdx.x == 0) write_row(p, r, row, l);
+    __syncthreads();
+    const int target = p.target[at];
+    const float g_target = exp2_fast(fmaf(p.z_target[at], kLog2e, -lse2)) - 1.0f;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < vectors; i += 256) {
+      const uint4 u = values[i];
+      const float f = s_factor[i * 8 / kCols];
+      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+      float x[8];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&w[k]));
+        x[2 * k] = y.x * f;
+        x[2 * k + 1] = y.y * f;
+      }
+      if (i == target / 8) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (k == target % 8) x[k] = g_target;
+      }
+      values[i] = make_uint4(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]), bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7]));
+    }
+  } else if (row < (count + kBlockK - 1) / kBlockK * kBlockK) {
+    for (int i = threadIdx.x; i < vectors; i += 256) values[i] = make_uint4(0, 0, 0, 0);
+  }
+  finish_block(p, r, gridDim.x);
 }
 
 // dH: adds the partial sums over the vocabulary in their order, scales, rounds once and puts rows back at their tokens.
@@ -919,19 +1048,21 @@ bool table_fits(const hdet_token_loss_args* d) {
 }
 
 constexpr int64_t kDefaultPieceBytes = 512ll << 20;
+constexpr int64_t kMaxScaleTiles = 4096;      // scale_kernel keeps two factors a tile in shared memory (32 KB)
 constexpr int kSlots = 74;       // pairs of SMs: tiles that run at once
 
 // Sizes, launches and the workspace's layout; host arithmetic only, the same for the size query and the call.
 struct Plan {
   int ctas, tile;
-  int64_t rows_pad, packed_row, m_tiles, n_tiles, join_blocks;
+  int64_t rows_pad, packed_row, m_tiles, n_tiles;
   bool grads, two, h_two, w_two;
+  bool numerators;                // the logits are formed once: their exponentials wait in the workspace for lse
   int64_t group;                  // replicas per launch
   int64_t piece;                  // rows of the table per launch (a multiple of the tile)
   int64_t n_pieces, h_len, h_splits;
   bool h_slabs;
   bool pack_table;
-  int64_t off_count, off_target, off_token, off_z, off_lse, off_part, off_sum, off_hidden, off_table, off_hi, off_lo,
+  int64_t off_count, off_target, off_token, off_z, off_lse, off_part, off_loss, off_hidden, off_table, off_hi, off_lo,
       off_slabs, total;
 };
 
@@ -944,7 +1075,6 @@ Plan plan_of(const hdet_token_loss_args* d) {
   q.packed_row = round_up(D, 8);
   q.m_tiles = q.rows_pad / q.tile;
   q.n_tiles = div_up(V, q.tile);
-  q.join_blocks = q.rows_pad / 32;
   q.grads = d->d_hidden || d->d_weight;
   q.h_two = d->d_hidden && d->d_hidden_dtype == HDET_DTYPE_F32;
   q.w_two = d->d_weight && d->d_weight_dtype == HDET_DTYPE_F32;
@@ -966,6 +1096,9 @@ Plan plan_of(const hdet_token_loss_args* d) {
       q.piece = tiles * q.tile;
     }
     q.n_pieces = div_up(v_all, q.piece);
+    // With all of a replica's G in the workspace, and G in bf16, its place can hold the numerators until lse is known: a pass
+    // over 2 bytes a logit in place of 2 x width operations.  REPLACE_NUMER
+    q.numerators = q.n_pieces == 1 && !q.two && q.n_tiles <= kMaxScaleTiles;
     if (d->d_hidden) {
       // dH's sums run over the piece, dW's over the tokens.  dH is split so that its tiles are not longer than an equal
       // share of the launch's work: otherwise a few of them would run on alone.
@@ -987,7 +1120,7 @@ Plan plan_of(const hdet_token_loss_args* d) {
   q.off_z = take(4 * R * q.rows_pad);
   q.off_lse = take(4 * R * q.rows_pad);
   q.off_part = take(8 * R * 2 * q.n_tiles * q.rows_pad);
-  q.off_sum = take(8 * R * q.join_blocks);
+  q.off_loss = take(4 * R * q.rows_pad);
   q.off_hidden = take(2 * R * q.rows_pad * q.packed_row);
   if (q.pack_table) q.off_table = take(2 * (d->n_replicas > 1 && d->weight_stride ? R : 1) * V * q.packed_row);
   if (q.grads) {
@@ -1038,8 +1171,10 @@ cudaError_t prepare(int device, int* sms) {
     *sms = g_sms[device];
     return cudaSuccess;
   }
-  const void* kernels[] = {(const void*)gemm_kernel<1, kStats>, (const void*)gemm_kernel<1, kProbs>, (const void*)gemm_kernel<1, kGrads>,
-                           (const void*)gemm_kernel<2, kStats>, (const void*)gemm_kernel<2, kProbs>, (const void*)gemm_kernel<2, kGrads>};
+  const void* kernels[] = {(const void*)gemm_kernel<1, kStats>, (const void*)gemm_kernel<1, kNumerators>, (const void*)gemm_kernel<1, kProbs>,
+                           (const void*)gemm_kernel<1, kGrads>,
+                           (const void*)gemm_kernel<2, kStats>, (const void*)gemm_kernel<2, kNumerators>, (const void*)gemm_kernel<2, kProbs>,
+                           (const void*)gemm_kernel<2, kGrads>};
   for (const void* k : kernels) {
     const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmem);
     if (e != cudaSuccess) return e;
@@ -1137,6 +1272,9 @@ extern "C" HDET_API int hdet_token_loss(const hdet_token_loss_args* d, void* wor
   p.z_target = reinterpret_cast<float*>(ws + q.off_z);
   p.lse2 = reinterpret_cast<float*>(ws + q.off_lse);
   p.part = reinterpret_cast<float2*>(ws + q.off_part);
+  p.row_loss = reinterpret_cast<float*>(ws + q.off_loss);
+  p.token_loss = static_cast<float*>(d->token_loss);
+  p.token_loss_stride = many ? d->token_loss_stride : 0;
   p.loss = d->loss;
   p.loss_f64 = d->loss_dtype == HDET_DTYPE_F64;
   p.control = reinterpret_cast<Control*>(ws);
@@ -1160,8 +1298,8 @@ extern "C" HDET_API int hdet_token_loss(const hdet_token_loss_args* d, void* wor
   k.count = const_cast<int*>(p.count);
   k.target = const_cast<int*>(p.target);
   k.token_of = const_cast<int*>(p.token_of);
-  k.token_loss = static_cast<float*>(d->token_loss);
-  k.token_loss_stride = many ? d->token_loss_stride : 0;
+  k.token_loss = p.token_loss;
+  k.token_loss_stride = p.token_loss_stride;
   k.control = p.control;
   const unsigned pack_blocks = (unsigned)(d->n_tokens > 0 ? div_up(d->n_tokens, kPackRows) : 1);
   pack_kernel<<<dim3(pack_blocks, d->n_replicas), 256, 0, st>>>(k);
@@ -1189,23 +1327,19 @@ extern "C" HDET_API int hdet_token_loss(const hdet_token_loss_args* d, void* wor
 
   // the loss
   p.r0 = 0; p.n_r = d->n_replicas;
-  p.v0 = 0; p.v_len = p.vocab;
+  p.v0 = 0; p.v_len = p.vocab; p.v_pitch = (int)q.piece;
   p.m_tiles = (int)q.m_tiles; p.n_tiles = (int)q.n_tiles;
+  const bool any = d->n_tokens > 0;
   e = cudaGetLastError();
-  if (e == cudaSuccess && d->n_tokens > 0) e = launch_gemm<kStats>(p, q.ctas, q.m_tiles * q.n_tiles * d->n_replicas, sms, st);
+  if (e == cudaSuccess && !q.numerators) {
+    if (any) e = launch_gemm<kStats>(p, q.ctas, q.m_tiles * q.n_tiles * d->n_replicas, sms, st);
+    if (e == cudaSuccess) join_kernel<<<dim3((unsigned)(q.rows_pad / 8), d->n_replicas), 256, 0, st>>>(p);
+  }
   if (e != cudaSuccess) return fail_cuda(who, e);
-  JoinParams f{};
-  f.count = p.count; f.token_of = p.token_of; f.part = p.part; f.z_target = p.z_target; f.lse2 = p.lse2;
-  f.token_loss = k.token_loss; f.token_loss_stride = k.token_loss_stride;
-  f.block_sum = reinterpret_cast<double*>(ws + q.off_sum);
-  f.rows_pad = p.rows_pad; f.n_tiles = 2 * p.n_tiles;
-  f.loss = d->loss; f.loss_f64 = p.loss_f64; f.control = p.control;
-  join_kernel<<<dim3((unsigned)q.join_blocks, d->n_replicas), dim3(32, 32), 0, st>>>(f);
 
   // the gradients, piece by piece
   if (q.grads) {
     p.slabs = reinterpret_cast<float*>(ws + q.off_slabs);
-    p.v_pitch = (int)q.piece;
     p.h_two = q.h_two; p.w_two = q.w_two;
     p.h_slabs = q.h_slabs;
     p.h_splits = (int)q.h_splits; p.h_len = (int)q.h_len;
@@ -1218,14 +1352,26 @@ extern "C" HDET_API int hdet_token_loss(const hdet_token_loss_args* d, void* wor
         p.v_len = (int)(d->vocab - p.v0 < q.piece ? d->vocab - p.v0 : q.piece);
         p.n_tiles = (int)div_up(p.v_len, q.tile);
         p.w_tiles_m = d->d_weight ? p.n_tiles : 0;
-        p.h_jobs = d->d_hidden && d->n_tokens > 0 ? p.h_splits * p.n_r * p.h_tiles_m * p.h_tiles_n : 0;
+        p.h_jobs = d->d_hidden && any ? p.h_splits * p.n_r * p.h_tiles_m * p.h_tiles_n : 0;
         p.h_add = piece > 0;
-        if (d->n_tokens > 0) e = launch_gemm<kProbs>(p, q.ctas, (int64_t)p.n_r * p.m_tiles * p.n_tiles, sms, st);
+        const int64_t tiles = (int64_t)p.n_r * p.m_tiles * p.n_tiles;
+        if (!q.numerators) {
+          if (any) e = launch_gemm<kProbs>(p, q.ctas, tiles, sms, st);
+        } else {
+          if (any) e = launch_gemm<kNumerators>(p, q.ctas, tiles, sms, st);
+          if (e == cudaSuccess) {
+            const dim3 grid((unsigned)q.rows_pad, p.n_r);
+            const size_t factors = sizeof(float) * 2 * p.n_tiles;
+            if (q.ctas == 1) scale_kernel<1><<<grid, 256, factors, st>>>(p);
+            else scale_kernel<2><<<grid, 256, factors, st>>>(p);
+            e = cudaGetLastError();
+          }
+        }
         if (e == cudaSuccess)
           e = launch_gemm<kGrads>(p, q.ctas, p.h_jobs + (int64_t)p.n_r * p.w_tiles_m * p.w_tiles_n, sms, st);
         if (e != cudaSuccess) return fail_cuda(who, e);
       }
-      if (d->d_hidden && d->n_tokens > 0 && q.h_slabs)
+      if (d->d_hidden && any && q.h_slabs)
         join_hidden_kernel<<<dim3((unsigned)q.rows_pad, p.n_r), 256, 0, st>>>(p);
     }
   }
