@@ -339,54 +339,66 @@ def hdet_converge_static(tensors: Sequence[hdet_tensor], n_replicas: int, device
 HDET_MAX_TOKENS = 1 << 24
 HDET_MAX_VOCAB = 1 << 24
 HDET_MAX_WIDTH = 1 << 16
-_dtype_codes = {}
 
 
-def _code(tensor) -> int:
-    """HDET_DTYPE_* of a torch tensor."""
-    if not _dtype_codes:
+class _DtypeCodes(dict):
+    """torch dtype -> HDET_DTYPE_*; filled on first use, so that importing this module does not import torch."""
+
+    def __missing__(self, dtype):
         import torch
-        _dtype_codes.update({torch.float32: HDET_DTYPE_F32, torch.bfloat16: HDET_DTYPE_BF16, torch.float64: HDET_DTYPE_F64,
-                             torch.int32: HDET_DTYPE_I32, torch.int64: HDET_DTYPE_I64})
-    code = _dtype_codes.get(tensor.dtype)
-    if code is None:
-        raise ValueError(f"dtype {tensor.dtype} is not supported")
-    return code
+        self.update({torch.float32: HDET_DTYPE_F32, torch.bfloat16: HDET_DTYPE_BF16, torch.float64: HDET_DTYPE_F64,
+                     torch.int32: HDET_DTYPE_I32, torch.int64: HDET_DTYPE_I64})
+        if dtype not in self:
+            raise ValueError(f"dtype {dtype} is not supported")
+        return self[dtype]
 
 
-def _one_device(*tensors) -> int:
-    """Ordinal of the CUDA device that all tensors are on."""
-    device = tensors[0].device
-    for t in tensors:
-        if not t.is_cuda or t.device != device:
-            raise ValueError("all tensors must be on one CUDA device")
-    return device.index
+_dtype_code = _DtypeCodes()
 
 
-def _replica_stride(tensor, dims: int, n: int, what: str) -> int:
-    """Replica stride of [N, ...] (``dims`` + 1 axes), 0 for one copy without that axis; the last axis must be contiguous."""
+# The calls below are used once per token by a model that is sampled, so their checks read every attribute once.
+def _rows_layout(tensor, n: int, what: str):
+    """(replica stride, row stride) of [n, rows, width], or of [rows, width] (replica stride 0: one copy for all)."""
     shape, stride = tensor.shape, tensor.stride()
-    if shape[-1] > 1 and stride[-1] != 1:
+    axes = len(shape)
+    if axes == 3 and shape[0] == n:
+        replica = stride[0]
+    elif axes == 2:
+        replica = 0
+    else:
+        raise ValueError(f"{what}: expected 2 axes, or 3 with {n} replicas first")
+    width = shape[-1]
+    if stride[-1] != 1 and width > 1:
         raise ValueError(f"{what}: the last axis must be contiguous")
-    if len(shape) == dims:
+    return replica, (stride[-2] if shape[-2] > 1 else width)
+
+
+def _ids_stride(tensor, n: int, what: str) -> int:
+    """Replica stride of [n, T] (or [T]: 0)."""
+    shape, stride = tensor.shape, tensor.stride()
+    if stride[-1] != 1 and shape[-1] > 1:
+        raise ValueError(f"{what}: the last axis must be contiguous")
+    if len(shape) == 1:
         return 0
-    if len(shape) != dims + 1 or shape[0] != n:
-        raise ValueError(f"{what}: expected {dims} axes, or {dims + 1} with {n} replicas first")
+    if len(shape) != 2 or shape[0] != n:
+        raise ValueError(f"{what}: expected 1 axis, or 2 with {n} replicas first")
     return stride[0]
 
 
-def _row_stride(tensor, width: int) -> int:
-    return tensor.stride(-2) if tensor.shape[-2] > 1 else width
-
-
 def _embedding(tokens, rows, table, n: int, scale: float) -> hdet_embedding:
-    T, D, V = rows.shape[-2], rows.shape[-1], table.shape[-2]
-    if tokens.shape[-1] != T or table.shape[-1] != D:
+    shape = rows.shape
+    T, D = shape[-2], shape[-1]
+    V, width = table.shape[-2:]
+    if tokens.shape[-1] != T or width != D:
         raise ValueError("tokens, rows and table disagree on the number of tokens or the width")
-    return hdet_embedding(
-        tokens.data_ptr(), rows.data_ptr(), table.data_ptr(), T, V, D, _replica_stride(tokens, 1, n, "tokens"),
-        _replica_stride(rows, 2, n, "rows"), _row_stride(rows, D), _replica_stride(table, 2, n, "table"),
-        _row_stride(table, D), scale, n, _code(tokens), _code(rows), _code(table), _one_device(tokens, rows, table), 0)
+    device = tokens.get_device()
+    if device < 0 or rows.get_device() != device or table.get_device() != device:
+        raise ValueError("all tensors must be on one CUDA device")
+    rows_stride, rows_row = _rows_layout(rows, n, "rows")
+    table_stride, table_row = _rows_layout(table, n, "table")
+    return hdet_embedding(tokens.data_ptr(), rows.data_ptr(), table.data_ptr(), T, V, D, _ids_stride(tokens, n, "tokens"),
+                          rows_stride, rows_row, table_stride, table_row, scale, n, _dtype_code[tokens.dtype],
+                          _dtype_code[rows.dtype], _dtype_code[table.dtype], device)
 
 
 def hdet_embed(tokens, table, out, scale: float = 1.0, stream: int = 0) -> None:
@@ -394,8 +406,9 @@ def hdet_embed(tokens, table, out, scale: float = 1.0, stream: int = 0) -> None:
     [V, D] (one for all replicas) and out [N, T, D], float32 or bfloat16 each.  Tokens outside 0 .. V-1 give zeros."""
     if out.dim() != 3:
         raise ValueError("out must be [N, T, D]")
-    d = _embedding(tokens, out, table, out.shape[0], scale)
-    _check(_lib.hdet_embed(C.byref(d), stream), None)
+    status = _lib.hdet_embed(C.byref(_embedding(tokens, out, table, out.shape[0], scale)), stream)
+    if status:
+        _check(status, None)
 
 
 def hdet_embed_grad_workspace(tokens, d_out, d_table) -> int:
@@ -413,38 +426,43 @@ def hdet_embed_grad(tokens, d_out, d_table, workspace, scale: float = 1.0, accum
         raise ValueError("d_table must be [N, V, D]")
     d = _embedding(tokens, d_out, d_table, d_table.shape[0], scale)
     ptr, size = _workspace(workspace, d.device)
-    _check(_lib.hdet_embed_grad(C.byref(d), 1 if accumulate else 0, ptr, size, stream), None)
+    status = _lib.hdet_embed_grad(C.byref(d), 1 if accumulate else 0, ptr, size, stream)
+    if status:
+        _check(status, None)
 
 
 def _token_loss_args(hidden, weight, targets, loss, token_loss, d_hidden, d_weight, n, grad_scale, accumulate, piece_bytes):
-    T, D, V = hidden.shape[-2], hidden.shape[-1], weight.shape[-2]
-    if targets.shape[-1] != T or weight.shape[-1] != D:
+    T, D = hidden.shape[-2:]
+    V, width = weight.shape[-2:]
+    if targets.shape[-1] != T or width != D:
         raise ValueError("hidden, weight and targets disagree on the number of tokens or the width")
-    given = [t for t in (hidden, weight, targets, loss, token_loss, d_hidden, d_weight) if t is not None]
+    device = hidden.get_device()
+    if device < 0 or weight.get_device() != device or targets.get_device() != device:
+        raise ValueError("all tensors must be on one CUDA device")
+    hidden_stride, hidden_row = _rows_layout(hidden, n, "hidden")
+    weight_stride, weight_row = _rows_layout(weight, n, "weight")
     a = hdet_token_loss_args(
-        hidden.data_ptr(), weight.data_ptr(), targets.data_ptr(), None, None, None, None, T, V, D,
-        _replica_stride(hidden, 2, n, "hidden"), _row_stride(hidden, D), _replica_stride(weight, 2, n, "weight"),
-        _row_stride(weight, D), _replica_stride(targets, 1, n, "targets"), 0, 0, D, 0, D, grad_scale, piece_bytes, n,
-        _code(hidden), _code(weight), _code(targets), HDET_DTYPE_F32, HDET_DTYPE_F32, HDET_DTYPE_F32, 1 if accumulate else 0,
-        _one_device(*given), 0)
+        hidden.data_ptr(), weight.data_ptr(), targets.data_ptr(), None, None, None, None, T, V, D, hidden_stride, hidden_row,
+        weight_stride, weight_row, _ids_stride(targets, n, "targets"), 0, 0, D, 0, D, grad_scale, piece_bytes, n,
+        _dtype_code[hidden.dtype], _dtype_code[weight.dtype], _dtype_code[targets.dtype], 0, 0, 0, 1 if accumulate else 0, device)
     if loss is not None:
-        if loss.shape != (n,) or not loss.is_contiguous():
-            raise ValueError("loss must be a contiguous [N]")
-        a.loss, a.loss_dtype = loss.data_ptr(), _code(loss)
+        if loss.shape != (n,) or loss.get_device() != device or (n > 1 and loss.stride(0) != 1):
+            raise ValueError("loss must be a contiguous [N] on the inputs' device")
+        a.loss, a.loss_dtype = loss.data_ptr(), _dtype_code[loss.dtype]
     if token_loss is not None:
-        if token_loss.shape != (n, T) or _code(token_loss) != HDET_DTYPE_F32:
-            raise ValueError("token_loss must be float32 [N, T]")
-        a.token_loss, a.token_loss_stride = token_loss.data_ptr(), _replica_stride(token_loss, 1, n, "token_loss")
+        if token_loss.shape != (n, T) or token_loss.get_device() != device or _dtype_code[token_loss.dtype] != HDET_DTYPE_F32:
+            raise ValueError("token_loss must be float32 [N, T] on the inputs' device")
+        a.token_loss, a.token_loss_stride = token_loss.data_ptr(), _ids_stride(token_loss, n, "token_loss")
     if d_hidden is not None:
-        if d_hidden.shape != (n, T, D):
-            raise ValueError("d_hidden must be [N, T, D]")
-        a.d_hidden, a.d_hidden_dtype = d_hidden.data_ptr(), _code(d_hidden)
-        a.d_hidden_stride, a.d_hidden_row = _replica_stride(d_hidden, 2, n, "d_hidden"), _row_stride(d_hidden, D)
+        if d_hidden.shape != (n, T, D) or d_hidden.get_device() != device:
+            raise ValueError("d_hidden must be [N, T, D] on the inputs' device")
+        a.d_hidden, a.d_hidden_dtype = d_hidden.data_ptr(), _dtype_code[d_hidden.dtype]
+        a.d_hidden_stride, a.d_hidden_row = _rows_layout(d_hidden, n, "d_hidden")
     if d_weight is not None:
-        if d_weight.shape != (n, V, D):
-            raise ValueError("d_weight must be [N, V, D]")
-        a.d_weight, a.d_weight_dtype = d_weight.data_ptr(), _code(d_weight)
-        a.d_weight_stride, a.d_weight_row = _replica_stride(d_weight, 2, n, "d_weight"), _row_stride(d_weight, D)
+        if d_weight.shape != (n, V, D) or d_weight.get_device() != device:
+            raise ValueError("d_weight must be [N, V, D] on the inputs' device")
+        a.d_weight, a.d_weight_dtype = d_weight.data_ptr(), _dtype_code[d_weight.dtype]
+        a.d_weight_stride, a.d_weight_row = _rows_layout(d_weight, n, "d_weight")
     return a
 
 
@@ -474,11 +492,13 @@ def hdet_token_loss(hidden, weight, targets, loss, workspace, token_loss=None, d
     a = _token_loss_args(hidden, weight, targets, loss, token_loss, d_hidden, d_weight, loss.shape[0], grad_scale, accumulate,
                          piece_bytes)
     ptr, size = _workspace(workspace, a.device)
-    _check(_lib.hdet_token_loss(C.byref(a), ptr, size, stream), None)
+    status = _lib.hdet_token_loss(C.byref(a), ptr, size, stream)
+    if status:
+        _check(status, None)
 
 
 def _workspace(workspace, device: int):
-    if not workspace.is_cuda or workspace.device.index != device or not workspace.is_contiguous():
+    if workspace.get_device() != device or not workspace.is_contiguous():
         raise ValueError("the workspace must be a contiguous tensor on the inputs' CUDA device")
     return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 

@@ -74,7 +74,8 @@ struct LossParams {
   const int* token_of;
   float* z_target;
   float* lse2;              // lse in units of log 2
-  float2* part;             // [replica][rows_pad][halves of column tiles]: maximum, sum of exp
+  float2* part;             // [replica][rows_pad][n_parts]: maximum and sum of exp of a part of the row
+  int n_parts;
   float* row_loss;          // [replica][rows_pad]
   // piece of the vocabulary
   int r0, n_r;              // replicas of this launch
@@ -341,7 +342,7 @@ __device__ __forceinline__ void stats_epilogue(const LossParams& p, const Job& j
     sum = fmaf(sum, exp2_fast(fmaf(top, kLog2e, -shift)), s);
     top = now;
   }
-  p.part[at * 2 * p.n_tiles + v0 / kCols] = make_float2(top, sum);
+  p.part[at * p.n_parts + v0 / kCols] = make_float2(top, sum);
   if (target >= v0 && target < v0 + kCols) p.z_target[at] = picked;
 }
 
@@ -382,7 +383,7 @@ __device__ __forceinline__ void numerators_epilogue(const LossParams& p, const J
     }
     write_staged(rows, staging, lane, 2 * c, 2 * kCols);
   }
-  p.part[at * 2 * p.n_tiles + v0 / kCols] = make_float2(top, sum);
+  p.part[at * p.n_parts + v0 / kCols] = make_float2(top, sum);
   if (target >= v0 && target < v0 + kCols) p.z_target[at] = picked;
 }
 
@@ -540,6 +541,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
   const uint32_t rank = CTAS == 1 ? 0 : cluster_rank();
   const auto bar = [](const uint64_t& b) { return bulk::smem_addr(&b); };
 
+  let_next_start();
   if (threadIdx.x == 0) {
     sh.failed = 0;
     sh.issued = 0;
@@ -557,8 +559,9 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
     }
     bulk::barrier_init_fence();
   }
-  if (threadIdx.x < p.n_replicas) sh.count[threadIdx.x] = p.count[threadIdx.x];
   if (warp == 1) tmem_alloc<CTAS>(bulk::smem_addr(&sh.tmem), 2 * 128 * CTAS);
+  wait_for_previous();
+  if (threadIdx.x < p.n_replicas) sh.count[threadIdx.x] = p.count[threadIdx.x];
   fence_before_sync();
   __syncthreads();
   if constexpr (CTAS == 2) cluster_sync();       // the peer's barriers exist before anything arrives there
@@ -660,8 +663,11 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
           failed = 1;
           break;
         }
-        const unsigned t = atomicAdd(&p.control->ticket, 1u) - p.first_ticket;
-        const int tile = t < (unsigned)p.jobs ? (int)t : p.jobs;
+        int tile = blockIdx.x / CTAS;              // the first is the cluster's own
+        if (i > 0) {
+          const unsigned t = atomicAdd(&p.control->ticket, 1u) - p.first_ticket;
+          tile = t < (unsigned)p.jobs - gridDim.x / CTAS ? (int)(t + gridDim.x / CTAS) : p.jobs;
+        }
 #pragma unroll
         for (int c = 0; c < CTAS; ++c) {
           store_cluster(in_cta(bulk::smem_addr(&sh.tile[q]), c), tile);
@@ -737,28 +743,31 @@ struct PackParams {
 
 constexpr int kPackRows = 32;
 
+// The target of a token, -1 for padding.
+__device__ __forceinline__ int target_of(const PackParams& p, int r, int t) {
+  const int64_t at = r * p.target_stride + t;
+  if (p.wide) {
+    const long long v = static_cast<const long long*>(p.targets)[at];
+    return v >= 0 && v < p.vocab ? (int)v : -1;
+  }
+  const int v = static_cast<const int*>(p.targets)[at];
+  return v >= 0 && v < p.vocab ? v : -1;
+}
+
 // Moves the hidden states of counted tokens together, 32 tokens a block.  Every block counts the targets before its own
 // (and all of them) itself: that is 4 bytes a token from L2 instead of a launch of its own for the offsets.
 __global__ void __launch_bounds__(256) pack_kernel(const PackParams p) {
   __shared__ int s_before[8], s_all[8], s_to[kPackRows];
   const int r = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int t0 = blockIdx.x * kPackRows;
+  let_next_start();
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     p.control->done[r] = 0;
     if (r == 0) p.control->status = p.control->ticket = 0;
   }
-  const auto target_of = [&](int t) -> int {
-    const int64_t at = r * p.target_stride + t;
-    if (p.wide) {
-      const long long v = static_cast<const long long*>(p.targets)[at];
-      return v >= 0 && v < p.vocab ? (int)v : -1;
-    }
-    const int v = static_cast<const int*>(p.targets)[at];
-    return v >= 0 && v < p.vocab ? v : -1;
-  };
   int before = 0, all = 0;
   for (int t = threadIdx.x; t < p.n_tokens; t += 256) {
-    const int one = target_of(t) >= 0;
+    const int one = target_of(p, r, t) >= 0;
     all += one;
     before += t < t0 ? one : 0;
   }
@@ -772,7 +781,7 @@ __global__ void __launch_bounds__(256) pack_kernel(const PackParams p) {
   const int64_t base = (int64_t)r * p.rows_pad;
   if (warp == 0) {
     const int t = t0 + lane;
-    const int y = t < p.n_tokens ? target_of(t) : -1;
+    const int y = t < p.n_tokens ? target_of(p, r, t) : -1;
     const unsigned counted = __ballot_sync(0xffffffffu, y >= 0);
     const int to = y >= 0 ? before + __popc(counted & ((1u << lane) - 1)) : -1;
     s_to[lane] = to;
@@ -824,6 +833,8 @@ __global__ void __launch_bounds__(256) pack_kernel(const PackParams p) {
 __global__ void __launch_bounds__(256) pack_table_kernel(const __nv_bfloat16* table, int64_t stride, int64_t row, int vocab,
                                                          int width, int packed_row, __nv_bfloat16* packed) {
   const int v = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  let_next_start();
+  wait_for_previous();
   if (v >= vocab) return;
   const __nv_bfloat16* from = table + blockIdx.y * stride + v * row;
   __nv_bfloat16* to = packed + ((int64_t)blockIdx.y * vocab + v) * packed_row;
@@ -884,9 +895,11 @@ __device__ __forceinline__ void finish_block(const LossParams& p, int r, unsigne
 // lse and loss of a row from its parts, one warp a row.
 __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ LossParams p) {
   const int r = blockIdx.y, row = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  let_next_start();
+  wait_for_previous();
   if (row < p.count[r]) {
     const int64_t at = (int64_t)r * p.rows_pad + row;
-    const int n = 2 * p.n_tiles;
+    const int n = p.n_parts;
     const float2* part = p.part + at * n;
     Lse l{-INFINITY, 0.0f};
 #pragma unroll 4
@@ -908,8 +921,10 @@ __global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ Loss
   constexpr int kCols = 64 * CTAS;
   extern __shared__ float s_factor[];              // per half tile: exp(m - lse)
   __shared__ Lse s_lse[8];
+  let_next_start();
+  wait_for_previous();
   const int g = blockIdx.y, r = p.r0 + g, row = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int count = p.count[r], n = 2 * p.n_tiles;
+  const int count = p.count[r], n = p.n_parts;
   uint4* values = reinterpret_cast<uint4*>(p.g_hi + ((int64_t)g * p.rows_pad + row) * p.v_pitch);
   const int vectors = p.n_tiles * 2 * kCols / 8;
   if (row < count) {
@@ -958,8 +973,114 @@ __global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ Loss
   finish_block(p, r, gridDim.x);
 }
 
+// ------------------------------------------------------------------------------------------------ few tokens
+// The losses of up to kFew tokens a replica: the table is read once, so that is what bounds it, and a product of 128 rows
+// would leave the tensor cores 124 of them empty.  A warp takes a run of the table's rows, four at a time, a lane 8 elements of
+// each per step; hidden states come from L1.  Sums are fp32.  REPLACE_FEW
+constexpr int kFew = 4, kFewRows = 4;
+
+template <int NT>
+__global__ void __launch_bounds__(256, 3) few_kernel(const __grid_constant__ LossParams p, const __grid_constant__ PackParams k,
+                                                  const __nv_bfloat16* __restrict__ table, int64_t table_stride, int64_t table_row) {
+  __shared__ Lse s_lse[8][NT];
+  let_next_start();
+  const int r = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int target[NT], count = 0;
+  const __nv_bfloat16* hidden[NT];                 // of the counted tokens, in order
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    target[t] = -1;
+    hidden[t] = k.hidden + r * k.hidden_stride;
+  }
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int y = t < k.n_tokens ? target_of(k, r, t) : -1;
+    if (y >= 0) {
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+        if (i == count) {
+          target[i] = y;
+          hidden[i] = k.hidden + r * k.hidden_stride + t * k.hidden_row;
+        }
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0 && t < k.n_tokens) {
+      if (y >= 0) {
+        k.target[(int64_t)r * p.rows_pad + count] = y;
+        k.token_of[(int64_t)r * p.rows_pad + count] = t;
+      } else if (p.token_loss) {
+        p.token_loss[r * p.token_loss_stride + t] = 0.0f;
+      }
+    }
+    count += y >= 0;
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    k.count[r] = count;
+    p.control->done[r] = 0;
+    if (r == 0) p.control->status = 0;
+  }
+  if (count == 0) return;
+  const int64_t w = (int64_t)blockIdx.x * 8 + warp, warps = (int64_t)gridDim.x * 8;
+  const int from = (int)(p.vocab * w / warps), to = (int)(p.vocab * (w + 1) / warps);
+  const __nv_bfloat16* base = table + r * table_stride;
+  Lse l[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) l[t] = Lse{-INFINITY, 0.0f};
+  for (int v = from; v < to; v += kFewRows) {
+    float z[kFewRows][NT];
+    const __nv_bfloat16* row[kFewRows];
+#pragma unroll
+    for (int i = 0; i < kFewRows; ++i) {
+      row[i] = base + min(v + i, to - 1) * table_row;   // behind the run's end: its last row again, not counted
+#pragma unroll
+      for (int t = 0; t < NT; ++t) z[i][t] = 0.0f;
+    }
+#pragma unroll 3
+    for (int c = lane * 8; c < p.width; c += 256) {
+      uint4 u[kFewRows];
+#pragma unroll
+      for (int i = 0; i < kFewRows; ++i) u[i] = __ldcs(reinterpret_cast<const uint4*>(row[i] + c));
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const uint4 h4 = *reinterpret_cast<const uint4*>(hidden[t] + c);
+        const uint32_t h[4] = {h4.x, h4.y, h4.z, h4.w};
+#pragma unroll
+        for (int i = 0; i < kFewRows; ++i) {
+          const uint32_t x[4] = {u[i].x, u[i].y, u[i].z, u[i].w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            z[i][t] = fmaf(__uint_as_float(x[e] << 16), __uint_as_float(h[e] << 16), z[i][t]);
+            z[i][t] = fmaf(__uint_as_float(x[e] & 0xffff0000u), __uint_as_float(h[e] & 0xffff0000u), z[i][t]);
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kFewRows; ++i)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) z[i][t] += __shfl_xor_sync(0xffffffffu, z[i][t], o);
+        if (v + i < to) {
+          l[t].add(make_float2(z[i][t], 1.0f));
+          if (v + i == target[t] && lane == 0) p.z_target[(int64_t)r * p.rows_pad + t] = z[i][t];
+        }
+      }
+  }
+  if (lane == 0)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) s_lse[warp][t] = l[t];
+  __syncthreads();
+  if (threadIdx.x < count) {
+    Lse all = s_lse[0][threadIdx.x];
+    for (int i = 1; i < 8; ++i) all.add(make_float2(s_lse[i][threadIdx.x].top, s_lse[i][threadIdx.x].sum));
+    p.part[((int64_t)r * p.rows_pad + threadIdx.x) * p.n_parts + blockIdx.x] = make_float2(all.top, all.sum);
+  }
+}
+
 // dH: adds the partial sums over the vocabulary in their order, scales, rounds once and puts rows back at their tokens.
 __global__ void __launch_bounds__(256) join_hidden_kernel(const __grid_constant__ LossParams p) {
+  let_next_start();
+  wait_for_previous();
   const int g = blockIdx.y, r = p.r0 + g, row = blockIdx.x;
   const int count = p.count[r];
   if (row >= count) return;
@@ -1049,6 +1170,7 @@ bool table_fits(const hdet_token_loss_args* d) {
 
 constexpr int64_t kDefaultPieceBytes = 512ll << 20;
 constexpr int64_t kMaxScaleTiles = 4096;      // scale_kernel keeps two factors a tile in shared memory (32 KB)
+constexpr int64_t kFewBlocks = 148 * 3;         // blocks of few_kernel that are resident at once
 constexpr int kSlots = 74;       // pairs of SMs: tiles that run at once
 
 // Sizes, launches and the workspace's layout; host arithmetic only, the same for the size query and the call.
@@ -1057,6 +1179,8 @@ struct Plan {
   int64_t rows_pad, packed_row, m_tiles, n_tiles;
   bool grads, two, h_two, w_two;
   bool numerators;                // the logits are formed once: their exponentials wait in the workspace for lse
+  bool few;                       // few_kernel takes the place of packing and product
+  int64_t n_parts;                // parts of a row's sum of exp
   int64_t group;                  // replicas per launch
   int64_t piece;                  // rows of the table per launch (a multiple of the tile)
   int64_t n_pieces, h_len, h_splits;
@@ -1080,6 +1204,13 @@ Plan plan_of(const hdet_token_loss_args* d) {
   q.w_two = d->d_weight && d->d_weight_dtype == HDET_DTYPE_F32;
   q.two = q.h_two || q.w_two;
   q.pack_table = !table_fits(d);
+  q.few = !q.grads && T <= kFew && T > 0 && !q.pack_table && D % 8 == 0 && aligned(d->hidden, 16) && d->hidden_row % 8 == 0 &&
+          (R == 1 || d->hidden_stride % 8 == 0);
+  q.n_parts = 2 * q.n_tiles;
+  if (q.few) {
+    const int64_t most = div_up(V, 8 * kFewRows), blocks = kFewBlocks / R;
+    q.n_parts = blocks < 1 ? 1 : blocks < most ? blocks : most;
+  }
   if (q.grads) {
     const int64_t budget = d->piece_bytes ? d->piece_bytes : kDefaultPieceBytes;
     const int64_t v_all = q.n_tiles * q.tile, per_row = q.rows_pad * 2 * (q.two ? 2 : 1);
@@ -1119,7 +1250,7 @@ Plan plan_of(const hdet_token_loss_args* d) {
   q.off_token = take(4 * R * q.rows_pad);
   q.off_z = take(4 * R * q.rows_pad);
   q.off_lse = take(4 * R * q.rows_pad);
-  q.off_part = take(8 * R * 2 * q.n_tiles * q.rows_pad);
+  q.off_part = take(8 * R * q.n_parts * q.rows_pad);
   q.off_loss = take(4 * R * q.rows_pad);
   q.off_hidden = take(2 * R * q.rows_pad * q.packed_row);
   if (q.pack_table) q.off_table = take(2 * (d->n_replicas > 1 && d->weight_stride ? R : 1) * V * q.packed_row);
@@ -1194,25 +1325,34 @@ bool encode(CUtensorMap* map, const void* base, int64_t x, int64_t y, int64_t z,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Launches a kernel that may start its prologue while the one before it ends (see let_next_start).
+template <typename... Params, typename... Args>
+cudaError_t launch(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, int cluster, cudaStream_t st, const Args&... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, Params(args)...);
+}
+
 template <int PHASE>
 cudaError_t launch_gemm(LossParams& p, int ctas, int64_t tiles, int sms, cudaStream_t st) {
   if (tiles == 0) return cudaSuccess;
   const int64_t clusters = tiles < sms / ctas ? tiles : sms / ctas;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(clusters * ctas));
   p.jobs = (int)tiles;
-  cfg.blockDim = dim3(kGemmThreads);
-  cfg.dynamicSmemBytes = kGemmSmem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = ctas;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  const cudaError_t e =
-      ctas == 1 ? cudaLaunchKernelEx(&cfg, gemm_kernel<1, PHASE>, p) : cudaLaunchKernelEx(&cfg, gemm_kernel<2, PHASE>, p);
-  p.first_ticket += (unsigned)(tiles + clusters);
+  const dim3 grid((unsigned)(clusters * ctas));
+  const cudaError_t e = ctas == 1 ? launch(gemm_kernel<1, PHASE>, grid, kGemmThreads, kGemmSmem, 1, st, p)
+                                  : launch(gemm_kernel<2, PHASE>, grid, kGemmThreads, kGemmSmem, 2, st, p);
+  p.first_ticket += (unsigned)tiles;
   return e;
 }
 
@@ -1301,16 +1441,28 @@ extern "C" HDET_API int hdet_token_loss(const hdet_token_loss_args* d, void* wor
   k.token_loss = p.token_loss;
   k.token_loss_stride = p.token_loss_stride;
   k.control = p.control;
-  const unsigned pack_blocks = (unsigned)(d->n_tokens > 0 ? div_up(d->n_tokens, kPackRows) : 1);
-  pack_kernel<<<dim3(pack_blocks, d->n_replicas), 256, 0, st>>>(k);
-
   const __nv_bfloat16* table = static_cast<const __nv_bfloat16*>(d->weight);
   int64_t table_row = d->weight_row, table_stride = shared_table ? d->weight_row * d->vocab : d->weight_stride;
   const int tables = shared_table ? 1 : d->n_replicas;
+  p.n_parts = (int)q.n_parts;
+  if (q.few) {
+    const dim3 grid((unsigned)q.n_parts, d->n_replicas);
+    const int64_t stride = shared_table ? 0 : table_stride;
+    if (d->n_tokens == 1) few_kernel<1><<<grid, 256, 0, st>>>(p, k, table, stride, table_row);
+    else if (d->n_tokens == 2) few_kernel<2><<<grid, 256, 0, st>>>(p, k, table, stride, table_row);
+    else few_kernel<kFew><<<grid, 256, 0, st>>>(p, k, table, stride, table_row);
+    e = cudaGetLastError();
+    if (e == cudaSuccess) e = launch(join_kernel, dim3(1, d->n_replicas), 256, 0, 1, st, p);
+    return e == cudaSuccess ? HDET_OK : fail_cuda(who, e);
+  }
+  const unsigned pack_blocks = (unsigned)(d->n_tokens > 0 ? div_up(d->n_tokens, kPackRows) : 1);
+  pack_kernel<<<dim3(pack_blocks, d->n_replicas), 256, 0, st>>>(k);
+
   if (q.pack_table) {
     __nv_bfloat16* packed = reinterpret_cast<__nv_bfloat16*>(ws + q.off_table);
-    pack_table_kernel<<<dim3((unsigned)div_up(d->vocab, 8), tables), 256, 0, st>>>(table, shared_table ? 0 : d->weight_stride,
-                                                                                table_row, p.vocab, p.width, k.packed_row, packed);
+    e = launch(pack_table_kernel, dim3((unsigned)div_up(d->vocab, 8), tables), 256, 0, 1, st, table,
+               shared_table ? (int64_t)0 : d->weight_stride, table_row, p.vocab, p.width, k.packed_row, packed);
+    if (e != cudaSuccess) return fail_cuda(who, e);
     table = packed;
     table_row = q.packed_row;
     table_stride = q.packed_row * d->vocab;
@@ -1333,7 +1485,7 @@ extern "C" HDET_API int hdet_token_loss(const hdet_token_loss_args* d, void* wor
   e = cudaGetLastError();
   if (e == cudaSuccess && !q.numerators) {
     if (any) e = launch_gemm<kStats>(p, q.ctas, q.m_tiles * q.n_tiles * d->n_replicas, sms, st);
-    if (e == cudaSuccess) join_kernel<<<dim3((unsigned)(q.rows_pad / 8), d->n_replicas), 256, 0, st>>>(p);
+    if (e == cudaSuccess) e = launch(join_kernel, dim3((unsigned)(q.rows_pad / 8), d->n_replicas), 256, 0, 1, st, p);
   }
   if (e != cudaSuccess) return fail_cuda(who, e);
 
@@ -1362,9 +1514,7 @@ extern "C" HDET_API int hdet_token_loss(const hdet_token_loss_args* d, void* wor
           if (e == cudaSuccess) {
             const dim3 grid((unsigned)q.rows_pad, p.n_r);
             const size_t factors = sizeof(float) * 2 * p.n_tiles;
-            if (q.ctas == 1) scale_kernel<1><<<grid, 256, factors, st>>>(p);
-            else scale_kernel<2><<<grid, 256, factors, st>>>(p);
-            e = cudaGetLastError();
+            e = launch(q.ctas == 1 ? scale_kernel<1> : scale_kernel<2>, grid, 256, factors, 1, st, p);
           }
         }
         if (e == cudaSuccess)
@@ -1372,7 +1522,8 @@ extern "C" HDET_API int hdet_token_loss(const hdet_token_loss_args* d, void* wor
         if (e != cudaSuccess) return fail_cuda(who, e);
       }
       if (d->d_hidden && any && q.h_slabs)
-        join_hidden_kernel<<<dim3((unsigned)q.rows_pad, p.n_r), 256, 0, st>>>(p);
+        e = launch(join_hidden_kernel, dim3((unsigned)q.rows_pad, p.n_r), 256, 0, 1, st, p);
+      if (e != cudaSuccess) return fail_cuda(who, e);
     }
   }
   e = cudaGetLastError();

@@ -239,6 +239,20 @@ def test_loss(size):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("T", [1, 2, 3, 4, 5])
+@pytest.mark.parametrize("V,D", [(1, 8), (33, 64), (5000, 776), (50257, 264)])
+def test_loss_of_few_tokens(T, V, D):
+    for R, shared, pad in [(1, False, 0.0), (3, False, 0.5), (2, True, 0.5)]:
+        h, w, y = _inputs(R, T, V, D, seed=T + V, pad=pad, target_dtype=torch.int64 if shared else torch.int32)
+        if T == 3:
+            y[0] = -100
+        _run(h, w[0] if shared else w, y)
+        _, hs = _strided((R, T, D), torch.bfloat16, 8, 8, 8, float("nan"))
+        hs.copy_(h)
+        _run(hs, w[0] if shared else w, y, token=False, loss_dtype=torch.float64, ws_fill=255)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dh_dt,dw_dt", [("bf16", "bf16"), ("f32", "f32"), ("bf16", "f32"), ("f32", "bf16"), ("bf16", None), (None, "bf16"),
                                          ("f32", None), (None, "f32")])
 @pytest.mark.parametrize("size", SMALL + PAIRS, ids=str)
