@@ -324,10 +324,9 @@ __device__ __forceinline__ float exponentials(float (&x)[2][32], float shift) {
 
 // `tmem`: the reader's lanes, at the first column of its half; `half`: that column within the tile.
 template <int CTAS>
-__device__ __forceinline__ void stats_epilogue(const LossParams& p, const Job& j, uint32_t tmem, int row, int half) {
+__device__ __forceinline__ void stats_epilogue(const LossParams& p, const Job& j, uint32_t tmem, int row, int half, int target) {
   constexpr int kCols = 64 * CTAS;
   const int64_t at = (int64_t)j.r * p.rows_pad + row;
-  const int target = p.target[at];                 // -1 behind the counted tokens
   const int v0 = j.n0 + half;
   float top = -INFINITY, sum = 0.0f, picked = 0.0f;
 #pragma unroll 1
@@ -351,10 +350,9 @@ __device__ __forceinline__ void stats_epilogue(const LossParams& p, const Job& j
 // G to bf16 that follows.  The sum is taken before that rounding.  The columns are read twice, once for the maximum.
 template <int CTAS>
 __device__ __forceinline__ void numerators_epilogue(const LossParams& p, const Job& j, uint32_t tmem, int row, int half,
-                                                    uint32_t staging, int lane) {
+                                                    int target, uint32_t staging, int lane) {
   constexpr int kCols = 64 * CTAS;
   const int64_t at = (int64_t)j.r * p.rows_pad + row;
-  const int target = p.target[at];
   const int v0 = j.n0 + half;
   float top = -INFINITY, sum = 0.0f, picked = 0.0f;
 #pragma unroll 1
@@ -388,13 +386,10 @@ __device__ __forceinline__ void numerators_epilogue(const LossParams& p, const J
 }
 
 template <int CTAS>
-__device__ __forceinline__ void probs_epilogue(const LossParams& p, const Job& j, uint32_t tmem, int row, int half, int count,
-                                               uint32_t staging, int lane) {
+__device__ __forceinline__ void probs_epilogue(const LossParams& p, const Job& j, uint32_t tmem, int row, int half, bool counted,
+                                               int target, float lse2, uint32_t staging, int lane) {
   constexpr int kCols = 64 * CTAS;
-  const int64_t at = (int64_t)j.r * p.rows_pad + row;
-  const bool counted = row < count;
-  const int target = counted ? p.target[at] - p.v0 : -1;
-  const float lse2 = counted ? p.lse2[at] : INFINITY;
+  target = counted ? target - p.v0 : -1;
   const int v0 = j.n0 + half;
   Rows rows;
   rows.offset = (((int64_t)(j.r - p.r0) * p.rows_pad + row) * p.v_pitch + v0) * 2;
@@ -542,6 +537,14 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
   const auto bar = [](const uint64_t& b) { return bulk::smem_addr(&b); };
 
   let_next_start();
+  if (threadIdx.x == 32 * (kFirstReader - 1)) {  // a thread that has nothing else to do
+    prefetch_map(&p.weight);
+    prefetch_map(&p.hidden);
+    if constexpr (PHASE == kGrads) {
+      prefetch_map(&p.grad_hi);
+      if (p.h_two || p.w_two) prefetch_map(&p.grad_lo);
+    }
+  }
   if (threadIdx.x == 0) {
     sh.failed = 0;
     sh.issued = 0;
@@ -568,10 +571,12 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
   fence_after_sync();
   const uint32_t tmem = sh.tmem;
 
-  // The i-th tile of this cluster; p.jobs when there is none left (or a wait ran out).
+  // The i-th tile of this cluster (the first is its own, the others are handed out); p.jobs when there is none left, or a
+  // wait ran out.
   const auto next_tile = [&](int i, bool whole_warp) -> int {
-    const int q = i % kTileSlots;
-    bool ok = wait_cluster(bar(sh.tile_full[q]), (i / kTileSlots) & 1, 2 * bulk::kWaitLimitCycles);
+    if (i == 0) return blockIdx.x / CTAS;
+    const int use = i - 1, q = use % kTileSlots;
+    bool ok = wait_cluster(bar(sh.tile_full[q]), (use / kTileSlots) & 1, 2 * bulk::kWaitLimitCycles);
     if (whole_warp) ok = __all_sync(0xffffffffu, ok);
     if (!ok) failed = 1;
     const int tile = ok ? *const_cast<volatile int*>(&sh.tile[q]) : p.jobs;
@@ -663,11 +668,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
           failed = 1;
           break;
         }
-        int tile = blockIdx.x / CTAS;              // the first is the cluster's own
-        if (i > 0) {
-          const unsigned t = atomicAdd(&p.control->ticket, 1u) - p.first_ticket;
-          tile = t < (unsigned)p.jobs - gridDim.x / CTAS ? (int)(t + gridDim.x / CTAS) : p.jobs;
-        }
+        const unsigned t = atomicAdd(&p.control->ticket, 1u) - p.first_ticket;
+        const int tile = t < (unsigned)p.jobs - gridDim.x / CTAS ? (int)(t + gridDim.x / CTAS) : p.jobs;
 #pragma unroll
         for (int c = 0; c < CTAS; ++c) {
           store_cluster(in_cta(bulk::smem_addr(&sh.tile[q]), c), tile);
@@ -686,6 +688,13 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
       Job j;
       if (!find_job<CTAS, PHASE>(p, sh.count, tile, j)) continue;
       const int b = uses & 1;
+      const int row = j.m0 + 128 * (int)rank + quarter * 32 + lane;
+      int target = -1;                             // -1 behind the counted tokens, too
+      float lse2 = INFINITY;
+      if constexpr (PHASE != kGrads) {
+        target = p.target[(int64_t)j.r * p.rows_pad + row];
+        if (PHASE == kProbs && row < sh.count[j.r]) lse2 = p.lse2[(int64_t)j.r * p.rows_pad + row];
+      }
       if (j.k_blocks > 0) {
         bool ok = bulk::barrier_wait(bar(sh.acc_full[b]), (uses / 2) & 1, 2 * bulk::kWaitLimitCycles);
         ok = __all_sync(0xffffffffu, ok);
@@ -696,10 +705,9 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
         fence_after_sync();
       }
       const uint32_t at = tmem + b * 128 * CTAS + half + ((uint32_t)(quarter * 32) << 16);
-      const int row = j.m0 + 128 * (int)rank + quarter * 32 + lane;
-      if constexpr (PHASE == kStats) stats_epilogue<CTAS>(p, j, at, row, half);
-      else if constexpr (PHASE == kNumerators) numerators_epilogue<CTAS>(p, j, at, row, half, staging, lane);
-      else if constexpr (PHASE == kProbs) probs_epilogue<CTAS>(p, j, at, row, half, sh.count[j.r], staging, lane);
+      if constexpr (PHASE == kStats) stats_epilogue<CTAS>(p, j, at, row, half, target);
+      else if constexpr (PHASE == kNumerators) numerators_epilogue<CTAS>(p, j, at, row, half, target, staging, lane);
+      else if constexpr (PHASE == kProbs) probs_epilogue<CTAS>(p, j, at, row, half, row < sh.count[j.r], target, lse2, staging, lane);
       else grads_epilogue<CTAS>(p, j, at, row, half, sh.count[j.r], staging, lane);
       if (j.k_blocks > 0) {
         fence_before_sync();
@@ -1015,8 +1023,6 @@ __global__ void __launch_bounds__(256, 3) few_kernel(const __grid_constant__ Los
   }
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     k.count[r] = count;
-    p.control->done[r] = 0;
-    if (r == 0) p.control->status = 0;
   }
   if (count == 0) return;
   const int64_t w = (int64_t)blockIdx.x * 8 + warp, warps = (int64_t)gridDim.x * 8;
@@ -1075,6 +1081,41 @@ __global__ void __launch_bounds__(256, 3) few_kernel(const __grid_constant__ Los
     for (int i = 1; i < 8; ++i) all.add(make_float2(s_lse[i][threadIdx.x].top, s_lse[i][threadIdx.x].sum));
     p.part[((int64_t)r * p.rows_pad + threadIdx.x) * p.n_parts + blockIdx.x] = make_float2(all.top, all.sum);
   }
+}
+
+// What follows few_kernel: a warp a token, all of its loads under way at once, then the mean.
+__global__ void __launch_bounds__(32 * kFew) few_join_kernel(const __grid_constant__ LossParams p) {
+  __shared__ float s_loss[kFew];
+  let_next_start();
+  wait_for_previous();
+  const int r = blockIdx.x, t = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int count = p.count[r];
+  const int64_t at = (int64_t)r * p.rows_pad + t;
+  const float picked = p.z_target[at];             // nothing of these is used behind the counted tokens
+  const int token = p.token_of[at];
+  Lse l{-INFINITY, 0.0f};
+  for (int i0 = 0; i0 < p.n_parts; i0 += 32 * 16) {
+    float2 part[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      const int i = i0 + 32 * k + lane;
+      part[k] = t < p.n_tokens && i < p.n_parts ? p.part[at * p.n_parts + i] : make_float2(-INFINITY, 0.0f);
+    }
+#pragma unroll
+    for (int k = 0; k < 16; ++k) l.add(part[k]);
+  }
+  l.add_warp();
+  const float loss = l.top + logf(l.sum) - picked;
+  if (lane == 0) {
+    s_loss[t] = loss;
+    if (t < count && p.token_loss) p.token_loss[r * p.token_loss_stride + token] = loss;
+  }
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  double sum = 0.0;
+  for (int i = 0; i < count; ++i) sum += (double)s_loss[i];
+  const double mean = count > 0 ? sum / (double)count : 0.0;
+  if (p.loss_f64) static_cast<double*>(p.loss)[r] = mean; else static_cast<float*>(p.loss)[r] = (float)mean;
 }
 
 // dH: adds the partial sums over the vocabulary in their order, scales, rounds once and puts rows back at their tokens.
@@ -1237,7 +1278,7 @@ Plan plan_of(const hdet_token_loss_args* d) {
       const int64_t w_tiles = d->d_weight ? q.group * (q.piece / q.tile) * div_up(D, q.tile) : 0;
       const int64_t work = h_tiles * all * (q.h_two ? 2 : 1) + w_tiles * div_up(T, kBlockK) * (q.w_two ? 2 : 1);
       int64_t share = work / (kSlots * (3 - q.ctas)) / (q.h_two ? 2 : 1);
-      if (share < 16) share = 16;
+      if (share < 8) share = 8;
       q.h_len = div_up(all, div_up(all, share));
       q.h_splits = div_up(all, q.h_len);
       q.h_slabs = q.h_splits > 1 || q.n_pieces > 1;
@@ -1452,7 +1493,7 @@ extern "C" HDET_API int hdet_token_loss(const hdet_token_loss_args* d, void* wor
     else if (d->n_tokens == 2) few_kernel<2><<<grid, 256, 0, st>>>(p, k, table, stride, table_row);
     else few_kernel<kFew><<<grid, 256, 0, st>>>(p, k, table, stride, table_row);
     e = cudaGetLastError();
-    if (e == cudaSuccess) e = launch(join_kernel, dim3(1, d->n_replicas), 256, 0, 1, st, p);
+    if (e == cudaSuccess) e = launch(few_join_kernel, dim3(d->n_replicas), 32 * kFew, 0, 1, st, p);
     return e == cudaSuccess ? HDET_OK : fail_cuda(who, e);
   }
   const unsigned pack_blocks = (unsigned)(d->n_tokens > 0 ? div_up(d->n_tokens, kPackRows) : 1);
