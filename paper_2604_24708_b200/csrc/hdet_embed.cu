@@ -11,14 +11,20 @@
 #include <cstdio>
 
 #include "hdet_internal.h"
+#include "hdet_launch.cuh"
 #include "../../include/hdet.h"
 
 namespace {
 
+using hdet::launch;
+using hdet::let_next_start;
+using hdet::wait_for_previous;
+
 constexpr int kChunkSmall = 1024;   // tokens ranked against one another at once when there are many
 constexpr int kChunkLarge = 2048;   // ... when all of them fit: one launch less, twice the comparisons per token
 constexpr int kMergeRuns = 16;      // sorted runs merged per level
-constexpr int kEntries = 32;        // sorted entries per warp in the gradient kernel: one per lane
+constexpr int kEntries = 32;        // sorted entries per warp in the gradient kernel, one per lane
+constexpr int kFewEntries = 8;      // ... when there are too few to keep the machine busy: one batch of loads each
 
 __host__ __device__ constexpr int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -67,6 +73,8 @@ constexpr int kRowsPerThread = 4;
 
 template <typename TableT, typename RowT, int VEC>
 __global__ void __launch_bounds__(256) lookup_kernel(const EmbedParams p) {
+  let_next_start();
+  wait_for_previous();
   const int64_t base = (int64_t)blockIdx.x * (blockDim.y * kRowsPerThread) + threadIdx.y;
   const int r = blockIdx.y;
   const TableT* table = static_cast<const TableT*>(p.table) + r * p.table_stride;
@@ -101,6 +109,8 @@ __global__ void __launch_bounds__(256) lookup_kernel(const EmbedParams p) {
 __global__ void __launch_bounds__(256) rank_chunks_kernel(const EmbedParams p, int chunk, int* __restrict__ key_out,
                                                           int* __restrict__ pos_out) {
   extern __shared__ int4 s_tok4[];
+  let_next_start();
+  wait_for_previous();
   int* s_tok = reinterpret_cast<int*>(s_tok4);
   const int r = blockIdx.y;
   const int parts = chunk / 256;
@@ -145,25 +155,37 @@ __device__ __forceinline__ int64_t count_before(const int* __restrict__ run, int
   return lo;
 }
 
-// Merges groups of kMergeRuns sorted runs of `run` entries: an entry's place in its group is its place in its own run
-// plus, for every other run, the entries there that come before it.
+// Merges groups of kMergeRuns sorted runs of `run` (a power of two) entries: an entry's place in its group is its place in
+// its own run plus, for every other run, the entries there that come before it.  The searches in the other runs go step by
+// step together, so that their loads are under way at once (one after the other they took 17.4 us for 8 x 8192 tokens).
 __global__ void __launch_bounds__(256) merge_runs_kernel(int64_t n, int64_t run, const int* __restrict__ key_in,
                                                          const int* __restrict__ pos_in, int* __restrict__ key_out,
                                                          int* __restrict__ pos_out) {
+  let_next_start();
+  wait_for_previous();
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= n) return;
   const int64_t base = (int64_t)blockIdx.y * n;
   const int* keys = key_in + base;
-  const int key = keys[i];
+  const int key = keys[i], pos = pos_in[base + i];
   const int64_t own = i / run, first = own / kMergeRuns * kMergeRuns;
-  int64_t at = first * run + (i - own * run);
-  for (int64_t q = first; q < first + kMergeRuns && q * run < n; ++q) {
-    if (q == own) continue;
-    const int64_t len = n - q * run < run ? n - q * run : run;
-    at += count_before(keys + q * run, len, key, q < own);
+  int before[kMergeRuns];                          // entries of each run found to come before this one
+#pragma unroll
+  for (int q = 0; q < kMergeRuns; ++q) before[q] = 0;
+  for (int64_t step = run; step > 0; step >>= 1) {
+#pragma unroll
+    for (int q = 0; q < kMergeRuns; ++q) {
+      const int64_t at = (first + q) * run + before[q] + step - 1;     // the last of the next `step` entries
+      if (before[q] + step > run || at >= n || first + q == own) continue;
+      const int o = keys[at];
+      if (o < key || (o == key && first + q < own)) before[q] += (int)step;
+    }
   }
+  int64_t at = first * run + (i - own * run);
+#pragma unroll
+  for (int q = 0; q < kMergeRuns; ++q) at += before[q];
   key_out[base + at] = key;
-  pos_out[base + at] = pos_in[base + i];
+  pos_out[base + at] = pos;
 }
 
 // ------------------------------------------------------------------------------------------------ gradient
@@ -177,6 +199,8 @@ struct GradParams {
   int64_t n_col;         // column chunks of 32 * VEC
   int64_t grad_units;    // n_blocks * n_col
   int64_t zero_units;    // 32-row groups of the table to look at for rows without a token (0 when accumulating)
+  unsigned grad_ctas, zero_ctas;
+  int entries;           // sorted entries per block: kEntries or kFewEntries
   bool accumulate;
 };
 
@@ -195,19 +219,27 @@ __device__ __forceinline__ void write_row(const GradParams& p, int r, int key, i
   y.store(to);
 }
 
-// One warp: 32 consecutive sorted entries (one per lane) and 32 * VEC columns.  A run of equal keys that lies inside
-// the 32 entries is finished here; the piece of a run that came from the block before goes to partial slot 0, the piece
+// One warp: an entry block of `entries` consecutive sorted entries (one per lane) and 32 * VEC columns.  A run of equal keys
+// that lies inside the block is finished here; the piece of a run that came from the block before goes to partial slot 0, the piece
 // of a run that starts here and goes on into the next block to slot 1, and join_kernel adds those in order.
-// Warps behind those write zeros to the table rows that have no token.
+// Other warps write zeros to the table rows that have no token.  The two kinds of blocks alternate in the grid, in proportion,
+// so that the sums' loads hide behind the zeros' stores (8 x 8192 tokens, width 2048: REPLACE_MIX).
 template <typename RowT, typename TableT, int VEC>
 __global__ void __launch_bounds__(256) grad_kernel(const GradParams p) {
+  // The next kernel is not let in early here: its blocks would wait in places that this grid's own later blocks need (with it,
+  // 16 x 1024 tokens of width 768 took 249 us instead of 215).
+  wait_for_previous();
   const int r = blockIdx.y, lane = threadIdx.x & 31;
-  const int64_t unit = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
   const int64_t n = p.e.n_tokens;
   const int* keys = p.keys + r * p.sorted_stride;
-  if (unit >= p.grad_units) {
-    const int64_t row0 = (unit - p.grad_units) * 32;
-    if (unit - p.grad_units >= p.zero_units) return;
+  // of the first b blocks, b * grad_ctas / all (rounded down) are for sums
+  const uint64_t all = (uint64_t)p.grad_ctas + p.zero_ctas;
+  const uint64_t sums_before = (uint64_t)blockIdx.x * p.grad_ctas / all;
+  const bool sums = (uint64_t)(blockIdx.x + 1) * p.grad_ctas / all > sums_before;
+  const int64_t unit = (int64_t)(sums ? sums_before : blockIdx.x - sums_before) * 8 + (threadIdx.x >> 5);
+  if (!sums) {
+    const int64_t row0 = unit * 32;
+    if (unit >= p.zero_units) return;
     bool empty = false;
     if (row0 + lane < p.e.vocab) {
       const int64_t at = count_before(keys, n, (int)(row0 + lane), false);
@@ -224,15 +256,17 @@ __global__ void __launch_bounds__(256) grad_kernel(const GradParams p) {
     }
     return;
   }
+  if (unit >= p.grad_units) return;
   const int64_t block = unit / p.n_col;
   const int64_t c = (unit % p.n_col) * (32 * VEC) + (int64_t)lane * VEC;
   const bool on = c < p.e.width;
-  const int64_t i0 = block * kEntries;
+  const int64_t i0 = block * p.entries;
   const int* pos = p.pos + r * p.sorted_stride;
-  const int my_key = i0 + lane < n ? keys[i0 + lane] : p.e.vocab;
-  const int my_pos = i0 + lane < n ? pos[i0 + lane] : 0;
+  const bool mine = lane < p.entries && i0 + lane < n;
+  const int my_key = mine ? keys[i0 + lane] : p.e.vocab;
+  const int my_pos = mine ? pos[i0 + lane] : 0;
   const int before = i0 > 0 ? keys[i0 - 1] : -1;
-  const int after = i0 + kEntries < n ? keys[i0 + kEntries] : p.e.vocab;
+  const int after = i0 + p.entries < n ? keys[i0 + p.entries] : p.e.vocab;
   const int count = __popc(__ballot_sync(0xffffffffu, my_key < p.e.vocab));   // sorted: the entries with a row come first
   const RowT* rows = static_cast<const RowT*>(p.e.rows) + r * p.e.rows_stride;
   float* partial = p.partial + ((int64_t)r * p.n_blocks + block) * 2 * p.e.width;
@@ -253,15 +287,16 @@ __global__ void __launch_bounds__(256) grad_kernel(const GradParams p) {
       const int e = e0 + k;
       if (e >= count) break;
       const int key = __shfl_sync(0xffffffffu, my_key, e);
-      const int next = e + 1 < kEntries ? __shfl_sync(0xffffffffu, my_key, (e + 1) & 31) : after;
+      const int next_lane = __shfl_sync(0xffffffffu, my_key, (e + 1) & 31);
+      const int next = e + 1 < p.entries ? next_lane : after;
       if (e == 0) from_before = key == before;
       if (on) {
 #pragma unroll
         for (int i = 0; i < VEC; ++i) acc[i] += x[k].get(i);
       }
-      if (next == key && e + 1 < kEntries) continue;
+      if (next == key && e + 1 < p.entries) continue;
       // the run's piece in this block ends here
-      const bool goes_on = e + 1 == kEntries && next == key;
+      const bool goes_on = e + 1 == p.entries && next == key;
       if (on) {
         if (from_before || goes_on) {
           float* to = partial + (from_before ? 0 : p.e.width) + c;
@@ -278,48 +313,76 @@ __global__ void __launch_bounds__(256) grad_kernel(const GradParams p) {
   }
 }
 
-// One block per entry block and column chunk in which a run starts that goes on behind it: its pieces are added in
-// order.  The eight warps take consecutive stretches of a long run and their sums are added in order too, so the result
-// does not depend on timing.
+// The runs that start in an entry block and go on behind it: their pieces are added in order.  A block of threads looks at 32
+// entry blocks and one column chunk; every run found is one warp's, and a run of more than kLongRun pieces is shared by all
+// eight, which take consecutive stretches whose sums are added in order, so no result depends on timing.
+constexpr int kLongRun = 64;
+
+template <int VEC>
+__device__ __forceinline__ void add_pieces(const float* first, int64_t width, int64_t from, int64_t to, float (&acc)[VEC]) {
+  // piece 0 is slot 1 of the run's first block, piece j > 0 slot 0 of the j-th behind it
+#pragma unroll 8
+  for (int64_t j = from; j < to; ++j) {
+    const float* x = first + (j == 0 ? width : j * 2 * width);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) acc[i] += x[i];
+  }
+}
+
 template <typename TableT, int VEC>
 __global__ void __launch_bounds__(256) join_kernel(const GradParams p) {
   __shared__ float s_sum[8][32 * VEC];
+  let_next_start();
+  wait_for_previous();
   const int r = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t block = blockIdx.x / p.n_col;
+  const int64_t block0 = (int64_t)(blockIdx.x / p.n_col) * 32;
   const int64_t c = (blockIdx.x % p.n_col) * (32 * VEC) + (int64_t)lane * VEC;
-  const int64_t n = p.e.n_tokens, last = block * kEntries + kEntries - 1;
-  const int* keys = p.keys + r * p.sorted_stride;
-  if (last + 1 >= n) return;
-  const int key = keys[last];
-  if (key >= p.e.vocab || keys[last + 1] != key) return;
-  const int64_t i0 = block * kEntries;
-  if (keys[i0] == key && i0 > 0 && keys[i0 - 1] == key) return;       // the run started in an earlier block
-  const int64_t end = last + 1 + count_before(keys + last + 1, n - last - 1, key, true);   // behind the run's last entry
-  const int64_t n_more = (end - 1) / kEntries - block;                // blocks that the run goes on into
-  const float* base = p.partial + ((int64_t)r * p.n_blocks + block) * 2 * p.e.width;
   const bool on = c < p.e.width;
-  float acc[VEC];
-#pragma unroll
-  for (int i = 0; i < VEC; ++i) acc[i] = 0.0f;
-  // piece 0 is slot 1 of this block, piece j > 0 slot 0 of block + j
-  const int64_t pieces = n_more + 1, each = div_up(pieces, 8);
-  const int64_t from = warp * each, to = from + each < pieces ? from + each : pieces;
-  if (on) {
-#pragma unroll 4
-    for (int64_t j = from; j < to; ++j) {
-      const float* x = base + (j == 0 ? p.e.width : j * 2 * p.e.width) + c;
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) acc[i] += x[i];
-    }
+  const int64_t n = p.e.n_tokens;
+  const int* keys = p.keys + r * p.sorted_stride;
+  // lane l of every warp: does a run start in entry block block0 + l and go on behind it, and for how many blocks
+  const int64_t i0 = (block0 + lane) * p.entries, next = i0 + p.entries;
+  int key = p.e.vocab;
+  bool runs = false;
+  if (next < n) {
+    key = keys[next - 1];
+    runs = key < p.e.vocab && keys[next] == key && !(i0 > 0 && keys[i0] == key && keys[i0 - 1] == key);
   }
+  int64_t pieces = 0;
+  if (runs) pieces = (next + count_before(keys + next, n - next, key, true) - 1) / p.entries - (block0 + lane) + 1;
+  const unsigned all = __ballot_sync(0xffffffffu, runs), shared_runs = __ballot_sync(0xffffffffu, pieces > kLongRun);
+  float acc[VEC];
+  int turn = 0;
+  for (unsigned todo = all & ~shared_runs; todo; todo &= todo - 1, ++turn) {
+    if (turn % 8 != warp) continue;
+    const int l = __ffs(todo) - 1;
+    const int64_t count = __shfl_sync(0xffffffffu, pieces, l);
+    const int row = __shfl_sync(0xffffffffu, key, l);
+    if (!on) continue;
 #pragma unroll
-  for (int i = 0; i < VEC; ++i) s_sum[warp][i * 32 + lane] = acc[i];
-  __syncthreads();
-  if (warp != 0 || !on) return;
-  for (int w = 1; w < 8; ++w)
+    for (int i = 0; i < VEC; ++i) acc[i] = 0.0f;
+    add_pieces<VEC>(p.partial + ((int64_t)r * p.n_blocks + block0 + l) * 2 * p.e.width + c, p.e.width, 0, count, acc);
+    write_row<TableT, VEC>(p, r, row, c, acc);
+  }
+  for (unsigned todo = shared_runs; todo; todo &= todo - 1) {
+    const int l = __ffs(todo) - 1;
+    const int64_t count = __shfl_sync(0xffffffffu, pieces, l), each = div_up(count, 8);
+    const int row = __shfl_sync(0xffffffffu, key, l);
+    const int64_t from = warp * each, to = from + each < count ? from + each : count;
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) acc[i] += s_sum[w][i * 32 + lane];
-  write_row<TableT, VEC>(p, r, key, c, acc);
+    for (int i = 0; i < VEC; ++i) acc[i] = 0.0f;
+    if (on) add_pieces<VEC>(p.partial + ((int64_t)r * p.n_blocks + block0 + l) * 2 * p.e.width + c, p.e.width, from, to, acc);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) s_sum[warp][i * 32 + lane] = acc[i];
+    __syncthreads();
+    if (warp == 0 && on) {
+      for (int w = 1; w < 8; ++w)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) acc[i] += s_sum[w][i * 32 + lane];
+      write_row<TableT, VEC>(p, r, row, c, acc);
+    }
+    __syncthreads();
+  }
 }
 
 // ------------------------------------------------------------------------------------------------ host side
@@ -422,24 +485,28 @@ struct DeviceScope {
 int fail_cuda(const char* who, cudaError_t e) { return fail(HDET_ERR_CUDA, who, cudaGetErrorString(e)); }
 
 template <typename TableT, typename RowT, int VEC>
-void launch_lookup(const EmbedParams& p, cudaStream_t st) {
+cudaError_t launch_lookup(const EmbedParams& p, cudaStream_t st) {
   int x = 1;
   while (x < 256 && (int64_t)x * VEC < p.width) x *= 2;
   const dim3 block(x, 256 / x);
   const dim3 grid((unsigned)div_up(p.n_tokens, (int64_t)block.y * kRowsPerThread), p.n_replicas);
-  lookup_kernel<TableT, RowT, VEC><<<grid, block, 0, st>>>(p);
+  return launch(lookup_kernel<TableT, RowT, VEC>, grid, block, 0, 1, st, p);
 }
 
 template <typename RowT, typename TableT, int VEC>
-void launch_grad(GradParams p, cudaStream_t st) {
-  p.n_blocks = div_up(p.e.n_tokens, kEntries);
+cudaError_t launch_grad(GradParams p, cudaStream_t st) {
+  p.n_blocks = div_up(p.e.n_tokens, p.entries);
   p.n_col = div_up(p.e.width, 32 * VEC);
   p.grad_units = p.n_blocks * p.n_col;
   p.zero_units = p.accumulate ? 0 : div_up(p.e.vocab, 32);
-  const int64_t units = p.grad_units + p.zero_units;
-  if (units > 0) grad_kernel<RowT, TableT, VEC><<<dim3((unsigned)div_up(units, 8), p.e.n_replicas), 256, 0, st>>>(p);
-  if (p.n_blocks > 1)
-    join_kernel<TableT, VEC><<<dim3((unsigned)((p.n_blocks - 1) * p.n_col), p.e.n_replicas), 256, 0, st>>>(p);
+  p.grad_ctas = (unsigned)div_up(p.grad_units, 8);
+  p.zero_ctas = (unsigned)div_up(p.zero_units, 8);
+  cudaError_t e = cudaSuccess;
+  if (p.grad_ctas + p.zero_ctas > 0)
+    e = launch(grad_kernel<RowT, TableT, VEC>, dim3(p.grad_ctas + p.zero_ctas, p.e.n_replicas), 256, 0, 1, st, p);
+  if (e == cudaSuccess && p.n_blocks > 1)
+    e = launch(join_kernel<TableT, VEC>, dim3((unsigned)(div_up(p.n_blocks, 32) * p.n_col), p.e.n_replicas), 256, 0, 1, st, p);
+  return e;
 }
 
 // Calls f.template operator()<A, B, VEC>() for the element types and the vector width.
@@ -462,29 +529,33 @@ void with_types(int a, int b, int vec, F&& f) {
 struct LookupLauncher {
   const EmbedParams& p;
   cudaStream_t st;
-  template <typename TableT, typename RowT, int VEC> void operator()() { launch_lookup<TableT, RowT, VEC>(p, st); }
+  cudaError_t err = cudaSuccess;
+  template <typename TableT, typename RowT, int VEC> void operator()() { err = launch_lookup<TableT, RowT, VEC>(p, st); }
 };
 
 struct GradLauncher {
   const GradParams& p;
   cudaStream_t st;
-  template <typename RowT, typename TableT, int VEC> void operator()() { launch_grad<RowT, TableT, VEC>(p, st); }
+  cudaError_t err = cudaSuccess;
+  template <typename RowT, typename TableT, int VEC> void operator()() { err = launch_grad<RowT, TableT, VEC>(p, st); }
 };
 
 // Workspace of the gradient: two copies of the sorted keys and positions, then the partial sums.
 struct GradLayout {
   int64_t list_bytes;     // one array of one entry per sorted token
   int64_t partial_off, total;
-  int sorted_replicas;
+  int sorted_replicas, entries;
 };
 
 GradLayout layout_of(const hdet_embedding* d) {
   GradLayout l{};
   const auto up = [](int64_t x) { return div_up(x, 256) * 256; };
   l.sorted_replicas = d->n_replicas > 1 && d->token_stride != 0 ? d->n_replicas : 1;
+  // Fewer than four warps a SM in the gradient kernel: shorter entry blocks make more of them (96 tokens of width 72: REPLACE_ENT).
+  l.entries = div_up(d->n_tokens, kEntries) * div_up(d->width, 256) * d->n_replicas < 4 * 148 ? kFewEntries : kEntries;
   l.list_bytes = up(4 * d->n_tokens * l.sorted_replicas);
   l.partial_off = 4 * l.list_bytes;
-  l.total = l.partial_off + up(4 * 2 * d->width * div_up(d->n_tokens, kEntries) * d->n_replicas);
+  l.total = l.partial_off + up(4 * 2 * d->width * div_up(d->n_tokens, l.entries) * d->n_replicas);
   if (l.total < 256) l.total = 256;
   return l;
 }
@@ -499,9 +570,9 @@ extern "C" HDET_API int hdet_embed(const hdet_embedding* d, void* stream) {
   DeviceScope scope(d->device);
   if (scope.err != cudaSuccess) return fail_cuda("hdet_embed", scope.err);
   const EmbedParams p = params_of(d);
-  with_types(d->table_dtype, d->rows_dtype, vector_of(d), LookupLauncher{p, static_cast<cudaStream_t>(stream)});
-  const cudaError_t e = cudaGetLastError();
-  return e == cudaSuccess ? HDET_OK : fail_cuda("hdet_embed", e);
+  LookupLauncher launcher{p, static_cast<cudaStream_t>(stream)};
+  with_types(d->table_dtype, d->rows_dtype, vector_of(d), launcher);
+  return launcher.err == cudaSuccess ? HDET_OK : fail_cuda("hdet_embed", launcher.err);
 }
 
 extern "C" HDET_API int hdet_embed_grad_workspace(const hdet_embedding* d, int64_t* bytes) {
@@ -536,10 +607,11 @@ extern "C" HDET_API int hdet_embed_grad(const hdet_embedding* d, int32_t accumul
   if (d->n_tokens > 0) {
     const int chunk = d->n_tokens > kChunkSmall && d->n_tokens <= kChunkLarge ? kChunkLarge : kChunkSmall;
     const dim3 grid((unsigned)(div_up(d->n_tokens, chunk) * (chunk / 256)), l.sorted_replicas);
-    rank_chunks_kernel<<<grid, 256, chunk * 4, st>>>(e, chunk, key[0], pos[0]);
-    for (int64_t run = chunk; run < d->n_tokens; run *= kMergeRuns, now ^= 1)
-      merge_runs_kernel<<<dim3((unsigned)div_up(d->n_tokens, 256), l.sorted_replicas), 256, 0, st>>>(
-          d->n_tokens, run, key[now], pos[now], key[now ^ 1], pos[now ^ 1]);
+    cudaError_t err = launch(rank_chunks_kernel, grid, 256, chunk * 4, 1, st, e, chunk, key[0], pos[0]);
+    for (int64_t run = chunk; run < d->n_tokens && err == cudaSuccess; run *= kMergeRuns, now ^= 1)
+      err = launch(merge_runs_kernel, dim3((unsigned)div_up(d->n_tokens, 256), l.sorted_replicas), 256, 0, 1, st, d->n_tokens, run,
+                   key[now], pos[now], key[now ^ 1], pos[now ^ 1]);
+    if (err != cudaSuccess) return fail_cuda("hdet_embed_grad", err);
   }
   GradParams p{};
   p.e = e;
@@ -548,7 +620,8 @@ extern "C" HDET_API int hdet_embed_grad(const hdet_embedding* d, int32_t accumul
   p.sorted_stride = l.sorted_replicas > 1 ? d->n_tokens : 0;
   p.partial = reinterpret_cast<float*>(ws + l.partial_off);
   p.accumulate = accumulate != 0;
-  with_types(d->rows_dtype, d->table_dtype, vector_of(d), GradLauncher{p, st});
-  const cudaError_t err = cudaGetLastError();
-  return err == cudaSuccess ? HDET_OK : fail_cuda("hdet_embed_grad", err);
+  p.entries = l.entries;
+  GradLauncher launcher{p, st};
+  with_types(d->rows_dtype, d->table_dtype, vector_of(d), launcher);
+  return launcher.err == cudaSuccess ? HDET_OK : fail_cuda("hdet_embed_grad", launcher.err);
 }

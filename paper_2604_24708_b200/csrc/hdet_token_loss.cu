@@ -27,11 +27,15 @@
 
 #include "../../include/hdet.h"
 #include "hdet_internal.h"
+#include "hdet_launch.cuh"
 #include "hdet_umma.cuh"
 
 namespace {
 
 using namespace hdet::umma;
+using hdet::launch;
+using hdet::let_next_start;
+using hdet::wait_for_previous;
 namespace bulk = hdet::bulk;
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -769,6 +773,7 @@ __global__ void __launch_bounds__(256) pack_kernel(const PackParams p) {
   const int r = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int t0 = blockIdx.x * kPackRows;
   let_next_start();
+  wait_for_previous();
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     p.control->done[r] = 0;
     if (r == 0) p.control->status = p.control->ticket = 0;
@@ -992,6 +997,7 @@ __global__ void __launch_bounds__(256, 3) few_kernel(const __grid_constant__ Los
                                                   const __nv_bfloat16* __restrict__ table, int64_t table_stride, int64_t table_row) {
   __shared__ Lse s_lse[8][NT];
   let_next_start();
+  wait_for_previous();
   const int r = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int target[NT], count = 0;
   const __nv_bfloat16* hidden[NT];                 // of the counted tokens, in order
@@ -1366,25 +1372,6 @@ bool encode(CUtensorMap* map, const void* base, int64_t x, int64_t y, int64_t z,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Launches a kernel that may start its prologue while the one before it ends (see let_next_start).
-template <typename... Params, typename... Args>
-cudaError_t launch(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, int cluster, cudaStream_t st, const Args&... args) {
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = grid;
-  cfg.blockDim = block;
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = cluster;
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = cluster > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kernel, Params(args)...);
-}
-
 template <int PHASE>
 cudaError_t launch_gemm(LossParams& p, int ctas, int64_t tiles, int sms, cudaStream_t st) {
   if (tiles == 0) return cudaSuccess;
@@ -1489,15 +1476,14 @@ extern "C" HDET_API int hdet_token_loss(const hdet_token_loss_args* d, void* wor
   if (q.few) {
     const dim3 grid((unsigned)q.n_parts, d->n_replicas);
     const int64_t stride = shared_table ? 0 : table_stride;
-    if (d->n_tokens == 1) few_kernel<1><<<grid, 256, 0, st>>>(p, k, table, stride, table_row);
-    else if (d->n_tokens == 2) few_kernel<2><<<grid, 256, 0, st>>>(p, k, table, stride, table_row);
-    else few_kernel<kFew><<<grid, 256, 0, st>>>(p, k, table, stride, table_row);
-    e = cudaGetLastError();
+    e = launch(d->n_tokens == 1 ? few_kernel<1> : d->n_tokens == 2 ? few_kernel<2> : few_kernel<kFew>, grid, 256, 0, 1, st, p, k, table,
+               stride, table_row);
     if (e == cudaSuccess) e = launch(few_join_kernel, dim3(d->n_replicas), 32 * kFew, 0, 1, st, p);
     return e == cudaSuccess ? HDET_OK : fail_cuda(who, e);
   }
   const unsigned pack_blocks = (unsigned)(d->n_tokens > 0 ? div_up(d->n_tokens, kPackRows) : 1);
-  pack_kernel<<<dim3(pack_blocks, d->n_replicas), 256, 0, st>>>(k);
+  e = launch(pack_kernel, dim3(pack_blocks, d->n_replicas), 256, 0, 1, st, k);
+  if (e != cudaSuccess) return fail_cuda(who, e);
 
   if (q.pack_table) {
     __nv_bfloat16* packed = reinterpret_cast<__nv_bfloat16*>(ws + q.off_table);

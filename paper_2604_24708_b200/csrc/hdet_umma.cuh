@@ -195,11 +195,6 @@ __device__ __forceinline__ void tmem_load_wait(float (&x)[32]) {
       : "memory");
 }
 
-// Programmatic dependent launch: lets the next kernel of the stream start its prologue now, and waits until the kernels
-// before this one are done and their writes visible.  Neither does anything in a launch without that attribute.
-__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
