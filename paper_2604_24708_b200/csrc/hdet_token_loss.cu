@@ -116,8 +116,13 @@ struct Job {
   int k_blocks;
   int a_row, a_k, a_z, b_row, b_k, b_z;   // where the operands start
   int r, m0, n0, split;
+  int b_boxes;              // boxes of 64 columns that a CTA loads: 2, or 1 where the last tile needs no more
   bool is_dw;
 };
+
+// Boxes per CTA for a tile with `left` columns from its first to the end.
+template <int CTAS>
+__device__ __forceinline__ int boxes_for(int left) { return left > 64 * CTAS ? 2 : 1; }
 
 template <int CTAS, int PHASE>
 __device__ __forceinline__ bool find_job(const LossParams& p, const int* counts, int tile, Job& j) {
@@ -136,6 +141,7 @@ __device__ __forceinline__ bool find_job(const LossParams& p, const int* counts,
     j.b_row = p.v0 + j.n0; j.b_k = 0; j.b_z = p.weight_shared ? 0 : j.r;
     j.k_half = j.k_blocks = (p.width + kBlockK - 1) / kBlockK;
     j.split = 0; j.is_dw = false;
+    j.b_boxes = boxes_for<CTAS>(p.v_len - j.n0);
     return true;
   } else {
     // dH first: its sums are the longest, so the short dW tiles fill the machine's end
@@ -146,6 +152,7 @@ __device__ __forceinline__ bool find_job(const LossParams& p, const int* counts,
       j.r = p.r0 + g;
       j.m0 = mn / p.h_tiles_n * kTile;
       j.n0 = mn % p.h_tiles_n * kTile;
+      j.b_boxes = boxes_for<CTAS>(p.width - j.n0);
       if (j.m0 >= counts[j.r]) return false;
       const int all = (p.v_len + kBlockK - 1) / kBlockK;
       const int from = min(j.split * p.h_len, all), to = min(from + p.h_len, all);
@@ -164,6 +171,7 @@ __device__ __forceinline__ bool find_job(const LossParams& p, const int* counts,
     j.r = p.r0 + g;
     j.m0 = mn / p.w_tiles_n * kTile;
     j.n0 = mn % p.w_tiles_n * kTile;
+    j.b_boxes = boxes_for<CTAS>(p.width - j.n0);
     j.k_half = (counts[j.r] + kBlockK - 1) / kBlockK;
     j.k_blocks = j.k_half * (p.w_two ? 2 : 1);
     j.a = &p.grad_hi; j.a2 = &p.grad_lo; j.b = &p.hidden;
@@ -597,7 +605,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
         if (tile >= p.jobs) break;
         Job j;
         if (!find_job<CTAS, PHASE>(p, sh.count, tile, j)) continue;
-        const int a_row = j.a_row + 128 * (int)rank, b_row = j.b_row + 128 * (int)rank;
+        const int a_row = j.a_row + 128 * (int)rank, b_row = j.b_row + 64 * j.b_boxes * (int)rank;
         for (int step = 0; step < j.k_blocks; ++step, ++kb) {
           const int s = kb % kStages;
           if (kb >= kStages && !bulk::barrier_wait(bar(sh.empty[s]), (kb / kStages - 1) & 1)) {
@@ -605,7 +613,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
             break;
           }
           const uint32_t full = bar(sh.full[s]);
-          if (rank == 0) bulk::barrier_expect(full, CTAS * kStageBytes);
+          if (rank == 0) bulk::barrier_expect(full, CTAS * (kOperandBytes + j.b_boxes * kBoxBytes));
           const uint32_t done = CTAS == 1 ? full : in_cta(full, 0);
           const uint32_t dst = smem + s * kStageBytes;
           const bool second = step >= j.k_half;
@@ -618,6 +626,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
           }
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
+            if (h >= j.b_boxes) break;
             if (j.b_mn) load_box<CTAS>(dst + kOperandBytes + h * kBoxBytes, j.b, b_row + 64 * h, j.b_k + k, j.b_z, done);
             else load_box<CTAS>(dst + kOperandBytes + h * kBoxBytes, j.b, j.b_k + k, b_row + 64 * h, j.b_z, done);
           }
@@ -644,7 +653,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
         }
         fence_after_sync();
         const uint32_t acc = tmem + b * 128 * CTAS;
-        const uint32_t idesc = instruction_desc<CTAS>(j.a_mn, j.b_mn);
+        const uint32_t idesc = instruction_desc<CTAS>(64 * CTAS * j.b_boxes, j.a_mn, j.b_mn);
         const uint32_t a_step = k_step_bytes(j.a_mn), b_step = k_step_bytes(j.b_mn);
         for (int step = 0; step < j.k_blocks; ++step, ++kb) {
           const int s = kb % kStages;
@@ -753,7 +762,7 @@ struct PackParams {
   Control* control;
 };
 
-constexpr int kPackRows = 32;
+constexpr int kPackBlocks = 256;   // blocks per replica, about: more would count the targets too often
 
 // The target of a token, -1 for padding.
 __device__ __forceinline__ int target_of(const PackParams& p, int r, int t) {
@@ -766,12 +775,13 @@ __device__ __forceinline__ int target_of(const PackParams& p, int r, int t) {
   return v >= 0 && v < p.vocab ? v : -1;
 }
 
-// Moves the hidden states of counted tokens together, 32 tokens a block.  Every block counts the targets before its own
-// (and all of them) itself: that is 4 bytes a token from L2 instead of a launch of its own for the offsets.
-__global__ void __launch_bounds__(256) pack_kernel(const PackParams p) {
-  __shared__ int s_before[8], s_all[8], s_to[kPackRows];
+// Moves the hidden states of counted tokens together, `rows` tokens a block (a multiple of 8: one a warp at a time).  Every
+// block counts the targets before its own (and all of them) itself: that is 4 bytes a token from L2 instead of a launch of its
+// own for the offsets.
+__global__ void __launch_bounds__(256) pack_kernel(const PackParams p, int rows) {
+  __shared__ int s_before[8], s_all[8];
   const int r = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int t0 = blockIdx.x * kPackRows;
+  const int t0 = (int)blockIdx.x * rows, t1 = min(t0 + rows, p.n_tokens);
   let_next_start();
   wait_for_previous();
   if (blockIdx.x == 0 && threadIdx.x == 0) {
@@ -779,6 +789,7 @@ __global__ void __launch_bounds__(256) pack_kernel(const PackParams p) {
     if (r == 0) p.control->status = p.control->ticket = 0;
   }
   int before = 0, all = 0;
+#pragma unroll 4
   for (int t = threadIdx.x; t < p.n_tokens; t += 256) {
     const int one = target_of(p, r, t) >= 0;
     all += one;
@@ -792,43 +803,47 @@ __global__ void __launch_bounds__(256) pack_kernel(const PackParams p) {
 #pragma unroll
   for (int w = 0; w < 8; ++w) { before += s_before[w]; all += s_all[w]; }
   const int64_t base = (int64_t)r * p.rows_pad;
-  if (warp == 0) {
-    const int t = t0 + lane;
-    const int y = t < p.n_tokens ? target_of(p, r, t) : -1;
+  if (blockIdx.x == 0 && threadIdx.x == 0) p.count[r] = all;
+  // 32 tokens at a time: every warp finds out where they go, and moves every eighth
+  for (int first = t0; first < t1; first += 32) {
+    const int mine = first + lane;
+    const int y = mine < t1 ? target_of(p, r, mine) : -1;
     const unsigned counted = __ballot_sync(0xffffffffu, y >= 0);
-    const int to = y >= 0 ? before + __popc(counted & ((1u << lane) - 1)) : -1;
-    s_to[lane] = to;
-    if (to >= 0) {
-      p.target[base + to] = y;
-      p.token_of[base + to] = t;
-    } else if (t < p.n_tokens && p.token_loss) {
-      p.token_loss[r * p.token_loss_stride + t] = 0.0f;
-    }
-    if (blockIdx.x == 0 && lane == 0) p.count[r] = all;
-  }
-  __syncthreads();
-  for (int i = warp; i < kPackRows && t0 + i < p.n_tokens; i += 8) {
-    const int to = s_to[i];
-    const int64_t t = t0 + i;
-    if (to >= 0) {
-      const __nv_bfloat16* from = p.hidden + r * p.hidden_stride + t * p.hidden_row;
-      __nv_bfloat16* dst = p.packed + (base + to) * p.packed_row;
-      if (p.hidden_vec) {
-        for (int c = lane * 8; c < p.width; c += 256)
-          *reinterpret_cast<uint4*>(dst + c) = *reinterpret_cast<const uint4*>(from + c);
-      } else {
-        for (int c = lane; c < p.width; c += 32) dst[c] = from[c];
+    const int place = before + __popc(counted & ((1u << lane) - 1));
+    before += __popc(counted);
+    if (warp == 0 && mine < t1) {
+      if (y >= 0) {
+        p.target[base + place] = y;
+        p.token_of[base + place] = mine;
+      } else if (p.token_loss) {
+        p.token_loss[r * p.token_loss_stride + mine] = 0.0f;
       }
-    } else if (p.d_hidden.p) {
-      const int64_t at = r * p.d_hidden.stride + t * p.d_hidden.row;
-      const int size = p.d_hidden.f32 ? 4 : 2;
-      char* dst = static_cast<char*>(p.d_hidden.p) + at * size;
-      if (p.d_hidden_vec) {
-        for (int b = lane * 16; b < p.width * size; b += 512) *reinterpret_cast<uint4*>(dst + b) = make_uint4(0, 0, 0, 0);
-      } else {
-        for (int c = lane; c < p.width; c += 32) {
-          if (p.d_hidden.f32) reinterpret_cast<float*>(dst)[c] = 0.0f;
-          else reinterpret_cast<__nv_bfloat16*>(dst)[c] = __float2bfloat16_rn(0.0f);
+    }
+    for (int i = warp; i < 32 && first + i < t1; i += 8) {
+      const int to = __shfl_sync(0xffffffffu, place, i);
+      const int64_t t = first + i;
+      if (counted >> i & 1) {
+        const __nv_bfloat16* from = p.hidden + r * p.hidden_stride + t * p.hidden_row;
+        __nv_bfloat16* dst = p.packed + (base + to) * p.packed_row;
+        if (p.hidden_vec) {
+#pragma unroll 4
+          for (int c = lane * 8; c < p.width; c += 256)
+            *reinterpret_cast<uint4*>(dst + c) = *reinterpret_cast<const uint4*>(from + c);
+        } else {
+#pragma unroll 4
+          for (int c = lane; c < p.width; c += 32) dst[c] = from[c];
+        }
+      } else if (p.d_hidden.p) {
+        const int64_t at = r * p.d_hidden.stride + t * p.d_hidden.row;
+        const int size = p.d_hidden.f32 ? 4 : 2;
+        char* dst = static_cast<char*>(p.d_hidden.p) + at * size;
+        if (p.d_hidden_vec) {
+          for (int b = lane * 16; b < p.width * size; b += 512) *reinterpret_cast<uint4*>(dst + b) = make_uint4(0, 0, 0, 0);
+        } else {
+          for (int c = lane; c < p.width; c += 32) {
+            if (p.d_hidden.f32) reinterpret_cast<float*>(dst)[c] = 0.0f;
+            else reinterpret_cast<__nv_bfloat16*>(dst)[c] = __float2bfloat16_rn(0.0f);
+          }
         }
       }
     }
@@ -871,11 +886,10 @@ struct Lse {
 };
 
 // A row's loss, where it belongs.
-__device__ __forceinline__ void write_row(const LossParams& p, int r, int row, const Lse& l) {
-  const int64_t at = (int64_t)r * p.rows_pad + row;
-  const float loss = l.top + logf(l.sum) - p.z_target[at];
-  p.row_loss[at] = loss;
-  if (p.token_loss) p.token_loss[r * p.token_loss_stride + p.token_of[at]] = loss;
+__device__ __forceinline__ void write_row(const LossParams& p, int r, int row, const Lse& l, float picked, int token) {
+  const float loss = l.top + logf(l.sum) - picked;
+  p.row_loss[(int64_t)r * p.rows_pad + row] = loss;
+  if (p.token_loss) p.token_loss[r * p.token_loss_stride + token] = loss;
 }
 
 // After a block has written its rows' losses: the last of a replica's `blocks` adds them up (fp64, in a fixed order) and
@@ -914,13 +928,15 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ LossP
     const int64_t at = (int64_t)r * p.rows_pad + row;
     const int n = p.n_parts;
     const float2* part = p.part + at * n;
+    const float picked = p.z_target[at];
+    const int token = p.token_of[at];
     Lse l{-INFINITY, 0.0f};
 #pragma unroll 4
     for (int i = lane; i < n; i += 32) l.add(part[i]);
     l.add_warp();
     if (lane == 0) {
       p.lse2[at] = l.lse2();
-      write_row(p, r, row, l);
+      write_row(p, r, row, l, picked, token);
     }
   }
   finish_block(p, r, gridDim.x);
@@ -943,6 +959,8 @@ __global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ Loss
   if (row < count) {
     const int64_t at = (int64_t)r * p.rows_pad + row;
     const float2* part = p.part + at * n;
+    const float picked = p.z_target[at];
+    const int token = p.token_of[at], target = p.target[at];
     Lse l{-INFINITY, 0.0f};
     for (int i = threadIdx.x; i < n; i += 256) {
       const float2 o = part[i];
@@ -957,10 +975,9 @@ __global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ Loss
     for (int w = 1; w < 8; ++w) l.add(make_float2(s_lse[w].top, s_lse[w].sum));
     const float lse2 = l.lse2();
     for (int i = threadIdx.x; i < n; i += 256) s_factor[i] = exp2_fast(fmaf(s_factor[i], kLog2e, -lse2));
-    if (threadIdx.x == 0) write_row(p, r, row, l);
+    if (threadIdx.x == 0) write_row(p, r, row, l, picked, token);
     __syncthreads();
-    const int target = p.target[at];
-    const float g_target = exp2_fast(fmaf(p.z_target[at], kLog2e, -lse2)) - 1.0f;
+    const float g_target = exp2_fast(fmaf(picked, kLog2e, -lse2)) - 1.0f;
 #pragma unroll 4
     for (int i = threadIdx.x; i < vectors; i += 256) {
       const uint4 u = values[i];
@@ -1481,8 +1498,9 @@ extern "C" HDET_API int hdet_token_loss(const hdet_token_loss_args* d, void* wor
     if (e == cudaSuccess) e = launch(few_join_kernel, dim3(d->n_replicas), 32 * kFew, 0, 1, st, p);
     return e == cudaSuccess ? HDET_OK : fail_cuda(who, e);
   }
-  const unsigned pack_blocks = (unsigned)(d->n_tokens > 0 ? div_up(d->n_tokens, kPackRows) : 1);
-  e = launch(pack_kernel, dim3(pack_blocks, d->n_replicas), 256, 0, 1, st, k);
+  const int64_t pack_rows = round_up(div_up(d->n_tokens > 0 ? d->n_tokens : 1, kPackBlocks), 8);
+  const unsigned pack_blocks = (unsigned)(d->n_tokens > 0 ? div_up(d->n_tokens, pack_rows) : 1);
+  e = launch(pack_kernel, dim3(pack_blocks, d->n_replicas), 256, 0, 1, st, k, (int)pack_rows);
   if (e != cudaSuccess) return fail_cuda(who, e);
 
   if (q.pack_table) {

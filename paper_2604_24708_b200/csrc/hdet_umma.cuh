@@ -133,11 +133,11 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t smem, bool mn_major) {
 // Bytes from one group of 16 summed indices to the next inside a stage.
 __device__ __forceinline__ uint32_t k_step_bytes(bool mn_major) { return mn_major ? 2048 : 32; }
 
-// Instruction descriptor: bf16 x bf16 -> fp32, (128 * CTAS) x (128 * CTAS) x 16.
+// Instruction descriptor: bf16 x bf16 -> fp32, (128 * CTAS) x columns x 16.
 template <int CTAS>
-__device__ __forceinline__ uint32_t instruction_desc(bool a_mn_major, bool b_mn_major) {
+__device__ __forceinline__ uint32_t instruction_desc(int columns, bool a_mn_major, bool b_mn_major) {
   return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)a_mn_major << 15) | ((uint32_t)b_mn_major << 16) |
-         ((uint32_t)(128 * CTAS / 8) << 17) | ((uint32_t)(128 * CTAS / 16) << 24);
+         ((uint32_t)(columns / 8) << 17) | ((uint32_t)(128 * CTAS / 16) << 24);
 }
 
 // D (+)= A B^T for 16 summed indices; one thread (of the leader's CTA).
