@@ -5,7 +5,7 @@ been built (``python -m paper_2604_24708_b200.build``); there is no CPU fallback
 """
 import importlib
 
-__all__ = ["binding", "build"]
+__all__ = ["arena", "binding", "build", "vocab"]
 
 
 def __getattr__(name):

@@ -75,6 +75,24 @@ class StackedArena:
             out.append(t)
         return out
 
+    def param_view(self, k: int, shape: Sequence[int]) -> torch.Tensor:
+        """Tensor k of every replica: [N, *shape], a view of the parameters."""
+        return self._view(self.param, k, shape)
+
+    def grad_view(self, k: int, shape: Sequence[int]) -> torch.Tensor:
+        """Its gradients: [N, *shape], a view of what the update reads ([1, *shape] when one gradient is shared)."""
+        return self._view(self.grad if self.grad.dim() == 2 else self.grad[None], k, shape)
+
+    def mean_view(self, k: int, shape: Sequence[int]) -> torch.Tensor:
+        """The bf16 copy of its average that every converge writes: [*shape]."""
+        if self.param_bf16 is None:
+            raise ValueError("the arena was built without the bf16 copy")
+        return self._view(self.param_bf16[None], k, shape)[0]
+
+    def _view(self, t: torch.Tensor, k: int, shape: Sequence[int]) -> torch.Tensor:
+        off, ne = self.offsets[k], self.numels[k]
+        return t[:, off:off + ne].unflatten(1, tuple(shape))
+
     def resident_bytes(self) -> int:
         ts = [t for t in (self.param, self.grad, self.exp_avg, self.exp_avg_sq, self.param_bf16) if t is not None]
         return sum(t.numel() * t.element_size() for t in ts)
