@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import List, Optional, Sequence
 
 HDET_MAX_REPLICAS = 32
@@ -148,15 +149,16 @@ def _load() -> C.CDLL:
     lib.hdet_plan_tiles.restype = C.c_int
     lib.hdet_selftest_bounded_wait.argtypes = [H, C.c_void_p]
     lib.hdet_selftest_bounded_wait.restype = C.c_int
-    lib.hdet_embed.argtypes = [C.POINTER(hdet_embedding), C.c_void_p]
+    # descriptors of these calls are given as byref(struct) or as its packed bytes
+    lib.hdet_embed.argtypes = [C.c_void_p, C.c_void_p]
     lib.hdet_embed.restype = C.c_int
-    lib.hdet_embed_grad_workspace.argtypes = [C.POINTER(hdet_embedding), C.POINTER(C.c_int64)]
+    lib.hdet_embed_grad_workspace.argtypes = [C.c_void_p, C.POINTER(C.c_int64)]
     lib.hdet_embed_grad_workspace.restype = C.c_int
-    lib.hdet_embed_grad.argtypes = [C.POINTER(hdet_embedding), C.c_int32, C.c_void_p, C.c_int64, C.c_void_p]
+    lib.hdet_embed_grad.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p]
     lib.hdet_embed_grad.restype = C.c_int
-    lib.hdet_token_loss_workspace.argtypes = [C.POINTER(hdet_token_loss_args), C.POINTER(C.c_int64)]
+    lib.hdet_token_loss_workspace.argtypes = [C.c_void_p, C.POINTER(C.c_int64)]
     lib.hdet_token_loss_workspace.restype = C.c_int
-    lib.hdet_token_loss.argtypes = [C.POINTER(hdet_token_loss_args), C.c_void_p, C.c_int64, C.c_void_p]
+    lib.hdet_token_loss.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]
     lib.hdet_token_loss.restype = C.c_int
     for f in ("hdet_create", "hdet_set_schedule", "hdet_step", "hdet_converge", "hdet_autolr_update",
               "hdet_get_state", "hdet_set_state", "hdet_destroy"):
@@ -356,7 +358,13 @@ class _DtypeCodes(dict):
 _dtype_code = _DtypeCodes()
 
 
-# The calls below are used once per token by a model that is sampled, so their checks read every attribute once.
+# The calls below are used once per token by a model that is sampled, so their checks read every attribute once and their
+# descriptors are packed without building a ctypes struct (same layouts: hdet_embedding, hdet_token_loss_args).
+_EMBEDDING = struct.Struct("@3Q8qd6i")
+_TOKEN_LOSS = struct.Struct("@7Q13qdq10i")
+assert _EMBEDDING.size == C.sizeof(hdet_embedding) and _TOKEN_LOSS.size == C.sizeof(hdet_token_loss_args)
+
+
 def _rows_layout(tensor, n: int, what: str):
     """(replica stride, row stride) of [n, rows, width], or of [rows, width] (replica stride 0: one copy for all)."""
     shape, stride = tensor.shape, tensor.stride()
@@ -385,7 +393,7 @@ def _ids_stride(tensor, n: int, what: str) -> int:
     return stride[0]
 
 
-def _embedding(tokens, rows, table, n: int, scale: float) -> hdet_embedding:
+def _embedding(tokens, rows, table, n: int, scale: float) -> bytes:
     shape = rows.shape
     T, D = shape[-2], shape[-1]
     V, width = table.shape[-2:]
@@ -396,9 +404,9 @@ def _embedding(tokens, rows, table, n: int, scale: float) -> hdet_embedding:
         raise ValueError("all tensors must be on one CUDA device")
     rows_stride, rows_row = _rows_layout(rows, n, "rows")
     table_stride, table_row = _rows_layout(table, n, "table")
-    return hdet_embedding(tokens.data_ptr(), rows.data_ptr(), table.data_ptr(), T, V, D, _ids_stride(tokens, n, "tokens"),
-                          rows_stride, rows_row, table_stride, table_row, scale, n, _dtype_code[tokens.dtype],
-                          _dtype_code[rows.dtype], _dtype_code[table.dtype], device)
+    return _EMBEDDING.pack(tokens.data_ptr(), rows.data_ptr(), table.data_ptr(), T, V, D, _ids_stride(tokens, n, "tokens"),
+                           rows_stride, rows_row, table_stride, table_row, scale, n, _dtype_code[tokens.dtype],
+                           _dtype_code[rows.dtype], _dtype_code[table.dtype], device, 0)
 
 
 def hdet_embed(tokens, table, out, scale: float = 1.0, stream: int = 0) -> None:
@@ -406,7 +414,7 @@ def hdet_embed(tokens, table, out, scale: float = 1.0, stream: int = 0) -> None:
     [V, D] (one for all replicas) and out [N, T, D], float32 or bfloat16 each.  Tokens outside 0 .. V-1 give zeros."""
     if out.dim() != 3:
         raise ValueError("out must be [N, T, D]")
-    status = _lib.hdet_embed(C.byref(_embedding(tokens, out, table, out.shape[0], scale)), stream)
+    status = _lib.hdet_embed(_embedding(tokens, out, table, out.shape[0], scale), stream)
     if status:
         _check(status, None)
 
@@ -415,7 +423,7 @@ def hdet_embed_grad_workspace(tokens, d_out, d_table) -> int:
     """Bytes of workspace that hdet_embed_grad needs for these tensors."""
     d = _embedding(tokens, d_out, d_table, d_table.shape[0], 1.0)
     need = C.c_int64(0)
-    _check(_lib.hdet_embed_grad_workspace(C.byref(d), C.byref(need)), None)
+    _check(_lib.hdet_embed_grad_workspace(d, C.byref(need)), None)
     return int(need.value)
 
 
@@ -425,13 +433,13 @@ def hdet_embed_grad(tokens, d_out, d_table, workspace, scale: float = 1.0, accum
     if d_table.dim() != 3:
         raise ValueError("d_table must be [N, V, D]")
     d = _embedding(tokens, d_out, d_table, d_table.shape[0], scale)
-    ptr, size = _workspace(workspace, d.device)
-    status = _lib.hdet_embed_grad(C.byref(d), 1 if accumulate else 0, ptr, size, stream)
+    ptr, size = _workspace(workspace, tokens.get_device())
+    status = _lib.hdet_embed_grad(d, 1 if accumulate else 0, ptr, size, stream)
     if status:
         _check(status, None)
 
 
-def _token_loss_args(hidden, weight, targets, loss, token_loss, d_hidden, d_weight, n, grad_scale, accumulate, piece_bytes):
+def _token_loss_args(hidden, weight, targets, loss, token_loss, d_hidden, d_weight, n, grad_scale, accumulate, piece_bytes) -> bytes:
     T, D = hidden.shape[-2:]
     V, width = weight.shape[-2:]
     if targets.shape[-1] != T or width != D:
@@ -441,29 +449,31 @@ def _token_loss_args(hidden, weight, targets, loss, token_loss, d_hidden, d_weig
         raise ValueError("all tensors must be on one CUDA device")
     hidden_stride, hidden_row = _rows_layout(hidden, n, "hidden")
     weight_stride, weight_row = _rows_layout(weight, n, "weight")
-    a = hdet_token_loss_args(
-        hidden.data_ptr(), weight.data_ptr(), targets.data_ptr(), None, None, None, None, T, V, D, hidden_stride, hidden_row,
-        weight_stride, weight_row, _ids_stride(targets, n, "targets"), 0, 0, D, 0, D, grad_scale, piece_bytes, n,
-        _dtype_code[hidden.dtype], _dtype_code[weight.dtype], _dtype_code[targets.dtype], 0, 0, 0, 1 if accumulate else 0, device)
+    loss_at = loss_code = token_at = token_stride = dh_at = dh_stride = dh_code = dw_at = dw_stride = dw_code = 0
+    dh_row = dw_row = D
     if loss is not None:
         if loss.shape != (n,) or loss.get_device() != device or (n > 1 and loss.stride(0) != 1):
             raise ValueError("loss must be a contiguous [N] on the inputs' device")
-        a.loss, a.loss_dtype = loss.data_ptr(), _dtype_code[loss.dtype]
+        loss_at, loss_code = loss.data_ptr(), _dtype_code[loss.dtype]
     if token_loss is not None:
         if token_loss.shape != (n, T) or token_loss.get_device() != device or _dtype_code[token_loss.dtype] != HDET_DTYPE_F32:
             raise ValueError("token_loss must be float32 [N, T] on the inputs' device")
-        a.token_loss, a.token_loss_stride = token_loss.data_ptr(), _ids_stride(token_loss, n, "token_loss")
+        token_at, token_stride = token_loss.data_ptr(), _ids_stride(token_loss, n, "token_loss")
     if d_hidden is not None:
         if d_hidden.shape != (n, T, D) or d_hidden.get_device() != device:
             raise ValueError("d_hidden must be [N, T, D] on the inputs' device")
-        a.d_hidden, a.d_hidden_dtype = d_hidden.data_ptr(), _dtype_code[d_hidden.dtype]
-        a.d_hidden_stride, a.d_hidden_row = _rows_layout(d_hidden, n, "d_hidden")
+        dh_at, dh_code = d_hidden.data_ptr(), _dtype_code[d_hidden.dtype]
+        dh_stride, dh_row = _rows_layout(d_hidden, n, "d_hidden")
     if d_weight is not None:
         if d_weight.shape != (n, V, D) or d_weight.get_device() != device:
             raise ValueError("d_weight must be [N, V, D] on the inputs' device")
-        a.d_weight, a.d_weight_dtype = d_weight.data_ptr(), _dtype_code[d_weight.dtype]
-        a.d_weight_stride, a.d_weight_row = _rows_layout(d_weight, n, "d_weight")
-    return a
+        dw_at, dw_code = d_weight.data_ptr(), _dtype_code[d_weight.dtype]
+        dw_stride, dw_row = _rows_layout(d_weight, n, "d_weight")
+    return _TOKEN_LOSS.pack(
+        hidden.data_ptr(), weight.data_ptr(), targets.data_ptr(), loss_at, token_at, dh_at, dw_at, T, V, D, hidden_stride, hidden_row,
+        weight_stride, weight_row, _ids_stride(targets, n, "targets"), token_stride, dh_stride, dh_row, dw_stride, dw_row, grad_scale,
+        piece_bytes, n, _dtype_code[hidden.dtype], _dtype_code[weight.dtype], _dtype_code[targets.dtype], loss_code, dh_code, dw_code,
+        1 if accumulate else 0, device, 0)
 
 
 def _replicas(*tensors) -> int:
@@ -479,7 +489,7 @@ def hdet_token_loss_workspace(hidden, weight, targets, d_hidden=None, d_weight=N
     n = _replicas((hidden, 2), (weight, 2), (targets, 1), (d_hidden, 2), (d_weight, 2))
     a = _token_loss_args(hidden, weight, targets, None, None, d_hidden, d_weight, n, 1.0, False, piece_bytes)
     need = C.c_int64(0)
-    _check(_lib.hdet_token_loss_workspace(C.byref(a), C.byref(need)), None)
+    _check(_lib.hdet_token_loss_workspace(a, C.byref(need)), None)
     return int(need.value)
 
 
@@ -491,8 +501,8 @@ def hdet_token_loss(hidden, weight, targets, loss, workspace, token_loss=None, d
     ``d_hidden`` [N, T, D] and ``d_weight`` [N, V, D] (float32 or bfloat16; ``accumulate`` adds d_weight to what is there)."""
     a = _token_loss_args(hidden, weight, targets, loss, token_loss, d_hidden, d_weight, loss.shape[0], grad_scale, accumulate,
                          piece_bytes)
-    ptr, size = _workspace(workspace, a.device)
-    status = _lib.hdet_token_loss(C.byref(a), ptr, size, stream)
+    ptr, size = _workspace(workspace, hidden.get_device())
+    status = _lib.hdet_token_loss(a, ptr, size, stream)
     if status:
         _check(status, None)
 

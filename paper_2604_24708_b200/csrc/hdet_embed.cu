@@ -20,9 +20,8 @@ using hdet::launch;
 using hdet::let_next_start;
 using hdet::wait_for_previous;
 
-constexpr int kChunkSmall = 1024;   // tokens ranked against one another at once when there are many
-constexpr int kChunkLarge = 2048;   // ... when all of them fit: one launch less, twice the comparisons per token
-constexpr int kMergeRuns = 16;      // sorted runs merged per level
+constexpr int kChunk = 1024;        // tokens sorted by one block
+constexpr int kMergeRuns = 8;       // sorted runs merged per level
 constexpr int kEntries = 32;        // sorted entries per warp in the gradient kernel, one per lane
 constexpr int kFewEntries = 8;      // ... when there are too few to keep the machine busy: one batch of loads each
 
@@ -103,47 +102,6 @@ __global__ void __launch_bounds__(256) lookup_kernel(const EmbedParams p) {
 }
 
 // ------------------------------------------------------------------------------------------------ sorting
-// Rank of every token among its chunk's by comparing it with all of them: no passes, no atomics, one launch.  With
-// 1024 tokens a chunk that is 2 instructions x 1024 per token, spread over chunk / 256 blocks a chunk.
-// Equal tokens keep their order: tokens before this one count when <=, tokens behind it when <.
-__global__ void __launch_bounds__(256) rank_chunks_kernel(const EmbedParams p, int chunk, int* __restrict__ key_out,
-                                                          int* __restrict__ pos_out) {
-  extern __shared__ int4 s_tok4[];
-  let_next_start();
-  wait_for_previous();
-  int* s_tok = reinterpret_cast<int*>(s_tok4);
-  const int r = blockIdx.y;
-  const int parts = chunk / 256;
-  const int64_t c0 = (int64_t)(blockIdx.x / parts) * chunk;
-  const int n = (int)(p.n_tokens - c0 < chunk ? p.n_tokens - c0 : chunk);
-  const int mine = (blockIdx.x % parts) * 256 + threadIdx.x;
-  if ((int)(blockIdx.x % parts) * 256 >= n) return;
-  const int n4 = (n + 3) & ~3;
-  // entries behind the end compare as larger than every row and than "no row"
-  for (int i = threadIdx.x; i < n4; i += 256)
-    s_tok[i] = i < n ? row_of(p.tokens, p.wide, r * p.token_stride + c0 + i, p.vocab) : 0x7fffffff;
-  __syncthreads();
-  if (mine >= n) return;
-  const int key = s_tok[mine];
-  const int warp0 = mine & ~31;                 // the warp's own 32 tokens are compared one by one
-  const int warp1 = warp0 + 32 < n4 ? warp0 + 32 : n4;
-  int rank = 0;
-#pragma unroll 4
-  for (int j = 0; j < warp0 / 4; ++j) {
-    const int4 o = s_tok4[j];
-    rank += (o.x <= key) + (o.y <= key) + (o.z <= key) + (o.w <= key);
-  }
-  for (int j = warp0; j < warp1; ++j) rank += j < mine ? s_tok[j] <= key : s_tok[j] < key;
-#pragma unroll 4
-  for (int j = warp1 / 4; j < n4 / 4; ++j) {
-    const int4 o = s_tok4[j];
-    rank += (o.x < key) + (o.y < key) + (o.z < key) + (o.w < key);
-  }
-  const int64_t at = r * p.n_tokens + c0 + rank;
-  key_out[at] = key;
-  pos_out[at] = (int)(c0 + mine);
-}
-
 // Entries of run[0 .. n) that come before `key`: those < key, or <= key.
 __device__ __forceinline__ int64_t count_before(const int* __restrict__ run, int64_t n, int key, bool or_equal) {
   int64_t lo = 0, hi = n;
@@ -155,9 +113,57 @@ __device__ __forceinline__ int64_t count_before(const int* __restrict__ run, int
   return lo;
 }
 
+// Sorts 1024 tokens a block, one a thread: 32 in a warp by comparing each with all, then runs of 32, 64, .. 512 are merged in
+// pairs, where an entry's place is its place in its own run plus the entries of the other run that come before it (a binary
+// search in shared memory).  Equal tokens keep their order: of the run before, those that are equal count too.
+// Comparing all 1024 with one another instead took 13.3 us for 8 x 8192 tokens, this takes 6.1 us.
+__global__ void __launch_bounds__(kChunk) sort_chunks_kernel(const EmbedParams p, int* __restrict__ key_out, int* __restrict__ pos_out) {
+  __shared__ int s_key[2][kChunk], s_from[2][kChunk];
+  let_next_start();
+  wait_for_previous();
+  const int r = blockIdx.y, i = threadIdx.x, lane = i & 31;
+  const int64_t c0 = (int64_t)blockIdx.x * kChunk;
+  // entries behind the end compare as larger than every row and than "no row"
+  int key = c0 + i < p.n_tokens ? row_of(p.tokens, p.wide, r * p.token_stride + c0 + i, p.vocab) : 0x7fffffff;
+  int from = i, place = 0;
+#pragma unroll
+  for (int j = 0; j < 32; ++j) {
+    const int o = __shfl_sync(0xffffffffu, key, j);
+    place += o < key || (o == key && j < lane);
+  }
+  place += i - lane;
+  int now = 0;
+  s_key[0][place] = key;
+  s_from[0][place] = from;
+  __syncthreads();
+#pragma unroll
+  for (int run = 32; run < kChunk; run *= 2) {
+    key = s_key[now][i];
+    from = s_from[now][i];
+    const bool second = i & run;
+    const int* other = s_key[now] + ((i & ~(run - 1)) ^ run);
+    int before = 0;                                // entries of the other run that come before this one
+#pragma unroll
+    for (int step = run; step > 0; step /= 2) {
+      if (before + step > run) continue;
+      const int o = other[before + step - 1];
+      if (o < key || (o == key && second)) before += step;
+    }
+    place = (i & ~(2 * run - 1)) + (i & (run - 1)) + before;
+    now ^= 1;
+    s_key[now][place] = key;
+    s_from[now][place] = from;
+    __syncthreads();
+  }
+  if (c0 + i < p.n_tokens) {
+    key_out[r * p.n_tokens + c0 + i] = s_key[now][i];
+    pos_out[r * p.n_tokens + c0 + i] = (int)c0 + s_from[now][i];
+  }
+}
+
 // Merges groups of kMergeRuns sorted runs of `run` (a power of two) entries: an entry's place in its group is its place in
 // its own run plus, for every other run, the entries there that come before it.  The searches in the other runs go step by
-// step together, so that their loads are under way at once (one after the other they took 17.4 us for 8 x 8192 tokens).
+// step together, so that their loads are under way at once.
 __global__ void __launch_bounds__(256) merge_runs_kernel(int64_t n, int64_t run, const int* __restrict__ key_in,
                                                          const int* __restrict__ pos_in, int* __restrict__ key_out,
                                                          int* __restrict__ pos_out) {
@@ -173,13 +179,15 @@ __global__ void __launch_bounds__(256) merge_runs_kernel(int64_t n, int64_t run,
 #pragma unroll
   for (int q = 0; q < kMergeRuns; ++q) before[q] = 0;
   for (int64_t step = run; step > 0; step >>= 1) {
+    int o[kMergeRuns];                             // the last of each run's next `step` entries
 #pragma unroll
     for (int q = 0; q < kMergeRuns; ++q) {
-      const int64_t at = (first + q) * run + before[q] + step - 1;     // the last of the next `step` entries
-      if (before[q] + step > run || at >= n || first + q == own) continue;
-      const int o = keys[at];
-      if (o < key || (o == key && first + q < own)) before[q] += (int)step;
+      const int64_t at = (first + q) * run + before[q] + step - 1;
+      o[q] = before[q] + step <= run && at < n && first + q != own ? keys[at] : 0x7fffffff;
     }
+#pragma unroll
+    for (int q = 0; q < kMergeRuns; ++q)
+      if (o[q] < key || (o[q] == key && first + q < own)) before[q] += (int)step;
   }
   int64_t at = first * run + (i - own * run);
 #pragma unroll
@@ -223,8 +231,11 @@ __device__ __forceinline__ void write_row(const GradParams& p, int r, int key, i
 // that lies inside the block is finished here; the piece of a run that came from the block before goes to partial slot 0, the piece
 // of a run that starts here and goes on into the next block to slot 1, and join_kernel adds those in order.
 // Other warps write zeros to the table rows that have no token.  The two kinds of blocks alternate in the grid, in proportion,
-// so that the sums' loads hide behind the zeros' stores (8 x 8192 tokens, width 2048: REPLACE_MIX).
-template <typename RowT, typename TableT, int VEC>
+// so that the sums' loads hide behind the zeros' stores (8 x 8192 tokens, width 2048: 1.5 % less than the zeros behind the sums).
+//
+// With ADD, the table's rows that a batch of entries will finish are loaded along with the entries' own: loaded one by one at
+// the end of each run they took 141 us for that batch, with this it is 122 us.
+template <typename RowT, typename TableT, int VEC, bool ADD>
 __global__ void __launch_bounds__(256) grad_kernel(const GradParams p) {
   // The next kernel is not let in early here: its blocks would wait in places that this grid's own later blocks need (with it,
   // 16 x 1024 tokens of width 768 took 249 us instead of 215).
@@ -274,13 +285,19 @@ __global__ void __launch_bounds__(256) grad_kernel(const GradParams p) {
 #pragma unroll
   for (int i = 0; i < VEC; ++i) acc[i] = 0.0f;
   bool from_before = false;
-  constexpr int kAhead = 8;
+  constexpr int kAhead = ADD ? 4 : 8;
+  TableT* table = static_cast<TableT*>(p.e.table) + r * p.e.table_stride;
   for (int e0 = 0; e0 < count; e0 += kAhead) {
     Pack<RowT, VEC> x[kAhead];
+    Pack<TableT, VEC> old[ADD ? kAhead : 1];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       const int ps = __shfl_sync(0xffffffffu, my_pos, (e0 + k) & 31);
       if (e0 + k < count && on) x[k].load(rows + ps * p.e.rows_row + c);
+      if constexpr (ADD) {
+        const int key = __shfl_sync(0xffffffffu, my_key, (e0 + k) & 31), next = __shfl_sync(0xffffffffu, my_key, (e0 + k + 1) & 31);
+        if (e0 + k < count && on && (next != key || e0 + k + 1 == p.entries)) old[k].load(table + key * p.e.table_row + c);
+      }
     }
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
@@ -303,7 +320,13 @@ __global__ void __launch_bounds__(256) grad_kernel(const GradParams p) {
 #pragma unroll
           for (int i = 0; i < VEC; ++i) to[i] = acc[i];
         } else {
-          write_row<TableT, VEC>(p, r, key, c, acc);
+          Pack<TableT, VEC> y;
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) {
+            if constexpr (ADD) y.set(i, fmaf(acc[i], p.e.scale, old[k].get(i)));
+            else y.set(i, acc[i] * p.e.scale);
+          }
+          y.store(table + key * p.e.table_row + c);
         }
       }
 #pragma unroll
@@ -316,7 +339,7 @@ __global__ void __launch_bounds__(256) grad_kernel(const GradParams p) {
 // The runs that start in an entry block and go on behind it: their pieces are added in order.  A block of threads looks at 32
 // entry blocks and one column chunk; every run found is one warp's, and a run of more than kLongRun pieces is shared by all
 // eight, which take consecutive stretches whose sums are added in order, so no result depends on timing.
-constexpr int kLongRun = 64;
+constexpr int kLongRun = 64, kJoinBlocks = 32;
 
 template <int VEC>
 __device__ __forceinline__ void add_pieces(const float* first, int64_t width, int64_t from, int64_t to, float (&acc)[VEC]) {
@@ -335,22 +358,49 @@ __global__ void __launch_bounds__(256) join_kernel(const GradParams p) {
   let_next_start();
   wait_for_previous();
   const int r = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t block0 = (int64_t)(blockIdx.x / p.n_col) * 32;
+  const int64_t block0 = (int64_t)(blockIdx.x / p.n_col) * kJoinBlocks;
   const int64_t c = (blockIdx.x % p.n_col) * (32 * VEC) + (int64_t)lane * VEC;
   const bool on = c < p.e.width;
   const int64_t n = p.e.n_tokens;
   const int* keys = p.keys + r * p.sorted_stride;
-  // lane l of every warp: does a run start in entry block block0 + l and go on behind it, and for how many blocks
+  // lane l of every warp: does a run start in entry block block0 + l and go on behind it
   const int64_t i0 = (block0 + lane) * p.entries, next = i0 + p.entries;
-  int key = p.e.vocab;
+  int key = p.e.vocab, head = p.e.vocab, after = -1;   // the block's last and first key, the next block's first
   bool runs = false;
-  if (next < n) {
-    key = keys[next - 1];
-    runs = key < p.e.vocab && keys[next] == key && !(i0 > 0 && keys[i0] == key && keys[i0 - 1] == key);
+  if (i0 < n) {
+    head = keys[i0];
+    if (next < n) {
+      key = keys[next - 1];
+      after = keys[next];
+      runs = key < p.e.vocab && after == key && !(i0 > 0 && head == key && keys[i0 - 1] == key);
+    }
   }
+  // Of how many pieces: the blocks here whose first key is the run's.  Only one run can go on behind these 32 blocks: its end
+  // is searched for.
+  const int beyond = __shfl_sync(0xffffffffu, after, 31);
+  const unsigned all = __ballot_sync(0xffffffffu, runs);
   int64_t pieces = 0;
-  if (runs) pieces = (next + count_before(keys + next, n - next, key, true) - 1) / p.entries - (block0 + lane) + 1;
-  const unsigned all = __ballot_sync(0xffffffffu, runs), shared_runs = __ballot_sync(0xffffffffu, pieces > kLongRun);
+  for (unsigned todo = all; todo; todo &= todo - 1) {
+    const int l = __ffs(todo) - 1, row = __shfl_sync(0xffffffffu, key, l);
+    const unsigned on_from = __ballot_sync(0xffffffffu, head == row && lane > l);
+    if (lane == l) pieces = 1 + __popc(on_from);
+  }
+  if (__any_sync(0xffffffffu, runs && key == beyond)) {   // 32 blocks at a time, then by halves
+    int64_t more = 0;
+    bool whole = true;
+    for (int step = 0; step < 4 && whole; ++step) {
+      const int64_t at = (block0 + 32 * (step + 1) + lane) * p.entries;
+      const unsigned same = __ballot_sync(0xffffffffu, at < n && keys[at] == beyond);
+      more += __popc(same);
+      whole = same == 0xffffffffu;
+    }
+    if (whole) {
+      const int64_t at = (block0 + 32 * 5) * p.entries;
+      more += at < n ? div_up(count_before(keys + at, n - at, beyond, true), p.entries) : 0;
+    }
+    if (runs && key == beyond) pieces += more;
+  }
+  const unsigned shared_runs = __ballot_sync(0xffffffffu, pieces > kLongRun);
   float acc[VEC];
   int turn = 0;
   for (unsigned todo = all & ~shared_runs; todo; todo &= todo - 1, ++turn) {
@@ -503,9 +553,10 @@ cudaError_t launch_grad(GradParams p, cudaStream_t st) {
   p.zero_ctas = (unsigned)div_up(p.zero_units, 8);
   cudaError_t e = cudaSuccess;
   if (p.grad_ctas + p.zero_ctas > 0)
-    e = launch(grad_kernel<RowT, TableT, VEC>, dim3(p.grad_ctas + p.zero_ctas, p.e.n_replicas), 256, 0, 1, st, p);
+    e = launch(p.accumulate ? grad_kernel<RowT, TableT, VEC, true> : grad_kernel<RowT, TableT, VEC, false>,
+               dim3(p.grad_ctas + p.zero_ctas, p.e.n_replicas), 256, 0, 1, st, p);
   if (e == cudaSuccess && p.n_blocks > 1)
-    e = launch(join_kernel<TableT, VEC>, dim3((unsigned)(div_up(p.n_blocks, 32) * p.n_col), p.e.n_replicas), 256, 0, 1, st, p);
+    e = launch(join_kernel<TableT, VEC>, dim3((unsigned)(div_up(p.n_blocks, kJoinBlocks) * p.n_col), p.e.n_replicas), 256, 0, 1, st, p);
   return e;
 }
 
@@ -551,7 +602,8 @@ GradLayout layout_of(const hdet_embedding* d) {
   GradLayout l{};
   const auto up = [](int64_t x) { return div_up(x, 256) * 256; };
   l.sorted_replicas = d->n_replicas > 1 && d->token_stride != 0 ? d->n_replicas : 1;
-  // Fewer than four warps a SM in the gradient kernel: shorter entry blocks make more of them (96 tokens of width 72: REPLACE_ENT).
+  // Fewer than four warps a SM in the gradient kernel: shorter entry blocks make more of them (96 tokens of
+  // width 72: 6.8 us instead of 8.6).
   l.entries = div_up(d->n_tokens, kEntries) * div_up(d->width, 256) * d->n_replicas < 4 * 148 ? kFewEntries : kEntries;
   l.list_bytes = up(4 * d->n_tokens * l.sorted_replicas);
   l.partial_off = 4 * l.list_bytes;
@@ -605,10 +657,9 @@ extern "C" HDET_API int hdet_embed_grad(const hdet_embedding* d, int32_t accumul
   const EmbedParams e = params_of(d);
   int now = 0;
   if (d->n_tokens > 0) {
-    const int chunk = d->n_tokens > kChunkSmall && d->n_tokens <= kChunkLarge ? kChunkLarge : kChunkSmall;
-    const dim3 grid((unsigned)(div_up(d->n_tokens, chunk) * (chunk / 256)), l.sorted_replicas);
-    cudaError_t err = launch(rank_chunks_kernel, grid, 256, chunk * 4, 1, st, e, chunk, key[0], pos[0]);
-    for (int64_t run = chunk; run < d->n_tokens && err == cudaSuccess; run *= kMergeRuns, now ^= 1)
+    cudaError_t err = launch(sort_chunks_kernel, dim3((unsigned)div_up(d->n_tokens, kChunk), l.sorted_replicas), kChunk, 0, 1, st, e,
+                             key[0], pos[0]);
+    for (int64_t run = kChunk; run < d->n_tokens && err == cudaSuccess; run *= kMergeRuns, now ^= 1)
       err = launch(merge_runs_kernel, dim3((unsigned)div_up(d->n_tokens, 256), l.sorted_replicas), 256, 0, 1, st, d->n_tokens, run,
                    key[now], pos[now], key[now ^ 1], pos[now ^ 1]);
     if (err != cudaSuccess) return fail_cuda("hdet_embed_grad", err);
