@@ -520,8 +520,8 @@ typedef struct {
  *   loss[r] = mean of token_loss[r,t] over the counted targets,
  *   d_hidden, d_weight = grad_scale x the gradients of loss[r].
  * The logits are formed on the tensor cores (bf16 products, fp32 sums) tile by tile, twice when gradients are asked for;
- * losses and softmax are fp32, means fp64.  The softmax's gradient is a bf16 operand of the two products behind it, a
- * pair of bf16 numbers for fp32 gradients (then they cost twice the products).  The same inputs give the same bits.
+ * losses and softmax are fp32, means fp64.  The softmax's gradient is a bf16 operand of the two products behind it; for
+ * fp32 gradients it is the sum of three bf16 numbers (24 bits), and they cost three times the products.  The same inputs give the same bits.
  * Work goes with the counted targets: padding is left out of the products.
  * If a bounded wait inside a kernel runs out, every loss is set to NaN.
  * hdet_token_loss_workspace gives the bytes that the call needs; it looks at sizes, strides, dtypes, piece_bytes, the

@@ -78,22 +78,43 @@ __device__ __forceinline__ bool wait_cluster(uint32_t bar, uint32_t parity, long
   }
 }
 
+// The instructions below are issued by one lane, which `elect.sync` picks, while the whole warp runs the loop around them with
+// the same values in every lane: their operands live in registers that the warp shares.  In a loop that one lane runs alone,
+// every operand is moved there first, and the loop of the products took longer than the tensor cores need (282 us instead
+// of 263 for 2048 x 50176 logits of width 2048).
+
 // One 64 x 64 box into this CTA's shared memory; completion counted in bytes on `bar` (in the leader's CTA for a pair).
-// Coordinates: x in elements along the contiguous axis (a multiple of 64 here, so 16-byte aligned), y, z.
+// Coordinates: x in elements along the contiguous axis (a multiple of 64 here, so 16-byte aligned), y, z.  Whole warp.
 template <int CTAS>
 __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
   if constexpr (CTAS == 1) {
     asm volatile(
-        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+        "{\n .reg .pred q;\n .reg .b32 r;\n elect.sync r|q, 0xffffffff;\n"
+        " @q cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n}" ::"r"(dst),
         "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
         : "memory");
   } else {
     asm volatile(
-        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], "
-        "[%5];" ::"r"(dst),
+        "{\n .reg .pred q;\n .reg .b32 r;\n elect.sync r|q, 0xffffffff;\n"
+        " @q cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], "
+        "[%5];\n}" ::"r"(dst),
         "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
         : "memory");
   }
+}
+
+// bulk::barrier_expect by one lane.
+__device__ __forceinline__ void expect_bytes(uint32_t bar, uint32_t bytes) {
+  asm volatile(
+      "{\n .reg .pred q;\n .reg .b32 r;\n elect.sync r|q, 0xffffffff;\n @q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n}" ::"r"(bar),
+      "r"(bytes)
+      : "memory");
+}
+
+// bulk::barrier_wait by a whole warp, with one answer for all of its lanes.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, long long limit_cycles = bulk::kWaitLimitCycles) {
+  if (__all_sync(0xffffffffu, bulk::barrier_try_wait(bar, parity))) return true;
+  return __all_sync(0xffffffffu, bulk::barrier_wait(bar, parity, limit_cycles));
 }
 
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
@@ -140,31 +161,37 @@ __device__ __forceinline__ uint32_t instruction_desc(int columns, bool a_mn_majo
          ((uint32_t)(columns / 8) << 17) | ((uint32_t)(128 * CTAS / 16) << 24);
 }
 
-// D (+)= A B^T for 16 summed indices; one thread (of the leader's CTA).
+// D (+)= A B^T for 16 summed indices.  Whole warp (of the leader's CTA).
 template <int CTAS>
 __device__ __forceinline__ void mma(uint32_t tmem, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
   if constexpr (CTAS == 1) {
     asm volatile(
-        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(tmem),
+        "{\n .reg .pred p, q;\n .reg .b32 r;\n elect.sync r|q, 0xffffffff;\n setp.ne.b32 p, %4, 0;\n"
+        " @q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(tmem),
         "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
         : "memory");
   } else {
     asm volatile(
-        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(tmem),
+        "{\n .reg .pred p, q;\n .reg .b32 r;\n elect.sync r|q, 0xffffffff;\n setp.ne.b32 p, %4, 0;\n"
+        " @q tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(tmem),
         "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
         : "memory");
   }
 }
 
-// Arrives on `bar` once everything this thread has issued to the tensor core is done; for a pair, on the barrier at the
-// same place in both CTAs.
+// Arrives on `bar` once everything that this warp's lane has issued to the tensor core is done; for a pair, on the barrier at
+// the same place in both CTAs.  Whole warp.
 template <int CTAS>
 __device__ __forceinline__ void commit(uint32_t bar) {
   if constexpr (CTAS == 1) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    asm volatile(
+        "{\n .reg .pred q;\n .reg .b32 r;\n elect.sync r|q, 0xffffffff;\n"
+        " @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}" ::"r"(bar)
+        : "memory");
   } else {
     asm volatile(
-        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+        "{\n .reg .pred q;\n .reg .b32 r;\n elect.sync r|q, 0xffffffff;\n"
+        " @q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n}" ::"r"(bar),
         "h"((uint16_t)3)
         : "memory");
   }
@@ -191,6 +218,25 @@ __device__ __forceinline__ void tmem_load_wait(float (&x)[32]) {
         "+f"(x[8]), "+f"(x[9]), "+f"(x[10]), "+f"(x[11]), "+f"(x[12]), "+f"(x[13]), "+f"(x[14]), "+f"(x[15]),
         "+f"(x[16]), "+f"(x[17]), "+f"(x[18]), "+f"(x[19]), "+f"(x[20]), "+f"(x[21]), "+f"(x[22]), "+f"(x[23]),
         "+f"(x[24]), "+f"(x[25]), "+f"(x[26]), "+f"(x[27]), "+f"(x[28]), "+f"(x[29]), "+f"(x[30]), "+f"(x[31])
+      :
+      : "memory");
+}
+
+// The same for 16 columns, and the wait for them.
+__device__ __forceinline__ void tmem_load16(uint32_t tmem, float (&x)[16]) {
+  uint32_t* u = reinterpret_cast<uint32_t*>(x);
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]),
+        "=r"(u[9]), "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15])
+      : "r"(tmem));
+}
+
+__device__ __forceinline__ void tmem_load_wait(float (&x)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+      : "+f"(x[0]), "+f"(x[1]), "+f"(x[2]), "+f"(x[3]), "+f"(x[4]), "+f"(x[5]), "+f"(x[6]), "+f"(x[7]),
+        "+f"(x[8]), "+f"(x[9]), "+f"(x[10]), "+f"(x[11]), "+f"(x[12]), "+f"(x[13]), "+f"(x[14]), "+f"(x[15])
       :
       : "memory");
 }
