@@ -21,6 +21,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <algorithm>
 #include <climits>
 #include <cmath>
 #include <cstdio>
@@ -291,6 +292,8 @@ template <int CTAS>
 struct Columns {            // of one row: half of a tile's columns
   float x[CTAS][2][32];
 };
+template <>
+struct Columns<0> {};
 
 template <int CTAS>
 __device__ __forceinline__ void clear(Columns<CTAS>& acc) {
@@ -318,6 +321,33 @@ __device__ __forceinline__ void take_columns(uint32_t tmem, Columns<CTAS>& acc, 
     }
   }
 }
+
+// Where an epilogue finds its columns: in the accumulator (SUMS false: one chunk, read 64 columns at a time, which leaves the
+// kernel's registers to the loads), or in registers.
+template <int CTAS, bool SUMS>
+struct Source {
+  uint32_t tmem;            // the reader's lanes, at the first column of its half
+  Columns<CTAS>* acc;
+  bool empty;               // nothing was summed
+  // Columns c .. c + 63: those in registers themselves, or `x` with what the accumulator holds.
+  __device__ __forceinline__ float (&get(int c, float (&x)[2][32]) const)[2][32] {
+    if constexpr (SUMS) {
+      return acc->x[c / 64];
+    } else {
+      if (empty) {
+#pragma unroll
+        for (int i = 0; i < 64; ++i) x[i / 32][i % 32] = 0.0f;
+      } else {
+        __syncwarp();
+        tmem_load32(tmem + c, x[0]);
+        tmem_load32(tmem + c + 32, x[1]);
+        tmem_load_wait(x[0]);
+        tmem_load_wait(x[1]);
+      }
+      return x;
+    }
+  }
+};
 
 __device__ __forceinline__ float largest(const float (&x)[2][32]) {
   float top[4] = {x[0][0], x[0][1], x[1][0], x[1][1]};
@@ -360,16 +390,17 @@ __device__ __forceinline__ float exponentials(float (&x)[2][32], float shift) {
   return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
-// `acc`: the reader's row, its half of the tile's columns; `half`: the first of those within the tile.
-template <int CTAS>
-__device__ __forceinline__ void stats_epilogue(const LossParams& p, const Job& j, Columns<CTAS>& acc, int row, int half, int target) {
+// `from`: the reader's row, its half of the tile's columns; `half`: the first of those within the tile.
+template <int CTAS, bool SUMS>
+__device__ __forceinline__ void stats_epilogue(const LossParams& p, const Job& j, const Source<CTAS, SUMS>& from, int row, int half, int target) {
   constexpr int kCols = 64 * CTAS;
   const int64_t at = (int64_t)j.r * p.rows_pad + row;
   const int v0 = j.n0 + half;
   float top = -INFINITY, sum = 0.0f, picked = 0.0f;
-#pragma unroll
+#pragma unroll (SUMS ? CTAS : 1)
   for (int c = 0; c < kCols; c += 64) {
-    float (&x)[2][32] = acc.x[c / 64];
+    float loaded[2][32];
+    float (&x)[2][32] = from.get(c, loaded);
     cut_columns(x, v0 + c, p.vocab);
     pick_column(x, v0 + c, target, picked);
     const float now = fmaxf(top, largest(x));
@@ -385,16 +416,17 @@ __device__ __forceinline__ void stats_epilogue(const LossParams& p, const Job& j
 // The same, and the numerators exp(z - maximum of the half tile's row) go to the workspace, where scale_kernel turns them
 // into G.  They are fp16: between 0 and 1 it is off by 2^-12 of the value, or 2^-25 below 2^-14, less than the rounding of
 // G to bf16 that follows.  The sum is taken before that rounding.
-template <int CTAS>
-__device__ __forceinline__ void numerators_epilogue(const LossParams& p, const Job& j, Columns<CTAS>& acc, int row, int half,
+template <int CTAS, bool SUMS>
+__device__ __forceinline__ void numerators_epilogue(const LossParams& p, const Job& j, const Source<CTAS, SUMS>& from, int row, int half,
                                                     int target, uint32_t staging, int lane) {
   constexpr int kCols = 64 * CTAS;
   const int64_t at = (int64_t)j.r * p.rows_pad + row;
   const int v0 = j.n0 + half;
   float top = -INFINITY, sum = 0.0f, picked = 0.0f;
-#pragma unroll
+#pragma unroll (SUMS ? CTAS : 1)
   for (int c = 0; c < kCols; c += 64) {
-    float (&x)[2][32] = acc.x[c / 64];
+    float loaded[2][32];
+    float (&x)[2][32] = from.get(c, loaded);
     cut_columns(x, v0 + c, p.vocab);
     pick_column(x, v0 + c, target, picked);
     top = fmaxf(top, largest(x));
@@ -404,9 +436,11 @@ __device__ __forceinline__ void numerators_epilogue(const LossParams& p, const J
   rows.base = reinterpret_cast<char*>(p.g);
   rows.offset = (((int64_t)(j.r - p.r0) * p.rows_pad + row) * p.v_pitch + v0) * 2;
   rows.on = 0xffffffffu;
-#pragma unroll
+#pragma unroll (SUMS ? CTAS : 1)
   for (int c = 0; c < kCols; c += 64) {
-    float (&x)[2][32] = acc.x[c / 64];
+    float loaded[2][32];
+    float (&x)[2][32] = from.get(c, loaded);
+    cut_columns(x, v0 + c, p.vocab);
     sum += exponentials(x, shift);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
@@ -419,8 +453,8 @@ __device__ __forceinline__ void numerators_epilogue(const LossParams& p, const J
   if (target >= v0 && target < v0 + kCols) p.z_target[at] = picked;
 }
 
-template <int CTAS>
-__device__ __forceinline__ void probs_epilogue(const LossParams& p, const Job& j, Columns<CTAS>& acc, int row, int half, bool counted,
+template <int CTAS, bool SUMS>
+__device__ __forceinline__ void probs_epilogue(const LossParams& p, const Job& j, const Source<CTAS, SUMS>& from, int row, int half, bool counted,
                                                int target, float lse2, uint32_t staging, int lane) {
   constexpr int kCols = 64 * CTAS;
   target = counted ? target - p.v0 : -1;
@@ -428,9 +462,10 @@ __device__ __forceinline__ void probs_epilogue(const LossParams& p, const Job& j
   Rows rows;
   rows.offset = (((int64_t)(j.r - p.r0) * p.rows_pad + row) * p.v_pitch + v0) * 2;
   rows.on = 0xffffffffu;
-#pragma unroll
+#pragma unroll (SUMS ? CTAS : 1)
   for (int c = 0; c < kCols; c += 64) {
-    float (&x)[2][32] = acc.x[c / 64];
+    float loaded[2][32];
+    float (&x)[2][32] = from.get(c, loaded);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int v = v0 + c + 32 * h;
@@ -467,8 +502,8 @@ __device__ __forceinline__ void probs_epilogue(const LossParams& p, const Job& j
   }
 }
 
-template <int CTAS>
-__device__ __forceinline__ void grads_epilogue(const LossParams& p, const Job& j, Columns<CTAS>& acc, int row, int half, int count,
+template <int CTAS, bool SUMS>
+__device__ __forceinline__ void grads_epilogue(const LossParams& p, const Job& j, const Source<CTAS, SUMS>& from, int row, int half, int count,
                                                uint32_t staging, int lane) {
   constexpr int kCols = 64 * CTAS;
   Out o;
@@ -494,10 +529,11 @@ __device__ __forceinline__ void grads_epilogue(const LossParams& p, const Job& j
   rows.base = static_cast<char*>(o.p);
   rows.offset = base * (o.f32 ? 4 : 2);
   rows.on = __ballot_sync(0xffffffffu, on);
-#pragma unroll
+#pragma unroll (SUMS ? CTAS : 1)
   for (int c = 0; c < kCols; c += 64) {
     if (n0 + c >= p.width) break;
-    float (&x)[2][32] = acc.x[c / 64];
+    float loaded[2][32];
+    float (&x)[2][32] = from.get(c, loaded);
 #pragma unroll
     for (int i = 0; i < 32; ++i) { x[0][i] *= scale; x[1][i] *= scale; }
     if (!o.vec) {
@@ -550,7 +586,7 @@ static_assert(kGemmSmem <= 227 * 1024, "shared memory of one CTA");
 // products, which adds up.  A table of 50257 rows makes 6284 times of it, and dH in fp32 was 9.6e-5 off.  So the sum is
 // taken out every `chunk` steps and goes on in the readers' registers, in fp32 and rounded, while the other accumulator
 // fills.
-template <int CTAS, int PHASE>
+template <int CTAS, int PHASE, bool SUMS>
 __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_constant__ LossParams p) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t smem = (bulk::smem_addr(smem_raw) + 1023u) & ~1023u;
@@ -711,7 +747,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
             mma<CTAS>(acc, a_desc + (uint32_t)(s * kStageBytes + k * a_step) / 16, b_desc + (uint32_t)(s * kStageBytes + k * b_step) / 16, idesc,
                       in_chunk > 0 || k > 0);
           commit<CTAS>(bar(sh.empty[s]));
-          if (++in_chunk == p.chunk || step + 1 == j.k_blocks) {
+          ++in_chunk;
+          if ((SUMS && in_chunk == p.chunk) || step + 1 == j.k_blocks) {
             commit<CTAS>(bar(sh.acc_full[uses & 1]));
             ++uses;
             in_chunk = 0;
@@ -770,28 +807,42 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
         target = p.target[(int64_t)j.r * p.rows_pad + row];
         if (PHASE == kProbs && row < sh.count[j.r]) lse2 = p.lse2[(int64_t)j.r * p.rows_pad + row];
       }
-      Columns<CTAS> acc;
-      if (j.k_blocks == 0) clear(acc);
-      bool ok = true;
-      for (int step = 0; step < j.k_blocks; step += p.chunk, ++uses) {
-        const int b = uses & 1;
-        ok = bulk::barrier_wait(bar(sh.acc_full[b]), (uses / 2) & 1, 2 * bulk::kWaitLimitCycles);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        fence_after_sync();
-        take_columns(tmem + b * 128 * CTAS + half + ((uint32_t)(quarter * 32) << 16), acc, step > 0);
+      Columns<SUMS ? CTAS : 0> acc;
+      if constexpr (SUMS) {
+        if (j.k_blocks == 0) clear(acc);
+      }
+      const auto acc_at = [&] { return tmem + (uses & 1) * 128 * CTAS + half + ((uint32_t)(quarter * 32) << 16); };
+      const auto acc_done = [&] {
         fence_before_sync();
         __syncwarp();
-        if (lane == 0) arrive_leader(bar(sh.acc_empty[b]));
+        if (lane == 0) arrive_leader(bar(sh.acc_empty[uses & 1]));
+        ++uses;
+      };
+      bool ok = true;
+      for (int step = 0; step < j.k_blocks; step += SUMS ? p.chunk : j.k_blocks) {
+        ok = warp_wait(bar(sh.acc_full[uses & 1]), (uses / 2) & 1, 2 * bulk::kWaitLimitCycles);
+        if (!ok) break;
+        fence_after_sync();
+        if constexpr (SUMS) {
+          take_columns(acc_at(), acc, step > 0);
+          acc_done();
+        }
       }
       if (!ok) {
         failed = 1;
         break;
       }
-      if constexpr (PHASE == kStats) stats_epilogue<CTAS>(p, j, acc, row, half, target);
-      else if constexpr (PHASE == kNumerators) numerators_epilogue<CTAS>(p, j, acc, row, half, target, staging, lane);
-      else if constexpr (PHASE == kProbs) probs_epilogue<CTAS>(p, j, acc, row, half, row < sh.count[j.r], target, lse2, staging, lane);
-      else grads_epilogue<CTAS>(p, j, acc, row, half, sh.count[j.r], staging, lane);
+      Source<CTAS, SUMS> from;
+      from.tmem = acc_at();
+      from.empty = j.k_blocks == 0;
+      if constexpr (SUMS) from.acc = &acc;
+      if constexpr (PHASE == kStats) stats_epilogue(p, j, from, row, half, target);
+      else if constexpr (PHASE == kNumerators) numerators_epilogue(p, j, from, row, half, target, staging, lane);
+      else if constexpr (PHASE == kProbs) probs_epilogue(p, j, from, row, half, row < sh.count[j.r], target, lse2, staging, lane);
+      else grads_epilogue(p, j, from, row, half, sh.count[j.r], staging, lane);
+      if constexpr (!SUMS) {
+        if (j.k_blocks > 0) acc_done();
+      }
     }
   }
   __syncwarp();
@@ -1433,10 +1484,12 @@ cudaError_t prepare(int device, int* sms) {
     *sms = g_sms[device];
     return cudaSuccess;
   }
-  const void* kernels[] = {(const void*)gemm_kernel<1, kStats>, (const void*)gemm_kernel<1, kNumerators>, (const void*)gemm_kernel<1, kProbs>,
-                           (const void*)gemm_kernel<1, kGrads>,
-                           (const void*)gemm_kernel<2, kStats>, (const void*)gemm_kernel<2, kNumerators>, (const void*)gemm_kernel<2, kProbs>,
-                           (const void*)gemm_kernel<2, kGrads>};
+  const void* kernels[] = {
+#define HDET_PHASES(ctas, sums)                                                                              \
+  (const void*)gemm_kernel<ctas, kStats, sums>, (const void*)gemm_kernel<ctas, kNumerators, sums>,           \
+      (const void*)gemm_kernel<ctas, kProbs, sums>, (const void*)gemm_kernel<ctas, kGrads, sums>
+      HDET_PHASES(1, false), HDET_PHASES(1, true), HDET_PHASES(2, false), HDET_PHASES(2, true)};
+#undef HDET_PHASES
   for (const void* k : kernels) {
     const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmem);
     if (e != cudaSuccess) return e;
@@ -1460,16 +1513,23 @@ bool encode(CUtensorMap* map, const void* base, int64_t x, int64_t y, int64_t z,
 // 3e-8 to 5e-7, 14 % slower; 16 steps up to 1.9e-6, 6 % faster).  Logits: 64, all of a width up to 4096 (their terms' signs
 // vary: the loss is 1.4e-7 off).  bf16 gradients: 256, 3e-5, far below their rounding.
 constexpr int kChunkLogits = 64, kChunkF32 = 8, kChunkBf16 = 256;
+constexpr int kWholeBf16 = 1024;   // bf16 gradients up to this many steps are not cut at all: 1e-4
 
 template <int PHASE>
 cudaError_t launch_gemm(LossParams& p, int ctas, int64_t tiles, int sms, cudaStream_t st) {
   if (tiles == 0) return cudaSuccess;
   const int64_t clusters = tiles < sms / ctas ? tiles : sms / ctas;
   p.jobs = (int)tiles;
+  // the longest sum of this launch, and what it is cut into
+  const int64_t longest = PHASE != kGrads ? div_up(p.width, kBlockK)
+                                          : std::max<int64_t>(p.h_jobs ? (int64_t)p.h_len * p.h_terms : 0,
+                                                              p.w_tiles_m ? div_up(p.n_tokens, kBlockK) * p.w_terms : 0);
   p.chunk = PHASE != kGrads ? kChunkLogits : p.g_terms > 1 ? kChunkF32 : kChunkBf16;
+  const bool sums = longest > (PHASE == kGrads && p.g_terms == 1 ? kWholeBf16 : p.chunk);
   const dim3 grid((unsigned)(clusters * ctas));
-  const cudaError_t e = ctas == 1 ? launch(gemm_kernel<1, PHASE>, grid, kGemmThreads, kGemmSmem, 1, st, p)
-                                  : launch(gemm_kernel<2, PHASE>, grid, kGemmThreads, kGemmSmem, 2, st, p);
+  const auto kernel = ctas == 1 ? (sums ? gemm_kernel<1, PHASE, true> : gemm_kernel<1, PHASE, false>)
+                                : (sums ? gemm_kernel<2, PHASE, true> : gemm_kernel<2, PHASE, false>);
+  const cudaError_t e = launch(kernel, grid, kGemmThreads, kGemmSmem, ctas, st, p);
   p.first_ticket += (unsigned)tiles;
   return e;
 }

@@ -284,6 +284,14 @@ def test_pieces_of_the_vocabulary(size, piece, dt):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("size", [(1, 20, 150, 4168), (2, 150, 300, 4200), (1, 70000, 130, 40), (1, 9000, 20000, 64)], ids=str)
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_long_sums(size, dt):
+    """Sums over the width, the tokens or the vocabulary that leave the tensor cores in several chunks."""
+    _run(*_inputs(*size, seed=13), dt, dt)
+
+
+@pytest.mark.gpu
 def test_one_table_one_batch_for_all_replicas():
     for T in (60, 260):
         h, w, y = _inputs(3, T, 500, 96, seed=20)
