@@ -47,8 +47,8 @@ constexpr int kStageBytes = 2 * kOperandBytes;
 // lanes (warp % 4) and half of its columns each
 constexpr int kGemmThreads = 384, kFirstReader = 4, kReaders = 8;
 constexpr int kStagingBytes = 4096;        // per reader: 32 rows x 128 bytes
-constexpr int kAskAt = 4;                  // step at which a tile's successor is looked up
-constexpr int kTileSlots = 4;              // tiles handed out ahead of the readers
+constexpr int kAskAhead = 8;               // steps before a tile's end at which its successor is looked up
+constexpr int kTileSlots = 4;              // tiles under way between the copies and the readers
 constexpr long long kDrainLimitCycles = 200000000ll;
 
 __host__ __device__ constexpr int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -564,7 +564,7 @@ __device__ __forceinline__ void grads_epilogue(const LossParams& p, const Job& j
 struct Shared {             // behind the stages and the readers' staging
   uint64_t full[kStages], empty[kStages];          // a stage holds its operands; the products have read it
   uint64_t acc_full[2], acc_empty[2];              // an accumulator is complete; its readers are done with it
-  uint64_t tile_full[kTileSlots], tile_empty[kTileSlots];
+  uint64_t tile_full[kTileSlots], tile_empty[kTileSlots], taken;   // taken: the leader's copies have the last tile published
   alignas(16) Job job[kTileSlots];
   uint32_t tmem;
   int failed, issued;
@@ -577,7 +577,7 @@ static_assert(kGemmSmem <= 227 * 1024, "shared memory of one CTA");
 // Tiles of (128 * CTAS) x (128 * CTAS), one CTA a SM (a pair for each two) that stays: the copies run ahead into the next
 // tile while the products finish this one, and two accumulators let the readers empty one while the other fills.  Tiles
 // differ in length (a replica's counted tokens, dH beside dW), so they are handed out one by one: a thread of the leader draws
-// the next number, works out what it means and gives that to both CTAs, up to four tiles ahead (worked out where it is used,
+// the next number, works out what it means and gives that to both CTAs, a tile ahead (worked out where it is used,
 // with its divisions, it held up the copies at every tile: 1.38 ms became 1.51 for 8 x 2048 tokens of width 1024).  The
 // counter goes on from launch to launch of a call; every launch draws `jobs` numbers (each cluster's first tile needs none, its
 // last number is one too many), so the host knows where the next begins.
@@ -618,6 +618,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
       bulk::barrier_init(bar(sh.tile_full[q]), 1);
       bulk::barrier_init(bar(sh.tile_empty[q]), (1 + kReaders) * CTAS + 1);   // copies and readers, and the leader's products
     }
+    bulk::barrier_init(bar(sh.taken), 1);
     bulk::barrier_init_fence();
   }
   if (warp == 1) tmem_alloc<CTAS>(bulk::smem_addr(&sh.tmem), 2 * 128 * CTAS);
@@ -656,7 +657,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
     // one value for the warp, so that what is worked out from it is the warp's too
 #pragma unroll
     for (int k = 0; k < 15; ++k) to[k] = __shfl_sync(0xffffffffu, to[k], 0);
-    if (lane == 0) arrive_leader(bar(sh.tile_empty[q]));
+    if (lane == 0) {
+      arrive_leader(bar(sh.tile_empty[q]));
+      if (warp == 0 && rank == 0) bulk::barrier_arrive(bar(sh.taken));
+    }
     return j.k_blocks >= 0 && __all_sync(0xffffffffu, !failed);
   };
   // operands of this kernel's products: G W, G^T H, or H W^T
@@ -671,7 +675,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
       Job j, next;
       bool more = next_job(0, j);
       for (int i = 0; more; ++i, j = next) {
-        const int ask_at = j.k_blocks > kAskAt ? kAskAt : j.k_blocks - 1;   // the next tile is looked up while this one is under way
+        const int ask_at = j.k_blocks > kAskAhead ? j.k_blocks - kAskAhead : 0;   // the next tile is looked up while this one is under way
         const CUtensorMap* const b_map = j.is_dw ? &p.hidden : &p.weight;
         const bool a_outer = a_mn(j);
         const int a_row = j.a_row + 128 * (int)rank, b_row = j.b_row + 64 * j.b_boxes * (int)rank;
@@ -722,7 +726,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
       Job j, next;
       bool more = next_job(0, j);
       for (int i = 0; more; ++i, j = next) {
-        const int ask_at = j.k_blocks > kAskAt ? kAskAt : j.k_blocks - 1;
+        const int ask_at = j.k_blocks > kAskAhead ? j.k_blocks - kAskAhead : 0;
         const uint32_t idesc = instruction_desc<CTAS>(64 * CTAS * j.b_boxes, a_mn(j), b_mn);
         const uint32_t a_step = k_step_bytes(a_mn(j)), b_step = k_step_bytes(b_mn);
         const uint64_t a_desc = operand_desc(smem, a_mn(j)), b_desc = operand_desc(smem + kOperandBytes, b_mn);
@@ -766,21 +770,20 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
   } else if (warp == 2) {
     if (lane == 0 && rank == 0) {
       const unsigned clusters = gridDim.x / CTAS;
-      unsigned ticket = atomicAdd(&p.control->ticket, 1u);
+      // A number is drawn when the copies have taken the one before: one drawn earlier may be a tile that another cluster, with
+      // nothing left to do, could have had (four drawn ahead: 102 us instead of 77 for 3 x 129 tokens x 4099, width 520).
       for (int use = 0;;) {
-        const unsigned t = ticket - p.first_ticket;
-        const bool last = t >= (unsigned)p.jobs - clusters;
-        Job j;
-        j.k_blocks = -1;
-        if (!last) {
-          ticket = atomicAdd(&p.control->ticket, 1u);         // on its way while this one is worked out
-          if (!find_job<CTAS, PHASE>(p, sh.count, (int)(t + clusters), j)) continue;
-        }
         const int q = use % kTileSlots;
-        if (use >= kTileSlots && !wait_cluster(bar(sh.tile_empty[q]), (use / kTileSlots - 1) & 1, 2 * bulk::kWaitLimitCycles)) {
+        if ((use > 0 && !bulk::barrier_wait(bar(sh.taken), (use - 1) & 1, 2 * bulk::kWaitLimitCycles)) ||
+            (use >= kTileSlots && !wait_cluster(bar(sh.tile_empty[q]), (use / kTileSlots - 1) & 1, 2 * bulk::kWaitLimitCycles))) {
           failed = 1;
           break;
         }
+        const unsigned t = atomicAdd(&p.control->ticket, 1u) - p.first_ticket;
+        const bool last = t >= (unsigned)p.jobs - clusters;
+        Job j;
+        if (!last && !find_job<CTAS, PHASE>(p, sh.count, (int)(t + clusters), j)) continue;   // nothing counted there
+        if (last) j.k_blocks = -1;
         ++use;
         const int* from = reinterpret_cast<const int*>(&j);
 #pragma unroll
@@ -1375,7 +1378,9 @@ struct Plan {
 Plan plan_of(const hdet_token_loss_args* d) {
   Plan q{};
   const int64_t R = d->n_replicas, T = d->n_tokens, V = d->vocab, D = d->width;
-  q.ctas = T > 128 ? 2 : 1;
+  // Pairs share operands, single CTAs make four times as many tiles.  1 x 1024 tokens x 50257 (width 768), loss and bf16
+  // gradients: 293 us in pairs, 348 in singles; 1 x 256 x 4099 (512): 42 and 39; 1 x 150 x 50257 (768): 125 and 110.
+  q.ctas = T <= 192 || R * div_up(T, 256) * div_up(V, 256) < 64 ? 1 : 2;
   q.tile = 128 * q.ctas;
   q.rows_pad = round_up(T > 0 ? T : 1, q.tile);
   q.packed_row = round_up(D, 8);
