@@ -1419,15 +1419,25 @@ Plan plan_of(const hdet_token_loss_args* d) {
     // twice 4.67; 8 x 2048 of width 2048: 8.39 and 10.1.)
     q.numerators = q.n_pieces == 1 && q.g_terms == 1 && q.n_tiles <= kMaxScaleTiles;
     if (d->d_hidden) {
-      // dH's sums run over the piece, dW's over the tokens.  dH is split so that its tiles are not longer than an equal
-      // share of the launch's work: otherwise a few of them would run on alone.
+      // dH's sums run over the piece, dW's over the tokens: dH has few tiles and long sums.  Cut into parts, it ends with the
+      // rest of the launch's work; every part more costs a pass over fp32 partial sums, about two steps a tile.  The cut taken
+      // is the one with the shortest end: rounds of dH's jobs, or an equal share of all the work where that is longer.
       const int64_t all = div_up(q.piece, kBlockK), h_tiles = q.group * q.m_tiles * div_up(D, q.tile);
       const int64_t w_tiles = d->d_weight ? q.group * (q.piece / q.tile) * div_up(D, q.tile) : 0;
       const int64_t work = h_tiles * all * q.h_terms + w_tiles * div_up(T, kBlockK) * q.w_terms;
-      int64_t share = work / (kSlots * (3 - q.ctas)) / q.h_terms;
-      if (share < 8) share = 8;
-      q.h_len = div_up(all, div_up(all, share));
-      q.h_splits = div_up(all, q.h_len);
+      const int64_t slots = kSlots * (3 - q.ctas);
+      double best = 0.0;
+      for (int64_t parts = 1; parts <= 64; ++parts) {
+        const int64_t len = div_up(all, parts), n = div_up(all, len);
+        if (n != parts || (parts > 1 && len < 8)) continue;
+        const double rounds = (double)(div_up(h_tiles * n, slots) * len * q.h_terms), share = (double)work / (double)slots;
+        const double end = (rounds > share ? rounds : share) + (n > 1 ? 2.0 * (double)(h_tiles * n) / (double)slots : 0.0);
+        if (best == 0.0 || end < 0.98 * best) {
+          best = end;
+          q.h_len = len;
+          q.h_splits = n;
+        }
+      }
       q.h_slabs = q.h_splits > 1 || q.n_pieces > 1;
     }
   }
