@@ -519,10 +519,13 @@ typedef struct {
  *   z = hidden[r,t] . weight[r,v],  lse = log sum_v exp z,  token_loss[r,t] = lse - z_target,
  *   loss[r] = mean of token_loss[r,t] over the counted targets,
  *   d_hidden, d_weight = grad_scale x the gradients of loss[r].
- * The logits are formed on the tensor cores (bf16 products, fp32 sums) tile by tile, twice when gradients are asked for;
+ * The logits are formed on the tensor cores (bf16 products, fp32 sums) tile by tile, for the gradients a second time (but see below);
  * losses and softmax are fp32, means fp64.  The softmax's gradient is a bf16 operand of the two products behind it; for
  * fp32 gradients it is the sum of three bf16 numbers (24 bits), and they cost three times the products.  The same inputs give the same bits.
  * Work goes with the counted targets: padding is left out of the products.
+ * With bf16 gradients and a piece that holds all of a replica's vocabulary the logits are formed once: the workspace then
+ * keeps their exponentials (fp16) until the row's sum is known.
+ * Outputs must not overlap inputs or one another, except that d_hidden may be the hidden states' own buffer.
  * If a bounded wait inside a kernel runs out, every loss is set to NaN.
  * hdet_token_loss_workspace gives the bytes that the call needs; it looks at sizes, strides, dtypes, piece_bytes, the
  * table's address (its alignment) and at which gradients are asked for.

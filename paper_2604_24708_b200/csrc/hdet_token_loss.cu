@@ -4,15 +4,22 @@
 //   Z = H W^T,  lse_t = log sum_v exp Z_tv,  l_t = lse_t - Z_{t,y_t},  loss = mean of l_t
 //   P = exp(Z - lse),  G = P - onehot(y),  dH = (c) G W,  dW = (c) G^T H,  c = grad_scale / counted tokens
 //
-// Three products of T x V x D, plus one more because Z is formed twice: once for lse, once for G, which needs it.
+// Three products of T x V x D.  G needs lse, which needs all of Z: a piece of the work is as much of G as the workspace holds, as
+// many whole replicas as fit, else a part of one replica's vocabulary.
 //
-//   pack      counted tokens move together (padding drops out: no work, and nothing it holds reaches a product)
-//   stats     Z tile by tile on the tensor cores; the epilogue keeps, of each tile's row, its maximum and sum of exp
-//   join      those over the vocabulary: lse, the token's loss, the replica's mean
-//   probs     Z again, for a piece of the vocabulary; the epilogue writes G as bf16 into the workspace
-//   grads     both products with G in one launch; after the last piece, dH's partial sums are joined
-//
-// A piece is as much of G as the workspace holds: as many whole replicas as fit, else a part of one replica's vocabulary.
+//   pack        counted tokens move together (padding drops out: no work, and nothing it holds reaches a product)
+// and then, where whole replicas fit and G is bf16, for each group of them
+//   numerators  Z tile by tile on the tensor cores; the epilogue keeps, of each half tile's row, its maximum m and the sum of
+//               exp(z - m), and leaves exp(z - m) in G's place
+//   scale       lse and the token's loss from those; exp(z - m) becomes G in place; the last block takes the replica's mean
+//   grads       both products with G in one launch
+// or, forming Z twice (a fourth product, but nothing kept but G),
+//   stats       Z, of which the epilogue keeps the maxima and sums
+//   join        lse, the token's loss, the replica's mean
+// and for each piece of the vocabulary
+//   probs       Z again; the epilogue writes G
+//   grads       as above; after the last piece, dH's partial sums are joined
+// Up to four tokens a replica without gradients take a kernel of their own (few).
 //
 // G is the operand of a bf16 product, so it is rounded to bf16, unscaled: the -1 of the target is then exact where the
 // target is unlikely.  Its relative error, 2^-9 a value, is that of a bf16 gradient's own rounding.  For fp32 gradients
@@ -1448,7 +1455,8 @@ Plan plan_of(const hdet_token_loss_args* d) {
   q.off_token = take(4 * R * q.rows_pad);
   q.off_z = take(4 * R * q.rows_pad);
   q.off_lse = take(4 * R * q.rows_pad);
-  q.off_part = take(8 * R * q.n_parts * q.rows_pad);
+  // room for either kernel's parts: the query does not know the hidden states' address
+  q.off_part = take(8 * R * (q.n_parts > 2 * q.n_tiles ? q.n_parts : 2 * q.n_tiles) * q.rows_pad);
   q.off_loss = take(4 * R * q.rows_pad);
   q.off_hidden = take(2 * R * q.rows_pad * q.packed_row);
   if (q.pack_table) q.off_table = take(2 * (d->n_replicas > 1 && d->weight_stride ? R : 1) * V * q.packed_row);

@@ -303,6 +303,28 @@ def test_one_table_one_batch_for_all_replicas():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("T", [3, 70, 300])
+def test_as_many_replicas_as_there_can_be(T):
+    h, w, y = _inputs(B.HDET_MAX_REPLICAS, T, 90, 72, seed=25)
+    y[5] = -1
+    _run(h, w, y)
+    _run(h, w, y, "bf16", "bf16")
+    _run(h, w, y, "f32", "f32", piece_bytes=1)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [70, 300])
+def test_the_gradient_in_the_place_of_the_hidden_states(T):
+    h, w, y = _inputs(2, T, 500, 96, seed=26)
+    loss, apart = torch.empty(2, device="cuda"), torch.empty_like(h)
+    ws = torch.empty(B.hdet_token_loss_workspace(h, w, y, d_hidden=apart), dtype=torch.uint8, device="cuda")
+    st = torch.cuda.current_stream().cuda_stream
+    B.hdet_token_loss(h, w, y, loss, ws, d_hidden=apart, stream=st)
+    B.hdet_token_loss(h, w, y, loss, ws, d_hidden=h, stream=st)
+    assert torch.equal(h, apart)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("T", [40, 400])
 def test_replicas_without_a_target_and_no_tokens(T):
     h, w, y = _inputs(3, T, 200, 64, seed=21)
