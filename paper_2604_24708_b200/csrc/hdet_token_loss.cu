@@ -203,21 +203,6 @@ __device__ __forceinline__ uint32_t f16_pair(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// Writes up to 32 consecutive values of one row of a gradient whose rows do not start and end on 16-byte boundaries.
-__device__ __forceinline__ void write_values(const Out& o, int64_t at, const float (&x)[32], int n) {
-  if (o.f32) {
-    float* to = static_cast<float*>(o.p) + at;
-#pragma unroll
-    for (int i = 0; i < 32; ++i)
-      if (i < n) to[i] = o.accumulate ? to[i] + x[i] : x[i];
-  } else {
-    __nv_bfloat16* to = static_cast<__nv_bfloat16*>(o.p) + at;
-#pragma unroll
-    for (int i = 0; i < 32; ++i)
-      if (i < n) to[i] = __float2bfloat16_rn(o.accumulate ? __bfloat162float(to[i]) + x[i] : x[i]);
-  }
-}
-
 // ------------------------------------------------------------------------------------------------ epilogues
 // One thread per row of the tile; a reader's half of the accumulator's columns passes through registers 64 at a time.
 //
@@ -290,6 +275,27 @@ __device__ __forceinline__ void add_staged(const Rows& rows, uint32_t at, int la
         v.z += __uint_as_float(old.y << 16); v.w += __uint_as_float(old.y & 0xffff0000u);
       }
       *to = make_uint2(bf16_pair(v.x, v.y), bf16_pair(v.z, v.w));
+    }
+  }
+  __syncwarp();
+}
+
+// The same for gradients whose rows do not start and end on 16-byte boundaries: a row's 32 values by 32 threads.
+__device__ __forceinline__ void write_elements(const Rows& rows, uint32_t at, int lane, int col, int width, bool f32, bool accumulate) {
+  __syncwarp();
+  const int c = col + lane;
+#pragma unroll 4
+  for (int row = 0; row < 32; ++row) {
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at + row * 128 + (((lane >> 2) ^ (row & 7)) << 4) + (lane & 3) * 4) : "memory");
+    const int64_t offset = __shfl_sync(0xffffffffu, rows.offset, row);
+    if (!(rows.on >> row & 1) || c >= width) continue;
+    if (f32) {
+      float* to = reinterpret_cast<float*>(rows.base + offset) + c;
+      *to = accumulate ? *to + v : v;
+    } else {
+      __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(rows.base + offset) + c;
+      *to = __float2bfloat16_rn(accumulate ? __bfloat162float(*to) + v : v);
     }
   }
   __syncwarp();
@@ -543,11 +549,7 @@ __device__ __forceinline__ void grads_epilogue(const LossParams& p, const Job& j
     float (&x)[2][32] = from.get(c, loaded);
 #pragma unroll
     for (int i = 0; i < 32; ++i) { x[0][i] *= scale; x[1][i] *= scale; }
-    if (!o.vec) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        if (on) write_values(o, base + n0 + c + 32 * h, x[h], min(32, p.width - n0 - c - 32 * h));
-    } else if (!o.f32 && !o.accumulate) {
+    if (o.vec && !o.f32 && !o.accumulate) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         const float* y = &x[k / 4][8 * (k % 4)];
@@ -561,7 +563,8 @@ __device__ __forceinline__ void grads_epilogue(const LossParams& p, const Job& j
         for (int k = 0; k < 8; ++k)
           stage(staging, lane, k, make_uint4(__float_as_uint(x[h][4 * k]), __float_as_uint(x[h][4 * k + 1]),
                                              __float_as_uint(x[h][4 * k + 2]), __float_as_uint(x[h][4 * k + 3])));
-        add_staged(rows, staging, lane, n0 + c + 32 * h, p.width, o.f32, o.accumulate);
+        if (o.vec) add_staged(rows, staging, lane, n0 + c + 32 * h, p.width, o.f32, o.accumulate);
+        else write_elements(rows, staging, lane, n0 + c + 32 * h, p.width, o.f32, o.accumulate);
       }
     }
   }
@@ -991,6 +994,7 @@ __global__ void __launch_bounds__(256) pack_table_kernel(const __nv_bfloat16* ta
   if (v >= vocab) return;
   const __nv_bfloat16* from = table + blockIdx.y * stride + v * row;
   __nv_bfloat16* to = packed + ((int64_t)blockIdx.y * vocab + v) * packed_row;
+#pragma unroll 8
   for (int c = lane; c < width; c += 32) to[c] = from[c];
 }
 
