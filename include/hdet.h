@@ -519,9 +519,10 @@ typedef struct {
  *   z = hidden[r,t] . weight[r,v],  lse = log sum_v exp z,  token_loss[r,t] = lse - z_target,
  *   loss[r] = mean of token_loss[r,t] over the counted targets,
  *   d_hidden, d_weight = grad_scale x the gradients of loss[r].
- * The logits are formed on the tensor cores (bf16 products, fp32 sums) tile by tile, for the gradients a second time (but see below);
- * losses and softmax are fp32, means fp64.  The softmax's gradient is a bf16 operand of the two products behind it; for
- * fp32 gradients it is the sum of three bf16 numbers (24 bits), and they cost three times the products.  The same inputs give the same bits.
+ * The logits are formed on the tensor cores (bf16 products, fp32 sums) tile by tile, for the gradients a second time (but
+ * see below); losses and softmax are fp32, means fp64.  The softmax's gradient is a bf16 operand of the two products behind
+ * it; for fp32 gradients it is the sum of three bf16 numbers (24 bits), and they cost three times the products.  The same
+ * inputs give the same bits.
  * Work goes with the counted targets: padding is left out of the products.
  * With bf16 gradients and a piece that holds all of a replica's vocabulary the logits are formed once: the workspace then
  * keeps their exponentials (fp16) until the row's sum is known.

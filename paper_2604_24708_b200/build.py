@@ -40,7 +40,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not needs_build():
         return LIB_PATH
     os.makedirs(LIB_DIR, exist_ok=True)
-    cmd = [_nvcc()] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + \
+    cmd = [_nvcc()] + NVCC_FLAGS + ["--threads", "0"] + (["-Xptxas", "-v"] if verbose else []) + \
           [os.path.join(CSRC, s) for s in SOURCES] + ["-o", LIB_PATH]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
@@ -56,7 +56,8 @@ def ptxas_table() -> str:
     import re
     import tempfile
     with tempfile.TemporaryDirectory() as tmp:
-        cmd = [_nvcc()] + NVCC_FLAGS + ["-Xptxas", "-v"] + [os.path.join(CSRC, s) for s in SOURCES] + \
+        # one source after the other: the reports of sources compiled at once could mix
+        cmd = [_nvcc()] + NVCC_FLAGS + ["--threads", "1", "-Xptxas", "-v"] + [os.path.join(CSRC, s) for s in SOURCES] + \
               ["-o", os.path.join(tmp, "scratch.so")]
         res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
