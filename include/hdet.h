@@ -517,6 +517,7 @@ typedef struct {
  * hdet_token_loss -- softmax cross entropy of every replica's hidden states against its table, with the gradients that
  * are asked for (d_hidden, d_weight, both or neither), in one call and without keeping the n_tokens x vocab logits:
  *   z = hidden[r,t] . weight[r,v],  lse = log sum_v exp z,  token_loss[r,t] = lse - z_target,
+ *     (computed as log(1 + exp(d)), d the logarithm of the other classes' sum less z_target: no cancellation for likely targets)
  *   loss[r] = mean of token_loss[r,t] over the counted targets,
  *   d_hidden, d_weight = grad_scale x the gradients of loss[r].
  * The logits are formed on the tensor cores (bf16 products, fp32 sums) tile by tile, for the gradients a second time (but

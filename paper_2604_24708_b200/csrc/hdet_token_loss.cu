@@ -4,18 +4,21 @@
 //   Z = H W^T,  lse_t = log sum_v exp Z_tv,  l_t = lse_t - Z_{t,y_t},  loss = mean of l_t
 //   P = exp(Z - lse),  G = P - onehot(y),  dH = (c) G W,  dW = (c) G^T H,  c = grad_scale / counted tokens
 //
+// A likely target's l_t and G are differences of numbers that are nearly equal, so neither is taken as one.  With d = (log of the
+// sum of exp over all classes but the target) - Z_{t,y_t}:  l_t = log(1 + exp d)  and  G_{t,y_t} = -1 / (1 + exp -d).
+//
 // Three products of T x V x D.  G needs lse, which needs all of Z: a piece of the work is as much of G as the workspace holds, as
 // many whole replicas as fit, else a part of one replica's vocabulary.
 //
 //   pack        counted tokens move together (padding drops out: no work, and nothing it holds reaches a product)
 // and then, where whole replicas fit and G is bf16, for each group of them
-//   numerators  Z tile by tile on the tensor cores; the epilogue keeps, of each half tile's row, its maximum m and the sum of
-//               exp(z - m), and leaves exp(z - m) in G's place
-//   scale       lse and the token's loss from those; exp(z - m) becomes G in place; the last block takes the replica's mean
+//   numerators  Z tile by tile on the tensor cores; the epilogue keeps, of each half tile's row, a power of two 2^k about as
+//               large as its largest exponential and the sum of exp(z) / 2^k, and leaves exp(z) / 2^k in G's place
+//   scale       the row's sum and the token's loss from those; they become G in place; the last block takes the replica's mean
 //   grads       both products with G in one launch
 // or, forming Z twice (a fourth product, but nothing kept but G),
-//   stats       Z, of which the epilogue keeps the maxima and sums
-//   join        lse, the token's loss, the replica's mean
+//   stats       Z, of which the epilogue keeps the powers of two and sums
+//   join        the row's sum, the token's loss, the replica's mean
 // and for each piece of the vocabulary
 //   probs       Z again; the epilogue writes G
 //   grads       as above; after the last piece, dH's partial sums are joined
@@ -47,7 +50,7 @@ using hdet::let_next_start;
 using hdet::wait_for_previous;
 namespace bulk = hdet::bulk;
 
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kStages = 6;
 constexpr int kStageBytes = 2 * kOperandBytes;
 // warp 0 copies, warp 1 issues the products, warp 2 hands out tiles, warps 4 - 11 read the accumulator: a quarter of its
@@ -75,6 +78,11 @@ struct Out {                // a gradient
   int f32, accumulate, vec; // vec: rows start and end on 16-byte boundaries
 };
 
+// What turns a row's logits into G: inverse * exp(z) / 2^k, and the target's own value.
+struct alignas(16) RowNorm {
+  float k, inverse, target, pad;
+};
+
 struct LossParams {
   CUtensorMap hidden, weight, grad;
   // problem
@@ -87,8 +95,8 @@ struct LossParams {
   const int* target;
   const int* token_of;
   float* z_target;
-  float* lse2;              // lse in units of log 2
-  float2* part;             // [replica][rows_pad][n_parts]: maximum and sum of exp of a part of the row
+  RowNorm* norm;
+  float2* part;             // [replica][rows_pad][n_parts]: Lse of a part of the row
   int n_parts;
   float* row_loss;          // [replica][rows_pad]
   // piece of the vocabulary
@@ -363,6 +371,52 @@ struct Source {
   }
 };
 
+// The least whole k with exp(x) <= 2^k (-inf for -inf).  From 2^24 on, where k itself is rounded (up), it may be a step more.
+__device__ __forceinline__ float exponent_above(float x) { return ceilf(__fmul_ru(x, kLog2e)); }
+
+// A sum of exponentials, sum * 2^k with k whole; k = -inf: of nothing.
+//
+// In units of a whole power of two no step rounds at the logits' size: x log2(e) - k is one fma, whose only rounding is that of its
+// (small) result, and sums are brought to one k exactly.  In units of exp(maximum), with the maximum's product with log2(e)
+// rounded, every exponential of a row was off by up to 2^-24 of its logits: the gradient of a target with P = 0.9998 by 2 %, one
+// with P = 0.999999 by several times its value.
+struct Lse {
+  float k, sum;
+  __device__ __forceinline__ void add(float2 o) {
+    const float now = fmaxf(k, o.x);
+    const float unit = now == -INFINITY ? 0.0f : now;
+    sum = sum * exp2_fast(k - unit) + o.y * exp2_fast(o.x - unit);
+    k = now;
+  }
+  __device__ __forceinline__ void add_logit(float z) {
+    const float now = fmaxf(k, exponent_above(z));
+    const float unit = now == -INFINITY ? 0.0f : now;
+    sum = sum * exp2_fast(k - unit) + exp2_fast(fmaf(z, kLog2e, -unit));
+    k = now;
+  }
+  __device__ __forceinline__ void add_warp() {     // over a warp's lanes, in a fixed order
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) add(make_float2(__shfl_xor_sync(0xffffffffu, k, o), __shfl_xor_sync(0xffffffffu, sum, o)));
+  }
+};
+
+// `others`: a row's classes but its target; `z`: the target's logit.
+struct Target {
+  float loss, grad;         // its loss, and its entry of G
+  __device__ __forceinline__ Target(const Lse& others, float z) {
+    float d = (fmaf(-z, kLog2e, others.k) + log2f(others.sum)) * kLn2;
+    if (z == INFINITY) d = NAN;                    // as inf - inf
+    const float e = expf(-fabsf(d));
+    loss = fmaxf(d, 0.0f) + log1pf(e);
+    grad = d < 0.0f ? -e / (1.0f + e) : -1.0f / (1.0f + e);
+  }
+};
+
+__device__ __forceinline__ RowNorm norm_of(const Lse& others, float z, float grad) {
+  const float k = others.k == -INFINITY ? exponent_above(z) : others.k;
+  return RowNorm{k, 1.0f / (others.sum + exp2_fast(fmaf(z, kLog2e, -k))), grad, 0.0f};
+}
+
 __device__ __forceinline__ float largest(const float (&x)[2][32]) {
   float top[4] = {x[0][0], x[0][1], x[1][0], x[1][1]};
 #pragma unroll
@@ -383,22 +437,23 @@ __device__ __forceinline__ void cut_columns(float (&x)[2][32], int v, int vocab)
   }
 }
 
-__device__ __forceinline__ void pick_column(const float (&x)[2][32], int v, int target, float& picked) {
+// Takes the target's logit out, -inf in its place.
+__device__ __forceinline__ void take_target(float (&x)[2][32], int v, int target, float& taken) {
   if ((unsigned)(target - v) >= 64u) return;
 #pragma unroll
   for (int i = 0; i < 32; ++i) {
-    if (v + i == target) picked = x[0][i];
-    if (v + 32 + i == target) picked = x[1][i];
+    if (v + i == target) { taken = x[0][i]; x[0][i] = -INFINITY; }
+    if (v + 32 + i == target) { taken = x[1][i]; x[1][i] = -INFINITY; }
   }
 }
 
-// exp(x - shift) in place, `shift` in units of log 2; returns the sum.
-__device__ __forceinline__ float exponentials(float (&x)[2][32], float shift) {
+// exp(x) / 2^k in place; returns the sum.
+__device__ __forceinline__ float exponentials(float (&x)[2][32], float k) {
   float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
   for (int i = 0; i < 32; i += 2) {
-    x[0][i] = exp2_fast(fmaf(x[0][i], kLog2e, -shift)); x[0][i + 1] = exp2_fast(fmaf(x[0][i + 1], kLog2e, -shift));
-    x[1][i] = exp2_fast(fmaf(x[1][i], kLog2e, -shift)); x[1][i + 1] = exp2_fast(fmaf(x[1][i + 1], kLog2e, -shift));
+    x[0][i] = exp2_fast(fmaf(x[0][i], kLog2e, -k)); x[0][i + 1] = exp2_fast(fmaf(x[0][i + 1], kLog2e, -k));
+    x[1][i] = exp2_fast(fmaf(x[1][i], kLog2e, -k)); x[1][i + 1] = exp2_fast(fmaf(x[1][i + 1], kLog2e, -k));
     s[0] += x[0][i]; s[1] += x[0][i + 1]; s[2] += x[1][i]; s[3] += x[1][i + 1];
   }
   return (s[0] + s[1]) + (s[2] + s[3]);
@@ -410,24 +465,23 @@ __device__ __forceinline__ void stats_epilogue(const LossParams& p, const Job& j
   constexpr int kCols = 64 * CTAS;
   const int64_t at = (int64_t)j.r * p.rows_pad + row;
   const int v0 = j.n0 + half;
-  float top = -INFINITY, sum = 0.0f, picked = 0.0f;
+  Lse l{-INFINITY, 0.0f};
+  float taken = 0.0f;
 #pragma unroll (SUMS ? CTAS : 1)
   for (int c = 0; c < kCols; c += 64) {
     float loaded[2][32];
     float (&x)[2][32] = from.get(c, loaded);
     cut_columns(x, v0 + c, p.vocab);
-    pick_column(x, v0 + c, target, picked);
-    const float now = fmaxf(top, largest(x));
-    const float shift = now == -INFINITY ? 0.0f : now * kLog2e;    // nothing finite yet: exp of -inf, not of NaN
-    const float s = exponentials(x, shift);
-    sum = fmaf(sum, exp2_fast(fmaf(top, kLog2e, -shift)), s);
-    top = now;
+    take_target(x, v0 + c, target, taken);
+    const float k = exponent_above(largest(x));
+    const float s = exponentials(x, k == -INFINITY ? 0.0f : k);    // nothing finite: exp of -inf, not of NaN
+    l.add(make_float2(k, s));
   }
-  p.part[at * p.n_parts + v0 / kCols] = make_float2(top, sum);
-  if (target >= v0 && target < v0 + kCols) p.z_target[at] = picked;
+  p.part[at * p.n_parts + v0 / kCols] = make_float2(l.k, l.sum);
+  if (target >= v0 && target < v0 + kCols) p.z_target[at] = taken;
 }
 
-// The same, and the numerators exp(z - maximum of the half tile's row) go to the workspace, where scale_kernel turns them
+// The same, and the numerators exp(z) / 2^k (one k for the half tile's row) go to the workspace, where scale_kernel turns them
 // into G.  They are fp16: between 0 and 1 it is off by 2^-12 of the value, or 2^-25 below 2^-14, less than the rounding of
 // G to bf16 that follows.  The sum is taken before that rounding.
 template <int CTAS, bool SUMS>
@@ -436,16 +490,16 @@ __device__ __forceinline__ void numerators_epilogue(const LossParams& p, const J
   constexpr int kCols = 64 * CTAS;
   const int64_t at = (int64_t)j.r * p.rows_pad + row;
   const int v0 = j.n0 + half;
-  float top = -INFINITY, sum = 0.0f, picked = 0.0f;
+  float top = -INFINITY, sum = 0.0f, taken = 0.0f;
 #pragma unroll (SUMS ? CTAS : 1)
   for (int c = 0; c < kCols; c += 64) {
     float loaded[2][32];
     float (&x)[2][32] = from.get(c, loaded);
     cut_columns(x, v0 + c, p.vocab);
-    pick_column(x, v0 + c, target, picked);
+    take_target(x, v0 + c, target, taken);
     top = fmaxf(top, largest(x));
   }
-  const float shift = top == -INFINITY ? 0.0f : top * kLog2e;
+  const float k = exponent_above(top), unit = k == -INFINITY ? 0.0f : k;
   Rows rows;
   rows.base = reinterpret_cast<char*>(p.g);
   rows.offset = (((int64_t)(j.r - p.r0) * p.rows_pad + row) * p.v_pitch + v0) * 2;
@@ -455,21 +509,23 @@ __device__ __forceinline__ void numerators_epilogue(const LossParams& p, const J
     float loaded[2][32];
     float (&x)[2][32] = from.get(c, loaded);
     cut_columns(x, v0 + c, p.vocab);
-    sum += exponentials(x, shift);
+    float again;
+    take_target(x, v0 + c, target, again);
+    sum += exponentials(x, unit);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float* y = &x[k / 4][8 * (k % 4)];
-      stage(staging, lane, k, make_uint4(f16_pair(y[0], y[1]), f16_pair(y[2], y[3]), f16_pair(y[4], y[5]), f16_pair(y[6], y[7])));
+    for (int i = 0; i < 8; ++i) {
+      const float* y = &x[i / 4][8 * (i % 4)];
+      stage(staging, lane, i, make_uint4(f16_pair(y[0], y[1]), f16_pair(y[2], y[3]), f16_pair(y[4], y[5]), f16_pair(y[6], y[7])));
     }
     write_staged(rows, staging, lane, 2 * c, 2 * kCols);
   }
-  p.part[at * p.n_parts + v0 / kCols] = make_float2(top, sum);
-  if (target >= v0 && target < v0 + kCols) p.z_target[at] = picked;
+  p.part[at * p.n_parts + v0 / kCols] = make_float2(k, sum);
+  if (target >= v0 && target < v0 + kCols) p.z_target[at] = taken;
 }
 
 template <int CTAS, bool SUMS>
 __device__ __forceinline__ void probs_epilogue(const LossParams& p, const Job& j, const Source<CTAS, SUMS>& from, int row, int half, bool counted,
-                                               int target, float lse2, uint32_t staging, int lane) {
+                                               int target, const RowNorm& norm, uint32_t staging, int lane) {
   constexpr int kCols = 64 * CTAS;
   target = counted ? target - p.v0 : -1;
   const int v0 = j.n0 + half;
@@ -484,11 +540,11 @@ __device__ __forceinline__ void probs_epilogue(const LossParams& p, const Job& j
     for (int h = 0; h < 2; ++h) {
       const int v = v0 + c + 32 * h;
 #pragma unroll
-      for (int i = 0; i < 32; ++i) x[h][i] = exp2_fast(fmaf(x[h][i], kLog2e, -lse2));
+      for (int i = 0; i < 32; ++i) x[h][i] = exp2_fast(fmaf(x[h][i], kLog2e, -norm.k)) * norm.inverse;
       if ((unsigned)(target - v) < 32u) {
 #pragma unroll
         for (int i = 0; i < 32; ++i)
-          if (v + i == target) x[h][i] -= 1.0f;
+          if (v + i == target) x[h][i] = norm.target;
       }
       if (!counted || v + 32 > p.v_len) {
 #pragma unroll
@@ -816,10 +872,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
       if (j.k_blocks < 0) continue;                // the cluster's first, with nothing counted
       const int row = j.m0 + 128 * (int)rank + quarter * 32 + lane;
       int target = -1;                             // -1 behind the counted tokens, too
-      float lse2 = INFINITY;
+      RowNorm norm{INFINITY, 0.0f, 0.0f, 0.0f};
       if constexpr (PHASE != kGrads) {
         target = p.target[(int64_t)j.r * p.rows_pad + row];
-        if (PHASE == kProbs && row < sh.count[j.r]) lse2 = p.lse2[(int64_t)j.r * p.rows_pad + row];
+        if (PHASE == kProbs && row < sh.count[j.r]) norm = p.norm[(int64_t)j.r * p.rows_pad + row];
       }
       Columns<SUMS ? CTAS : 0> acc;
       if constexpr (SUMS) {
@@ -852,7 +908,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
       if constexpr (SUMS) from.acc = &acc;
       if constexpr (PHASE == kStats) stats_epilogue(p, j, from, row, half, target);
       else if constexpr (PHASE == kNumerators) numerators_epilogue(p, j, from, row, half, target, staging, lane);
-      else if constexpr (PHASE == kProbs) probs_epilogue(p, j, from, row, half, row < sh.count[j.r], target, lse2, staging, lane);
+      else if constexpr (PHASE == kProbs) probs_epilogue(p, j, from, row, half, row < sh.count[j.r], target, norm, staging, lane);
       else grads_epilogue(p, j, from, row, half, sh.count[j.r], staging, lane);
       if constexpr (!SUMS) {
         if (j.k_blocks > 0) acc_done();
@@ -1003,24 +1059,8 @@ __global__ void __launch_bounds__(256) pack_table_kernel(const __nv_bfloat16* ta
 }
 
 // ------------------------------------------------------------------------------------------------ joining
-struct Lse {
-  float top, sum;           // sum of exp(z - top)
-  __device__ __forceinline__ void add(float2 o) {
-    const float now = fmaxf(top, o.x);
-    const float shift = now == -INFINITY ? 0.0f : now;
-    sum = sum * exp2_fast((top - shift) * kLog2e) + o.y * exp2_fast((o.x - shift) * kLog2e);
-    top = now;
-  }
-  __device__ __forceinline__ void add_warp() {     // over a warp's lanes, in a fixed order
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) add(make_float2(__shfl_xor_sync(0xffffffffu, top, o), __shfl_xor_sync(0xffffffffu, sum, o)));
-  }
-  __device__ __forceinline__ float lse2() const { return fmaf(top, kLog2e, log2f(sum)); }
-};
-
 // A row's loss, where it belongs.
-__device__ __forceinline__ void write_row(const LossParams& p, int r, int row, const Lse& l, float picked, int token) {
-  const float loss = l.top + logf(l.sum) - picked;
+__device__ __forceinline__ void write_row(const LossParams& p, int r, int row, float loss, int token) {
   p.row_loss[(int64_t)r * p.rows_pad + row] = loss;
   if (p.token_loss) p.token_loss[r * p.token_loss_stride + token] = loss;
 }
@@ -1052,7 +1092,7 @@ __device__ __forceinline__ void finish_block(const LossParams& p, int r, unsigne
   if (p.loss_f64) static_cast<double*>(p.loss)[r] = mean; else static_cast<float*>(p.loss)[r] = (float)mean;
 }
 
-// lse and loss of a row from its parts, one warp a row.
+// Sum and loss of a row from its parts, one warp a row.
 __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ LossParams p) {
   const int r = blockIdx.y, row = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   let_next_start();
@@ -1068,20 +1108,21 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ LossP
     for (int i = lane; i < n; i += 32) l.add(part[i]);
     l.add_warp();
     if (lane == 0) {
-      p.lse2[at] = l.lse2();
-      write_row(p, r, row, l, picked, token);
+      const Target t(l, picked);
+      p.norm[at] = norm_of(l, picked, t.grad);
+      write_row(p, r, row, t.loss, token);
     }
   }
   finish_block(p, r, gridDim.x);
 }
 
-// One block a row: lse and loss as above, then the row's numerators become G in place: exp(z - m) exp(m - lse), bf16.  The
-// target's own value comes from its fp32 logit: where it is likely, p - 1 is small and no rounding of p may reach it.
+// One block a row: sum and loss as above, then the row's numerators become G in place, bf16.  The target's own value is not P - 1
+// but what the sum of the others gives.
 // Rows behind the counted ones, up to the next 64, become zeros, since dW's sums run over them.
 template <int CTAS>
 __global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ LossParams p) {
   constexpr int kCols = 64 * CTAS;
-  extern __shared__ float s_factor[];              // per half tile: exp(m - lse)
+  extern __shared__ float s_factor[];              // per half tile: 2^k / the row's sum
   __shared__ Lse s_lse[8];
   let_next_start();
   wait_for_previous();
@@ -1105,12 +1146,12 @@ __global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ Loss
     __syncthreads();
     l = s_lse[0];
 #pragma unroll
-    for (int w = 1; w < 8; ++w) l.add(make_float2(s_lse[w].top, s_lse[w].sum));
-    const float lse2 = l.lse2();
-    for (int i = threadIdx.x; i < n; i += 256) s_factor[i] = exp2_fast(fmaf(s_factor[i], kLog2e, -lse2));
-    if (threadIdx.x == 0) write_row(p, r, row, l, picked, token);
+    for (int w = 1; w < 8; ++w) l.add(make_float2(s_lse[w].k, s_lse[w].sum));
+    const Target own(l, picked);
+    const RowNorm norm = norm_of(l, picked, own.grad);
+    for (int i = threadIdx.x; i < n; i += 256) s_factor[i] = exp2_fast(s_factor[i] - norm.k) * norm.inverse;
+    if (threadIdx.x == 0) write_row(p, r, row, own.loss, token);
     __syncthreads();
-    const float g_target = exp2_fast(fmaf(picked, kLog2e, -lse2)) - 1.0f;
 #pragma unroll 4
     for (int i = threadIdx.x; i < vectors; i += 256) {
       const uint4 u = values[i];
@@ -1126,7 +1167,7 @@ __global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ Loss
       if (i == target / 8) {
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-          if (k == target % 8) x[k] = g_target;
+          if (k == target % 8) x[k] = norm.target;
       }
       values[i] = make_uint4(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]), bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7]));
     }
@@ -1223,10 +1264,9 @@ __global__ void __launch_bounds__(256, 3) few_kernel(const __grid_constant__ Los
       for (int t = 0; t < NT; ++t) {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) z[i][t] += __shfl_xor_sync(0xffffffffu, z[i][t], o);
-        if (v + i < to) {
-          l[t].add(make_float2(z[i][t], 1.0f));
-          if (v + i == target[t] && lane == 0) p.z_target[(int64_t)r * p.rows_pad + t] = z[i][t];
-        }
+        if (v + i >= to) continue;
+        if (v + i != target[t]) l[t].add_logit(z[i][t]);
+        else if (lane == 0) p.z_target[(int64_t)r * p.rows_pad + t] = z[i][t];
       }
   }
   if (lane == 0)
@@ -1235,8 +1275,8 @@ __global__ void __launch_bounds__(256, 3) few_kernel(const __grid_constant__ Los
   __syncthreads();
   if (threadIdx.x < count) {
     Lse all = s_lse[0][threadIdx.x];
-    for (int i = 1; i < 8; ++i) all.add(make_float2(s_lse[i][threadIdx.x].top, s_lse[i][threadIdx.x].sum));
-    p.part[((int64_t)r * p.rows_pad + threadIdx.x) * p.n_parts + blockIdx.x] = make_float2(all.top, all.sum);
+    for (int i = 1; i < 8; ++i) all.add(make_float2(s_lse[i][threadIdx.x].k, s_lse[i][threadIdx.x].sum));
+    p.part[((int64_t)r * p.rows_pad + threadIdx.x) * p.n_parts + blockIdx.x] = make_float2(all.k, all.sum);
   }
 }
 
@@ -1262,7 +1302,7 @@ __global__ void __launch_bounds__(32 * kFew) few_join_kernel(const __grid_consta
     for (int k = 0; k < 16; ++k) l.add(part[k]);
   }
   l.add_warp();
-  const float loss = l.top + logf(l.sum) - picked;
+  const float loss = Target(l, picked).loss;
   if (lane == 0) {
     s_loss[t] = loss;
     if (t < count && p.token_loss) p.token_loss[r * p.token_loss_stride + token] = loss;
@@ -1386,7 +1426,7 @@ struct Plan {
   int64_t n_pieces, h_len, h_splits;
   bool h_slabs;
   bool pack_table;
-  int64_t off_count, off_target, off_token, off_z, off_lse, off_part, off_loss, off_hidden, off_table, off_g,
+  int64_t off_count, off_target, off_token, off_z, off_norm, off_part, off_loss, off_hidden, off_table, off_g,
       off_slabs, total;
 };
 
@@ -1462,7 +1502,7 @@ Plan plan_of(const hdet_token_loss_args* d) {
   q.off_target = take(4 * R * q.rows_pad);
   q.off_token = take(4 * R * q.rows_pad);
   q.off_z = take(4 * R * q.rows_pad);
-  q.off_lse = take(4 * R * q.rows_pad);
+  q.off_norm = take(sizeof(RowNorm) * R * q.rows_pad);
   // room for either kernel's parts: the query does not know the hidden states' address
   q.off_part = take(8 * R * (q.n_parts > 2 * q.n_tiles ? q.n_parts : 2 * q.n_tiles) * q.rows_pad);
   q.off_loss = take(4 * R * q.rows_pad);
@@ -1619,7 +1659,7 @@ extern "C" HDET_API int hdet_token_loss(const hdet_token_loss_args* d, void* wor
   p.target = reinterpret_cast<int*>(ws + q.off_target);
   p.token_of = reinterpret_cast<int*>(ws + q.off_token);
   p.z_target = reinterpret_cast<float*>(ws + q.off_z);
-  p.lse2 = reinterpret_cast<float*>(ws + q.off_lse);
+  p.norm = reinterpret_cast<RowNorm*>(ws + q.off_norm);
   p.part = reinterpret_cast<float2*>(ws + q.off_part);
   p.row_loss = reinterpret_cast<float*>(ws + q.off_loss);
   p.token_loss = static_cast<float*>(d->token_loss);
