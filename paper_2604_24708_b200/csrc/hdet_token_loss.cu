@@ -29,7 +29,6 @@
 // that would be too coarse: G is written as the sum of three bf16 numbers (24 bits; two would leave 2^-18, 1.3e-6 of a
 // gradient), and the products run over all three.
 #include <cuda_bf16.h>
-#include <cuda_fp16.h>
 
 #include <algorithm>
 #include <climits>
@@ -206,9 +205,18 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-__device__ __forceinline__ uint32_t f16_pair(float lo, float hi) {
-  const __half2 v = __floats2half2_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&v);
+// Numerators, 0 <= x <= 1, in 16 bits: ten bits of mantissa, six of exponent, no sign: the middle bits of x / 2^64 as fp32.  Off by
+// 2^-11 of the value down to 2^-62, an eighth of the rounding of G to bf16 that follows; zero below.  (fp16, used before, is off by
+// more than that rounding below 2^-16 of the row's largest neighbour and zero below 2^-25: gradients of unlikely classes were lost.)
+constexpr float kNumeratorBits = 64.0f, kNumeratorUnit = 18446744073709551616.0f;   // 2^64
+
+// Two values x / 2^64.
+__device__ __forceinline__ uint32_t numerator_pair(float lo, float hi) {
+  return __byte_perm((__float_as_uint(lo) + 0x1000u) << 3, (__float_as_uint(hi) + 0x1000u) << 3, 0x7632);
+}
+
+__device__ __forceinline__ float2 numerators_of(uint32_t pair) {
+  return make_float2(__uint_as_float((pair & 0xffffu) << 13), __uint_as_float(pair >> 16 << 13));
 }
 
 // ------------------------------------------------------------------------------------------------ epilogues
@@ -482,8 +490,7 @@ __device__ __forceinline__ void stats_epilogue(const LossParams& p, const Job& j
 }
 
 // The same, and the numerators exp(z) / 2^k (one k for the half tile's row) go to the workspace, where scale_kernel turns them
-// into G.  They are fp16: between 0 and 1 it is off by 2^-12 of the value, or 2^-25 below 2^-14, less than the rounding of
-// G to bf16 that follows.  The sum is taken before that rounding.
+// into G.  The sum is taken before they are rounded.
 template <int CTAS, bool SUMS>
 __device__ __forceinline__ void numerators_epilogue(const LossParams& p, const Job& j, const Source<CTAS, SUMS>& from, int row, int half,
                                                     int target, uint32_t staging, int lane) {
@@ -511,15 +518,16 @@ __device__ __forceinline__ void numerators_epilogue(const LossParams& p, const J
     cut_columns(x, v0 + c, p.vocab);
     float again;
     take_target(x, v0 + c, target, again);
-    sum += exponentials(x, unit);
+    sum += exponentials(x, unit + kNumeratorBits);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float* y = &x[i / 4][8 * (i % 4)];
-      stage(staging, lane, i, make_uint4(f16_pair(y[0], y[1]), f16_pair(y[2], y[3]), f16_pair(y[4], y[5]), f16_pair(y[6], y[7])));
+      stage(staging, lane, i, make_uint4(numerator_pair(y[0], y[1]), numerator_pair(y[2], y[3]), numerator_pair(y[4], y[5]),
+                                              numerator_pair(y[6], y[7])));
     }
     write_staged(rows, staging, lane, 2 * c, 2 * kCols);
   }
-  p.part[at * p.n_parts + v0 / kCols] = make_float2(k, sum);
+  p.part[at * p.n_parts + v0 / kCols] = make_float2(k, sum * kNumeratorUnit);
   if (target >= v0 && target < v0 + kCols) p.z_target[at] = taken;
 }
 
@@ -1122,7 +1130,7 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ LossP
 template <int CTAS>
 __global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ LossParams p) {
   constexpr int kCols = 64 * CTAS;
-  extern __shared__ float s_factor[];              // per half tile: 2^k / the row's sum
+  extern __shared__ float s_factor[];              // per half tile: 2^(k + 64) / the row's sum
   __shared__ Lse s_lse[8];
   let_next_start();
   wait_for_previous();
@@ -1149,7 +1157,7 @@ __global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ Loss
     for (int w = 1; w < 8; ++w) l.add(make_float2(s_lse[w].k, s_lse[w].sum));
     const Target own(l, picked);
     const RowNorm norm = norm_of(l, picked, own.grad);
-    for (int i = threadIdx.x; i < n; i += 256) s_factor[i] = exp2_fast(s_factor[i] - norm.k) * norm.inverse;
+    for (int i = threadIdx.x; i < n; i += 256) s_factor[i] = exp2_fast(s_factor[i] - norm.k + kNumeratorBits) * norm.inverse;
     if (threadIdx.x == 0) write_row(p, r, row, own.loss, token);
     __syncthreads();
 #pragma unroll 4
@@ -1160,7 +1168,7 @@ __global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ Loss
       float x[8];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&w[k]));
+        const float2 y = numerators_of(w[k]);
         x[2 * k] = y.x * f;
         x[2 * k + 1] = y.y * f;
       }

@@ -81,12 +81,11 @@ def test_gradients(T, dt, piece):
     for r in range(R):
         d, _, g = _reference(h[r], w[r], y[r])
         # an entry of G: as the loss, and its own exponential and its argument (of at most 126); G as operand: bf16, or three terms; bf16
-        # only: numerators of 2^-12, and those far below the largest of their 128 neighbours by its 2^-25 (of all the row's, at most
-        # V 2^-25 more of its largest)
-        e = _error_of_d(d, V) + (16 + 126 + d.abs()) * 2.0 ** -23 + (2.0 ** -24 if dt == "f32" else 2.0 ** -8 + 2.0 ** -12)
+        # only: numerators of 2^-11, and zero for those below 2^-61 of the row's largest
+        e = _error_of_d(d, V) + (16 + 126 + d.abs()) * 2.0 ** -23 + (2.0 ** -24 if dt == "f32" else 2.0 ** -8 + 2.0 ** -11 + 2.0 ** -18)
         a, wa = g.abs(), w[r].double().abs()
         size = a @ wa
-        flush = 0.0 if dt == "f32" else 2.0 ** -25 * V * a.amax(1, keepdim=True) * float(wa.max())
+        flush = 0.0 if dt == "f32" else 2.0 ** -61 * V * a.amax(1, keepdim=True) * float(wa.max())
         # sums of V products: cut every 16 products, at most 2^-23 of the magnitudes, and one addition a chunk
         steps = V / 16 + 8
         ref = g @ w[r].double() / T
@@ -125,3 +124,28 @@ def test_one_class_and_classes_without_weight(T):
         w[0, 5] = own
         out = _run(h, w.bfloat16().cuda(), torch.full((1, T), 5, dtype=torch.int32, device="cuda"))
         assert (torch.isnan(out["token_loss"]) if want is None else out["token_loss"] == want).all(), (own, other)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [90, 300])
+@pytest.mark.parametrize("dt,piece", [("f32", 0), ("bf16", 0), ("bf16", 1)])
+def test_gradients_of_unlikely_classes(T, dt, piece):
+    """Every class's row of the table's gradient beside its own size, down to classes of probability 1e-25."""
+    R, V, D = 1, 900, 128
+    gen = torch.Generator().manual_seed(T)
+    w = torch.randint(-4, 5, (R, V, D), generator=gen).float() / 8
+    w *= torch.tensor([0.0, 0.5, 1.0, 2.0])[torch.randint(0, 4, (R, V, 1), generator=gen)]
+    h = torch.randint(-4, 5, (R, T, D), generator=gen).float() / 2
+    h[..., 0], w[..., 0] = 8.0, torch.randint(-4, 1, (R, V), generator=gen).float() / 2      # classes that are unlikely for every token
+    h, w, y = h.bfloat16().cuda(), w.bfloat16().cuda(), torch.randint(0, V, (R, T), generator=gen).int().cuda()
+    out = _run(h, w, y, dt, piece)
+    d, _, g = _reference(h[0], w[0], y[0])
+    a, ha = g.abs(), h[0].double().abs()
+    assert float(a.amax(0).min()) < 1e-12 and float(a[a > 0].min()) < 1e-25
+    e = _error_of_d(d, V) + (16 + 126 + d.abs()) * 2.0 ** -23 + (2.0 ** -24 if dt == "f32" else 2.0 ** -8 + 2.0 ** -11 + 2.0 ** -18)
+    ref = g.t() @ h[0].double() / T
+    bound = ((a * e[:, None]).t() @ ha + (a.t() @ ha) * (T / 16 + 8) * 2.0 ** -23) / T + ref.abs() * (torch.finfo(DT[dt]).eps / 2 + 2.0 ** -22)
+    if dt == "bf16" and not piece:                   # what counts as zero: 2^-62 of a neighbour, twice that for its unit
+        bound += (2.0 ** -61 * a.amax(1, keepdim=True)).expand_as(a).t() @ ha / T
+    got = out["d_weight"][0].double()
+    assert ((got - ref).abs() <= bound).all(), float(((got - ref).abs() / bound).max())
