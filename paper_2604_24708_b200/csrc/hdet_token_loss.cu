@@ -1588,10 +1588,12 @@ bool encode(CUtensorMap* map, const void* base, int64_t x, int64_t y, int64_t z,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Steps of 64 summed by the tensor cores at a time.  fp32 gradients: 8 (errors of 4e-8 to 9e-7 of a gradient's norm; 4 steps
-// 3e-8 to 5e-7, 14 % slower; 16 steps up to 1.9e-6, 6 % faster).  Logits: 64, all of a width up to 4096 (their terms' signs
-// vary: the loss is 1.4e-7 off).  bf16 gradients: 256, 3e-5, far below their rounding.
-constexpr int kChunkLogits = 64, kChunkF32 = 8, kChunkBf16 = 256;
+// Steps of 64 summed by the tensor cores at a time.  fp32 gradients, and the logits for them: 8 (errors of 4e-8 to 9e-7 of a gradient's
+// norm; 4 steps 3e-8 to 5e-7, 14 % slower; 16 steps up to 1.9e-6, 6 % faster).  Other logits: 16.  A likely target's products
+// mostly have one sign, so their cuts add up: at a width of 2048 and a target's logit of 24 the loss of a token is 3.4e-5 of its value off
+// with 64 steps, 1.6e-5 with 16, 0.8e-5 with 8 (as an fp32 product); 8 x 2048 tokens with bf16 gradients take 8.35, 8.41 and 8.80 ms, 4 x 1024
+// of width 768 with fp32 gradients 2.56, 2.54 and 2.63.  bf16 gradients: 256, 3e-5, far below their rounding.
+constexpr int kChunkLogits = 16, kChunkF32 = 8, kChunkBf16 = 256;
 constexpr int kWholeBf16 = 1024;   // bf16 gradients up to this many steps are not cut at all: 1e-4
 
 template <int PHASE>
@@ -1603,7 +1605,7 @@ cudaError_t launch_gemm(LossParams& p, int ctas, int64_t tiles, int sms, cudaStr
   const int64_t longest = PHASE != kGrads ? div_up(p.width, kBlockK)
                                           : std::max<int64_t>(p.h_jobs ? (int64_t)p.h_len * p.h_terms : 0,
                                                               p.w_tiles_m ? div_up(p.n_tokens, kBlockK) * p.w_terms : 0);
-  p.chunk = PHASE != kGrads ? kChunkLogits : p.g_terms > 1 ? kChunkF32 : kChunkBf16;
+  p.chunk = p.g_terms > 1 ? kChunkF32 : PHASE != kGrads ? kChunkLogits : kChunkBf16;
   const bool sums = longest > (PHASE == kGrads && p.g_terms == 1 ? kWholeBf16 : p.chunk);
   const dim3 grid((unsigned)(clusters * ctas));
   const auto kernel = ctas == 1 ? (sums ? gemm_kernel<1, PHASE, true> : gemm_kernel<1, PHASE, false>)

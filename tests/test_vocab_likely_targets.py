@@ -149,3 +149,31 @@ def test_gradients_of_unlikely_classes(T, dt, piece):
         bound += (2.0 ** -61 * a.amax(1, keepdim=True)).expand_as(a).t() @ ha / T
     got = out["d_weight"][0].double()
     assert ((got - ref).abs() <= bound).all(), float(((got - ref).abs() / bound).max())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", [None, "bf16", "f32"])
+def test_wide_logits_of_one_sign(dt):
+    """The tensor cores cut a sum towards zero after every 16 products, and where the products have one sign the cuts add up.  They are
+    bounded by the partial sums since the last time the sum was taken out, every 16 x 64 products (8 x 64 for fp32 gradients)."""
+    T, V, D = 40, 200, 4096
+    gen = torch.Generator().manual_seed(1)
+    w = (torch.randn((1, V, D), generator=gen) * 0.02).bfloat16()
+    y = torch.randint(0, V, (1, T), generator=gen)
+    lean = torch.where(torch.rand((1, T, 1), generator=gen) < 0.5, -1.0, 1.0) * (0.5 + torch.rand((1, T, D), generator=gen)) * 0.4
+    h = (lean * torch.sign(w[0].float())[y]).bfloat16().cuda()                 # |z| of the targets about 25
+    w, y = w.cuda(), y.int().cuda()
+    out = _run(h, w, y, dt)
+    chunk = 64 * (8 if dt == "f32" else 16)
+    parts = (h[0].double()[:, None] * w[0].double()[None]).view(T, V, D // 16, 16).sum(-1)         # of 16 products
+    cuts = parts.view(T, V, D // chunk, chunk // 16).cumsum(-1).abs()
+    ez = cuts.sum((-1, -2)) * 2.0 ** -23 + cuts[..., -1].sum(-1) * 2.0 ** -24
+    d, loss, g = _reference(h[0], w[0], y[0])
+    at = torch.arange(T, device="cuda")
+    own = ez[at, y[0].long()]
+    others = torch.where(g > 0, g, 0.0)
+    e = own + (others * ez).sum(1) / others.sum(1) + _error_of_d(d, V)
+    got = out["token_loss"][0].double()
+    assert float(d.min()) < -15 and float(d.max()) > 15
+    bound = e * -g[at, y[0].long()] + loss * (8 + d.abs()) * 2.0 ** -23         # the derivative of the loss by d is that of -G's entry
+    assert ((got - loss).abs() <= bound).all(), float(((got - loss).abs() / bound).max())
