@@ -527,7 +527,7 @@ typedef struct {
  * Work goes with the counted targets: padding is left out of the products.
  * With bf16 gradients and a piece that holds all of a replica's vocabulary the logits are formed once: the workspace then
  * keeps their exponentials (16 bits, off by 2^-11, zero below 2^-62 of the largest of 64 or 128 neighbours) until the row's sum is known.
- * A table whose width, row stride or replica stride is not a multiple of 8 elements, or that is not 16-byte aligned, is laid
+ * A table whose row stride or replica stride is not a multiple of 8 elements, or that is not 16-byte aligned, is laid
  * out in the workspace by every call first.
  * Outputs must not overlap inputs or one another, except that d_hidden may be the hidden states' own buffer.
  * If a bounded wait inside a kernel runs out, every loss is set to NaN.

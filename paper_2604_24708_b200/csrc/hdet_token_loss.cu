@@ -1456,11 +1456,9 @@ Plan plan_of(const hdet_token_loss_args* d) {
   q.pack_table = !table_fits(d);
   q.few = !q.grads && T <= kFew && T > 0 && !q.pack_table && D % 8 == 0 && aligned(d->hidden, 16) && d->hidden_row % 8 == 0 &&
           (R == 1 || d->hidden_stride % 8 == 0);
-  q.n_parts = 2 * q.n_tiles;
-  if (q.few) {
-    const int64_t most = div_up(V, 8 * kFewRows), blocks = kFewBlocks / R;
-    q.n_parts = blocks < 1 ? 1 : blocks < most ? blocks : most;
-  }
+  const int64_t most = div_up(V, 8 * kFewRows), blocks = kFewBlocks / R;
+  const int64_t few_parts = blocks < 1 ? 1 : blocks < most ? blocks : most;
+  q.n_parts = q.few ? few_parts : 2 * q.n_tiles;
   if (q.grads) {
     const int64_t budget = d->piece_bytes ? d->piece_bytes : kDefaultPieceBytes;
     const int64_t v_all = q.n_tiles * q.tile, per_row = q.rows_pad * 2 * q.g_terms;
@@ -1511,8 +1509,8 @@ Plan plan_of(const hdet_token_loss_args* d) {
   q.off_token = take(4 * R * q.rows_pad);
   q.off_z = take(4 * R * q.rows_pad);
   q.off_norm = take(sizeof(RowNorm) * R * q.rows_pad);
-  // room for either kernel's parts: the query does not know the hidden states' address
-  q.off_part = take(8 * R * (q.n_parts > 2 * q.n_tiles ? q.n_parts : 2 * q.n_tiles) * q.rows_pad);
+  // room for either kernel's parts: which one runs depends on the hidden states' address, and the size does not
+  q.off_part = take(8 * R * std::max(2 * q.n_tiles, !q.grads && T <= kFew ? few_parts : 0) * q.rows_pad);
   q.off_loss = take(4 * R * q.rows_pad);
   q.off_hidden = take(2 * R * q.rows_pad * q.packed_row);
   if (q.pack_table) q.off_table = take(2 * (d->n_replicas > 1 && d->weight_stride ? R : 1) * V * q.packed_row);
