@@ -478,7 +478,8 @@ HDET_API int hdet_embed(const hdet_embedding* d, void* stream);
  * without a token are neither read nor written, so that the gradient joins the one hdet_token_loss left there.
  * The tokens are sorted (stably) and every row is summed in the order of t in fp32 by one owner and rounded once: no
  * atomics, the same bits on every run.
- * hdet_embed_grad_workspace gives the bytes that the call needs; it looks at sizes, strides and dtypes alone.
+ * hdet_embed_grad_workspace gives the bytes that this call, and any with fewer tokens and all else the same, needs; it looks at
+ * sizes, strides and dtypes alone.
  * Errors: as hdet_embed, plus INVALID_ARG (workspace NULL or too small) and ALIGN (workspace).
  */
 HDET_API int hdet_embed_grad_workspace(const hdet_embedding* d, int64_t* bytes);
@@ -531,8 +532,8 @@ typedef struct {
  * out in the workspace by every call first.
  * Outputs must not overlap inputs or one another, except that d_hidden may be the hidden states' own buffer.
  * If a bounded wait inside a kernel runs out, every loss is set to NaN.
- * hdet_token_loss_workspace gives the bytes that the call needs; it looks at sizes, strides, dtypes, piece_bytes, the
- * table's address (its alignment) and at which gradients are asked for.
+ * hdet_token_loss_workspace gives the bytes that this call, and any with fewer tokens and all else the same, needs; it looks at
+ * sizes, strides, dtypes, piece_bytes, the table's address (its alignment) and at which gradients are asked for.
  * Errors: INVALID_ARG (NULL, sizes, strides or dtypes out of range, workspace NULL or too small), ALIGN, UNSUPPORTED
  * (hidden states or table not bf16; too many tiles), CUDA.
  */

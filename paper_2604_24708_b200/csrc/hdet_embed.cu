@@ -8,6 +8,7 @@
 // row is summed in that order in fp32 by one owner, then rounded once.
 #include <cuda_bf16.h>
 
+#include <algorithm>
 #include <cstdio>
 
 #include "hdet_internal.h"
@@ -601,18 +602,27 @@ struct GradLayout {
   int sorted_replicas, entries;
 };
 
-GradLayout layout_of(const hdet_embedding* d) {
+// Up to how many tokens the gradient kernel has fewer than 4 x 148 warps with long entry blocks.
+int64_t few_tokens(const hdet_embedding* d) { return (4 * 148 - 1) / (div_up(d->width, 256) * d->n_replicas) * kEntries; }
+
+GradLayout layout_of(const hdet_embedding* d, int64_t n_tokens) {
   GradLayout l{};
   const auto up = [](int64_t x) { return div_up(x, 256) * 256; };
   l.sorted_replicas = d->n_replicas > 1 && d->token_stride != 0 ? d->n_replicas : 1;
   // Fewer than four warps a SM in the gradient kernel: shorter entry blocks make more of them (96 tokens of
   // width 72: 6.8 us instead of 8.6).
-  l.entries = div_up(d->n_tokens, kEntries) * div_up(d->width, 256) * d->n_replicas < 4 * 148 ? kFewEntries : kEntries;
-  l.list_bytes = up(4 * d->n_tokens * l.sorted_replicas);
+  l.entries = n_tokens <= few_tokens(d) ? kFewEntries : kEntries;
+  l.list_bytes = up(4 * n_tokens * l.sorted_replicas);
   l.partial_off = 4 * l.list_bytes;
-  l.total = l.partial_off + up(4 * 2 * d->width * div_up(d->n_tokens, l.entries) * d->n_replicas);
+  l.total = l.partial_off + up(4 * 2 * d->width * div_up(n_tokens, l.entries) * d->n_replicas);
   if (l.total < 256) l.total = 256;
   return l;
+}
+
+// The most that a call with up to n_tokens tokens needs: the last batch with short entry blocks has more partial sums than the first with
+// long ones.
+int64_t workspace_of(const hdet_embedding* d) {
+  return std::max(layout_of(d, d->n_tokens).total, layout_of(d, std::min(d->n_tokens, few_tokens(d))).total);
 }
 
 }  // namespace
@@ -634,7 +644,7 @@ extern "C" HDET_API int hdet_embed_grad_workspace(const hdet_embedding* d, int64
   if (!bytes) return fail(HDET_ERR_INVALID_ARG, "hdet_embed_grad_workspace", "bytes is NULL");
   *bytes = 0;
   if (const int rc = check("hdet_embed_grad_workspace", d)) return rc;
-  *bytes = layout_of(d).total;
+  *bytes = workspace_of(d);
   return HDET_OK;
 }
 
@@ -643,7 +653,7 @@ extern "C" HDET_API int hdet_embed_grad(const hdet_embedding* d, int32_t accumul
   hdet::TraceRange trace("hdet_embed_grad");
   if (const int rc = check("hdet_embed_grad", d)) return rc;
   if (const int rc = check_pointers("hdet_embed_grad", d, true)) return rc;
-  const GradLayout l = layout_of(d);
+  const GradLayout l = layout_of(d, d->n_tokens);
   if (!workspace || workspace_bytes < l.total)
     return fail(HDET_ERR_INVALID_ARG, "hdet_embed_grad", "the workspace is NULL or smaller than hdet_embed_grad_workspace says");
   if (reinterpret_cast<uintptr_t>(workspace) % 256)

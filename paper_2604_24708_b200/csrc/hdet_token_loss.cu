@@ -1487,11 +1487,13 @@ Plan plan_of(const hdet_token_loss_args* d) {
       const int64_t w_tiles = d->d_weight ? q.group * (q.piece / q.tile) * div_up(D, q.tile) : 0;
       const int64_t work = h_tiles * all * q.h_terms + w_tiles * div_up(T, kBlockK) * q.w_terms;
       const int64_t slots = kSlots * (3 - q.ctas);
+      const double share = (double)work / (double)slots;
       double best = 0.0;
       for (int64_t parts = 1; parts <= 64; ++parts) {
+        if (best != 0.0 && share >= 0.98 * best) break;        // no cut ends before the equal share
         const int64_t len = div_up(all, parts), n = div_up(all, len);
         if (n != parts || (parts > 1 && len < 8)) continue;
-        const double rounds = (double)(div_up(h_tiles * n, slots) * len * q.h_terms), share = (double)work / (double)slots;
+        const double rounds = (double)(div_up(h_tiles * n, slots) * len * q.h_terms);
         const double end = (rounds > share ? rounds : share) + (n > 1 ? 2.0 * (double)(h_tiles * n) / (double)slots : 0.0);
         if (best == 0.0 || end < 0.98 * best) {
           best = end;
@@ -1520,6 +1522,17 @@ Plan plan_of(const hdet_token_loss_args* d) {
   }
   q.total = at;
   return q;
+}
+
+// The most that a call with up to n_tokens tokens needs.  A shorter batch can need more than a longer one: more of its replicas share a
+// launch, or its sums are cut into more parts.  The plan is the same for tokens up to the same multiple of 64 (but for the few that
+// have a kernel of their own).
+int64_t workspace_of(const hdet_token_loss_args* d) {
+  hdet_token_loss_args a = *d;
+  int64_t most = plan_of(d).total;
+  for (a.n_tokens = kFew; a.n_tokens < d->n_tokens; a.n_tokens = a.n_tokens == kFew ? 64 : a.n_tokens + 64)
+    most = std::max(most, plan_of(&a).total);
+  return most;
 }
 
 struct DeviceScope {
@@ -1632,7 +1645,7 @@ extern "C" HDET_API int hdet_token_loss_workspace(const hdet_token_loss_args* d,
   if (!bytes) return fail(HDET_ERR_INVALID_ARG, who, "bytes is NULL");
   *bytes = 0;
   if (const int rc = check(who, d)) return rc;
-  *bytes = plan_of(d).total;
+  *bytes = workspace_of(d);
   return HDET_OK;
 }
 

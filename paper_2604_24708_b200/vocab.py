@@ -16,7 +16,7 @@ from .arena import StackedArena
 class TiedTable:
     def __init__(self, arena: StackedArena, k: int, vocab: int, width: int, n_tokens: int, scale: float = 1.0,
                  use_mean: bool = False, piece_bytes: int = 0):
-        """Tensor ``k`` of ``arena`` as a [vocab, width] table for batches of ``n_tokens`` tokens per replica.
+        """Tensor ``k`` of ``arena`` as a [vocab, width] table for batches of up to ``n_tokens`` tokens per replica.
 
         ``use_mean``: the loss reads the one averaged bf16 copy that every converge writes (bf16_copy=True, a converge
         every step); otherwise ``refresh`` rounds every replica's own parameters after each update.
@@ -34,10 +34,13 @@ class TiedTable:
         n, dev = arena.n, arena.device
         tokens = torch.empty((n, n_tokens), dtype=torch.int32, device=dev)
         rows = torch.empty((n, n_tokens, width), dtype=torch.bfloat16, device=dev)
-        loss_bytes = B.hdet_token_loss_workspace(rows, self.weight, tokens, d_hidden=rows, d_weight=self.grad, piece_bytes=piece_bytes)
-        embed_bytes = B.hdet_embed_grad_workspace(tokens, rows, self.grad)
+        need = [B.hdet_embed_grad_workspace(tokens, rows, self.grad)]
+        # the loss alone, and with gradients of the hidden states in either type
+        for d_hidden in (None, rows, torch.empty((n, n_tokens, width), dtype=torch.float32, device=dev)):
+            need.append(B.hdet_token_loss_workspace(rows, self.weight, tokens, d_hidden=d_hidden, d_weight=None if d_hidden is None else self.grad,
+                                                    piece_bytes=piece_bytes))
         # the two calls follow each other on one stream, so they share one workspace
-        self.workspace = torch.empty((max(loss_bytes, embed_bytes),), dtype=torch.uint8, device=dev)
+        self.workspace = torch.empty((max(need),), dtype=torch.uint8, device=dev)
         self.refresh()
 
     def refresh(self) -> None:
@@ -51,7 +54,7 @@ class TiedTable:
 
     def loss(self, hidden, targets, losses, d_hidden=None, token_loss=None, grad_scale: float = 1.0) -> None:
         """losses [N] = every replica's mean cross entropy of hidden [N, T, width] (bf16) against its table.  With ``d_hidden``
-        the gradients are taken too: the table's is written to the arena, over what was there."""
+        (bfloat16 or float32) the gradients are taken too: the table's is written to the arena, over what was there."""
         B.hdet_token_loss(hidden, self.weight, targets, losses, self.workspace, token_loss=token_loss, d_hidden=d_hidden,
                           d_weight=None if d_hidden is None else self.grad, grad_scale=grad_scale, piece_bytes=self.piece_bytes,
                           stream=self._stream())

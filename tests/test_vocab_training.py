@@ -190,3 +190,30 @@ def test_the_table_checks_its_tensor():
     Arena.shared_grad = True
     with pytest.raises(ValueError):
         TiedTable(Arena(), 0, 4, 3, 4)
+
+
+@pytest.mark.gpu
+def test_a_table_takes_shorter_batches():
+    """Batches of up to n_tokens, with the loss alone, and with gradients of the hidden states in either type."""
+    from paper_2604_24708_b200.arena import StackedArena
+    from paper_2604_24708_b200.vocab import TiedTable
+    n, T, V, D = 3, 400, 1000, 64
+    arena = StackedArena([V * D], [0], n, B.HDET_OPT_ADAMW, B.HDET_DTYPE_BF16)
+    arena.param.normal_(0, 0.3)
+    table = TiedTable(arena, 0, V, D, T, piece_bytes=1_000_000)
+    for t in (400, 399, 300, 200, 192, 130, 64, 5, 4, 1):
+        ids = torch.randint(0, V, (n, t + 1), device="cuda", dtype=torch.int32)
+        hidden = torch.randn((n, t, D), device="cuda").bfloat16()
+        losses, again = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+        for dt in (None, torch.bfloat16, torch.float32):
+            d_hidden = None if dt is None else torch.empty((n, t, D), dtype=dt, device="cuda")
+            table.loss(hidden, ids[:, 1:], losses, d_hidden=d_hidden)
+            if dt is None:
+                continue
+            apart, grad = torch.empty_like(d_hidden), torch.empty_like(table.grad)
+            ws = torch.empty(B.hdet_token_loss_workspace(hidden, table.weight, ids[:, 1:], d_hidden=apart, d_weight=grad, piece_bytes=1_000_000),
+                             dtype=torch.uint8, device="cuda")
+            B.hdet_token_loss(hidden, table.weight, ids[:, 1:], again, ws, d_hidden=apart, d_weight=grad, piece_bytes=1_000_000,
+                              stream=torch.cuda.current_stream().cuda_stream)
+            assert torch.equal(losses, again) and torch.equal(apart, d_hidden) and torch.equal(grad, table.grad)
+            table.embed_grad(ids[:, :t], d_hidden)
