@@ -536,7 +536,11 @@ struct DeviceScope {
   ~DeviceScope() { if (switched) cudaSetDevice(prev); }
 };
 
-int fail_cuda(const char* who, cudaError_t e) { return fail(HDET_ERR_CUDA, who, cudaGetErrorString(e)); }
+// The call's own error, which does not stay behind for whoever asks the runtime for its last one next.
+int fail_cuda(const char* who, cudaError_t e) {
+  cudaGetLastError();
+  return fail(HDET_ERR_CUDA, who, cudaGetErrorString(e));
+}
 
 template <typename TableT, typename RowT, int VEC>
 cudaError_t launch_lookup(const EmbedParams& p, cudaStream_t st) {

@@ -1,0 +1,40 @@
+"""Errors of the vocabulary ends: a failed call is over when it has returned."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2604_24708_b200 import binding as B
+
+NO_DEVICE = 1000
+
+
+def _fail():
+    """A call that the runtime refuses: there is no such device."""
+    d = B.hdet_embedding(0x1000, 0x2000, 0x3000, 4, 10, 8, 4, 32, 8, 80, 8, 1.0, 2, B.HDET_DTYPE_I32, B.HDET_DTYPE_F32, B.HDET_DTYPE_F32, NO_DEVICE, 0)
+    assert B.raw_library().hdet_embed(C.byref(d), None) == B.HDET_ERR_CUDA
+    assert B.raw_library().hdet_embed_grad(C.byref(d), 0, 0x10000, 1 << 30, None) == B.HDET_ERR_CUDA
+    a = B.hdet_token_loss_args(hidden=0x1000, weight=0x2000, targets=0x3000, loss=0x4000, n_tokens=4, vocab=10, width=8, hidden_stride=32, hidden_row=8,
+                               weight_stride=80, weight_row=8, target_stride=4, grad_scale=1.0, n_replicas=2, hidden_dtype=B.HDET_DTYPE_BF16,
+                               weight_dtype=B.HDET_DTYPE_BF16, target_dtype=B.HDET_DTYPE_I32, loss_dtype=B.HDET_DTYPE_F32, device=NO_DEVICE)
+    assert B.raw_library().hdet_token_loss(C.byref(a), 0x10000, 1 << 30, None) == B.HDET_ERR_CUDA
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("grads", [False, True])
+def test_a_failed_call_is_not_the_next_ones(grads):
+    """The loss, and calls that were there before it, after a failure on this thread."""
+    h, w = torch.randn((2, 200, 64), device="cuda").bfloat16(), torch.randn((2, 300, 64), device="cuda").bfloat16()
+    y, loss = torch.randint(0, 300, (2, 200), device="cuda", dtype=torch.int32), torch.empty(2, device="cuda")
+    out = dict(d_hidden=torch.empty_like(h), d_weight=torch.empty_like(w)) if grads else {}
+    ws = torch.empty(B.hdet_token_loss_workspace(h, w, y, **out), dtype=torch.uint8, device="cuda")
+    _fail()
+    B.hdet_token_loss(h, w, y, loss, ws, stream=torch.cuda.current_stream().cuda_stream, **out)
+    want = torch.nn.functional.cross_entropy((h.double() @ w.double().transpose(1, 2)).flatten(0, 1), y.flatten().long(), reduction="none")
+    assert torch.allclose(loss.double(), want.view(2, 200).mean(1), rtol=1e-5)
+    _fail()
+    p = torch.randn((2, 64), device="cuda")
+    mean = p.mean(0)
+    t = B.hdet_tensor(param=p.data_ptr(), numel=64, param_stride=64)
+    B.hdet_converge_static([t], 2, 0, torch.cuda.current_stream().cuda_stream)
+    assert torch.equal(p[0], mean) and torch.equal(p[1], mean)
