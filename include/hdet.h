@@ -444,6 +444,9 @@ HDET_API int hdet_converge_static(const hdet_tensor* tensors, int64_t n_tensors,
 #define HDET_MAX_TOKENS (1 << 24) /* tokens per replica */
 #define HDET_MAX_VOCAB (1 << 24)
 #define HDET_MAX_WIDTH (1 << 16)
+/* largest strides, in elements: with these no offset of a call passes 64 bits */
+#define HDET_MAX_ROW_STRIDE (INT64_C(1) << 36)
+#define HDET_MAX_REPLICA_STRIDE (INT64_C(1) << 48)
 
 typedef struct {
   const void* tokens;    /* [N] x n_tokens, token_dtype                                                        */

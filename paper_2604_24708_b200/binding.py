@@ -341,6 +341,8 @@ def hdet_converge_static(tensors: Sequence[hdet_tensor], n_replicas: int, device
 HDET_MAX_TOKENS = 1 << 24
 HDET_MAX_VOCAB = 1 << 24
 HDET_MAX_WIDTH = 1 << 16
+HDET_MAX_ROW_STRIDE = 1 << 36
+HDET_MAX_REPLICA_STRIDE = 1 << 48
 
 
 class _DtypeCodes(dict):

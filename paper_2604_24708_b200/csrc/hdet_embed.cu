@@ -466,6 +466,10 @@ int check(const char* who, const hdet_embedding* d) {
   if (!(d->scale == d->scale) || d->scale - d->scale != 0.0) return fail(HDET_ERR_INVALID_ARG, who, "scale must be finite");
   if (d->table_row < d->width || d->rows_row < d->width)
     return fail(HDET_ERR_INVALID_ARG, who, "a row stride is smaller than width");
+  if (std::max(d->table_row, d->rows_row) > HDET_MAX_ROW_STRIDE)
+    return fail(HDET_ERR_INVALID_ARG, who, "a row stride is out of range");
+  if (d->n_replicas > 1 && std::max({d->table_stride, d->rows_stride, d->token_stride}) > HDET_MAX_REPLICA_STRIDE)
+    return fail(HDET_ERR_INVALID_ARG, who, "a replica stride is out of range");
   return HDET_OK;
 }
 

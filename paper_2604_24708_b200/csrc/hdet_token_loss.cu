@@ -1386,8 +1386,12 @@ int check(const char* who, const hdet_token_loss_args* d) {
     return fail(HDET_ERR_INVALID_ARG, who, "a row stride is smaller than width");
   const int64_t strides[] = {d->hidden_stride, d->weight_stride, d->target_stride, d->token_loss_stride, d->d_hidden_stride,
                              d->d_weight_stride};
-  for (const int64_t s : strides)
+  for (const int64_t s : strides) {
     if (s < 0) return fail(HDET_ERR_INVALID_ARG, who, "negative stride");
+    if (d->n_replicas > 1 && s > HDET_MAX_REPLICA_STRIDE) return fail(HDET_ERR_INVALID_ARG, who, "a replica stride is out of range");
+  }
+  if (std::max({d->hidden_row, d->weight_row, d->d_hidden ? d->d_hidden_row : 0, d->d_weight ? d->d_weight_row : 0}) > HDET_MAX_ROW_STRIDE)
+    return fail(HDET_ERR_INVALID_ARG, who, "a row stride is out of range");
   return HDET_OK;
 }
 
