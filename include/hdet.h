@@ -459,7 +459,7 @@ typedef struct {
                                       rows_stride 0 (one gradient for all replicas)                            */
   int64_t table_stride, table_row; /* between replicas and between rows; hdet_embed accepts table_stride 0 (one
                                       table for all replicas)                                                  */
-  double scale;
+  double scale;          /* finite in fp32                                                                     */
   int32_t n_replicas;    /* 1 .. HDET_MAX_REPLICAS                                                             */
   int32_t token_dtype;   /* HDET_DTYPE_I32 or HDET_DTYPE_I64                                                   */
   int32_t rows_dtype, table_dtype; /* HDET_DTYPE_F32 or HDET_DTYPE_BF16 each                                   */
@@ -504,7 +504,7 @@ typedef struct {
   int64_t target_stride, token_loss_stride;
   int64_t d_hidden_stride, d_hidden_row;
   int64_t d_weight_stride, d_weight_row;
-  double grad_scale;     /* the gradients are those of grad_scale x loss (a loss scale; 1 otherwise)           */
+  double grad_scale;     /* the gradients are those of grad_scale x loss (a loss scale, finite in fp32; or 1)  */
   int64_t piece_bytes;   /* workspace for the softmax's gradient, the largest part; 0 = 512 MB.  Smaller pieces
                             mean more launches, at least one tile of 256 rows of the table x n_tokens          */
   int32_t n_replicas;

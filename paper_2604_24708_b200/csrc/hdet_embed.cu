@@ -9,6 +9,7 @@
 #include <cuda_bf16.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdio>
 
 #include "hdet_internal.h"
@@ -463,7 +464,7 @@ int check(const char* who, const hdet_embedding* d) {
       (d->rows_dtype != HDET_DTYPE_F32 && d->rows_dtype != HDET_DTYPE_BF16))
     return fail(HDET_ERR_INVALID_ARG, who, "table_dtype and rows_dtype must be HDET_DTYPE_F32 or HDET_DTYPE_BF16");
   if (d->device < 0) return fail(HDET_ERR_INVALID_ARG, who, "device must be >= 0");
-  if (!(d->scale == d->scale) || d->scale - d->scale != 0.0) return fail(HDET_ERR_INVALID_ARG, who, "scale must be finite");
+  if (!std::isfinite((float)d->scale)) return fail(HDET_ERR_INVALID_ARG, who, "scale must be finite in fp32");
   if (d->table_row < d->width || d->rows_row < d->width)
     return fail(HDET_ERR_INVALID_ARG, who, "a row stride is smaller than width");
   if (std::max(d->table_row, d->rows_row) > HDET_MAX_ROW_STRIDE)

@@ -1379,7 +1379,7 @@ int check(const char* who, const hdet_token_loss_args* d) {
   if ((d->d_hidden && !is_float(d->d_hidden_dtype)) || (d->d_weight && !is_float(d->d_weight_dtype)))
     return fail(HDET_ERR_INVALID_ARG, who, "the gradients' dtypes must be HDET_DTYPE_F32 or HDET_DTYPE_BF16");
   if (d->device < 0) return fail(HDET_ERR_INVALID_ARG, who, "device must be >= 0");
-  if (!std::isfinite(d->grad_scale)) return fail(HDET_ERR_INVALID_ARG, who, "grad_scale must be finite");
+  if (!std::isfinite((float)d->grad_scale)) return fail(HDET_ERR_INVALID_ARG, who, "grad_scale must be finite in fp32");
   if (d->piece_bytes < 0) return fail(HDET_ERR_INVALID_ARG, who, "piece_bytes must be >= 0");
   if (d->hidden_row < d->width || d->weight_row < d->width || (d->d_hidden && d->d_hidden_row < d->width) ||
       (d->d_weight && d->d_weight_row < d->width))

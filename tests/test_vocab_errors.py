@@ -82,3 +82,10 @@ def test_replica_strides_whose_offsets_pass_64_bits(stride):
         assert _embed_status(**{name: stride}) == _embed_status(grad=True, **{name: stride}) == ARG
     for name in ("hidden_stride", "weight_stride", "target_stride", "token_loss_stride", "d_hidden_stride", "d_weight_stride"):
         assert _loss_status(**{name: stride}) == ARG
+
+
+@pytest.mark.parametrize("scale", [1e39, -1e39, 1e300, float("inf"), float("nan")])
+def test_scales_that_fp32_does_not_hold(scale):
+    """They would turn into infinity, and zeros times that into NaN."""
+    assert _embed_status(scale=scale) == _embed_status(grad=True, scale=scale) == _loss_status(grad_scale=scale) == ARG
+    assert _embed_status(scale=3e38) == _loss_status(grad_scale=-3e38) == CUDA
