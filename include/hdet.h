@@ -533,7 +533,8 @@ typedef struct {
  * keeps their exponentials (16 bits, off by 2^-11, zero below 2^-62 of the largest of 64 or 128 neighbours) until the row's sum is known.
  * A table whose row stride or replica stride is not a multiple of 8 elements, or that is not 16-byte aligned, is laid
  * out in the workspace by every call first.
- * Outputs must not overlap inputs or one another, except that d_hidden may be the hidden states' own buffer.
+ * Outputs must not overlap inputs or one another, except that d_hidden may be the hidden states' own buffer, as bf16 and with their
+ * strides.
  * If a bounded wait inside a kernel runs out, every loss is set to NaN.
  * hdet_token_loss_workspace gives the bytes that this call, and any with fewer tokens and all else the same, needs; it looks at
  * sizes, strides, dtypes, piece_bytes, the table's address (its alignment) and at which gradients are asked for.

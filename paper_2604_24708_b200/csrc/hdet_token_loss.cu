@@ -1408,6 +1408,10 @@ int check_pointers(const char* who, const hdet_token_loss_args* d) {
         (d->d_weight && d->d_weight_stride < span(d->vocab, d->d_weight_row)))
       return fail(HDET_ERR_INVALID_ARG, who, "a replica stride is smaller than one replica");
   }
+  // In the hidden states' own buffer every row of d_hidden has to lie on its own hidden state's: other rows are still to be read.
+  if (d->d_hidden && d->d_hidden == d->hidden && d->n_tokens > 0 &&
+      (d->d_hidden_dtype != HDET_DTYPE_BF16 || d->d_hidden_row != d->hidden_row || (d->n_replicas > 1 && d->d_hidden_stride != d->hidden_stride)))
+    return fail(HDET_ERR_INVALID_ARG, who, "d_hidden in the place of the hidden states needs their dtype and strides");
   if (!aligned(d->hidden, 2) || !aligned(d->weight, 2) || !aligned(d->targets, d->target_dtype == HDET_DTYPE_I64 ? 8 : 4) ||
       !aligned(d->loss, d->loss_dtype == HDET_DTYPE_F64 ? 8 : 4) || !aligned(d->token_loss, 4) ||
       (d->d_hidden && !aligned(d->d_hidden, elem_size(d->d_hidden_dtype))) ||

@@ -89,3 +89,13 @@ def test_scales_that_fp32_does_not_hold(scale):
     """They would turn into infinity, and zeros times that into NaN."""
     assert _embed_status(scale=scale) == _embed_status(grad=True, scale=scale) == _loss_status(grad_scale=scale) == ARG
     assert _embed_status(scale=3e38) == _loss_status(grad_scale=-3e38) == CUDA
+
+
+def test_a_gradient_in_the_place_of_the_hidden_states_lies_on_them():
+    same = dict(d_hidden=0x1000)
+    assert _loss_status(**same) == CUDA
+    assert _loss_status(**same, d_hidden_dtype=B.HDET_DTYPE_F32) == ARG
+    assert _loss_status(**same, d_hidden_row=16, d_hidden_stride=64) == ARG
+    assert _loss_status(**same, d_hidden_stride=40) == ARG
+    assert _loss_status(**same, hidden_stride=0) == ARG             # one batch for all replicas, and a gradient for each
+    assert _loss_status(**same, d_hidden_stride=40, n_replicas=1) == CUDA
