@@ -480,9 +480,9 @@ int check_pointers(const char* who, const hdet_embedding* d, bool writes_table) 
     return fail(HDET_ERR_INVALID_ARG, who, "a pointer is NULL");
   const int64_t table_len = (d->vocab - 1) * d->table_row + d->width;
   const int64_t rows_len = d->n_tokens > 0 ? (d->n_tokens - 1) * d->rows_row + d->width : 0;
-  if (d->table_stride < 0 || d->rows_stride < 0 || d->token_stride < 0)
-    return fail(HDET_ERR_INVALID_ARG, who, "negative stride");
   if (d->n_replicas > 1) {
+    if (d->table_stride < 0 || d->rows_stride < 0 || d->token_stride < 0)
+      return fail(HDET_ERR_INVALID_ARG, who, "negative stride");
     if (d->table_stride < table_len && (writes_table || d->table_stride != 0))
       return fail(HDET_ERR_INVALID_ARG, who, "table_stride is smaller than one table");
     if (d->rows_stride < rows_len && (!writes_table || d->rows_stride != 0))

@@ -1387,8 +1387,9 @@ int check(const char* who, const hdet_token_loss_args* d) {
   const int64_t strides[] = {d->hidden_stride, d->weight_stride, d->target_stride, d->token_loss_stride, d->d_hidden_stride,
                              d->d_weight_stride};
   for (const int64_t s : strides) {
+    if (d->n_replicas == 1) break;
     if (s < 0) return fail(HDET_ERR_INVALID_ARG, who, "negative stride");
-    if (d->n_replicas > 1 && s > HDET_MAX_REPLICA_STRIDE) return fail(HDET_ERR_INVALID_ARG, who, "a replica stride is out of range");
+    if (s > HDET_MAX_REPLICA_STRIDE) return fail(HDET_ERR_INVALID_ARG, who, "a replica stride is out of range");
   }
   if (std::max({d->hidden_row, d->weight_row, d->d_hidden ? d->d_hidden_row : 0, d->d_weight ? d->d_weight_row : 0}) > HDET_MAX_ROW_STRIDE)
     return fail(HDET_ERR_INVALID_ARG, who, "a row stride is out of range");
@@ -1671,7 +1672,7 @@ extern "C" HDET_API int hdet_token_loss(const hdet_token_loss_args* d, void* wor
     return fail(HDET_ERR_INVALID_ARG, who, "the workspace is NULL or smaller than hdet_token_loss_workspace says");
   if (!aligned(workspace, 256)) return fail(HDET_ERR_ALIGN, who, "the workspace is not 256-byte aligned");
   if (q.m_tiles * q.n_tiles * d->n_replicas * q.ctas > INT32_MAX || q.rows_pad * q.packed_row * 2 >= (1ll << 40) ||
-      d->weight_row * d->vocab * 2 >= (1ll << 40) || d->weight_stride * 2 >= (1ll << 40))
+      d->weight_row * d->vocab * 2 >= (1ll << 40) || (d->n_replicas > 1 && d->weight_stride * 2 >= (1ll << 40)))
     return fail(HDET_ERR_UNSUPPORTED, who, "too many tiles, or a stride of 2^40 bytes or more");
   DeviceScope scope(d->device);
   if (scope.err != cudaSuccess) return fail_cuda(who, scope.err);

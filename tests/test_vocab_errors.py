@@ -99,3 +99,20 @@ def test_a_gradient_in_the_place_of_the_hidden_states_lies_on_them():
     assert _loss_status(**same, d_hidden_stride=40) == ARG
     assert _loss_status(**same, hidden_stride=0) == ARG             # one batch for all replicas, and a gradient for each
     assert _loss_status(**same, d_hidden_stride=40, n_replicas=1) == CUDA
+
+
+@pytest.mark.parametrize("stride", [-1, -(1 << 62), 1 << 62, 3])
+def test_one_replica_has_no_replica_strides(stride):
+    """With one replica they are not looked at, whatever they hold."""
+    names = ("table_stride", "rows_stride", "token_stride")
+    assert _embed_status(n_replicas=1, **dict.fromkeys(names, stride)) == _embed_status(grad=True, n_replicas=1, **dict.fromkeys(names, stride)) == CUDA
+    names = ("hidden_stride", "weight_stride", "target_stride", "token_loss_stride", "d_hidden_stride", "d_weight_stride")
+    assert _loss_status(n_replicas=1, **dict.fromkeys(names, stride)) == CUDA
+    need = []
+    for s in (0, stride):
+        a = B.hdet_token_loss_args(weight=0x2000, n_tokens=4, vocab=10, width=8, hidden_row=8, weight_row=8, grad_scale=1.0, n_replicas=1,
+                                   hidden_dtype=B.HDET_DTYPE_BF16, weight_dtype=B.HDET_DTYPE_BF16, target_dtype=B.HDET_DTYPE_I32, **dict.fromkeys(names, s))
+        size = C.c_int64(0)
+        assert B.raw_library().hdet_token_loss_workspace(C.byref(a), C.byref(size)) == B.HDET_OK
+        need.append(size.value)
+    assert need[0] == need[1]
