@@ -21,6 +21,7 @@
  *   hdet_converge_static   allocation-free variant of hdet_converge
  *   hdet_plan_tiles        host-only view of the work plan (tests, tools)
  *   hdet_selftest_bounded_wait   makes a kernel's bounded wait run out, to show the timeout status
+ *   hdet_selftest_token_loss_wait   the same in the token loss
  * and where the replicas' models meet their vocabulary (no handle needed):
  *   hdet_embed / hdet_embed_grad   embedding lookup with scaling, and the table's gradient
  *   hdet_token_loss                softmax cross entropy against the table, one mean per replica (the losses that
@@ -535,7 +536,7 @@ typedef struct {
  * out in the workspace by every call first.
  * Outputs must not overlap inputs or one another, except that d_hidden may be the hidden states' own buffer, as bf16 and with their
  * strides.
- * If a bounded wait inside a kernel runs out, every loss is set to NaN.
+ * If a bounded wait inside a kernel runs out, every loss is set to NaN, and the other outputs are not defined.
  * hdet_token_loss_workspace gives the bytes that this call, and any with fewer tokens and all else the same, needs; it looks at
  * sizes, strides, dtypes, piece_bytes, the table's address (its alignment) and at which gradients are asked for.
  * Errors: INVALID_ARG (NULL, sizes, strides or dtypes out of range, workspace NULL or too small), ALIGN, UNSUPPORTED
@@ -543,6 +544,14 @@ typedef struct {
  */
 HDET_API int hdet_token_loss_workspace(const hdet_token_loss_args* d, int64_t* bytes);
 HDET_API int hdet_token_loss(const hdet_token_loss_args* d, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * hdet_selftest_token_loss_wait -- (a diagnostic, as hdet_selftest_bounded_wait.)  hdet_token_loss with waits of about 2 ms and its
+ * kernels' tiles withheld after the first, so that the waits for them run out: every loss becomes NaN, the CUDA context
+ * stays usable, and the next call on the same workspace is an ordinary one.  Needs more than four tokens, or a gradient.
+ * Errors: as hdet_token_loss, plus UNSUPPORTED (no kernel of this call waits).
+ */
+HDET_API int hdet_selftest_token_loss_wait(const hdet_token_loss_args* d, void* workspace, int64_t workspace_bytes, void* stream);
 
 /* hdet_last_error -- text of the last failure on h (when h is NULL: of the last failed call
  * that has no handle, hdet_create, hdet_converge_static or a call of the vocabulary ends, on this thread).  The pointer stays valid until the next call on that handle. */

@@ -158,8 +158,9 @@ def _load() -> C.CDLL:
     lib.hdet_embed_grad.restype = C.c_int
     lib.hdet_token_loss_workspace.argtypes = [C.c_void_p, C.POINTER(C.c_int64)]
     lib.hdet_token_loss_workspace.restype = C.c_int
-    lib.hdet_token_loss.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]
-    lib.hdet_token_loss.restype = C.c_int
+    for f in (lib.hdet_token_loss, lib.hdet_selftest_token_loss_wait):
+        f.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]
+        f.restype = C.c_int
     for f in ("hdet_create", "hdet_set_schedule", "hdet_step", "hdet_converge", "hdet_autolr_update",
               "hdet_get_state", "hdet_set_state", "hdet_destroy"):
         getattr(lib, f).restype = C.c_int
@@ -507,6 +508,13 @@ def hdet_token_loss(hidden, weight, targets, loss, workspace, token_loss=None, d
     status = _lib.hdet_token_loss(a, ptr, size, stream)
     if status:
         _check(status, None)
+
+
+def hdet_selftest_token_loss_wait(hidden, weight, targets, loss, workspace, d_hidden=None, d_weight=None, piece_bytes: int = 0, stream: int = 0) -> None:
+    """hdet_token_loss whose kernels' waits run out after some milliseconds: every loss becomes NaN, gradients are not defined."""
+    a = _token_loss_args(hidden, weight, targets, loss, None, d_hidden, d_weight, loss.shape[0], 1.0, False, piece_bytes)
+    ptr, size = _workspace(workspace, hidden.get_device())
+    _check(_lib.hdet_selftest_token_loss_wait(a, ptr, size, stream), None)
 
 
 def _workspace(workspace, device: int):

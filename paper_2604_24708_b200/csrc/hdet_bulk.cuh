@@ -1,8 +1,8 @@
 // Bulk asynchronous copies between global and shared memory (sm_90+ `cp.async.bulk`, the untiled
 // form of the tensor memory accelerator) and the shared-memory barriers that track them.
 //
-// Every copy stays inside one CTA and one GPU: the destination of a load is the issuing CTA's own
-// shared memory, no cluster is launched and no copy is sent to more than one CTA.  Rules of the
+// Every copy of this file stays inside one CTA and one GPU: the destination of a load is the issuing CTA's own
+// shared memory, and no copy is sent to more than one CTA (hdet_umma.cuh uses the barriers in clusters of two).  Rules of the
 // instruction: both addresses 16-byte aligned, size a multiple of 16 bytes.
 //
 // Every wait in this file is bounded: a barrier that does not complete within about a second makes

@@ -58,7 +58,8 @@ constexpr int kGemmThreads = 384, kFirstReader = 4, kReaders = 8;
 constexpr int kStagingBytes = 4096;        // per reader: 32 rows x 128 bytes
 constexpr int kAskAhead = 8;               // steps before a tile's end at which its successor is looked up
 constexpr int kTileSlots = 4;              // tiles under way between the copies and the readers
-constexpr long long kDrainLimitCycles = 200000000ll;
+constexpr long long kDrainCycles = 20000000ll;          // 10 ms: thousands of times what a copy or a product takes
+constexpr long long kSelftestLimitCycles = 4000000ll;   // 2 ms
 
 __host__ __device__ constexpr int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 __host__ __device__ constexpr int64_t round_up(int64_t a, int64_t b) { return div_up(a, b) * b; }
@@ -119,6 +120,8 @@ struct LossParams {
   int jobs;                 // tiles of this launch
   int chunk;                // steps of 64 that the tensor core sums before a reader takes them over
   unsigned first_ticket;    // Control::ticket when it starts
+  long long wait_limit;     // of every wait, in cycles; twice that where one waits for whole tiles
+  bool withhold;            // hands no tile over, so that the waits for it run out (hdet_selftest_token_loss_wait)
 };
 
 __device__ __forceinline__ void poison_loss(const LossParams& p) {
@@ -642,7 +645,7 @@ struct Shared {             // behind the stages and the readers' staging
   uint64_t tile_full[kTileSlots], tile_empty[kTileSlots], taken;   // taken: the leader's copies have the last tile published
   alignas(16) Job job[kTileSlots];
   uint32_t tmem;
-  int failed, issued;
+  int failed;
   int count[HDET_MAX_REPLICAS];
 };
 
@@ -680,7 +683,6 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
   }
   if (threadIdx.x == 0) {
     sh.failed = 0;
-    sh.issued = 0;
     for (int s = 0; s < kStages; ++s) {
       bulk::barrier_init(bar(sh.full[s]), 1);
       bulk::barrier_init(bar(sh.empty[s]), 1);
@@ -716,7 +718,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
       return true;
     }
     const int use = i - 1, q = use % kTileSlots;
-    const bool ok = wait_cluster(bar(sh.tile_full[q]), (use / kTileSlots) & 1, 2 * bulk::kWaitLimitCycles);
+    const bool ok = wait_cluster(bar(sh.tile_full[q]), (use / kTileSlots) & 1, 2 * p.wait_limit);
     if (!__all_sync(0xffffffffu, ok)) {
       failed = 1;
       return false;
@@ -756,7 +758,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
         const int a_row = j.a_row + 128 * (int)rank, b_row = j.b_row + 64 * j.b_boxes * (int)rank;
         int in_pass = 0, a_z = j.a_z;
         for (int step = 0; step < j.k_blocks; ++step, ++kb) {
-          if (kb >= kStages && !warp_wait(bar(sh.empty[s]), parity ^ 1)) {
+          if (kb >= kStages && !warp_wait(bar(sh.empty[s]), parity ^ 1, p.wait_limit)) {
             failed = 1;
             break;
           }
@@ -780,7 +782,6 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
             if (b_mn) load_box<CTAS>(dst + kOperandBytes + h * kBoxBytes, b_map, b_row + 64 * h, j.b_k + k, j.b_z, done);
             else load_box<CTAS>(dst + kOperandBytes + h * kBoxBytes, b_map, j.b_k + k, b_row + 64 * h, j.b_z, done);
           }
-          sh.issued = kb + 1;
           if (++s == kStages) {
             s = 0;
             parity ^= 1;
@@ -792,7 +793,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
       }
       // the products have read the last stages: every arrival that was sent to this CTA's barriers is in
       for (int k = kb > kStages ? kb - kStages : 0; k < kb && __all_sync(0xffffffffu, !failed); ++k)
-        if (!warp_wait(bar(sh.empty[k % kStages]), (k / kStages) & 1)) failed = 1;
+        if (!warp_wait(bar(sh.empty[k % kStages]), (k / kStages) & 1, p.wait_limit)) failed = 1;
     }
   } else if (warp == 1) {
     if (rank == 0) {
@@ -809,14 +810,14 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
         for (int step = 0, in_chunk = 0; step < j.k_blocks; ++step) {
           if (in_chunk == 0) {
             const int b = uses & 1;
-            if (uses >= 2 && !__all_sync(0xffffffffu, wait_cluster(bar(sh.acc_empty[b]), (uses / 2 - 1) & 1))) {
+            if (uses >= 2 && !__all_sync(0xffffffffu, wait_cluster(bar(sh.acc_empty[b]), (uses / 2 - 1) & 1, p.wait_limit))) {
               failed = 1;
               break;
             }
             fence_after_sync();
             acc = tmem + b * 128 * CTAS;
           }
-          if (!warp_wait(bar(sh.full[s]), parity)) {
+          if (!warp_wait(bar(sh.full[s]), parity, p.wait_limit)) {
             failed = 1;
             break;
           }
@@ -843,14 +844,14 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
       }
     }
   } else if (warp == 2) {
-    if (lane == 0 && rank == 0) {
+    if (lane == 0 && rank == 0 && !p.withhold) {
       const unsigned clusters = gridDim.x / CTAS;
       // A number is drawn when the copies have taken the one before: one drawn earlier may be a tile that another cluster, with
       // nothing left to do, could have had (four drawn ahead: 102 us instead of 77 for 3 x 129 tokens x 4099, width 520).
       for (int use = 0;;) {
         const int q = use % kTileSlots;
-        if ((use > 0 && !bulk::barrier_wait(bar(sh.taken), (use - 1) & 1, 2 * bulk::kWaitLimitCycles)) ||
-            (use >= kTileSlots && !wait_cluster(bar(sh.tile_empty[q]), (use / kTileSlots - 1) & 1, 2 * bulk::kWaitLimitCycles))) {
+        if ((use > 0 && !bulk::barrier_wait(bar(sh.taken), (use - 1) & 1, 2 * p.wait_limit)) ||
+            (use >= kTileSlots && !wait_cluster(bar(sh.tile_empty[q]), (use / kTileSlots - 1) & 1, 2 * p.wait_limit))) {
           failed = 1;
           break;
         }
@@ -898,7 +899,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
       };
       bool ok = true;
       for (int step = 0; step < j.k_blocks; step += SUMS ? p.chunk : j.k_blocks) {
-        ok = warp_wait(bar(sh.acc_full[uses & 1]), (uses / 2) & 1, 2 * bulk::kWaitLimitCycles);
+        ok = warp_wait(bar(sh.acc_full[uses & 1]), (uses / 2) & 1, 2 * p.wait_limit);
         if (!ok) break;
         fence_after_sync();
         if constexpr (SUMS) {
@@ -929,10 +930,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
   if (sh.failed && threadIdx.x == 0) {
     atomicExch(&p.control->status, 1u);
     poison_loss(p);
-    // copies still on their way may write this CTA's shared memory: a bounded wait for each (the leader sees both CTAs')
-    if (rank == 0)
-      for (int kb = max(0, sh.issued - kStages); kb < sh.issued; ++kb)
-        bulk::barrier_wait(bar(sh.full[kb % kStages]), (kb / kStages) & 1, kDrainLimitCycles);
+    // Copies into this CTA's shared memory and products that read it may still be under way; after this they are not.  A wait on their
+    // barriers would not see all of them: a pair's second CTA may have issued copies that the first, whose barriers count them, has not
+    // announced.
+    for (const long long start = clock64(); clock64() - start < kDrainCycles;) __nanosleep(1000);
   }
   if constexpr (CTAS == 2) cluster_sync();       // neither CTA leaves while the other may still reach into it
   fence_after_sync();
@@ -1662,8 +1663,9 @@ extern "C" HDET_API int hdet_token_loss_workspace(const hdet_token_loss_args* d,
   return HDET_OK;
 }
 
-extern "C" HDET_API int hdet_token_loss(const hdet_token_loss_args* d, void* workspace, int64_t workspace_bytes, void* stream) {
-  const char* who = "hdet_token_loss";
+namespace {
+
+int token_loss(const char* who, const hdet_token_loss_args* d, void* workspace, int64_t workspace_bytes, void* stream, bool selftest) {
   hdet::TraceRange trace(who);
   if (const int rc = check(who, d)) return rc;
   if (const int rc = check_pointers(who, d)) return rc;
@@ -1689,6 +1691,8 @@ extern "C" HDET_API int hdet_token_loss(const hdet_token_loss_args* d, void* wor
   p.vocab = (int)d->vocab; p.width = (int)d->width; p.n_tokens = (int)d->n_tokens; p.rows_pad = (int)q.rows_pad;
   p.weight_shared = shared_table;
   p.grad_scale = d->grad_scale;
+  p.wait_limit = selftest ? kSelftestLimitCycles : bulk::kWaitLimitCycles;
+  p.withhold = selftest;
   p.count = reinterpret_cast<int*>(ws + q.off_count);
   p.target = reinterpret_cast<int*>(ws + q.off_target);
   p.token_of = reinterpret_cast<int*>(ws + q.off_token);
@@ -1729,6 +1733,7 @@ extern "C" HDET_API int hdet_token_loss(const hdet_token_loss_args* d, void* wor
   const int tables = shared_table ? 1 : d->n_replicas;
   p.n_parts = (int)q.n_parts;
   if (q.few) {
+    if (selftest) return fail(HDET_ERR_UNSUPPORTED, who, "the kernel for so few tokens waits for nothing");
     const dim3 grid((unsigned)q.n_parts, d->n_replicas);
     const int64_t stride = shared_table ? 0 : table_stride;
     e = launch(d->n_tokens == 1 ? few_kernel<1> : d->n_tokens == 2 ? few_kernel<2> : few_kernel<kFew>, grid, 256, 0, 1, st, p, k, table,
@@ -1811,4 +1816,14 @@ extern "C" HDET_API int hdet_token_loss(const hdet_token_loss_args* d, void* wor
     }
   }
   return HDET_OK;
+}
+
+}  // namespace
+
+extern "C" HDET_API int hdet_token_loss(const hdet_token_loss_args* d, void* workspace, int64_t workspace_bytes, void* stream) {
+  return token_loss("hdet_token_loss", d, workspace, workspace_bytes, stream, false);
+}
+
+extern "C" HDET_API int hdet_selftest_token_loss_wait(const hdet_token_loss_args* d, void* workspace, int64_t workspace_bytes, void* stream) {
+  return token_loss("hdet_selftest_token_loss_wait", d, workspace, workspace_bytes, stream, true);
 }
