@@ -548,7 +548,7 @@ HDET_API int hdet_token_loss(const hdet_token_loss_args* d, void* workspace, int
 /*
  * hdet_selftest_token_loss_wait -- (a diagnostic, as hdet_selftest_bounded_wait.)  hdet_token_loss with waits of about 2 ms and its
  * kernels' tiles withheld after the first, so that the waits for them run out: every loss becomes NaN, the CUDA context
- * stays usable, and the next call on the same workspace is an ordinary one.  Needs more than four tokens, or a gradient.
+ * stays usable, and the next call on the same workspace is an ordinary one.  Needs more than two tokens a replica, or a gradient.
  * Errors: as hdet_token_loss, plus UNSUPPORTED (no kernel of this call waits).
  */
 HDET_API int hdet_selftest_token_loss_wait(const hdet_token_loss_args* d, void* workspace, int64_t workspace_bytes, void* stream);

@@ -22,7 +22,7 @@
 // and for each piece of the vocabulary
 //   probs       Z again; the epilogue writes G
 //   grads       as above; after the last piece, dH's partial sums are joined
-// Up to four tokens a replica without gradients take a kernel of their own (few).
+// Up to two tokens a replica without gradients take a kernel of their own (few).
 //
 // G is the operand of a bf16 product, so it is rounded to bf16, unscaled: the -1 of the target is then exact where the
 // target is unlikely.  Its relative error, 2^-9 a value, is that of a bf16 gradient's own rounding.  For fp32 gradients
@@ -1187,11 +1187,17 @@ __global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ Loss
 }
 
 // ------------------------------------------------------------------------------------------------ few tokens
-// The losses of up to kFew tokens a replica: the table is read once, so that is what bounds it, and a product of 128 rows
-// would leave the tensor cores 124 of them empty.  A warp takes a run of the table's rows, three at a time, a lane 8 elements of
-// each per step; hidden states come from L1.  Sums are fp32.  One token of width 768 against 50257 rows (77 MB): the loss takes
-// 18.1 us with this kernel and 41 us through packing and the product; four rows at a time 19.2, two 20.2, eight 20.5.
-constexpr int kFew = 4, kFewRows = 3;
+// The losses of one or two tokens a replica: the table is read once, so that is what bounds it, and a product of 128 rows
+// would leave the tensor cores 126 of them empty.  A warp takes a run of the table's rows, three at a time, a lane 8 elements of
+// each per step; hidden states come from L1.  Sums are fp32.  Its arithmetic grows with the tokens, the product's does not.  One replica,
+// 50257 rows, replayed from graphs over three tables in turn, with this kernel, and through packing and the product:
+//   1 token   width 768: 19.9 and 34 us    width 2048: 41.9 and 59 us    eight replicas of width 768: 105 and 118 us
+//   2 tokens             24.0 and 34                   46.5 and 59                                    132 and 118
+// and with a form for four tokens, 40.3 and 34 us at three and four, 72 with one for eight.  So two tokens of larger tables than kFewElements,
+// in all, take the product.  Two rows at a time: 19.2 us for one token, 27.9 for two; four rows: 21.0 and 24.5.
+// 80 registers, which leaves three blocks a SM; up to 28 bytes a thread are spilled for it.
+constexpr int kFew = 2, kFewRows = 3;
+constexpr int64_t kFewElements = 150000000;
 
 template <int NT>
 __global__ void __launch_bounds__(256, 3) few_kernel(const __grid_constant__ LossParams p, const __grid_constant__ PackParams k,
@@ -1468,7 +1474,7 @@ Plan plan_of(const hdet_token_loss_args* d) {
   q.w_terms = d->d_weight && d->d_weight_dtype == HDET_DTYPE_F32 ? kTermsF32 : 1;
   q.g_terms = q.h_terms > q.w_terms ? q.h_terms : q.w_terms;
   q.pack_table = !table_fits(d);
-  q.few = !q.grads && T <= kFew && T > 0 && !q.pack_table && D % 8 == 0 && aligned(d->hidden, 16) && d->hidden_row % 8 == 0 &&
+  q.few = !q.grads && T <= kFew && T > 0 && (T == 1 || R * V * D <= kFewElements) && !q.pack_table && D % 8 == 0 && aligned(d->hidden, 16) && d->hidden_row % 8 == 0 &&
           (R == 1 || d->hidden_stride % 8 == 0);
   const int64_t most = div_up(V, 8 * kFewRows), blocks = kFewBlocks / R;
   const int64_t few_parts = blocks < 1 ? 1 : blocks < most ? blocks : most;
@@ -1736,7 +1742,7 @@ int token_loss(const char* who, const hdet_token_loss_args* d, void* workspace, 
     if (selftest) return fail(HDET_ERR_UNSUPPORTED, who, "the kernel for so few tokens waits for nothing");
     const dim3 grid((unsigned)q.n_parts, d->n_replicas);
     const int64_t stride = shared_table ? 0 : table_stride;
-    e = launch(d->n_tokens == 1 ? few_kernel<1> : d->n_tokens == 2 ? few_kernel<2> : few_kernel<kFew>, grid, 256, 0, 1, st, p, k, table,
+    e = launch(d->n_tokens == 1 ? few_kernel<1> : few_kernel<2>, grid, 256, 0, 1, st, p, k, table,
                stride, table_row);
     if (e == cudaSuccess) e = launch(few_join_kernel, dim3(d->n_replicas), 32 * kFew, 0, 1, st, p);
     return e == cudaSuccess ? HDET_OK : fail_cuda(who, e);
