@@ -18,8 +18,9 @@ class TiedTable:
                  use_mean: bool = False, piece_bytes: int = 0):
         """Tensor ``k`` of ``arena`` as a [vocab, width] table for batches of up to ``n_tokens`` tokens per replica.
 
-        ``use_mean``: the loss reads the one averaged bf16 copy that every converge writes (bf16_copy=True, a converge
-        every step); otherwise ``refresh`` rounds every replica's own parameters after each update.
+        ``use_mean``: the loss reads the one averaged bf16 copy that every converge writes (bf16_copy=True).  It is the average of the
+        last converge, whatever has happened to the replicas since, so this is for a converge every step; and before the first loss the copy has
+        to be there: one hdet_converge writes it.  Otherwise ``refresh`` rounds every replica's own parameters after each update.
         """
         if arena.numels[k] != vocab * width:
             raise ValueError(f"tensor {k} has {arena.numels[k]} elements, not {vocab} x {width}")
@@ -60,7 +61,7 @@ class TiedTable:
                           stream=self._stream())
 
     def embed_grad(self, tokens, d_out) -> None:
-        """Adds the lookup's gradient to the table's in the arena; call it after ``loss``."""
+        """Adds the lookup's gradient to the table's in the arena; call it after ``loss``.  (A bf16 gradient is rounded by each.)"""
         B.hdet_embed_grad(tokens, d_out, self.grad, self.workspace, scale=self.scale, accumulate=True, stream=self._stream())
 
     def _stream(self) -> int:
