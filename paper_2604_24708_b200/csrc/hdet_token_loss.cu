@@ -12,12 +12,12 @@
 //
 //   pack        counted tokens move together (padding drops out: no work, and nothing it holds reaches a product)
 // and then, where whole replicas fit and G is bf16, for each group of them
-//   numerators  Z tile by tile on the tensor cores; the epilogue keeps, of each half tile's row, a power of two 2^k about as
-//               large as its largest exponential and the sum of exp(z) / 2^k, and leaves exp(z) / 2^k in G's place
+//   numerators  Z tile by tile on the tensor cores; the epilogue keeps, of each half tile's row, its maximum m and the sum of
+//               exp(z - m), and leaves exp(z - m) in G's place
 //   scale       the row's sum and the token's loss from those; they become G in place; the last block takes the replica's mean
 //   grads       both products with G in one launch
 // or, forming Z twice (a fourth product, but nothing kept but G),
-//   stats       Z, of which the epilogue keeps the powers of two and sums
+//   stats       Z, of which the epilogue keeps the maxima and sums
 //   join        the row's sum, the token's loss, the replica's mean
 // and for each piece of the vocabulary
 //   probs       Z again; the epilogue writes G
@@ -48,7 +48,7 @@ using hdet::let_next_start;
 using hdet::wait_for_previous;
 namespace bulk = hdet::bulk;
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kStages = 6;
 constexpr int kStageBytes = 2 * kOperandBytes;
 // warp 0 copies, warp 1 issues the products, warp 2 hands out tiles, warps 4 - 11 read the accumulator: a quarter of its
@@ -77,9 +77,9 @@ struct Out {                // a gradient
   int f32, accumulate, vec; // vec: rows start and end on 16-byte boundaries
 };
 
-// What turns a row's logits into G: inverse * exp(z) / 2^k, and the target's own value.
+// What turns a row's logits into G: inverse * exp(z - top), and the target's own value.
 struct alignas(16) RowNorm {
-  float k, inverse, target, pad;
+  float top, inverse, target, pad;
 };
 
 struct LossParams {
@@ -381,32 +381,24 @@ struct Source {
   }
 };
 
-// The least whole k with exp(x) <= 2^k (-inf for -inf).  From 2^24 on, where k itself is rounded (up), it may be a step more.
-__device__ __forceinline__ float exponent_above(float x) { return ceilf(__fmul_ru(x, kLog2e)); }
+// exp(x - top) 2^shift.  The subtraction comes first: x log2(e) - top log2(e) in one fma, with the second product rounded, is off by up to
+// 2^-24 of the logits themselves, all of a row by the same factor: the gradient of a target with P = 0.9998 was 2 % off for it, one with
+// P = 0.999999 by several times its value.
+__device__ __forceinline__ float exp_from(float x, float top, float shift = 0.0f) { return exp2_fast(fmaf(x - top, kLog2e, shift)); }
 
-// A sum of exponentials, sum * 2^k with k whole; k = -inf: of nothing.
-//
-// In units of a whole power of two no step rounds at the logits' size: x log2(e) - k is one fma, whose only rounding is that of its
-// (small) result, and sums are brought to one k exactly.  In units of exp(maximum), with the maximum's product with log2(e)
-// rounded, every exponential of a row was off by up to 2^-24 of its logits: the gradient of a target with P = 0.9998 by 2 %, one
-// with P = 0.999999 by several times its value.
+// A sum of exponentials, sum * exp(top); top = -inf: of nothing.
 struct Lse {
-  float k, sum;
+  float top, sum;
   __device__ __forceinline__ void add(float2 o) {
-    const float now = fmaxf(k, o.x);
-    const float unit = now == -INFINITY ? 0.0f : now;
-    sum = sum * exp2_fast(k - unit) + o.y * exp2_fast(o.x - unit);
-    k = now;
+    const float now = fmaxf(top, o.x);
+    const float from = now == -INFINITY ? 0.0f : now;
+    sum = sum * exp_from(top, from) + o.y * exp_from(o.x, from);
+    top = now;
   }
-  __device__ __forceinline__ void add_logit(float z) {
-    const float now = fmaxf(k, exponent_above(z));
-    const float unit = now == -INFINITY ? 0.0f : now;
-    sum = sum * exp2_fast(k - unit) + exp2_fast(fmaf(z, kLog2e, -unit));
-    k = now;
-  }
+  __device__ __forceinline__ void add_logit(float z) { add(make_float2(z, 1.0f)); }
   __device__ __forceinline__ void add_warp() {     // over a warp's lanes, in a fixed order
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) add(make_float2(__shfl_xor_sync(0xffffffffu, k, o), __shfl_xor_sync(0xffffffffu, sum, o)));
+    for (int o = 16; o > 0; o >>= 1) add(make_float2(__shfl_xor_sync(0xffffffffu, top, o), __shfl_xor_sync(0xffffffffu, sum, o)));
   }
 };
 
@@ -414,7 +406,7 @@ struct Lse {
 struct Target {
   float loss, grad;         // its loss, and its entry of G
   __device__ __forceinline__ Target(const Lse& others, float z) {
-    float d = (fmaf(-z, kLog2e, others.k) + log2f(others.sum)) * kLn2;
+    float d = (others.top - z) + logf(others.sum);
     if (z == INFINITY) d = NAN;                    // as inf - inf
     const float e = expf(-fabsf(d));
     loss = fmaxf(d, 0.0f) + log1pf(e);
@@ -423,8 +415,8 @@ struct Target {
 };
 
 __device__ __forceinline__ RowNorm norm_of(const Lse& others, float z, float grad) {
-  const float k = others.k == -INFINITY ? exponent_above(z) : others.k;
-  return RowNorm{k, 1.0f / (others.sum + exp2_fast(fmaf(z, kLog2e, -k))), grad, 0.0f};
+  const float top = others.top == -INFINITY ? z : others.top;
+  return RowNorm{top, 1.0f / (others.sum + exp_from(z, top)), grad, 0.0f};
 }
 
 __device__ __forceinline__ float largest(const float (&x)[2][32]) {
@@ -457,13 +449,13 @@ __device__ __forceinline__ void take_target(float (&x)[2][32], int v, int target
   }
 }
 
-// exp(x) / 2^k in place; returns the sum.
-__device__ __forceinline__ float exponentials(float (&x)[2][32], float k) {
+// exp(x - top) 2^shift in place; returns the sum.
+__device__ __forceinline__ float exponentials(float (&x)[2][32], float top, float shift = 0.0f) {
   float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
   for (int i = 0; i < 32; i += 2) {
-    x[0][i] = exp2_fast(fmaf(x[0][i], kLog2e, -k)); x[0][i + 1] = exp2_fast(fmaf(x[0][i + 1], kLog2e, -k));
-    x[1][i] = exp2_fast(fmaf(x[1][i], kLog2e, -k)); x[1][i + 1] = exp2_fast(fmaf(x[1][i + 1], kLog2e, -k));
+    x[0][i] = exp_from(x[0][i], top, shift); x[0][i + 1] = exp_from(x[0][i + 1], top, shift);
+    x[1][i] = exp_from(x[1][i], top, shift); x[1][i + 1] = exp_from(x[1][i + 1], top, shift);
     s[0] += x[0][i]; s[1] += x[0][i + 1]; s[2] += x[1][i]; s[3] += x[1][i + 1];
   }
   return (s[0] + s[1]) + (s[2] + s[3]);
@@ -483,15 +475,15 @@ __device__ __forceinline__ void stats_epilogue(const LossParams& p, const Job& j
     float (&x)[2][32] = from.get(c, loaded);
     cut_columns(x, v0 + c, p.vocab);
     take_target(x, v0 + c, target, taken);
-    const float k = exponent_above(largest(x));
-    const float s = exponentials(x, k == -INFINITY ? 0.0f : k);    // nothing finite: exp of -inf, not of NaN
-    l.add(make_float2(k, s));
+    const float top = largest(x);
+    const float s = exponentials(x, top == -INFINITY ? 0.0f : top);    // nothing finite: exp of -inf, not of NaN
+    l.add(make_float2(top, s));
   }
-  p.part[at * p.n_parts + v0 / kCols] = make_float2(l.k, l.sum);
+  p.part[at * p.n_parts + v0 / kCols] = make_float2(l.top, l.sum);
   if (target >= v0 && target < v0 + kCols) p.z_target[at] = taken;
 }
 
-// The same, and the numerators exp(z) / 2^k (one k for the half tile's row) go to the workspace, where scale_kernel turns them
+// The same, and the numerators exp(z - maximum of the half tile's row) go to the workspace, where scale_kernel turns them
 // into G.  The sum is taken before they are rounded.
 template <int CTAS, bool SUMS>
 __device__ __forceinline__ void numerators_epilogue(const LossParams& p, const Job& j, const Source<CTAS, SUMS>& from, int row, int half,
@@ -508,7 +500,7 @@ __device__ __forceinline__ void numerators_epilogue(const LossParams& p, const J
     take_target(x, v0 + c, target, taken);
     top = fmaxf(top, largest(x));
   }
-  const float k = exponent_above(top), unit = k == -INFINITY ? 0.0f : k;
+  const float from_top = top == -INFINITY ? 0.0f : top;
   Rows rows;
   rows.base = reinterpret_cast<char*>(p.g);
   rows.offset = (((int64_t)(j.r - p.r0) * p.rows_pad + row) * p.v_pitch + v0) * 2;
@@ -520,7 +512,7 @@ __device__ __forceinline__ void numerators_epilogue(const LossParams& p, const J
     cut_columns(x, v0 + c, p.vocab);
     float again;
     take_target(x, v0 + c, target, again);
-    sum += exponentials(x, unit + kNumeratorBits);
+    sum += exponentials(x, from_top, -kNumeratorBits);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float* y = &x[i / 4][8 * (i % 4)];
@@ -529,7 +521,7 @@ __device__ __forceinline__ void numerators_epilogue(const LossParams& p, const J
     }
     write_staged(rows, staging, lane, 2 * c, 2 * kCols);
   }
-  p.part[at * p.n_parts + v0 / kCols] = make_float2(k, sum * kNumeratorUnit);
+  p.part[at * p.n_parts + v0 / kCols] = make_float2(top, sum * kNumeratorUnit);
   if (target >= v0 && target < v0 + kCols) p.z_target[at] = taken;
 }
 
@@ -550,7 +542,7 @@ __device__ __forceinline__ void probs_epilogue(const LossParams& p, const Job& j
     for (int h = 0; h < 2; ++h) {
       const int v = v0 + c + 32 * h;
 #pragma unroll
-      for (int i = 0; i < 32; ++i) x[h][i] = exp2_fast(fmaf(x[h][i], kLog2e, -norm.k)) * norm.inverse;
+      for (int i = 0; i < 32; ++i) x[h][i] = exp_from(x[h][i], norm.top) * norm.inverse;
       if ((unsigned)(target - v) < 32u) {
 #pragma unroll
         for (int i = 0; i < 32; ++i)
@@ -1130,7 +1122,7 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ LossP
 template <int CTAS>
 __global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ LossParams p) {
   constexpr int kCols = 64 * CTAS;
-  extern __shared__ float s_factor[];              // per half tile: 2^(k + 64) / the row's sum
+  extern __shared__ float s_factor[];              // per half tile: 2^64 exp(m) / the row's sum
   __shared__ Lse s_lse[8];
   let_next_start();
   wait_for_previous();
@@ -1154,10 +1146,10 @@ __global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ Loss
     __syncthreads();
     l = s_lse[0];
 #pragma unroll
-    for (int w = 1; w < 8; ++w) l.add(make_float2(s_lse[w].k, s_lse[w].sum));
+    for (int w = 1; w < 8; ++w) l.add(make_float2(s_lse[w].top, s_lse[w].sum));
     const Target own(l, picked);
     const RowNorm norm = norm_of(l, picked, own.grad);
-    for (int i = threadIdx.x; i < n; i += 256) s_factor[i] = exp2_fast(s_factor[i] - norm.k + kNumeratorBits) * norm.inverse;
+    for (int i = threadIdx.x; i < n; i += 256) s_factor[i] = exp_from(s_factor[i], norm.top, kNumeratorBits) * norm.inverse;
     if (threadIdx.x == 0) write_row(p, r, row, own.loss, token);
     __syncthreads();
 #pragma unroll 4
@@ -1289,8 +1281,8 @@ __global__ void __launch_bounds__(256, 3) few_kernel(const __grid_constant__ Los
   __syncthreads();
   if (threadIdx.x < count) {
     Lse all = s_lse[0][threadIdx.x];
-    for (int i = 1; i < 8; ++i) all.add(make_float2(s_lse[i][threadIdx.x].k, s_lse[i][threadIdx.x].sum));
-    p.part[((int64_t)r * p.rows_pad + threadIdx.x) * p.n_parts + blockIdx.x] = make_float2(all.k, all.sum);
+    for (int i = 1; i < 8; ++i) all.add(make_float2(s_lse[i][threadIdx.x].top, s_lse[i][threadIdx.x].sum));
+    p.part[((int64_t)r * p.rows_pad + threadIdx.x) * p.n_parts + blockIdx.x] = make_float2(all.top, all.sum);
   }
 }
 

@@ -177,3 +177,32 @@ def test_wide_logits_of_one_sign(dt):
     assert float(d.min()) < -15 and float(d.max()) > 15
     bound = e * -g[at, y[0].long()] + loss * (8 + d.abs()) * 2.0 ** -23         # the derivative of the loss by d is that of -G's entry
     assert ((got - loss).abs() <= bound).all(), float(((got - loss).abs() / bound).max())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [2, 20, 300])
+@pytest.mark.parametrize("power", [10, 28, 31, 60, 120])
+def test_huge_logits(T, power):
+    """Logits that are whole multiples of a large power of two: the classes of the largest share all of the probability, and the losses of
+    the others are the distances to it.  Neither is uncertain, whatever the logits' size."""
+    V, D = 300, 64
+    gen = torch.Generator().manual_seed(power)
+    w = torch.zeros((1, V, D))
+    w[0, :, 0] = torch.randint(-3, 4, (V,), generator=gen).float()
+    h = torch.zeros((1, T, D))
+    h[..., 0] = 2.0 ** power
+    y = torch.randint(0, V, (1, T), generator=gen).int().cuda()
+    top = w[0, :, 0] == 3
+    for dt in (None, "f32", "bf16"):
+        out = _run(h.bfloat16().cuda(), w.bfloat16().cuda(), y, dt)
+        n = int(top.sum())
+        steps = 3 - w[0, y[0].cpu().long(), 0].double()
+        loss = torch.where(steps > 0, steps * 2.0 ** power, 0.0) + torch.log(torch.tensor(float(n)).double())
+        got = out["token_loss"][0].double().cpu()
+        assert ((got - loss).abs() <= loss * 2.0 ** -21).all()        # ex2, log, log1p, two additions: 2^-22 and four times 2^-24
+        if dt:
+            g = top.double().repeat(T, 1) / n
+            g[torch.arange(T), y[0].cpu().long()] -= 1.0
+            ref = g.t() @ h[0].double() / T
+            bound = (g.abs().t() @ h[0].double() / T) * (2.0 ** -20 if dt == "f32" else 2.0 ** -8 + 2.0 ** -10) + ref.abs() * torch.finfo(DT[dt]).eps
+            assert ((out["d_weight"][0].double().cpu() - ref).abs() <= bound).all()
