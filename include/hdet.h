@@ -19,6 +19,7 @@
  *   hdet_step_sharded / hdet_apply_mean / hdet_apply_mean_peers / hdet_partial_layout   replica axis split over GPUs
  *   hdet_warm_init         warm noisy initialisation (Eq. 10)
  *   hdet_converge_static   allocation-free variant of hdet_converge
+ *   hdet_grad_norm / hdet_set_clip   the replicas' global gradient norms; steps with clipped gradients
  *   hdet_plan_tiles        host-only view of the work plan (tests, tools)
  *   hdet_selftest_bounded_wait   makes a kernel's bounded wait run out, to show the timeout status
  *   hdet_selftest_token_loss_wait   the same in the token loss
@@ -321,6 +322,29 @@ HDET_API int hdet_apply_mean_peers(hdet_handle h, const void* const* d_partials,
  */
 HDET_API int hdet_step_device(hdet_handle h, const void* d_step_losses, int32_t loss_dtype, void* stream,
                               int32_t* did_converge);
+
+/*
+ * hdet_grad_norm -- the replicas' global gradient norms, n_r = sqrt(sum over all tensors and elements of g_r^2), from the
+ * gradients as they lie (hdet_tensor.grad), to d_norms: DEVICE, N values of norm_dtype HDET_DTYPE_F32 or HDET_DTYPE_F64.
+ * With grad_mode HDET_GRAD_REPLICA_MEAN, or one gradient for all replicas, all N values are the one norm (of the mean).
+ * (Not in the paper.)  A handle that holds a shard of the replica axis
+ * measures its own replicas.  Squares are added in fp64 beyond 16 bytes, in a fixed order: the same bits on every run.  The handle
+ * keeps partial sums and counters, so these launches must be ordered with the handle's others.
+ * Errors: INVALID_ARG (NULL, norm_dtype), ALIGN, UNSUPPORTED (handle without tensors), CUDA.
+ */
+HDET_API int hdet_grad_norm(hdet_handle h, void* d_norms, int32_t norm_dtype, void* stream);
+
+/*
+ * hdet_set_clip -- from now on every hdet_step, hdet_step_device, hdet_step_host_grads and hdet_step_sharded first measures the norms
+ * as hdet_grad_norm does, and replica r steps with g_r min(1, max_norm / n_r).  The factor is applied in fp32 inside the
+ * update: gradients in memory stay as they are.  A norm that is not finite clips nothing; what is not finite in the gradient then
+ * reaches the parameters and the device status, as without clipping.  d_norms (DEVICE, N values of norm_dtype, or NULL) receives the
+ * norms at every step and must stay valid until clipping is set again.  max_norm = 0 ends it.  Steps that are captured
+ * into a graph keep what was set when they were captured.  hdet_step_host_grads measures each run of tensors when it has landed, but
+ * updates only behind the last.  The scalar state has no part in it: hdet_get_state and hdet_set_state leave it as it is.
+ * Errors: INVALID_ARG (max_norm negative or not finite, norm_dtype), ALIGN.
+ */
+HDET_API int hdet_set_clip(hdet_handle h, double max_norm, void* d_norms, int32_t norm_dtype);
 
 /*
  * hdet_warm_init -- warm noisy initialisation (Section 3.5, Eq. 10), to be called before the first

@@ -130,6 +130,10 @@ def _load() -> C.CDLL:
     lib.hdet_apply_mean_peers.restype = C.c_int
     lib.hdet_partial_layout.argtypes = [H, C.POINTER(C.c_int64), C.c_int64, C.POINTER(C.c_int64)]
     lib.hdet_partial_layout.restype = C.c_int
+    lib.hdet_grad_norm.argtypes = [H, C.c_void_p, C.c_int32, C.c_void_p]
+    lib.hdet_grad_norm.restype = C.c_int
+    lib.hdet_set_clip.argtypes = [H, C.c_double, C.c_void_p, C.c_int32]
+    lib.hdet_set_clip.restype = C.c_int
     lib.hdet_warm_init.argtypes = [H, C.c_double, C.c_uint64, C.c_void_p]
     lib.hdet_warm_init.restype = C.c_int
     lib.hdet_converge.argtypes = [H, C.c_void_p]
@@ -233,6 +237,7 @@ def hdet_create(cfg: hdet_config, tensors: Sequence[hdet_tensor]) -> C.c_void_p:
     h = C.c_void_p()
     status = _lib.hdet_create(C.byref(cfg), arr, len(tensors), C.byref(h))
     _check(status, None)
+    h.n_replicas = int(cfg.n_replicas)
     return h
 
 
@@ -313,6 +318,26 @@ def hdet_plan_tiles(cfg: hdet_config, tensors: Sequence[hdet_tensor]):
 def hdet_selftest_bounded_wait(h, stream: int = 0) -> None:
     """Launches a kernel whose bounded wait runs out (about a second): sets the timeout bit of the status word."""
     _check(_lib.hdet_selftest_bounded_wait(h, C.c_void_p(stream)), h)
+
+
+def _norms(h, norms):
+    """(pointer, dtype code) of a contiguous CUDA tensor of N float32 or float64 norms."""
+    if not norms.is_cuda or norms.shape != (h.n_replicas,) or not norms.is_contiguous():
+        raise ValueError("norms must be a contiguous CUDA tensor with one value per replica")
+    return norms.data_ptr(), _dtype_code[norms.dtype]
+
+
+def hdet_grad_norm(h, norms, stream: int = 0) -> None:
+    """norms [N] (CUDA, float32 or float64) = every replica's global gradient norm over the handle's tensors."""
+    ptr, code = _norms(h, norms)
+    _check(_lib.hdet_grad_norm(h, ptr, code, stream), h)
+
+
+def hdet_set_clip(h, max_norm: float, norms=None) -> None:
+    """Every step from now on clips each replica's gradient to ``max_norm`` (0: none) and leaves the norms in ``norms`` [N]
+    (CUDA, float32 or float64, kept by the caller while clipping is on), if given."""
+    ptr, code = (None, HDET_DTYPE_F32) if norms is None else _norms(h, norms)
+    _check(_lib.hdet_set_clip(h, max_norm, ptr, code), h)
 
 
 def hdet_warm_init(h, nu: float = 0.01, seed: int = 0, stream: int = 0) -> None:

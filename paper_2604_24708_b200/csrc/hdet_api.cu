@@ -1,5 +1,6 @@
 // C ABI of libhdet (see include/hdet.h): argument checks, the host-side scalar state of
 // Algorithm 1 in double precision, and the kernel launches.
+#include <algorithm>
 #include <cmath>
 #include <cstdio>
 #include <cstring>
@@ -49,6 +50,11 @@ struct hdet_ctx {
   unsigned* d_status = nullptr;
   double* d_warm = nullptr;      // scratch of hdet_warm_init (n_tiles + 1 doubles), allocated on its first call
   double total_numel = 0.0;      // d of Eq. 10
+  void* d_norm = nullptr;        // spans, partial sums, counters and factors of the gradient norms
+  NormPlan norm{};               // pointers into it
+  double max_norm = 0.0;         // hdet_set_clip; 0: gradients are not clipped
+  void* norms_out = nullptr;     // where clipped steps leave the norms, or NULL
+  bool norms_f64 = false;
   DevState* d_state = nullptr;   // device-resident scalar state (used by hdet_step_device)
   bool device_mode = false;      // the device copy of the state is the authoritative one
   int n_tiles = 0;
@@ -62,7 +68,7 @@ struct hdet_ctx {
   std::vector<hdet_tensor> tensors;      // the caller's descriptors (for hdet_step_host_grads)
   // hdet_step_host_grads uploads the gradients in a few runs of consecutive tensors on a stream of its own and
   // updates each run's tiles as soon as its copies have landed, so that copies and updates overlap.
-  struct UploadRun { int64_t first_tensor, n_tensors; int first_tile, n_tiles; };
+  struct UploadRun { int64_t first_tensor, n_tensors; int first_tile, n_tiles, first_span, n_spans; };
   std::vector<UploadRun> upload_runs;
   cudaStream_t copy_stream = nullptr;    // created by the first hdet_step_host_grads call
   cudaEvent_t upload_begin = nullptr;
@@ -107,11 +113,13 @@ void free_device(hdet_ctx* h) {
   if (h->d_status) cudaFree(h->d_status);
   if (h->d_state) cudaFree(h->d_state);
   if (h->d_warm) cudaFree(h->d_warm);
+  if (h->d_norm) cudaFree(h->d_norm);
   if (h->copy_stream) cudaStreamDestroy(h->copy_stream);
   if (h->upload_begin) cudaEventDestroy(h->upload_begin);
   for (cudaEvent_t ev : h->upload_done) cudaEventDestroy(ev);
   h->copy_stream = nullptr; h->upload_begin = nullptr; h->upload_done.clear();
   h->d_warm = nullptr;
+  h->d_norm = nullptr;
   h->d_tensors = nullptr; h->d_tiles = nullptr; h->d_status = nullptr; h->d_state = nullptr;
 }
 
@@ -214,6 +222,8 @@ DevConst device_constants(const hdet_ctx* h) {
 struct WorkPlan {
   std::vector<TensorDesc> descs;
   std::vector<Tile> tiles;
+  std::vector<GradSpan> spans;
+  bool shared_grads = true;   // every tensor has one gradient for all replicas
   int64_t n_shared_state = 0;
   int64_t partial_numel = 0;
 };
@@ -316,6 +326,9 @@ int plan_work(const hdet_config* cfg, const hdet_tensor* tensors, int64_t n_tens
     partial_numel += (t.numel + 3) / 4 * 4;
     descs.push_back(d);
     for (int64_t j = 0; j < n_tiles_t; ++j) tiles.push_back(Tile{(int)k, (int)j});
+    for (int64_t off = 0; off < t.numel; off += kSpanElems)
+      out.spans.push_back(GradSpan{off, (int)k, (int)std::min<int64_t>(kSpanElems, t.numel - off)});
+    out.shared_grads = out.shared_grads && t.grad_stride == 0;
   }
 
   if (n_shared_state != 0 && n_shared_state != n_tensors)
@@ -359,18 +372,21 @@ int hdet_create(const hdet_config* cfg, const hdet_tensor* tensors, int64_t n_te
   {   // upload runs: at most kUploadRuns runs of consecutive tensors holding about the same number of elements each
     constexpr int kUploadRuns = 8;
     const double per_run = h->total_numel / kUploadRuns;
-    hdet_ctx::UploadRun run{0, 0, 0, 0};
+    hdet_ctx::UploadRun run{};
     double in_run = 0.0;
-    int tile_cursor = 0;
+    int tile_cursor = 0, span_cursor = 0;
     for (int64_t k = 0; k < n_tensors; ++k) {
       const int n_tiles_k = (int)((tensors[k].numel + kTileElems - 1) / kTileElems);
       run.n_tensors += 1;
       run.n_tiles += n_tiles_k;
+      const int n_spans_k = (int)((tensors[k].numel + kSpanElems - 1) / kSpanElems);
+      run.n_spans += n_spans_k;
+      span_cursor += n_spans_k;
       in_run += (double)tensors[k].numel;
       tile_cursor += n_tiles_k;
       if ((in_run >= per_run && (int)h->upload_runs.size() < kUploadRuns - 1) || k == n_tensors - 1) {
         h->upload_runs.push_back(run);
-        run = hdet_ctx::UploadRun{k + 1, 0, tile_cursor, 0};
+        run = hdet_ctx::UploadRun{k + 1, 0, tile_cursor, 0, span_cursor, 0};
         in_run = 0.0;
       }
     }
@@ -391,6 +407,25 @@ int hdet_create(const hdet_config* cfg, const hdet_tensor* tensors, int64_t n_te
     if (e == cudaSuccess) e = cudaMemcpy(h->d_tensors, descs.data(), descs.size() * sizeof(TensorDesc), cudaMemcpyHostToDevice);
     if (e == cudaSuccess) e = cudaMemcpy(h->d_tiles, tiles.data(), tiles.size() * sizeof(Tile), cudaMemcpyHostToDevice);
     if (e == cudaSuccess) e = cudaMemset(h->d_status, 0, sizeof(unsigned));
+    NormPlan& m = h->norm;
+    m.tensors = h->d_tensors;
+    m.n_spans = (int)work.spans.size();
+    m.n_replicas = n;
+    m.mean = cfg->grad_mode == HDET_GRAD_REPLICA_MEAN;
+    m.rows = m.mean || work.shared_grads ? 1 : n;
+    m.grad_dtype = cfg->grad_dtype;
+    const size_t spans = sizeof(GradSpan) * (size_t)m.n_spans, sums = sizeof(double) * (size_t)m.n_spans * (size_t)m.rows;
+    const size_t words = sizeof(unsigned) * HDET_MAX_REPLICAS;
+    if (e == cudaSuccess) e = cudaMalloc(&h->d_norm, spans + sums + 2 * words);
+    if (e == cudaSuccess) {
+      char* at = static_cast<char*>(h->d_norm);
+      m.spans = reinterpret_cast<GradSpan*>(at);
+      m.partial = reinterpret_cast<double*>(at + spans);
+      m.done = reinterpret_cast<unsigned*>(at + spans + sums);
+      m.clip = reinterpret_cast<float*>(at + spans + sums + words);
+      e = cudaMemcpy(h->d_norm, work.spans.data(), spans, cudaMemcpyHostToDevice);
+    }
+    if (e == cudaSuccess) e = cudaMemset(m.done, 0, 2 * words);
     if (e == cudaSuccess)
       e = prepare_fanout(cfg->optimizer, cfg->grad_dtype, cfg->grad_mode == HDET_GRAD_REPLICA_MEAN, h->shared_state);
     if (e != cudaSuccess) {
@@ -489,6 +524,15 @@ static cudaError_t upload_gradients(hdet_ctx* h, const void* const* host_grads, 
   return cudaSuccess;
 }
 
+// With clipping on, before an update: the norms, and the factors that the update will read.
+static cudaError_t measure_for_clip(hdet_ctx* h, LaunchPlan& plan, int first_span, int n_spans, cudaStream_t st) {
+  if (h->max_norm == 0.0) return cudaSuccess;
+  plan.clip = h->norm.clip;
+  const cudaError_t e = launch_grad_norm(h->norm, first_span, n_spans, h->max_norm, h->norms_out, h->norms_f64, st);
+  if (e == cudaSuccess) ++h->launches;
+  return e;
+}
+
 // `host_grads` != NULL: the gradients are uploaded from host memory first, run by run, each run's tiles updated as
 // soon as its copies have landed (hdet_step_host_grads).
 static int step_impl(hdet_handle h, const double* step_losses, bool sharded_call, float* partial, void* stream,
@@ -532,11 +576,13 @@ static int step_impl(hdet_handle h, const double* step_losses, bool sharded_call
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool fuse = ends_round && (h->cfg.fuse_converge || partial);
     LaunchPlan plan{h->d_tensors, h->d_tiles, h->n_tiles, h->grid_fanout, h->d_status, nullptr,
-                    ends_round ? partial : nullptr};
+                    ends_round ? partial : nullptr, nullptr};
     const bool sgd_momentum = h->cfg.optimizer == HDET_OPT_SGD && h->cfg.momentum != 0.0;
     const bool grad_mean = h->cfg.grad_mode == HDET_GRAD_REPLICA_MEAN;
     cudaError_t e = cudaSuccess;
     if (!host_grads) {
+      e = measure_for_clip(h, plan, 0, h->norm.n_spans, st);
+      if (e != cudaSuccess) return fail_cuda(h, "hdet_step: norm launch", e);
       e = launch_fanout(h->cfg.optimizer, sgd_momentum, h->cfg.grad_dtype, fuse, grad_mean, h->shared_state, plan, s, st);
       if (e != cudaSuccess) return fail_cuda(h, "hdet_step: fan-out launch", e);
       ++h->launches;
@@ -561,12 +607,24 @@ static int step_impl(hdet_handle h, const double* step_losses, bool sharded_call
         if (e == cudaSuccess) e = cudaEventRecord(h->upload_done[c], h->copy_stream);
         if (e == cudaSuccess) e = cudaStreamWaitEvent(st, h->upload_done[c], 0);
         if (e != cudaSuccess) break;
+        if (h->max_norm > 0.0) {     // the update needs every gradient's part of the norm, so it follows the last run
+          e = measure_for_clip(h, plan, run.first_span, run.n_spans, st);
+          continue;
+        }
         LaunchPlan part = plan;
         part.tiles = h->d_tiles + run.first_tile;
         part.n_tiles = run.n_tiles;
         part.grid = run.n_tiles;
         e = launch_fanout(h->cfg.optimizer, sgd_momentum, h->cfg.grad_dtype, fuse, grad_mean, h->shared_state, part, s, st);
         if (e == cudaSuccess) ++h->launches;
+      }
+      if (h->max_norm > 0.0) {
+        if (e == cudaSuccess) {
+          e = launch_fanout(h->cfg.optimizer, sgd_momentum, h->cfg.grad_dtype, fuse, grad_mean, h->shared_state, plan, s, st);
+          if (e == cudaSuccess) ++h->launches;
+        } else {                     // some runs are counted, others never will be: the next pass starts from zero
+          cudaMemsetAsync(h->norm.done, 0, sizeof(unsigned) * HDET_MAX_REPLICAS, st);
+        }
       }
       if (e != cudaSuccess) return fail_cuda(h, "hdet_step_host_grads: upload and update", e);
     }
@@ -697,8 +755,10 @@ int hdet_step_device(hdet_handle h, const void* d_step_losses, int32_t loss_dtyp
   if (e != cudaSuccess) return fail_cuda(h, "hdet_step_device: scalar kernel launch", e);
   ++h->launches;
   const bool fuse = ends_round && h->cfg.fuse_converge;
-  LaunchPlan plan{h->d_tensors, h->d_tiles, h->n_tiles, h->grid_fanout, h->d_status, &h->d_state->scal, nullptr};
+  LaunchPlan plan{h->d_tensors, h->d_tiles, h->n_tiles, h->grid_fanout, h->d_status, &h->d_state->scal, nullptr, nullptr};
   const StepScalars unused{};
+  e = measure_for_clip(h, plan, 0, h->norm.n_spans, st);
+  if (e != cudaSuccess) return fail_cuda(h, "hdet_step_device: norm launch", e);
   e = launch_fanout(h->cfg.optimizer, h->cfg.optimizer == HDET_OPT_SGD && h->cfg.momentum != 0.0, h->cfg.grad_dtype, fuse,
                                   h->cfg.grad_mode == HDET_GRAD_REPLICA_MEAN,
                     h->shared_state, plan, unused, st);
@@ -722,6 +782,43 @@ int hdet_step_device(hdet_handle h, const void* d_step_losses, int32_t loss_dtyp
     if (h->sched.autolr && t >= h->sched.warmup_steps) h->fired = true;
     if (did_converge) *did_converge = 1;
   }
+  return HDET_OK;
+}
+
+// The checks that the two calls below share: where N norms go.
+static int check_norms(hdet_ctx* h, const char* who, const void* d_norms, int32_t dtype) {
+  if (dtype != HDET_DTYPE_F32 && dtype != HDET_DTYPE_F64)
+    return fail(h, HDET_ERR_INVALID_ARG, std::string(who) + ": norms must be fp32 or fp64");
+  if (!aligned(d_norms, dtype == HDET_DTYPE_F64 ? 8 : 4))
+    return fail(h, HDET_ERR_ALIGN, std::string(who) + ": d_norms is not aligned to its element type");
+  return HDET_OK;
+}
+
+int hdet_grad_norm(hdet_handle h, void* d_norms, int32_t norm_dtype, void* stream) {
+  TraceRange trace("hdet_grad_norm");
+  if (!h) return HDET_ERR_INVALID_ARG;
+  if (!d_norms) return fail(h, HDET_ERR_INVALID_ARG, "hdet_grad_norm: d_norms is NULL");
+  if (const int rc = check_norms(h, "hdet_grad_norm", d_norms, norm_dtype)) return rc;
+  if (h->n_tiles == 0) return fail(h, HDET_ERR_UNSUPPORTED, "hdet_grad_norm: the handle has no tensors, hence no device");
+  DeviceScope scope(h->cfg.device);
+  if (scope.err != cudaSuccess) return fail_cuda(h, "hdet_grad_norm", scope.err);
+  const cudaError_t e = launch_grad_norm(h->norm, 0, h->norm.n_spans, 0.0, d_norms, norm_dtype == HDET_DTYPE_F64,
+                                         static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return fail_cuda(h, "hdet_grad_norm: launch", e);
+  ++h->launches;
+  return HDET_OK;
+}
+
+int hdet_set_clip(hdet_handle h, double max_norm, void* d_norms, int32_t norm_dtype) {
+  TraceRange trace("hdet_set_clip");
+  if (!h) return HDET_ERR_INVALID_ARG;
+  if (!(max_norm >= 0.0) || !std::isfinite(max_norm))
+    return fail(h, HDET_ERR_INVALID_ARG, "hdet_set_clip: max_norm must be finite and >= 0 (0 = no clipping)");
+  if (d_norms)
+    if (const int rc = check_norms(h, "hdet_set_clip", d_norms, norm_dtype)) return rc;
+  h->max_norm = max_norm;
+  h->norms_out = max_norm > 0.0 ? d_norms : nullptr;
+  h->norms_f64 = norm_dtype == HDET_DTYPE_F64;
   return HDET_OK;
 }
 

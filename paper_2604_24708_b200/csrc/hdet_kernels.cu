@@ -26,6 +26,21 @@ struct AdamConsts {
   float one_minus_beta1, one_minus_beta2, rsqrt_bc2, eps, momentum;
 };
 
+// Clipped updates (kClip) multiply replica r's gradient by clip[r] where it is read, in fp32 and before anything else uses it: a
+// gradient that was scaled in memory would cost a pass over it, and bf16 ones a second rounding.  They are kernels of their own, so
+// that the others stay as they are (some have no register left).
+struct ClipScalars : StepScalars {
+  float clip[HDET_MAX_REPLICAS];
+};
+template <bool kClip>
+using Scalars = std::conditional_t<kClip, ClipScalars, StepScalars>;
+
+template <bool kClip>
+__device__ __forceinline__ float clipped(float g, const StepScalars& s, int r) {
+  if constexpr (kClip) return g * static_cast<const ClipScalars&>(s).clip[r];
+  else return g;
+}
+
 // Adam with decoupled weight decay on one element (Section 4.1 names Adam; weight decay is a
 // spreadable scalar per Remark 1):
 //   theta *= 1 - lr*wd ; m = b1 m + (1-b1) g ; v = b2 v + (1-b2) g^2 ;
@@ -76,7 +91,7 @@ __device__ __forceinline__ float load_scalar(const __nv_bfloat16* p) {
 }
 
 // ---- scalar path: elements [begin, end) of one tensor, any alignment -----------------------
-template <typename GradT, int kOpt, bool kConv, bool kMean>
+template <typename GradT, int kOpt, bool kConv, bool kMean, bool kClip>
 __device__ void range_scalar(const TensorDesc& td, long long begin, long long end, const StepScalars& s,
                              const AdamConsts& c, bool& bad) {
   constexpr bool kAdam = kOpt == kOptAdamW, kMom = kOpt == kOptSgdMomentum;
@@ -88,11 +103,11 @@ __device__ void range_scalar(const TensorDesc& td, long long begin, long long en
     if (kMean) {
       double acc = 0.0;
       for (int r = 0; r < n; ++r) acc += (double)load_scalar(grad + r * td.grad_stride + e);
-      gbar = (float)(acc * s.inv_n);
+      gbar = clipped<kClip>((float)(acc * s.inv_n), s, 0);      // all replicas have the same mean, norm and factor
     }
     for (int r = 0; r < n; ++r) {
       float th = __ldcs(td.param + r * td.param_stride + e);
-      const float g = kMean ? gbar : load_scalar(grad + r * td.grad_stride + e);
+      const float g = kMean ? gbar : clipped<kClip>(load_scalar(grad + r * td.grad_stride + e), s, r);
       if (kAdam) {
         float m = __ldcs(td.exp_avg + r * td.state_stride + e);
         float v = __ldcs(td.exp_avg_sq + r * td.state_stride + e);
@@ -162,7 +177,7 @@ struct ReplicaRegs {
 
 // Processes float4 vectors j = (first + k) * kThreads + threadIdx.x, k = 0..kV-1, j < nvec, of the tile that
 // starts at element `off` of the tensor.  kFull: every such j is below nvec.
-template <typename GradT, int kOpt, bool kConv, bool kMean, bool kFull, int kV>
+template <typename GradT, int kOpt, bool kConv, bool kMean, bool kClip, bool kFull, int kV>
 __device__ __forceinline__ void tile_vector_pass(const TensorDesc& td, long long off, int first, int nvec,
                                                  const StepScalars& s, const AdamConsts& c, bool& bad) {
   constexpr bool kAdam = kOpt == kOptAdamW, kMom = kOpt == kOptSgdMomentum;
@@ -206,7 +221,15 @@ __device__ __forceinline__ void tile_vector_pass(const TensorDesc& td, long long
   Regs a, b;
   load(a, 0);
   float gbar[kV][4];
-  if constexpr (kMean) mean_gradient<GradT, kV>(Gp, gs, idx, ok, n, s.inv_n, gbar);
+  if constexpr (kMean) {
+    mean_gradient<GradT, kV>(Gp, gs, idx, ok, n, s.inv_n, gbar);
+    if constexpr (kClip) {
+#pragma unroll
+      for (int k = 0; k < kV; ++k)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) gbar[k][q] = clipped<kClip>(gbar[k][q], s, 0);
+    }
+  }
 
   double sum[kConv ? kV : 1][4];
   if (kConv) {
@@ -227,6 +250,10 @@ __device__ __forceinline__ void tile_vector_pass(const TensorDesc& td, long long
         for (int q = 0; q < 4; ++q) g[q] = gbar[k][q];
       } else {
         unpack(b.g[k], g);
+        if constexpr (kClip) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) g[q] = clipped<kClip>(g[q], s, r);
+        }
       }
       float th[4] = {b.th[k].x, b.th[k].y, b.th[k].z, b.th[k].w};
       if (kAdam) {
@@ -290,14 +317,14 @@ __device__ __forceinline__ void tile_vector_pass(const TensorDesc& td, long long
 
 // The whole tile in passes of kV vectors per thread.  Two vectors per pass keep more loads in flight; the
 // kernels that also hold the bulk-copy path have fewer registers per thread and take one vector per pass.
-template <typename GradT, int kOpt, bool kConv, bool kMean, bool kFull, int kV>
+template <typename GradT, int kOpt, bool kConv, bool kMean, bool kClip, bool kFull, int kV>
 __device__ __forceinline__ void tile_vector(const TensorDesc& td, long long off, int nvec, const StepScalars& s,
                                             const AdamConsts& c, bool& bad) {
   static_assert(kTileVecs % kV == 0, "passes cover the tile");
 #pragma unroll 1
   for (int first = 0; first < kTileVecs; first += kV) {
     if (!kFull && first * kThreads >= nvec) break;
-    tile_vector_pass<GradT, kOpt, kConv, kMean, kFull, kV>(td, off, first, nvec, s, c, bad);
+    tile_vector_pass<GradT, kOpt, kConv, kMean, kClip, kFull, kV>(td, off, first, nvec, s, c, bad);
   }
 }
 
@@ -349,7 +376,7 @@ __device__ __forceinline__ void bulk_init_barriers(unsigned char* smem) {
   bulk::barrier_init_fence();
 }
 
-template <typename GradT, bool kConv, bool kMean>
+template <typename GradT, bool kConv, bool kMean, bool kClip>
 __device__ __forceinline__ void tile_bulk(const TensorDesc& td, long long off, const StepScalars& s,
                                           const AdamConsts& c, bool& bad, unsigned char* smem, unsigned* status) {
   using L = BulkLayout<GradT>;
@@ -458,7 +485,7 @@ __device__ __forceinline__ void tile_bulk(const TensorDesc& td, long long off, c
 #pragma unroll
     for (int k = 0; k < kTileVecs; ++k)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) gbar[k][q] = (float)(acc[k][q] * s.inv_n);
+      for (int q = 0; q < 4; ++q) gbar[k][q] = clipped<kClip>((float)(acc[k][q] * s.inv_n), s, 0);
   }
 
   double sum[kConv ? kTileVecs : 1][4];
@@ -488,6 +515,10 @@ __device__ __forceinline__ void tile_bulk(const TensorDesc& td, long long off, c
         for (int q = 0; q < 4; ++q) g[q] = gbar[k][q];
       } else {
         read_grad(slot + 3 * L::kF32Bytes, j, g, GradT{});
+        if constexpr (kClip) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) g[q] = clipped<kClip>(g[q], s, r);
+        }
       }
       float th[4] = {t4.x, t4.y, t4.z, t4.w};
       float m[4] = {m4.x, m4.y, m4.z, m4.w};
@@ -529,7 +560,9 @@ __device__ __forceinline__ void tile_bulk(const TensorDesc& td, long long off, c
 // or from the device-resident copy (device stepping); the update loops then read them with broadcast
 // shared-memory loads.  Selecting between the two sources by pointer instead costs 7 % of the kernel's
 // bandwidth: the by-value parameter is then no longer read through the constant bank.
-__device__ __forceinline__ void stage_scalars(StepScalars& sh, const StepScalars& s_param, const StepScalars* s_dev) {
+template <bool kClip>
+__device__ __forceinline__ void stage_scalars(Scalars<kClip>& sh, const StepScalars& s_param, const LaunchPlan& plan) {
+  const StepScalars* const s_dev = plan.scal_dev;
   static_assert(HDET_MAX_GROUPS * HDET_MAX_REPLICAS == kThreads, "one (group, replica) pair per thread");
   if (threadIdx.x < kThreads) {     // a CTA of the bulk-copy kernels has one more warp than there are pairs
     const int g = threadIdx.x / HDET_MAX_REPLICAS, r = threadIdx.x % HDET_MAX_REPLICAS;
@@ -550,25 +583,28 @@ __device__ __forceinline__ void stage_scalars(StepScalars& sh, const StepScalars
         sh.momentum = s_param.momentum;
       }
     }
+    if constexpr (kClip) {
+      if (threadIdx.x < HDET_MAX_REPLICAS) sh.clip[threadIdx.x] = plan.clip[threadIdx.x];
+    }
   }
   __syncthreads();
 }
 
 // One tile through the register path: 128-bit accesses where the tensor allows them, scalar accesses for the
 // rest (a tail of 1-3 elements, or a tensor that is not 16-byte aligned).
-template <typename GradT, int kOpt, bool kConv, bool kMean, int kV>
+template <typename GradT, int kOpt, bool kConv, bool kMean, bool kClip, int kV>
 __device__ __forceinline__ void tile_registers(const TensorDesc& td, long long off, int len, const StepScalars& s,
                                                const AdamConsts& c, bool& bad) {
   if (td.vec) {
     if (len == kTileElems) {
-      tile_vector<GradT, kOpt, kConv, kMean, true, kV>(td, off, kThreads * kTileVecs, s, c, bad);
+      tile_vector<GradT, kOpt, kConv, kMean, kClip, true, kV>(td, off, kThreads * kTileVecs, s, c, bad);
     } else {
       const int nvec = len >> 2;
-      if (nvec) tile_vector<GradT, kOpt, kConv, kMean, false, kV>(td, off, nvec, s, c, bad);
-      if (len & 3) range_scalar<GradT, kOpt, kConv, kMean>(td, off + 4ll * nvec, off + len, s, c, bad);
+      if (nvec) tile_vector<GradT, kOpt, kConv, kMean, kClip, false, kV>(td, off, nvec, s, c, bad);
+      if (len & 3) range_scalar<GradT, kOpt, kConv, kMean, kClip>(td, off + 4ll * nvec, off + len, s, c, bad);
     }
   } else {
-    range_scalar<GradT, kOpt, kConv, kMean>(td, off, off + len, s, c, bad);
+    range_scalar<GradT, kOpt, kConv, kMean, kClip>(td, off, off + len, s, c, bad);
   }
 }
 
@@ -576,11 +612,11 @@ __device__ __forceinline__ void tile_registers(const TensorDesc& td, long long o
 // serves the few tiles that path cannot take, and must not raise the register count of the common case.
 // Everything is passed and returned BY VALUE: a reference would force the caller to keep the descriptor in
 // its stack frame, and then every CTA of the common case would write it to local memory first.
-template <typename GradT, int kOpt, bool kConv, bool kMean>
+template <typename GradT, int kOpt, bool kConv, bool kMean, bool kClip>
 __device__ __noinline__ bool tile_registers_outlined(TensorDesc td, long long off, int len, const StepScalars* s,
                                                      AdamConsts c) {
   bool bad = false;
-  tile_registers<GradT, kOpt, kConv, kMean, 1>(td, off, len, *s, c, bad);
+  tile_registers<GradT, kOpt, kConv, kMean, kClip, 1>(td, off, len, *s, c, bad);
   return bad;
 }
 
@@ -590,10 +626,10 @@ __device__ __noinline__ bool tile_registers_outlined(TensorDesc td, long long of
 template <int kOpt>
 constexpr bool kHasBulkPath = kOpt == kOptAdamW;
 
-template <typename GradT, int kOpt, bool kConv, bool kMean>
+template <typename GradT, int kOpt, bool kConv, bool kMean, bool kClip>
 __global__ void __launch_bounds__(kHasBulkPath<kOpt> ? kThreads + kProducerThreads : kThreads, (kOpt == kOptSgd && !kMean) ? 3 : 2)
 fanout_kernel(const __grid_constant__ LaunchPlan plan, const __grid_constant__ StepScalars s_param) {
-  __shared__ StepScalars s;
+  __shared__ Scalars<kClip> s;
   if constexpr (kHasBulkPath<kOpt>) {
     // One tile per CTA (the barriers are set up for one tile).
     extern __shared__ __align__(128) unsigned char stage_smem[];   // BulkLayout<GradT>::kBytes
@@ -607,21 +643,21 @@ fanout_kernel(const __grid_constant__ LaunchPlan plan, const __grid_constant__ S
     }
     TensorDesc td = plan.tensors[tile.tensor];
     td.partial = plan.partial ? plan.partial + td.partial_off : nullptr;
-    stage_scalars(s, s_param, plan.scal_dev);
+    stage_scalars<kClip>(s, s_param, plan);
     if (abandoned) return;
     const AdamConsts c{s.one_minus_beta1, s.one_minus_beta2, s.rsqrt_bc2, s.eps, s.momentum};
     bool bad = false;
     const long long off = (long long)tile.tile * kTileElems;
     const long long rest = td.numel - off;
     if ((td.vec & kVecBulk) && rest >= kTileElems) {
-      tile_bulk<GradT, kConv, kMean>(td, off, s, c, bad, stage_smem, plan.status);
+      tile_bulk<GradT, kConv, kMean, kClip>(td, off, s, c, bad, stage_smem, plan.status);
     } else {
       if (threadIdx.x >= kThreads) return;     // the producer warp has no part in the register path
-      bad = tile_registers_outlined<GradT, kOpt, kConv, kMean>(td, off, rest < kTileElems ? (int)rest : kTileElems, &s, c);
+      bad = tile_registers_outlined<GradT, kOpt, kConv, kMean, kClip>(td, off, rest < kTileElems ? (int)rest : kTileElems, &s, c);
     }
     if (bad) atomicOr(plan.status, 1u);
   } else {
-    stage_scalars(s, s_param, plan.scal_dev);
+    stage_scalars<kClip>(s, s_param, plan);
     const AdamConsts c{s.one_minus_beta1, s.one_minus_beta2, s.rsqrt_bc2, s.eps, s.momentum};
     bool bad = false;
     for (int t = blockIdx.x; t < plan.n_tiles; t += gridDim.x) {
@@ -630,7 +666,7 @@ fanout_kernel(const __grid_constant__ LaunchPlan plan, const __grid_constant__ S
       td.partial = plan.partial ? plan.partial + td.partial_off : nullptr;
       const long long off = (long long)tile.tile * kTileElems;
       const long long rest = td.numel - off;
-      tile_registers<GradT, kOpt, kConv, kMean, kTileVecs>(td, off, rest < kTileElems ? (int)rest : kTileElems, s, c, bad);
+      tile_registers<GradT, kOpt, kConv, kMean, kClip, kTileVecs>(td, off, rest < kTileElems ? (int)rest : kTileElems, s, c, bad);
     }
     if (bad) atomicOr(plan.status, 1u);
   }
@@ -646,7 +682,7 @@ fanout_kernel(const __grid_constant__ LaunchPlan plan, const __grid_constant__ S
 constexpr int kChunk = 8;      // replicas of one vector whose parameters are loaded together
 constexpr int kGradChunk = 4;  // replicas whose bf16 gradients are loaded together for the mean (fp32: half)
 
-template <typename GradT, bool kConv, bool kMean>
+template <typename GradT, bool kConv, bool kMean, bool kClip>
 __device__ void range_scalar_shared(const TensorDesc& td, long long begin, long long end, const StepScalars& s,
                                     const AdamConsts& c, bool& bad) {
   const int n = s.n_replicas;
@@ -660,6 +696,7 @@ __device__ void range_scalar_shared(const TensorDesc& td, long long begin, long 
     } else {
       g = load_scalar(grad + e);
     }
+    g = clipped<kClip>(g, s, 0);      // all replicas have the same gradient, norm and factor
     float m = __ldcs(td.exp_avg + e), v = __ldcs(td.exp_avg_sq + e);
     m = fmaf(c.one_minus_beta1, g - m, m);
     v = fmaf(c.one_minus_beta2, fmaf(g, g, -v), v);
@@ -686,7 +723,7 @@ __device__ void range_scalar_shared(const TensorDesc& td, long long begin, long 
   }
 }
 
-template <typename GradT, bool kConv, bool kMean, bool kFull>
+template <typename GradT, bool kConv, bool kMean, bool kClip, bool kFull>
 __device__ __forceinline__ void tile_vector_shared(const TensorDesc& td, long long off, int nvec,
                                                    const StepScalars& s, const AdamConsts& c, bool& bad) {
   const int n = s.n_replicas;
@@ -762,6 +799,10 @@ __device__ __forceinline__ void tile_vector_shared(const TensorDesc& td, long lo
       v4 = __ldcs(reinterpret_cast<const float4*>(V + at));
       unpack(load_raw(Gp + at), g);
     }
+    if constexpr (kClip) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) g[q] = clipped<kClip>(g[q], s, 0);
+    }
 
     // Step direction u = m' / (sqrt(v')/sqrt(bc2) + eps), once per element for all replicas.
     float m[4] = {m4.x, m4.y, m4.z, m4.w};
@@ -823,11 +864,11 @@ __device__ __forceinline__ void tile_vector_shared(const TensorDesc& td, long lo
 // those two CTAs and 128 registers instead removes the spills and measured 2 - 10 % SLOWER on the 1.3 B list
 // (6.26 against 6.63 TB/s for the gradient mean with converge): the third CTA's loads in flight are worth more
 // than the few spilled values, which stay in L1.
-template <typename GradT, bool kConv, bool kMean>
+template <typename GradT, bool kConv, bool kMean, bool kClip>
 __global__ void __launch_bounds__(kThreads, 3)
 fanout_shared_kernel(const __grid_constant__ LaunchPlan plan, const __grid_constant__ StepScalars s_param) {
-  __shared__ StepScalars s;
-  stage_scalars(s, s_param, plan.scal_dev);
+  __shared__ Scalars<kClip> s;
+  stage_scalars<kClip>(s, s_param, plan);
   const AdamConsts c{s.one_minus_beta1, s.one_minus_beta2, s.rsqrt_bc2, s.eps, s.momentum};
   bool bad = false;
   for (int t = blockIdx.x; t < plan.n_tiles; t += gridDim.x) {
@@ -839,14 +880,14 @@ fanout_shared_kernel(const __grid_constant__ LaunchPlan plan, const __grid_const
     const int len = rest < kTileElems ? (int)rest : kTileElems;
     if (td.vec) {
       if (len == kTileElems) {
-        tile_vector_shared<GradT, kConv, kMean, true>(td, off, kThreads * kTileVecs, s, c, bad);
+        tile_vector_shared<GradT, kConv, kMean, kClip, true>(td, off, kThreads * kTileVecs, s, c, bad);
       } else {
         const int nvec = len >> 2;
-        if (nvec) tile_vector_shared<GradT, kConv, kMean, false>(td, off, nvec, s, c, bad);
-        if (len & 3) range_scalar_shared<GradT, kConv, kMean>(td, off + 4ll * nvec, off + len, s, c, bad);
+        if (nvec) tile_vector_shared<GradT, kConv, kMean, kClip, false>(td, off, nvec, s, c, bad);
+        if (len & 3) range_scalar_shared<GradT, kConv, kMean, kClip>(td, off + 4ll * nvec, off + len, s, c, bad);
       }
     } else {
-      range_scalar_shared<GradT, kConv, kMean>(td, off, off + len, s, c, bad);
+      range_scalar_shared<GradT, kConv, kMean, kClip>(td, off, off + len, s, c, bad);
     }
   }
   if (bad) atomicOr(plan.status, 1u);
@@ -952,66 +993,64 @@ cudaError_t opt_in_shared_memory(Kernel kernel, int bytes, bool (&opted_in)[kMax
   return cudaSuccess;
 }
 
-template <typename GradT, int kOpt, bool kConv, bool kMean>
+template <typename GradT, int kOpt, bool kConv, bool kMean, bool kClip>
 cudaError_t opt_in_one() {
   if constexpr (kHasBulkPath<kOpt>) {
     static bool opted_in[kMaxDevices] = {};
-    return opt_in_shared_memory(fanout_kernel<GradT, kOpt, kConv, kMean>, (int)BulkLayout<GradT>::kBytes, opted_in);
+    return opt_in_shared_memory(fanout_kernel<GradT, kOpt, kConv, kMean, kClip>, (int)BulkLayout<GradT>::kBytes, opted_in);
   }
   return cudaSuccess;
 }
 
-template <typename GradT, int kOpt, bool kConv, bool kMean>
+template <typename GradT, int kOpt, bool kConv, bool kMean, bool kClip>
 cudaError_t launch_one(const LaunchPlan& plan, const StepScalars& s, cudaStream_t stream) {
   if constexpr (kHasBulkPath<kOpt>) {
-    const cudaError_t e = opt_in_one<GradT, kOpt, kConv, kMean>();   // a flag check after the first time
+    const cudaError_t e = opt_in_one<GradT, kOpt, kConv, kMean, kClip>();   // a flag check after the first time
     if (e != cudaSuccess) return e;
-    fanout_kernel<GradT, kOpt, kConv, kMean>
+    fanout_kernel<GradT, kOpt, kConv, kMean, kClip>
         <<<plan.n_tiles, kThreads + kProducerThreads, BulkLayout<GradT>::kBytes, stream>>>(plan, s);
   } else {
-    fanout_kernel<GradT, kOpt, kConv, kMean><<<plan.grid, kThreads, 0, stream>>>(plan, s);
+    fanout_kernel<GradT, kOpt, kConv, kMean, kClip><<<plan.grid, kThreads, 0, stream>>>(plan, s);
   }
   return cudaGetLastError();
 }
 
-template <typename GradT, bool kConv, bool kMean>
-cudaError_t launch_shared(const LaunchPlan& plan, const StepScalars& s, cudaStream_t stream) {
-  fanout_shared_kernel<GradT, kConv, kMean><<<plan.grid, kThreads, 0, stream>>>(plan, s);
-  return cudaGetLastError();
-}
-
-template <typename GradT, bool kConv, bool kMean>
+template <typename GradT, bool kConv, bool kMean, bool kClip>
 cudaError_t pick_state(int opt, bool shared_state, const LaunchPlan& plan, const StepScalars& s, cudaStream_t st) {
-  if (opt == kOptAdamW && shared_state) return launch_shared<GradT, kConv, kMean>(plan, s, st);
-  if (opt == kOptAdamW) return launch_one<GradT, kOptAdamW, kConv, kMean>(plan, s, st);
-  if (opt == kOptSgdMomentum) return launch_one<GradT, kOptSgdMomentum, kConv, kMean>(plan, s, st);
-  return launch_one<GradT, kOptSgd, kConv, kMean>(plan, s, st);
+  if (opt == kOptAdamW && shared_state) {
+    fanout_shared_kernel<GradT, kConv, kMean, kClip><<<plan.grid, kThreads, 0, st>>>(plan, s);
+    return cudaGetLastError();
+  }
+  if (opt == kOptAdamW) return launch_one<GradT, kOptAdamW, kConv, kMean, kClip>(plan, s, st);
+  if (opt == kOptSgdMomentum) return launch_one<GradT, kOptSgdMomentum, kConv, kMean, kClip>(plan, s, st);
+  return launch_one<GradT, kOptSgd, kConv, kMean, kClip>(plan, s, st);
 }
 
-template <typename GradT>
+template <typename GradT, bool kClip>
 cudaError_t pick_flags(int opt, bool converge, bool mean, bool shared_state, const LaunchPlan& plan,
                        const StepScalars& s, cudaStream_t st) {
-  if (converge) return mean ? pick_state<GradT, true, true>(opt, shared_state, plan, s, st)
-                            : pick_state<GradT, true, false>(opt, shared_state, plan, s, st);
-  return mean ? pick_state<GradT, false, true>(opt, shared_state, plan, s, st)
-              : pick_state<GradT, false, false>(opt, shared_state, plan, s, st);
+  if (converge) return mean ? pick_state<GradT, true, true, kClip>(opt, shared_state, plan, s, st)
+                            : pick_state<GradT, true, false, kClip>(opt, shared_state, plan, s, st);
+  return mean ? pick_state<GradT, false, true, kClip>(opt, shared_state, plan, s, st)
+              : pick_state<GradT, false, false, kClip>(opt, shared_state, plan, s, st);
+}
+
+template <typename GradT, bool kClip>
+cudaError_t opt_in_adamw(bool mean) {
+  cudaError_t e = mean ? opt_in_one<GradT, kOptAdamW, true, true, kClip>() : opt_in_one<GradT, kOptAdamW, true, false, kClip>();
+  if (e == cudaSuccess)
+    e = mean ? opt_in_one<GradT, kOptAdamW, false, true, kClip>() : opt_in_one<GradT, kOptAdamW, false, false, kClip>();
+  return e;
 }
 
 }  // namespace
 
 cudaError_t prepare_fanout(int optimizer, int grad_dtype, bool grad_mean, bool shared_state) {
   if (optimizer != HDET_OPT_ADAMW || shared_state) return cudaSuccess;     // only the bulk-copy kernels need it
-  cudaError_t e;
-  if (grad_dtype == HDET_DTYPE_BF16) {
-    e = grad_mean ? opt_in_one<__nv_bfloat16, kOptAdamW, true, true>() : opt_in_one<__nv_bfloat16, kOptAdamW, true, false>();
-    if (e == cudaSuccess)
-      e = grad_mean ? opt_in_one<__nv_bfloat16, kOptAdamW, false, true>() : opt_in_one<__nv_bfloat16, kOptAdamW, false, false>();
-  } else {
-    e = grad_mean ? opt_in_one<float, kOptAdamW, true, true>() : opt_in_one<float, kOptAdamW, true, false>();
-    if (e == cudaSuccess)
-      e = grad_mean ? opt_in_one<float, kOptAdamW, false, true>() : opt_in_one<float, kOptAdamW, false, false>();
-  }
-  return e;
+  const bool bf16 = grad_dtype == HDET_DTYPE_BF16;
+  const cudaError_t e = bf16 ? opt_in_adamw<__nv_bfloat16, false>(grad_mean) : opt_in_adamw<float, false>(grad_mean);
+  if (e != cudaSuccess) return e;
+  return bf16 ? opt_in_adamw<__nv_bfloat16, true>(grad_mean) : opt_in_adamw<float, true>(grad_mean);
 }
 
 cudaError_t launch_fanout(int optimizer, bool sgd_momentum, int grad_dtype, bool converge, bool grad_mean,
@@ -1019,8 +1058,10 @@ cudaError_t launch_fanout(int optimizer, bool sgd_momentum, int grad_dtype, bool
   if (plan.n_tiles == 0) return cudaSuccess;
   const int opt = optimizer == HDET_OPT_ADAMW ? kOptAdamW : (sgd_momentum ? kOptSgdMomentum : kOptSgd);
   if (grad_dtype == HDET_DTYPE_BF16)
-    return pick_flags<__nv_bfloat16>(opt, converge, grad_mean, shared_state, plan, s, stream);
-  return pick_flags<float>(opt, converge, grad_mean, shared_state, plan, s, stream);
+    return plan.clip ? pick_flags<__nv_bfloat16, true>(opt, converge, grad_mean, shared_state, plan, s, stream)
+                     : pick_flags<__nv_bfloat16, false>(opt, converge, grad_mean, shared_state, plan, s, stream);
+  return plan.clip ? pick_flags<float, true>(opt, converge, grad_mean, shared_state, plan, s, stream)
+                   : pick_flags<float, false>(opt, converge, grad_mean, shared_state, plan, s, stream);
 }
 
 // One CTA waits, with the limit every bulk-copy wait has, on a barrier that nothing will complete, and records

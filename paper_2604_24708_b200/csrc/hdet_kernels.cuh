@@ -99,6 +99,7 @@ struct LaunchPlan {
   unsigned* status;    // device status word; bit 0 = non-finite parameter seen
   const StepScalars* scal_dev;  // device-resident launch scalars; NULL = use the by-value kernel parameter
   float* partial;      // non-NULL: a fused converge writes local replica sums here instead of the mean
+  const float* clip;   // non-NULL: factors of the replicas' gradients (HDET_MAX_REPLICAS values)
 };
 
 // Fan-out update of every replica of every tile (Eq. 2 or Adam); with `converge` the
@@ -108,6 +109,31 @@ struct LaunchPlan {
 // `sgd_momentum`: SGD keeps a momentum buffer in exp_avg.
 cudaError_t launch_fanout(int optimizer, bool sgd_momentum, int grad_dtype, bool converge, bool grad_mean,
                           bool shared_state, const LaunchPlan& plan, const StepScalars& s, cudaStream_t stream);
+
+// Consecutive elements of one tensor's gradient: the unit of work of the norm.
+struct GradSpan {
+  long long off;
+  int tensor, len;
+};
+// A span is as long as fills its CTA for ten times what starting the CTA costs, and short enough to spread a small list.
+constexpr int kSpanElems = 32768;
+
+// Sizes and device memory of a handle's norms (built once by hdet_create).
+struct NormPlan {
+  const TensorDesc* tensors;
+  const GradSpan* spans;
+  int n_spans;         // of the list
+  int n_replicas, rows;  // rows: norms that differ (1: all replicas have one gradient, or its mean)
+  bool mean;           // of the replicas' mean gradient
+  int grad_dtype;
+  double* partial;     // [rows][n_spans] sums of squares
+  unsigned* done;      // [HDET_MAX_REPLICAS] spans of the row that are done; zero between calls
+  float* clip;         // [HDET_MAX_REPLICAS]
+};
+
+// Partial sums of spans first .. first + count - 1; the launch that completes the row also writes norms (fp32 or fp64, or NULL) and,
+// with max_norm > 0, the factors min(1, max_norm / norm).  The launches of one pass cover every span once.
+cudaError_t launch_grad_norm(const NormPlan& plan, int first, int count, double max_norm, void* norms, bool norms_f64, cudaStream_t stream);
 
 // Per device, before the first launch: lets the bulk-copy kernels this handle will use take their shared-memory
 // ring (an attribute of the kernel).  Called by hdet_create so that no attribute call falls into a stream capture.
