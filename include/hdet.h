@@ -27,6 +27,8 @@
  *   hdet_embed / hdet_embed_grad   embedding lookup with scaling, and the table's gradient
  *   hdet_token_loss                softmax cross entropy against the table, one mean per replica (the losses that
  *                                  hdet_step_device reads), with the gradients of hidden states and table
+ *   hdet_token_scores / hdet_token_scores_grad   log probabilities of given tokens, entropies and the best alternatives against
+ *                                  the table, and the gradients of hidden states and table for given gradients of the first two
  *
  * Conventions
  *   - Every tensor pointer is a DEVICE pointer owned by the caller; it must stay
@@ -576,6 +578,84 @@ HDET_API int hdet_token_loss(const hdet_token_loss_args* d, void* workspace, int
  * Errors: as hdet_token_loss, plus UNSUPPORTED (no kernel of this call waits).
  */
 HDET_API int hdet_selftest_token_loss_wait(const hdet_token_loss_args* d, void* workspace, int64_t workspace_bytes, void* stream);
+
+typedef struct {
+  const void* hidden;    /* bf16 [N] x n_tokens x width                                                        */
+  const void* weight;    /* bf16 [N] x vocab x width: the table; stride 0 = one for all replicas (param_bf16)  */
+  const void* targets;   /* [N] x n_tokens, target_dtype: the given tokens; NULL = none are given (then every token counts) */
+  void* logprob;         /* fp32 [N] x n_tokens: of the given tokens, or NULL                                  */
+  void* entropy;         /* fp32 [N] x n_tokens, or NULL                                                       */
+  void* lse;             /* fp32 [N] x n_tokens: the normaliser log sum exp z, or NULL                         */
+  void* top_ids;         /* int32 [N] x n_tokens x n_top, or NULL with n_top 0                                 */
+  void* top_logprob;     /* fp32 [N] x n_tokens x n_top, or NULL                                               */
+  const void* d_logprob; /* fp32 [N] x n_tokens, or NULL (hdet_token_scores_grad only, as all that follows)    */
+  const void* d_entropy; /* fp32 [N] x n_tokens, or NULL                                                       */
+  void* d_hidden;        /* [N] x n_tokens x width, d_hidden_dtype, or NULL (rows of padding get zeros)        */
+  void* d_weight;        /* [N] x vocab x width, d_weight_dtype, or NULL                                       */
+  int64_t n_tokens;      /* tokens per replica, 0 .. HDET_MAX_TOKENS                                           */
+  int64_t vocab, width;
+  int64_t hidden_stride, hidden_row;     /* between replicas (0 = the same for all) and between tokens         */
+  int64_t weight_stride, weight_row;
+  int64_t target_stride;                 /* 0 = the same for all                                               */
+  int64_t logprob_stride, entropy_stride, lse_stride, top_ids_stride, top_logprob_stride;  /* between replicas */
+  int64_t d_logprob_stride, d_entropy_stride;
+  int64_t d_hidden_stride, d_hidden_row;
+  int64_t d_weight_stride, d_weight_row;
+  int64_t piece_bytes;   /* as in hdet_token_loss_args                                                         */
+  int32_t n_replicas;
+  int32_t n_top;         /* alternatives a token, 0 .. min(HDET_MAX_TOP, vocab)                                */
+  int32_t hidden_dtype, weight_dtype;    /* HDET_DTYPE_BF16                                                    */
+  int32_t target_dtype;  /* HDET_DTYPE_I32 or HDET_DTYPE_I64                                                   */
+  int32_t d_hidden_dtype, d_weight_dtype; /* HDET_DTYPE_F32 or HDET_DTYPE_BF16                                 */
+  int32_t accumulate;    /* != 0: d_weight is added to what is there                                           */
+  int32_t device;
+  int32_t reserved;      /* set to 0                                                                           */
+} hdet_token_scores_args;
+
+#define HDET_MAX_TOP 20
+
+/*
+ * hdet_token_scores -- what a token's hidden state says about the next one, in one pass over the table and without keeping the logits:
+ *   z = hidden[r,t] . weight[r,v],  lse = log sum_v exp z,  p = exp(z - lse),
+ *   logprob[r,t] = z_y - lse for the given token y,  entropy[r,t] = - sum_v p log p,
+ *   top_ids[r,t,:], top_logprob[r,t,:] = the n_top classes with the largest z, in falling order, and their z - lse.
+ * Logits are formed on the tensor cores (bf16 products, fp32 sums); log probabilities and entropies are sums of terms of one sign, so
+ * that those near zero keep their relative precision.  Alternatives are found by the fp32 logits, n_top and a few more; these are
+ * summed again in fp64, which decides their order and which of them stay; equal ones go by their ids.  (Values are those of the fp32 logits.)
+ * A class with the logit -inf has probability 0.  A token whose normaliser is not finite (a NaN or +inf among its logits) has NaN
+ * everywhere and -1 for its ids; the same marks all tokens if a bounded wait inside a kernel runs out.  With fewer than n_top logits
+ * above -inf the rest are -1, with a log probability of -inf.
+ * At padding (a target outside 0 .. vocab - 1) all values are 0 and all ids -1.  The same inputs give the same bits.
+ * Outputs must not overlap inputs or one another.
+ * hdet_token_scores_workspace gives the bytes that this call, and any with fewer tokens and all else the same, needs; it looks at
+ * sizes, strides, dtypes, n_top and the table's address (its alignment).
+ * Errors: INVALID_ARG (NULL, sizes, strides or dtypes out of range, n_top without top_ids or above vocab, logprob without targets, no
+ * output, workspace NULL or too small), ALIGN, UNSUPPORTED (hidden states or table not bf16; too many tiles), CUDA.
+ */
+HDET_API int hdet_token_scores_workspace(const hdet_token_scores_args* d, int64_t* bytes);
+HDET_API int hdet_token_scores(const hdet_token_scores_args* d, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * hdet_token_scores_grad -- gradients of any loss that is made of log probabilities and entropies: with a = d_logprob[r,t] and
+ * b = d_entropy[r,t] (NULL: zeros),
+ *   G = a (onehot(y) - p) - b p (log p + entropy),   d_hidden = G . weight,   d_weight = G^T . hidden.
+ * lse, and entropy with d_entropy, and logprob with targets, are READ: what hdet_token_scores left for the same hidden states, table
+ * and targets.  Without targets d_logprob has to be NULL.  The logits are formed again; G is a bf16 operand (three bf16 numbers for
+ * fp32 gradients), as in hdet_token_loss, and the rounding and overlap rules of its gradients hold.  Nothing is read at padding.
+ * If a bounded wait inside a kernel runs out, the first element of every replica's gradients is NaN and the rest undefined.
+ * hdet_token_scores_grad_workspace: as hdet_token_loss_workspace.
+ * Errors: INVALID_ARG (NULL where one is needed, no gradient asked for, sizes, strides or dtypes out of range, workspace NULL or too
+ * small), ALIGN, UNSUPPORTED, CUDA.
+ */
+HDET_API int hdet_token_scores_grad_workspace(const hdet_token_scores_args* d, int64_t* bytes);
+HDET_API int hdet_token_scores_grad(const hdet_token_scores_args* d, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * hdet_selftest_token_scores_wait -- (a diagnostic, as hdet_selftest_token_loss_wait.)  hdet_token_scores with waits of about 2 ms
+ * and copies withheld, so that the waits for them run out: every counted token's values become NaN and its ids -1.
+ * Errors: as hdet_token_scores, plus UNSUPPORTED (no kernel of this call waits).
+ */
+HDET_API int hdet_selftest_token_scores_wait(const hdet_token_scores_args* d, void* workspace, int64_t workspace_bytes, void* stream);
 
 /* hdet_last_error -- text of the last failure on h (when h is NULL: of the last failed call
  * that has no handle, hdet_create, hdet_converge_static or a call of the vocabulary ends, on this thread).  The pointer stays valid until the next call on that handle. */

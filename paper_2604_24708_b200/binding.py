@@ -90,6 +90,21 @@ class hdet_token_loss_args(C.Structure):
     ]
 
 
+class hdet_token_scores_args(C.Structure):
+    _fields_ = [
+        ("hidden", C.c_void_p), ("weight", C.c_void_p), ("targets", C.c_void_p), ("logprob", C.c_void_p), ("entropy", C.c_void_p),
+        ("lse", C.c_void_p), ("top_ids", C.c_void_p), ("top_logprob", C.c_void_p), ("d_logprob", C.c_void_p), ("d_entropy", C.c_void_p),
+        ("d_hidden", C.c_void_p), ("d_weight", C.c_void_p),
+        ("n_tokens", C.c_int64), ("vocab", C.c_int64), ("width", C.c_int64), ("hidden_stride", C.c_int64), ("hidden_row", C.c_int64),
+        ("weight_stride", C.c_int64), ("weight_row", C.c_int64), ("target_stride", C.c_int64), ("logprob_stride", C.c_int64),
+        ("entropy_stride", C.c_int64), ("lse_stride", C.c_int64), ("top_ids_stride", C.c_int64), ("top_logprob_stride", C.c_int64),
+        ("d_logprob_stride", C.c_int64), ("d_entropy_stride", C.c_int64), ("d_hidden_stride", C.c_int64), ("d_hidden_row", C.c_int64),
+        ("d_weight_stride", C.c_int64), ("d_weight_row", C.c_int64), ("piece_bytes", C.c_int64),
+        ("n_replicas", C.c_int32), ("n_top", C.c_int32), ("hidden_dtype", C.c_int32), ("weight_dtype", C.c_int32), ("target_dtype", C.c_int32),
+        ("d_hidden_dtype", C.c_int32), ("d_weight_dtype", C.c_int32), ("accumulate", C.c_int32), ("device", C.c_int32), ("reserved", C.c_int32),
+    ]
+
+
 _GD = C.c_double * HDET_MAX_GROUPS
 _ND = C.c_double * HDET_MAX_REPLICAS
 _GND = (C.c_double * HDET_MAX_REPLICAS) * HDET_MAX_GROUPS
@@ -162,7 +177,11 @@ def _load() -> C.CDLL:
     lib.hdet_embed_grad.restype = C.c_int
     lib.hdet_token_loss_workspace.argtypes = [C.c_void_p, C.POINTER(C.c_int64)]
     lib.hdet_token_loss_workspace.restype = C.c_int
-    for f in (lib.hdet_token_loss, lib.hdet_selftest_token_loss_wait):
+    for f in (lib.hdet_token_scores_workspace, lib.hdet_token_scores_grad_workspace):
+        f.argtypes = [C.c_void_p, C.POINTER(C.c_int64)]
+        f.restype = C.c_int
+    for f in (lib.hdet_token_loss, lib.hdet_selftest_token_loss_wait, lib.hdet_token_scores, lib.hdet_token_scores_grad,
+              lib.hdet_selftest_token_scores_wait):
         f.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]
         f.restype = C.c_int
     for f in ("hdet_create", "hdet_set_schedule", "hdet_step", "hdet_converge", "hdet_autolr_update",
@@ -369,6 +388,7 @@ HDET_MAX_VOCAB = 1 << 24
 HDET_MAX_WIDTH = 1 << 16
 HDET_MAX_ROW_STRIDE = 1 << 36
 HDET_MAX_REPLICA_STRIDE = 1 << 48
+HDET_MAX_TOP = 20
 
 
 class _DtypeCodes(dict):
@@ -387,10 +407,12 @@ _dtype_code = _DtypeCodes()
 
 
 # The calls below are used once per token by a model that is sampled, so their checks read every attribute once and their
-# descriptors are packed without building a ctypes struct (same layouts: hdet_embedding, hdet_token_loss_args).
+# descriptors are packed without building a ctypes struct (same layouts: hdet_embedding, hdet_token_loss_args, hdet_token_scores_args).
 _EMBEDDING = struct.Struct("@3Q8qd6i")
 _TOKEN_LOSS = struct.Struct("@7Q13qdq10i")
+_TOKEN_SCORES = struct.Struct("@12Q20q10i")
 assert _EMBEDDING.size == C.sizeof(hdet_embedding) and _TOKEN_LOSS.size == C.sizeof(hdet_token_loss_args)
+assert _TOKEN_SCORES.size == C.sizeof(hdet_token_scores_args)
 
 
 def _rows_layout(tensor, n: int, what: str):
@@ -540,6 +562,132 @@ def hdet_selftest_token_loss_wait(hidden, weight, targets, loss, workspace, d_hi
     a = _token_loss_args(hidden, weight, targets, loss, None, d_hidden, d_weight, loss.shape[0], 1.0, False, piece_bytes)
     ptr, size = _workspace(workspace, hidden.get_device())
     _check(_lib.hdet_selftest_token_loss_wait(a, ptr, size, stream), None)
+
+
+def _per_token(tensor, n: int, T: int, device: int, what: str, dtype_code: int = HDET_DTYPE_F32, read: bool = False):
+    """(address, replica stride) of one value a token: [n, T], or with ``read`` [T] for all replicas; (0, 0) for None."""
+    if tensor is None:
+        return 0, 0
+    shape = tensor.shape
+    if (shape != (n, T) and not (read and shape == (T,))) or tensor.get_device() != device or _dtype_code[tensor.dtype] != dtype_code:
+        raise ValueError(f"{what} must be {'int32' if dtype_code == HDET_DTYPE_I32 else 'float32'} [N, T] on the inputs' device")
+    return tensor.data_ptr(), _ids_stride(tensor, n, what)
+
+
+def _per_alternative(tensor, n: int, T: int, device: int, what: str, dtype_code: int):
+    """(address, replica stride) of n_top values a token, [n, T, n_top] with the last two axes contiguous; (0, 0) for None."""
+    if tensor is None:
+        return 0, 0
+    shape, stride = tensor.shape, tensor.stride()
+    if len(shape) != 3 or shape[:2] != (n, T) or tensor.get_device() != device or _dtype_code[tensor.dtype] != dtype_code:
+        raise ValueError(f"{what} must be {'int32' if dtype_code == HDET_DTYPE_I32 else 'float32'} [N, T, n_top] on the inputs' device")
+    if (shape[2] > 1 and stride[2] != 1) or (T > 1 and stride[1] != shape[2]):
+        raise ValueError(f"{what}: the last two axes must be contiguous")
+    return tensor.data_ptr(), stride[0]
+
+
+def _token_scores_args(hidden, weight, targets, n, logprob=None, entropy=None, lse=None, top_ids=None, top_logprob=None, n_top=0,
+                       d_logprob=None, d_entropy=None, d_hidden=None, d_weight=None, accumulate=False, piece_bytes=0, read=False) -> bytes:
+    T, D = hidden.shape[-2:]
+    V, width = weight.shape[-2:]
+    if width != D or (targets is not None and targets.shape[-1] != T):
+        raise ValueError("hidden, weight and targets disagree on the number of tokens or the width")
+    device = hidden.get_device()
+    if device < 0 or weight.get_device() != device or (targets is not None and targets.get_device() != device):
+        raise ValueError("all tensors must be on one CUDA device")
+    hidden_stride, hidden_row = _rows_layout(hidden, n, "hidden")
+    weight_stride, weight_row = _rows_layout(weight, n, "weight")
+    y_at = y_stride = dh_at = dh_stride = dh_code = dw_at = dw_stride = dw_code = 0
+    y_code, dh_row, dw_row = HDET_DTYPE_I32, D, D
+    if targets is not None:
+        y_at, y_stride, y_code = targets.data_ptr(), _ids_stride(targets, n, "targets"), _dtype_code[targets.dtype]
+    lp_at, lp_stride = _per_token(logprob, n, T, device, "logprob", read=read)
+    en_at, en_stride = _per_token(entropy, n, T, device, "entropy", read=read)
+    ls_at, ls_stride = _per_token(lse, n, T, device, "lse", read=read)
+    id_at, id_stride = _per_alternative(top_ids, n, T, device, "top_ids", HDET_DTYPE_I32)
+    tl_at, tl_stride = _per_alternative(top_logprob, n, T, device, "top_logprob", HDET_DTYPE_F32)
+    if top_ids is not None:
+        n_top = top_ids.shape[2]
+        if top_logprob is not None and top_logprob.shape[2] != n_top:
+            raise ValueError("top_ids and top_logprob disagree on the number of alternatives")
+    dl_at, dl_stride = _per_token(d_logprob, n, T, device, "d_logprob", read=True)
+    de_at, de_stride = _per_token(d_entropy, n, T, device, "d_entropy", read=True)
+    if d_hidden is not None:
+        if d_hidden.shape != (n, T, D) or d_hidden.get_device() != device:
+            raise ValueError("d_hidden must be [N, T, D] on the inputs' device")
+        dh_at, dh_code = d_hidden.data_ptr(), _dtype_code[d_hidden.dtype]
+        dh_stride, dh_row = _rows_layout(d_hidden, n, "d_hidden")
+    if d_weight is not None:
+        if d_weight.shape != (n, V, D) or d_weight.get_device() != device:
+            raise ValueError("d_weight must be [N, V, D] on the inputs' device")
+        dw_at, dw_code = d_weight.data_ptr(), _dtype_code[d_weight.dtype]
+        dw_stride, dw_row = _rows_layout(d_weight, n, "d_weight")
+    return _TOKEN_SCORES.pack(
+        hidden.data_ptr(), weight.data_ptr(), y_at, lp_at, en_at, ls_at, id_at, tl_at, dl_at, de_at, dh_at, dw_at, T, V, D,
+        hidden_stride, hidden_row, weight_stride, weight_row, y_stride, lp_stride, en_stride, ls_stride, id_stride, tl_stride, dl_stride,
+        de_stride, dh_stride, dh_row, dw_stride, dw_row, piece_bytes, n, n_top, _dtype_code[hidden.dtype], _dtype_code[weight.dtype], y_code,
+        dh_code, dw_code, 1 if accumulate else 0, device, 0)
+
+
+def _scores_replicas(hidden, weight, targets, *outputs) -> int:
+    for t in outputs:
+        if t is not None:
+            return t.shape[0]
+    return _replicas((hidden, 2), (weight, 2), (targets, 1))
+
+
+def hdet_token_scores_workspace(hidden, weight, targets=None, n_top: int = 0) -> int:
+    """Bytes of workspace that hdet_token_scores needs for these tensors and ``n_top`` alternatives a token."""
+    a = _token_scores_args(hidden, weight, targets, _scores_replicas(hidden, weight, targets), n_top=n_top)
+    need = C.c_int64(0)
+    _check(_lib.hdet_token_scores_workspace(a, C.byref(need)), None)
+    return int(need.value)
+
+
+def hdet_token_scores(hidden, weight, targets, workspace, logprob=None, entropy=None, lse=None, top_ids=None, top_logprob=None,
+                      stream: int = 0) -> None:
+    """Of hidden [N, T, D] (or [T, D] for all replicas) against the table weight [N, V, D] (or [V, D]), both bf16, whichever is given:
+    ``logprob`` of the tokens in targets [N, T] (or [T]; int32 or int64; outside 0 .. V-1: padding), ``entropy`` and ``lse`` (log sum
+    exp), each float32 [N, T], and the best alternatives, ``top_ids`` (int32) and ``top_logprob`` (float32) [N, T, n_top].
+    Without targets (None) every token counts."""
+    n = _scores_replicas(hidden, weight, targets, logprob, entropy, lse, top_ids)
+    a = _token_scores_args(hidden, weight, targets, n, logprob, entropy, lse, top_ids, top_logprob)
+    ptr, size = _workspace(workspace, hidden.get_device())
+    status = _lib.hdet_token_scores(a, ptr, size, stream)
+    if status:
+        _check(status, None)
+
+
+def hdet_selftest_token_scores_wait(hidden, weight, targets, workspace, logprob=None, entropy=None, lse=None, top_ids=None, top_logprob=None,
+                                    stream: int = 0) -> None:
+    """hdet_token_scores whose kernels' waits run out after some milliseconds: every counted token has NaN, and -1 for its ids."""
+    n = _scores_replicas(hidden, weight, targets, logprob, entropy, lse, top_ids)
+    a = _token_scores_args(hidden, weight, targets, n, logprob, entropy, lse, top_ids, top_logprob)
+    ptr, size = _workspace(workspace, hidden.get_device())
+    _check(_lib.hdet_selftest_token_scores_wait(a, ptr, size, stream), None)
+
+
+def hdet_token_scores_grad_workspace(hidden, weight, targets=None, d_hidden=None, d_weight=None, piece_bytes: int = 0) -> int:
+    """Bytes of workspace that hdet_token_scores_grad needs for these tensors and gradients."""
+    n = _scores_replicas(hidden, weight, targets, d_hidden, d_weight)
+    a = _token_scores_args(hidden, weight, targets, n, d_hidden=d_hidden, d_weight=d_weight, piece_bytes=piece_bytes)
+    need = C.c_int64(0)
+    _check(_lib.hdet_token_scores_grad_workspace(a, C.byref(need)), None)
+    return int(need.value)
+
+
+def hdet_token_scores_grad(hidden, weight, targets, workspace, lse, logprob=None, entropy=None, d_logprob=None, d_entropy=None,
+                           d_hidden=None, d_weight=None, accumulate: bool = False, piece_bytes: int = 0, stream: int = 0) -> None:
+    """Gradients of a loss of log probabilities and entropies: given d_logprob and / or d_entropy (float32 [N, T] or [T]) and what
+    hdet_token_scores left (``lse``; ``logprob`` with targets; ``entropy`` with d_entropy), writes ``d_hidden`` [N, T, D] and / or
+    ``d_weight`` [N, V, D] (float32 or bfloat16; ``accumulate`` adds d_weight to what is there)."""
+    n = _scores_replicas(hidden, weight, targets, d_hidden, d_weight)
+    a = _token_scores_args(hidden, weight, targets, n, logprob, entropy, lse, d_logprob=d_logprob, d_entropy=d_entropy, d_hidden=d_hidden,
+                           d_weight=d_weight, accumulate=accumulate, piece_bytes=piece_bytes, read=True)
+    ptr, size = _workspace(workspace, hidden.get_device())
+    status = _lib.hdet_token_scores_grad(a, ptr, size, stream)
+    if status:
+        _check(status, None)
 
 
 def _workspace(workspace, device: int):

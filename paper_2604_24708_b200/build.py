@@ -11,8 +11,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB_DIR = os.path.join(HERE, "lib")
 LIB_PATH = os.path.join(LIB_DIR, "libhdet.so")
 SOURCES = ["hdet_api.cu", "hdet_kernels.cu", "hdet_device_state.cu", "hdet_noalloc.cu", "hdet_warm.cu",
-           "hdet_embed.cu", "hdet_token_loss.cu", "hdet_grad_norm.cu"]
-HEADERS = ["hdet_kernels.cuh", "hdet_device_state.cuh", "hdet_scalars.h", "hdet_internal.h", "hdet_bulk.cuh", "hdet_umma.cuh", "hdet_launch.cuh",
+           "hdet_embed.cu", "hdet_token_loss.cu", "hdet_token_scores.cu", "hdet_grad_norm.cu"]
+HEADERS = ["hdet_kernels.cuh", "hdet_device_state.cuh", "hdet_scalars.h", "hdet_internal.h", "hdet_bulk.cuh", "hdet_umma.cuh", "hdet_launch.cuh", "hdet_vocab.cuh",
            os.path.join("..", "..", "include", "hdet.h")]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

@@ -3,6 +3,8 @@
 
 #include <nvtx3/nvToolsExt.h>
 
+#include "../../include/hdet.h"
+
 namespace hdet {
 
 // A named NVTX range around one C-ABI call, so that a timeline tool shows where the library's host time
@@ -16,5 +18,9 @@ struct TraceRange {
 
 // Stores the text that hdet_last_error(NULL) returns on the calling thread.
 void set_handleless_error(const char* msg);
+
+// The checks of hdet_token_scores and, with `gradient`, hdet_token_scores_grad: sizes, strides and dtypes; pointers.
+int check_token_scores(const char* who, const hdet_token_scores_args* d, bool gradient);
+int check_token_scores_pointers(const char* who, const hdet_token_scores_args* d, bool gradient);
 
 }  // namespace hdet

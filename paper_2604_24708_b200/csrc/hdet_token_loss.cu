@@ -27,28 +27,14 @@
 // G is the operand of a bf16 product, so it is rounded to bf16, unscaled, as the last step of its own.  Its relative error, 2^-8 of a
 // value at most, is that of a bf16 gradient's own rounding.  For fp32 gradients that would be too coarse: G is written as the sum of
 // three bf16 numbers (24 bits; two would leave up to 2^-16 of a value, 1.3e-6 of a gradient's norm), and the products run over all three.
-#include <cuda_bf16.h>
-
 #include <algorithm>
 #include <climits>
-#include <cmath>
-#include <cstdio>
-#include <mutex>
 
-#include "../../include/hdet.h"
-#include "hdet_internal.h"
-#include "hdet_launch.cuh"
-#include "hdet_umma.cuh"
+#include "hdet_vocab.cuh"
 
+namespace hdet {
 namespace {
 
-using namespace hdet::umma;
-using hdet::launch;
-using hdet::let_next_start;
-using hdet::wait_for_previous;
-namespace bulk = hdet::bulk;
-
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kStages = 6;
 constexpr int kStageBytes = 2 * kOperandBytes;
 // warp 0 copies, warp 1 issues the products, warp 2 hands out tiles, warps 4 - 11 read the accumulator: a quarter of its
@@ -57,30 +43,9 @@ constexpr int kGemmThreads = 384, kFirstReader = 4, kReaders = 8;
 constexpr int kStagingBytes = 4096;        // per reader: 32 rows x 128 bytes
 constexpr int kAskAhead = 8;               // steps before a tile's end at which its successor is looked up
 constexpr int kTileSlots = 4;              // tiles under way between the copies and the readers
-constexpr long long kDrainCycles = 20000000ll;          // 10 ms: thousands of times what a copy or a product takes
 constexpr long long kSelftestLimitCycles = 4000000ll;   // 2 ms
 
-__host__ __device__ constexpr int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
-__host__ __device__ constexpr int64_t round_up(int64_t a, int64_t b) { return div_up(a, b) * b; }
-
-enum Phase { kStats, kNumerators, kProbs, kGrads };
-
-struct Control {            // first bytes of the workspace; zeroed by pack_kernel
-  unsigned status;          // a bounded wait ran out
-  unsigned ticket;          // tiles handed out by all product kernels of the call so far
-  unsigned done[HDET_MAX_REPLICAS];   // blocks of join_kernel that have finished
-};
-
-struct Out {                // a gradient
-  void* p;
-  int64_t stride, row;
-  int f32, accumulate, vec; // vec: rows start and end on 16-byte boundaries
-};
-
-// What turns a row's logits into G: inverse * exp(z - top), and the target's own value.
-struct alignas(16) RowNorm {
-  float top, inverse, target, pad;
-};
+enum Phase { kStats, kNumerators, kProbs, kGrads, kGiven };
 
 struct LossParams {
   CUtensorMap hidden, weight, grad;
@@ -89,6 +54,7 @@ struct LossParams {
   int rows_pad;             // rows per replica of everything packed
   bool weight_shared;
   double grad_scale;
+  bool of_mean;             // the gradients are those of a mean over the counted tokens
   // packed inputs and per-row values [replica][rows_pad]
   const int* count;
   const int* target;
@@ -124,6 +90,7 @@ struct LossParams {
 };
 
 __device__ __forceinline__ void poison_loss(const LossParams& p) {
+  if (!p.loss) return;
   for (int r = 0; r < p.n_replicas; ++r) {
     if (p.loss_f64) static_cast<double*>(p.loss)[r] = NAN; else static_cast<float*>(p.loss)[r] = NAN;
   }
@@ -141,10 +108,6 @@ struct Job {
   int pad;
 };
 static_assert(sizeof(Job) == 64, "four stores of 16 bytes");
-
-// Boxes per CTA for a tile with `left` columns from its first to the end.
-template <int CTAS>
-__device__ __forceinline__ int boxes_for(int left) { return left > 64 * CTAS ? 2 : 1; }
 
 template <int CTAS, int PHASE>
 __device__ __forceinline__ bool find_job(const LossParams& p, const int* counts, int tile, Job& j) {
@@ -320,72 +283,6 @@ __device__ __forceinline__ void write_elements(const Rows& rows, uint32_t at, in
   __syncwarp();
 }
 
-template <int CTAS>
-struct Columns {            // of one row: half of a tile's columns
-  float x[CTAS][2][32];
-};
-template <>
-struct Columns<0> {};
-
-template <int CTAS>
-__device__ __forceinline__ void clear(Columns<CTAS>& acc) {
-#pragma unroll
-  for (int i = 0; i < 64 * CTAS; ++i) acc.x[i / 64][i / 32 % 2][i % 32] = 0.0f;
-}
-
-// The accumulator's columns from `tmem` on, in the place of what acc holds, or added to it.
-template <int CTAS>
-__device__ __forceinline__ void take_columns(uint32_t tmem, Columns<CTAS>& acc, bool add) {
-  __syncwarp();
-  if (!add) {
-#pragma unroll
-    for (int i = 0; i < 2 * CTAS; ++i) tmem_load32(tmem + 32 * i, acc.x[i / 2][i % 2]);
-#pragma unroll
-    for (int i = 0; i < 2 * CTAS; ++i) tmem_load_wait(acc.x[i / 2][i % 2]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4 * CTAS; ++i) {
-      float x[16];
-      tmem_load16(tmem + 16 * i, x);
-      tmem_load_wait(x);
-#pragma unroll
-      for (int k = 0; k < 16; ++k) acc.x[i / 4][i / 2 % 2][16 * (i % 2) + k] += x[k];
-    }
-  }
-}
-
-// Where an epilogue finds its columns: in the accumulator (SUMS false: one chunk, read 64 columns at a time, which leaves the
-// kernel's registers to the loads), or in registers.
-template <int CTAS, bool SUMS>
-struct Source {
-  uint32_t tmem;            // the reader's lanes, at the first column of its half
-  Columns<CTAS>* acc;
-  bool empty;               // nothing was summed
-  // Columns c .. c + 63: those in registers themselves, or `x` with what the accumulator holds.
-  __device__ __forceinline__ float (&get(int c, float (&x)[2][32]) const)[2][32] {
-    if constexpr (SUMS) {
-      return acc->x[c / 64];
-    } else {
-      if (empty) {
-#pragma unroll
-        for (int i = 0; i < 64; ++i) x[i / 32][i % 32] = 0.0f;
-      } else {
-        __syncwarp();
-        tmem_load32(tmem + c, x[0]);
-        tmem_load32(tmem + c + 32, x[1]);
-        tmem_load_wait(x[0]);
-        tmem_load_wait(x[1]);
-      }
-      return x;
-    }
-  }
-};
-
-// exp(x - top) 2^shift.  The subtraction comes first: x log2(e) - top log2(e) in one fma, with the second product rounded, is off by up to
-// 2^-24 of the logits themselves, all of a row by the same factor: the gradient of a target with P = 0.9998 was 2 % off for it, one with
-// P = 0.999999 by several times its value.
-__device__ __forceinline__ float exp_from(float x, float top, float shift = 0.0f) { return exp2_fast(fmaf(x - top, kLog2e, shift)); }
-
 // A sum of exponentials, sum * exp(top); top = -inf: of nothing.
 struct Lse {
   float top, sum;
@@ -417,26 +314,6 @@ struct Target {
 __device__ __forceinline__ RowNorm norm_of(const Lse& others, float z, float grad) {
   const float top = others.top == -INFINITY ? z : others.top;
   return RowNorm{top, 1.0f / (others.sum + exp_from(z, top)), grad, 0.0f};
-}
-
-__device__ __forceinline__ float largest(const float (&x)[2][32]) {
-  float top[4] = {x[0][0], x[0][1], x[1][0], x[1][1]};
-#pragma unroll
-  for (int i = 2; i < 32; i += 2) {
-    top[0] = fmaxf(top[0], x[0][i]); top[1] = fmaxf(top[1], x[0][i + 1]);
-    top[2] = fmaxf(top[2], x[1][i]); top[3] = fmaxf(top[3], x[1][i + 1]);
-  }
-  return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-}
-
-// Columns at or behind the vocabulary's end become -inf (nothing of theirs is left in exp).
-__device__ __forceinline__ void cut_columns(float (&x)[2][32], int v, int vocab) {
-  if (v + 64 <= vocab) return;
-#pragma unroll
-  for (int i = 0; i < 32; ++i) {
-    if (v + i >= vocab) x[0][i] = -INFINITY;
-    if (v + 32 + i >= vocab) x[1][i] = -INFINITY;
-  }
 }
 
 // Takes the target's logit out, -inf in its place.
@@ -525,7 +402,8 @@ __device__ __forceinline__ void numerators_epilogue(const LossParams& p, const J
   if (target >= v0 && target < v0 + kCols) p.z_target[at] = taken;
 }
 
-template <int CTAS, bool SUMS>
+// kGiven: G from given gradients of log probabilities and entropies in place of the loss's.
+template <int CTAS, int PHASE, bool SUMS>
 __device__ __forceinline__ void probs_epilogue(const LossParams& p, const Job& j, const Source<CTAS, SUMS>& from, int row, int half, bool counted,
                                                int target, const RowNorm& norm, uint32_t staging, int lane) {
   constexpr int kCols = 64 * CTAS;
@@ -542,7 +420,14 @@ __device__ __forceinline__ void probs_epilogue(const LossParams& p, const Job& j
     for (int h = 0; h < 2; ++h) {
       const int v = v0 + c + 32 * h;
 #pragma unroll
-      for (int i = 0; i < 32; ++i) x[h][i] = exp_from(x[h][i], norm.top) * norm.inverse;
+      for (int i = 0; i < 32; ++i) {
+        if constexpr (PHASE == kGiven) {           // a logit of -inf: 0, not NaN; one that is NaN stays so
+          const float d = x[h][i] - norm.top;
+          x[h][i] = -exp2_fast(d * kLog2e) * fmaf(norm.slope, fmaxf(d, -1e4f), norm.inverse);
+        } else {
+          x[h][i] = exp_from(x[h][i], norm.top) * norm.inverse;
+        }
+      }
       if ((unsigned)(target - v) < 32u) {
 #pragma unroll
         for (int i = 0; i < 32; ++i)
@@ -580,7 +465,7 @@ __device__ __forceinline__ void grads_epilogue(const LossParams& p, const Job& j
   constexpr int kCols = 64 * CTAS;
   Out o;
   int64_t base;
-  float scale = (float)(p.grad_scale / (double)(count > 0 ? count : 1));
+  float scale = (float)(p.grad_scale / (double)(p.of_mean && count > 0 ? count : 1));
   bool on;
   if (j.is_dw) {
     o = p.d_weight;
@@ -875,7 +760,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
       RowNorm norm{INFINITY, 0.0f, 0.0f, 0.0f};
       if constexpr (PHASE != kGrads) {
         target = p.target[(int64_t)j.r * p.rows_pad + row];
-        if (PHASE == kProbs && row < sh.count[j.r]) norm = p.norm[(int64_t)j.r * p.rows_pad + row];
+        if ((PHASE == kProbs || PHASE == kGiven) && row < sh.count[j.r]) norm = p.norm[(int64_t)j.r * p.rows_pad + row];
       }
       Columns<SUMS ? CTAS : 0> acc;
       if constexpr (SUMS) {
@@ -908,7 +793,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
       if constexpr (SUMS) from.acc = &acc;
       if constexpr (PHASE == kStats) stats_epilogue(p, j, from, row, half, target);
       else if constexpr (PHASE == kNumerators) numerators_epilogue(p, j, from, row, half, target, staging, lane);
-      else if constexpr (PHASE == kProbs) probs_epilogue(p, j, from, row, half, row < sh.count[j.r], target, norm, staging, lane);
+      else if constexpr (PHASE == kProbs || PHASE == kGiven)
+        probs_epilogue<CTAS, PHASE>(p, j, from, row, half, row < sh.count[j.r], target, norm, staging, lane);
       else grads_epilogue(p, j, from, row, half, sh.count[j.r], staging, lane);
       if constexpr (!SUMS) {
         if (j.k_blocks > 0) acc_done();
@@ -929,133 +815,6 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
   if constexpr (CTAS == 2) cluster_sync();       // neither CTA leaves while the other may still reach into it
   fence_after_sync();
   if (warp == 1) tmem_free<CTAS>(tmem, 2 * 128 * CTAS);
-}
-
-// ------------------------------------------------------------------------------------------------ packing
-struct PackParams {
-  const __nv_bfloat16* hidden;
-  int64_t hidden_stride, hidden_row;
-  const void* targets;
-  int64_t target_stride;
-  bool wide, hidden_vec, d_hidden_vec;
-  int n_tokens, vocab, width, rows_pad, row_tile, packed_row;
-  __nv_bfloat16* packed;
-  int *count, *target, *token_of;
-  float* token_loss;
-  int64_t token_loss_stride;
-  Out d_hidden;             // p NULL: none
-  Control* control;
-};
-
-constexpr int kPackBlocks = 256;   // blocks per replica, about: more would count the targets too often
-
-// The target of a token, -1 for padding.
-__device__ __forceinline__ int target_of(const PackParams& p, int r, int t) {
-  const int64_t at = r * p.target_stride + t;
-  if (p.wide) {
-    const long long v = static_cast<const long long*>(p.targets)[at];
-    return v >= 0 && v < p.vocab ? (int)v : -1;
-  }
-  const int v = static_cast<const int*>(p.targets)[at];
-  return v >= 0 && v < p.vocab ? v : -1;
-}
-
-// Moves the hidden states of counted tokens together, `rows` tokens a block (a multiple of 8: one a warp at a time).  Every
-// block counts the targets before its own (and all of them) itself: that is 4 bytes a token from L2 instead of a launch of its
-// own for the offsets.
-__global__ void __launch_bounds__(256) pack_kernel(const PackParams p, int rows) {
-  __shared__ int s_before[8], s_all[8];
-  const int r = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int t0 = (int)blockIdx.x * rows, t1 = min(t0 + rows, p.n_tokens);
-  let_next_start();
-  wait_for_previous();
-  if (blockIdx.x == 0 && threadIdx.x == 0) {
-    p.control->done[r] = 0;
-    if (r == 0) p.control->status = p.control->ticket = 0;
-  }
-  int before = 0, all = 0;
-#pragma unroll 4
-  for (int t = threadIdx.x; t < p.n_tokens; t += 256) {
-    const int one = target_of(p, r, t) >= 0;
-    all += one;
-    before += t < t0 ? one : 0;
-  }
-  before = __reduce_add_sync(0xffffffffu, before);
-  all = __reduce_add_sync(0xffffffffu, all);
-  if (lane == 0) { s_before[warp] = before; s_all[warp] = all; }
-  __syncthreads();
-  before = all = 0;
-#pragma unroll
-  for (int w = 0; w < 8; ++w) { before += s_before[w]; all += s_all[w]; }
-  const int64_t base = (int64_t)r * p.rows_pad;
-  if (blockIdx.x == 0 && threadIdx.x == 0) p.count[r] = all;
-  // 32 tokens at a time: every warp finds out where they go, and moves every eighth
-  for (int first = t0; first < t1; first += 32) {
-    const int mine = first + lane;
-    const int y = mine < t1 ? target_of(p, r, mine) : -1;
-    const unsigned counted = __ballot_sync(0xffffffffu, y >= 0);
-    const int place = before + __popc(counted & ((1u << lane) - 1));
-    before += __popc(counted);
-    if (warp == 0 && mine < t1) {
-      if (y >= 0) {
-        p.target[base + place] = y;
-        p.token_of[base + place] = mine;
-      } else if (p.token_loss) {
-        p.token_loss[r * p.token_loss_stride + mine] = 0.0f;
-      }
-    }
-    for (int i = warp; i < 32 && first + i < t1; i += 8) {
-      const int to = __shfl_sync(0xffffffffu, place, i);
-      const int64_t t = first + i;
-      if (counted >> i & 1) {
-        const __nv_bfloat16* from = p.hidden + r * p.hidden_stride + t * p.hidden_row;
-        __nv_bfloat16* dst = p.packed + (base + to) * p.packed_row;
-        if (p.hidden_vec) {
-#pragma unroll 4
-          for (int c = lane * 8; c < p.width; c += 256)
-            *reinterpret_cast<uint4*>(dst + c) = *reinterpret_cast<const uint4*>(from + c);
-        } else {
-#pragma unroll 4
-          for (int c = lane; c < p.width; c += 32) dst[c] = from[c];
-        }
-      } else if (p.d_hidden.p) {
-        const int64_t at = r * p.d_hidden.stride + t * p.d_hidden.row;
-        const int size = p.d_hidden.f32 ? 4 : 2;
-        char* dst = static_cast<char*>(p.d_hidden.p) + at * size;
-        if (p.d_hidden_vec) {
-          for (int b = lane * 16; b < p.width * size; b += 512) *reinterpret_cast<uint4*>(dst + b) = make_uint4(0, 0, 0, 0);
-        } else {
-          for (int c = lane; c < p.width; c += 32) {
-            if (p.d_hidden.f32) reinterpret_cast<float*>(dst)[c] = 0.0f;
-            else reinterpret_cast<__nv_bfloat16*>(dst)[c] = __float2bfloat16_rn(0.0f);
-          }
-        }
-      }
-    }
-  }
-  // rows behind the last counted token, up to the tile's end: zeros, since a product sums over them
-  const int end = min(p.rows_pad, (all + p.row_tile - 1) / p.row_tile * p.row_tile);
-  for (int row = all + (int)blockIdx.x * 8 + warp; row < end; row += (int)gridDim.x * 8) {
-    if (lane == 0) { p.target[base + row] = -1; p.token_of[base + row] = 0; }
-    __nv_bfloat16* dst = p.packed + (base + row) * p.packed_row;
-    for (int c = lane * 8; c < p.packed_row; c += 256) *reinterpret_cast<uint4*>(dst + c) = make_uint4(0, 0, 0, 0);
-  }
-}
-
-// A table whose rows cannot be copied as boxes (odd width, stride or address) is laid out once in the workspace, in accesses
-// of the largest T that its rows start and end on.  14 tables of 20474 x 996 (8-byte accesses) take 320 us, of 20474 x 997
-// (2-byte ones) 460: a width that is a multiple of 8 needs none of it.
-template <typename T>
-__global__ void __launch_bounds__(256) pack_table_kernel(const __nv_bfloat16* table, int64_t stride, int64_t row, int vocab,
-                                                         int width, int packed_row, __nv_bfloat16* packed) {
-  const int v = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-  let_next_start();
-  wait_for_previous();
-  if (v >= vocab) return;
-  const T* from = reinterpret_cast<const T*>(table + blockIdx.y * stride + v * row);
-  T* to = reinterpret_cast<T*>(packed + ((int64_t)blockIdx.y * vocab + v) * packed_row);
-#pragma unroll 8
-  for (int c = lane; c < width / (int)(sizeof(T) / 2); c += 32) to[c] = from[c];
 }
 
 // ------------------------------------------------------------------------------------------------ joining
@@ -1328,7 +1087,7 @@ __global__ void __launch_bounds__(256) join_hidden_kernel(const __grid_constant_
   const int g = blockIdx.y, r = p.r0 + g, row = blockIdx.x;
   const int count = p.count[r];
   if (row >= count) return;
-  const float scale = (float)(p.grad_scale / (double)count);
+  const float scale = (float)(p.grad_scale / (double)(p.of_mean ? count : 1));
   const Out o = p.d_hidden;
   const int64_t to = r * o.stride + (int64_t)p.token_of[(int64_t)r * p.rows_pad + row] * o.row;
   for (int c = threadIdx.x; c < p.width; c += 256) {
@@ -1340,24 +1099,20 @@ __global__ void __launch_bounds__(256) join_hidden_kernel(const __grid_constant_
   }
 }
 
+// After the gradients for given ones, which have no losses that could tell: if a wait ran out, the gradients' first elements do.
+__global__ void __launch_bounds__(32) poison_grads_kernel(const __grid_constant__ LossParams p) {
+  wait_for_previous();
+  if (!p.control->status || threadIdx.x >= p.n_replicas) return;
+  const auto poison = [&](const Out& o) {
+    if (!o.p) return;
+    if (o.f32) static_cast<float*>(o.p)[threadIdx.x * o.stride] = NAN;
+    else static_cast<__nv_bfloat16*>(o.p)[threadIdx.x * o.stride] = __float2bfloat16_rn(NAN);
+  };
+  if (p.n_tokens > 0) poison(p.d_hidden);
+  poison(p.d_weight);
+}
+
 // ------------------------------------------------------------------------------------------------ host side
-int fail(int code, const char* who, const char* what) {
-  char msg[240];
-  snprintf(msg, sizeof msg, "%s: %s", who, what);
-  hdet::set_handleless_error(msg);
-  return code;
-}
-
-// The call's own error, which does not stay behind for whoever asks the runtime for its last one next.
-int fail_cuda(const char* who, cudaError_t e) {
-  cudaGetLastError();
-  return fail(HDET_ERR_CUDA, who, cudaGetErrorString(e));
-}
-
-bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
-int elem_size(int dtype) { return dtype == HDET_DTYPE_BF16 ? 2 : 4; }
-bool is_float(int dtype) { return dtype == HDET_DTYPE_F32 || dtype == HDET_DTYPE_BF16; }
-
 int check(const char* who, const hdet_token_loss_args* d) {
   if (!d) return fail(HDET_ERR_INVALID_ARG, who, "the descriptor is NULL");
   if (d->n_replicas < 1 || d->n_replicas > HDET_MAX_REPLICAS)
@@ -1452,7 +1207,8 @@ struct Plan {
       off_slabs, total;
 };
 
-Plan plan_of(const hdet_token_loss_args* d) {
+// `given`: G comes from given gradients; there are no losses and nothing waits for a normaliser.
+Plan plan_of(const hdet_token_loss_args* d, bool given) {
   Plan q{};
   const int64_t R = d->n_replicas, T = d->n_tokens, V = d->vocab, D = d->width;
   // Pairs share operands, single CTAs make four times as many tiles.  1 x 1024 tokens x 50257 (width 768), loss and bf16
@@ -1492,7 +1248,7 @@ Plan plan_of(const hdet_token_loss_args* d) {
     // With all of a replica's G in the workspace, and G in bf16, its place can hold the numerators until lse is known: a pass
     // over 2 bytes a logit in place of 2 x width operations.  (16 x 1024 tokens of width 768: 4.16 ms, with the logits formed
     // twice 4.67; 8 x 2048 of width 2048: 8.39 and 10.1.)
-    q.numerators = q.n_pieces == 1 && q.g_terms == 1 && q.n_tiles <= kMaxScaleTiles;
+    q.numerators = !given && q.n_pieces == 1 && q.g_terms == 1 && q.n_tiles <= kMaxScaleTiles;
     if (d->d_hidden) {
       // dH's sums run over the piece, dW's over the tokens: dH has few tiles and long sums.  Cut into parts, it ends with the
       // rest of the launch's work; every part more costs a pass over fp32 partial sums, about two steps a tile.  The cut taken
@@ -1541,76 +1297,24 @@ Plan plan_of(const hdet_token_loss_args* d) {
 // The most that a call with up to n_tokens tokens needs.  A shorter batch can need more than a longer one: more of its replicas share a
 // launch, or its sums are cut into more parts.  The plan is the same for tokens up to the same multiple of 64 (but for the few that
 // have a kernel of their own).
-int64_t workspace_of(const hdet_token_loss_args* d) {
+int64_t workspace_of(const hdet_token_loss_args* d, bool given) {
   hdet_token_loss_args a = *d;
-  int64_t most = plan_of(d).total;
+  int64_t most = plan_of(d, given).total;
   for (a.n_tokens = kFew; a.n_tokens < d->n_tokens; a.n_tokens = a.n_tokens == kFew ? 64 : a.n_tokens + 64)
-    most = std::max(most, plan_of(&a).total);
+    most = std::max(most, plan_of(&a, given).total);
   return most;
 }
 
-struct DeviceScope {
-  int prev = -1;
-  bool switched = false;
-  cudaError_t err = cudaSuccess;
-  explicit DeviceScope(int dev) {
-    err = cudaGetDevice(&prev);
-    if (err == cudaSuccess && prev != dev) {
-      err = cudaSetDevice(dev);
-      switched = err == cudaSuccess;
-    }
-  }
-  ~DeviceScope() { if (switched) cudaSetDevice(prev); }
-};
-
-using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-constexpr int kMaxDevices = 64;
-std::mutex g_mutex;
-EncodeTiled g_encode = nullptr;
-int g_sms[kMaxDevices];      // SMs of the device, 0 until it is prepared
-
-// Once per process: the driver's tensor-map encoder.  Once per device: the kernels' shared-memory sizes and its SM count.
+// Once per device: the kernels' shared-memory sizes and its SM count.
 cudaError_t prepare(int device, int* sms) {
-  std::lock_guard<std::mutex> lock(g_mutex);
-  if (device >= kMaxDevices) return cudaErrorInvalidDevice;
-  if (!g_encode) {
-    void* f = nullptr;
-    cudaDriverEntryPointQueryResult found;
-    const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found);
-    if (e != cudaSuccess) return e;
-    if (found != cudaDriverEntryPointSuccess || !f) return cudaErrorNotSupported;
-    g_encode = reinterpret_cast<EncodeTiled>(f);
-  }
-  if (g_sms[device]) {
-    *sms = g_sms[device];
-    return cudaSuccess;
-  }
   const void* kernels[] = {
 #define HDET_PHASES(ctas, sums)                                                                              \
   (const void*)gemm_kernel<ctas, kStats, sums>, (const void*)gemm_kernel<ctas, kNumerators, sums>,           \
-      (const void*)gemm_kernel<ctas, kProbs, sums>, (const void*)gemm_kernel<ctas, kGrads, sums>
+      (const void*)gemm_kernel<ctas, kProbs, sums>, (const void*)gemm_kernel<ctas, kGrads, sums>,         \
+      (const void*)gemm_kernel<ctas, kGiven, sums>
       HDET_PHASES(1, false), HDET_PHASES(1, true), HDET_PHASES(2, false), HDET_PHASES(2, true)};
 #undef HDET_PHASES
-  for (const void* k : kernels) {
-    const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmem);
-    if (e != cudaSuccess) return e;
-  }
-  const cudaError_t e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, device);
-  if (e == cudaSuccess) g_sms[device] = *sms;
-  return e;
-}
-
-// [z][y][x] bf16, x contiguous, copied in boxes of 64 x 64; what lies outside reads as zero.
-bool encode(CUtensorMap* map, const void* base, int64_t x, int64_t y, int64_t z, int64_t y_stride, int64_t z_stride) {
-  const cuuint64_t dims[3] = {(cuuint64_t)x, (cuuint64_t)y, (cuuint64_t)z};
-  const cuuint64_t strides[2] = {(cuuint64_t)y_stride * 2, (cuuint64_t)z_stride * 2};
-  const cuuint32_t box[3] = {64, 64, 1}, step[3] = {1, 1, 1};
-  return g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, step,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  return prepare_device(device, sms, kernels, kGemmSmem);
 }
 
 // Steps of 64 summed by the tensor cores at a time.  fp32 gradients, and the logits for them: 8 (errors of 4e-8 to 9e-7 of a gradient's
@@ -1653,25 +1357,29 @@ Out out_of(void* p, int dtype, int64_t stride, int64_t row, int64_t width, bool 
 }
 
 }  // namespace
+}  // namespace hdet
+
+using namespace hdet;
 
 extern "C" HDET_API int hdet_token_loss_workspace(const hdet_token_loss_args* d, int64_t* bytes) {
   const char* who = "hdet_token_loss_workspace";
   if (!bytes) return fail(HDET_ERR_INVALID_ARG, who, "bytes is NULL");
   *bytes = 0;
   if (const int rc = check(who, d)) return rc;
-  *bytes = workspace_of(d);
+  *bytes = workspace_of(d, false);
   return HDET_OK;
 }
 
+namespace hdet {
 namespace {
 
-int token_loss(const char* who, const hdet_token_loss_args* d, void* workspace, int64_t workspace_bytes, void* stream, bool selftest) {
-  hdet::TraceRange trace(who);
-  if (const int rc = check(who, d)) return rc;
-  if (const int rc = check_pointers(who, d)) return rc;
-  const Plan q = plan_of(d);
+// Behind the checks of the descriptor.  `given`: no loss, and the gradients for given ones of log probabilities and entropies.
+int token_loss(const char* who, const hdet_token_loss_args* d, const ScoreGiven* given, void* workspace, int64_t workspace_bytes, void* stream,
+               bool selftest) {
+  const Plan q = plan_of(d, given != nullptr);
   if (!workspace || workspace_bytes < q.total)
-    return fail(HDET_ERR_INVALID_ARG, who, "the workspace is NULL or smaller than hdet_token_loss_workspace says");
+    return fail(HDET_ERR_INVALID_ARG, who, given ? "the workspace is NULL or smaller than hdet_token_scores_grad_workspace says"
+                                                 : "the workspace is NULL or smaller than hdet_token_loss_workspace says");
   if (!aligned(workspace, 256)) return fail(HDET_ERR_ALIGN, who, "the workspace is not 256-byte aligned");
   if (q.m_tiles * q.n_tiles * d->n_replicas * q.ctas > INT32_MAX || q.rows_pad * q.packed_row * 2 >= (1ll << 40) ||
       d->weight_row * d->vocab * 2 >= (1ll << 40) || (d->n_replicas > 1 && d->weight_stride * 2 >= (1ll << 40)))
@@ -1691,6 +1399,7 @@ int token_loss(const char* who, const hdet_token_loss_args* d, void* workspace, 
   p.vocab = (int)d->vocab; p.width = (int)d->width; p.n_tokens = (int)d->n_tokens; p.rows_pad = (int)q.rows_pad;
   p.weight_shared = shared_table;
   p.grad_scale = d->grad_scale;
+  p.of_mean = !given;
   p.wait_limit = selftest ? kSelftestLimitCycles : bulk::kWaitLimitCycles;
   p.withhold = selftest;
   p.count = reinterpret_cast<int*>(ws + q.off_count);
@@ -1743,15 +1452,19 @@ int token_loss(const char* who, const hdet_token_loss_args* d, void* workspace, 
   }
   const int64_t pack_rows = round_up(div_up(d->n_tokens > 0 ? d->n_tokens : 1, kPackBlocks), 8);
   const unsigned pack_blocks = (unsigned)(d->n_tokens > 0 ? div_up(d->n_tokens, pack_rows) : 1);
-  e = launch(pack_kernel, dim3(pack_blocks, d->n_replicas), 256, 0, 1, st, k, (int)pack_rows);
+  const dim3 pack_grid(pack_blocks, d->n_replicas);
+  if (given) {
+    ScoreGiven g = *given;
+    g.norm = const_cast<RowNorm*>(p.norm);
+    e = launch(pack_kernel<kPackGiven, ScoreGiven>, pack_grid, 256, 0, 1, st, k, (int)pack_rows, g);
+  } else {
+    e = launch(pack_kernel<kPackLoss, int>, pack_grid, 256, 0, 1, st, k, (int)pack_rows, 0);
+  }
   if (e != cudaSuccess) return fail_cuda(who, e);
 
   if (q.pack_table) {
     __nv_bfloat16* packed = reinterpret_cast<__nv_bfloat16*>(ws + q.off_table);
-    const int64_t all = d->weight_row | (shared_table ? 0 : d->weight_stride) | d->width;
-    const bool by8 = all % 4 == 0 && aligned(d->weight, 8), by4 = all % 2 == 0 && aligned(d->weight, 4);
-    e = launch(by8 ? pack_table_kernel<uint2> : by4 ? pack_table_kernel<uint32_t> : pack_table_kernel<uint16_t>, dim3((unsigned)div_up(d->vocab, 8), tables), 256, 0, 1, st, table,
-               shared_table ? (int64_t)0 : d->weight_stride, table_row, p.vocab, p.width, k.packed_row, packed);
+    e = launch_pack_table(table, shared_table ? 0 : d->weight_stride, table_row, p.vocab, p.width, k.packed_row, tables, packed, st);
     if (e != cudaSuccess) return fail_cuda(who, e);
     table = packed;
     table_row = q.packed_row;
@@ -1772,7 +1485,7 @@ int token_loss(const char* who, const hdet_token_loss_args* d, void* workspace, 
   p.v0 = 0; p.v_len = p.vocab; p.v_pitch = (int)q.piece;
   p.m_tiles = (int)q.m_tiles; p.n_tiles = (int)q.n_tiles;
   const bool any = d->n_tokens > 0;
-  if (!q.numerators) {
+  if (!q.numerators && !given) {
     if (any) e = launch_gemm<kStats>(p, q.ctas, q.m_tiles * q.n_tiles * d->n_replicas, sms, st);
     if (e == cudaSuccess) e = launch(join_kernel, dim3((unsigned)(q.rows_pad / 8), d->n_replicas), 256, 0, 1, st, p);
   }
@@ -1796,7 +1509,9 @@ int token_loss(const char* who, const hdet_token_loss_args* d, void* workspace, 
         p.h_jobs = d->d_hidden && any ? p.h_splits * p.n_r * p.h_tiles_m * p.h_tiles_n : 0;
         p.h_add = piece > 0;
         const int64_t tiles = (int64_t)p.n_r * p.m_tiles * p.n_tiles;
-        if (!q.numerators) {
+        if (given) {
+          if (any) e = launch_gemm<kGiven>(p, q.ctas, tiles, sms, st);
+        } else if (!q.numerators) {
           if (any) e = launch_gemm<kProbs>(p, q.ctas, tiles, sms, st);
         } else {
           if (any) e = launch_gemm<kNumerators>(p, q.ctas, tiles, sms, st);
@@ -1814,16 +1529,71 @@ int token_loss(const char* who, const hdet_token_loss_args* d, void* workspace, 
         e = launch(join_hidden_kernel, dim3((unsigned)q.rows_pad, p.n_r), 256, 0, 1, st, p);
       if (e != cudaSuccess) return fail_cuda(who, e);
     }
+    if (given) e = launch(poison_grads_kernel, dim3(1), 32, 0, 1, st, p);
+    if (e != cudaSuccess) return fail_cuda(who, e);
   }
   return HDET_OK;
 }
 
+int checked_token_loss(const char* who, const hdet_token_loss_args* d, void* workspace, int64_t workspace_bytes, void* stream, bool selftest) {
+  TraceRange trace(who);
+  if (const int rc = check(who, d)) return rc;
+  if (const int rc = check_pointers(who, d)) return rc;
+  return token_loss(who, d, nullptr, workspace, workspace_bytes, stream, selftest);
+}
+
+// The part of a call for given gradients that it has in common with the loss's.
+hdet_token_loss_args loss_args(const hdet_token_scores_args* d) {
+  hdet_token_loss_args a{};
+  a.hidden = d->hidden; a.weight = d->weight; a.targets = d->targets;
+  a.d_hidden = d->d_hidden; a.d_weight = d->d_weight;
+  a.n_tokens = d->n_tokens; a.vocab = d->vocab; a.width = d->width;
+  a.hidden_stride = d->hidden_stride; a.hidden_row = d->hidden_row;
+  a.weight_stride = d->weight_stride; a.weight_row = d->weight_row;
+  a.target_stride = d->target_stride;
+  a.d_hidden_stride = d->d_hidden_stride; a.d_hidden_row = d->d_hidden_row;
+  a.d_weight_stride = d->d_weight_stride; a.d_weight_row = d->d_weight_row;
+  a.grad_scale = 1.0;
+  a.piece_bytes = d->piece_bytes;
+  a.n_replicas = d->n_replicas;
+  a.hidden_dtype = d->hidden_dtype; a.weight_dtype = d->weight_dtype; a.target_dtype = d->target_dtype;
+  a.d_hidden_dtype = d->d_hidden_dtype; a.d_weight_dtype = d->d_weight_dtype;
+  a.accumulate = d->accumulate;
+  a.device = d->device;
+  return a;
+}
+
 }  // namespace
+}  // namespace hdet
 
 extern "C" HDET_API int hdet_token_loss(const hdet_token_loss_args* d, void* workspace, int64_t workspace_bytes, void* stream) {
-  return token_loss("hdet_token_loss", d, workspace, workspace_bytes, stream, false);
+  return checked_token_loss("hdet_token_loss", d, workspace, workspace_bytes, stream, false);
 }
 
 extern "C" HDET_API int hdet_selftest_token_loss_wait(const hdet_token_loss_args* d, void* workspace, int64_t workspace_bytes, void* stream) {
-  return token_loss("hdet_selftest_token_loss_wait", d, workspace, workspace_bytes, stream, true);
+  return checked_token_loss("hdet_selftest_token_loss_wait", d, workspace, workspace_bytes, stream, true);
+}
+
+extern "C" HDET_API int hdet_token_scores_grad_workspace(const hdet_token_scores_args* d, int64_t* bytes) {
+  const char* who = "hdet_token_scores_grad_workspace";
+  if (!bytes) return fail(HDET_ERR_INVALID_ARG, who, "bytes is NULL");
+  *bytes = 0;
+  if (const int rc = check_token_scores(who, d, true)) return rc;
+  const hdet_token_loss_args a = loss_args(d);
+  *bytes = workspace_of(&a, true);
+  return HDET_OK;
+}
+
+extern "C" HDET_API int hdet_token_scores_grad(const hdet_token_scores_args* d, void* workspace, int64_t workspace_bytes, void* stream) {
+  const char* who = "hdet_token_scores_grad";
+  TraceRange trace(who);
+  if (const int rc = check_token_scores(who, d, true)) return rc;
+  if (const int rc = check_token_scores_pointers(who, d, true)) return rc;
+  const bool many = d->n_replicas > 1;
+  const auto per_token = [&](const void* p, int64_t stride) { return PerToken<const float>{static_cast<const float*>(p), many ? stride : 0}; };
+  const ScoreGiven given{per_token(d->lse, d->lse_stride), per_token(d->targets ? d->logprob : nullptr, d->logprob_stride),
+                         per_token(d->entropy, d->entropy_stride), per_token(d->d_logprob, d->d_logprob_stride),
+                         per_token(d->d_entropy, d->d_entropy_stride), nullptr};
+  const hdet_token_loss_args a = loss_args(d);
+  return token_loss(who, &a, &given, workspace, workspace_bytes, stream, false);
 }
