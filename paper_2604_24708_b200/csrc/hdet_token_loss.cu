@@ -185,50 +185,6 @@ __device__ __forceinline__ float2 numerators_of(uint32_t pair) {
 }
 
 // ------------------------------------------------------------------------------------------------ epilogues
-// One thread per row of the tile; a reader's half of the accumulator's columns passes through registers 64 at a time.
-//
-// A thread's row is contiguous in memory and its warp's 32 rows are not, so values go through shared memory: every thread
-// leaves 128 bytes of its row there (16-byte chunk k at place k ^ (row % 8), so that neither side meets a bank twice), and
-// eight threads at a time write one row's 128 bytes.  Written straight from registers, 16 bytes to each of 32 rows at a
-// time, the same tile took the probs kernel of 16 x 1024 tokens x 50257 (width 768) 1684 us instead of 1115 us.
-
-// Where a warp's 32 rows go: byte offset of each lane's own row, and which rows are written.
-struct Rows {
-  char* base;
-  int64_t offset;
-  unsigned on;
-};
-
-__device__ __forceinline__ void stage(uint32_t at, int lane, int chunk, uint4 v) {
-  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + lane * 128 + ((chunk ^ (lane & 7)) << 4)), "r"(v.x), "r"(v.y),
-               "r"(v.z), "r"(v.w)
-               : "memory");
-}
-
-__device__ __forceinline__ uint4 unstage(uint32_t at, int row, int chunk) {
-  uint4 v;
-  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-               : "r"(at + row * 128 + ((chunk ^ (row & 7)) << 4))
-               : "memory");
-  return v;
-}
-
-// Staged rows of 128 bytes to memory, from byte `first` of each row on; chunks at or behind `limit` bytes are left out.
-__device__ __forceinline__ void write_staged(const Rows& rows, uint32_t at, int lane, int64_t first, int64_t limit) {
-  __syncwarp();
-  const int chunk = lane & 7;
-  const int64_t byte = first + 16 * chunk;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int row = 4 * i + (lane >> 3);
-    const uint4 v = unstage(at, row, chunk);
-    const int64_t offset = __shfl_sync(0xffffffffu, rows.offset, row);
-    if ((rows.on >> row & 1) && byte < limit) *reinterpret_cast<uint4*>(rows.base + offset + byte) = v;
-  }
-  __syncwarp();
-}
-
 // Staged rows of 32 fp32 values, columns col .., added to (or put in the place of) what a gradient holds.
 __device__ __forceinline__ void add_staged(const Rows& rows, uint32_t at, int lane, int col, int width, bool f32, bool accumulate) {
   __syncwarp();

@@ -14,7 +14,8 @@
 //   pack     counted tokens move together (padding drops out)
 //   scores   a CTA (or pair) takes 128 (256) tokens and a run of the vocabulary's tiles, one after the other: a reader keeps its row's
 //            state and its list of the best classes over the whole run
-//   join     a block a row: the runs' states and lists become the row's; the best are summed again in fp64 and ordered
+//            (or, where all logits together are few, leaves the logits and the largest of every 32)
+//   join     a warp or a block a row: the runs' states and lists become the row's; the best are summed again in fp64 and ordered
 // One or two tokens a replica take a kernel of their own in place of the first two (few).
 #include <algorithm>
 #include <climits>
@@ -31,10 +32,12 @@ constexpr int kScoreThreads = 384, kFirstReader = 4, kReaders = 8, kReaderThread
 constexpr int kMaxStages = 6;
 constexpr int kMargin = 4;                 // classes kept beyond n_top: as many could be out of order by the fp32 logits
 constexpr int kMaxList = HDET_MAX_TOP + kMargin;
-constexpr int kGroup = 16;                 // columns that are looked through at a time for a list
+constexpr int kShort = 16, kLong = 32;     // a reader's list has one of these lengths
+constexpr int kGroup = 8, kBuffer = 16;    // columns that are looked through at a time for a list; classes that wait to be put into it
+static_assert(kMaxList <= kLong, "every list fits");
 constexpr int kMaxSmem = 227 * 1024;
 constexpr long long kSelftestLimitCycles = 4000000ll;   // 2 ms
-constexpr int kChunk = 16;                 // steps of 64 that the tensor cores sum before fp32 registers take over, as in the loss
+constexpr int kChunk = 16;                 // steps of 64 that the tensor cores sum before fp32 additions take over, as in the loss
 
 using Key = unsigned long long;            // a class in a list: falling order of its logit, then rising order of its id; 0: none
 
@@ -47,6 +50,50 @@ __device__ __forceinline__ float logit_of(Key k) {
   return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u);
 }
 __device__ __forceinline__ int class_of(Key k) { return (int)~(unsigned)k; }
+
+// 32 keys, one in each lane, into falling order; and the 32 largest of two such.
+__device__ __forceinline__ Key exchange(Key k, int stride, bool larger) {
+  const Key o = __shfl_xor_sync(0xffffffffu, k, stride);
+  return larger == (k > o) ? k : o;
+}
+__device__ __forceinline__ float exchange(float x, int stride, bool larger);
+template <typename T>
+__device__ __forceinline__ T sorted(T k) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int size = 2; size <= 32; size *= 2)
+#pragma unroll
+    for (int stride = size / 2; stride > 0; stride /= 2) k = exchange(k, stride, ((lane & stride) == 0) == ((lane & size) == 0));
+  return k;
+}
+template <typename T>
+__device__ __forceinline__ T merged(T a, T b) {
+  const int lane = threadIdx.x & 31;
+  b = __shfl_sync(0xffffffffu, b, 31 - lane);
+  T k = a > b ? a : b;
+#pragma unroll
+  for (int stride = 16; stride > 0; stride /= 2) k = exchange(k, stride, (lane & stride) == 0);
+  return k;
+}
+
+// The same for 32 floats.
+__device__ __forceinline__ float exchange(float x, int stride, bool larger) {
+  const float o = __shfl_xor_sync(0xffffffffu, x, stride);
+  return larger ? fmaxf(x, o) : fminf(x, o);
+}
+
+// The 32 largest of WARPS warps' sorted keys, in warp 0.  All threads of those warps; s: WARPS rows, free for the next use after a barrier.
+template <int WARPS, typename T>
+__device__ __forceinline__ T merged_of_warps(T mine, int warp, T (*s)[32]) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int half = WARPS / 2; half > 0; half /= 2) {
+    if (warp >= half && warp < 2 * half) s[warp][lane] = mine;
+    __syncthreads();
+    if (warp < half) mine = merged(mine, s[warp + half][lane]);
+  }
+  return mine;
+}
 
 // A row's state over some of its classes.
 struct State {
@@ -68,23 +115,57 @@ struct State {
     weighted += o.weighted;
     ties += o.ties;
   }
-  __device__ __forceinline__ void add_logit(float z) {
-    if (z > top) raise(z);
-    if (z == top) {
-      ties += z > -INFINITY;
-    } else {
-      const float d = z - top, e = exp_from(z, top);
-      others += e;
-      weighted = fmaf(e, fmaxf(d, -1e4f), weighted);       // a logit of -inf adds 0, not NaN; one that is NaN makes others NaN
+  // A warp's logits, one in each lane (-inf: none), into a state that all lanes hold.
+  __device__ __forceinline__ void add_warp(float z) {
+    float most = z;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+    if (most > top) raise(most);
+    const bool is = z == top && z > -INFINITY;
+    const float d = z - (top > -INFINITY ? top : 0.0f);
+    float e = is ? 0.0f : exp2_fast(d * kLog2e);
+    float u = e * fmaxf(d, -1e4f);                         // a logit of -inf adds 0, not NaN; one that is NaN makes others NaN
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      e += __shfl_xor_sync(0xffffffffu, e, o);
+      u += __shfl_xor_sync(0xffffffffu, u, o);
+    }
+    others += e;
+    weighted += u;
+    ties += (float)__popc(__ballot_sync(0xffffffffu, is));
+  }
+  // All of WARPS warps' lanes' states, in all of them.  Everything first moves to the common maximum.
+  template <int WARPS>
+  __device__ __forceinline__ void add_all(int warp, float (*s)[4]) {
+    const int lane = threadIdx.x & 31;
+    float most = top;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+    if constexpr (WARPS > 1) {
+      if (lane == 0) s[warp][0] = most;
+      __syncthreads();
+      most = lane < WARPS ? s[lane][0] : -INFINITY;
+#pragma unroll
+      for (int o = WARPS / 2; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+      most = __shfl_sync(0xffffffffu, most, 0);
+    }
+    if (most > top) raise(most);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) add_sums(o);
+    if constexpr (WARPS > 1) {
+      if (lane == 0) { s[warp][1] = others; s[warp][2] = weighted; s[warp][3] = ties; }
+      __syncthreads();
+      others = lane < WARPS ? s[lane][1] : 0.0f;
+      weighted = lane < WARPS ? s[lane][2] : 0.0f;
+      ties = lane < WARPS ? s[lane][3] : 0.0f;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) add_sums(o);
     }
   }
-  __device__ __forceinline__ void add_lane(int o) {
-    State s;
-    s.top = __shfl_xor_sync(0xffffffffu, top, o);
-    s.others = __shfl_xor_sync(0xffffffffu, others, o);
-    s.weighted = __shfl_xor_sync(0xffffffffu, weighted, o);
-    s.ties = __shfl_xor_sync(0xffffffffu, ties, o);
-    add(s);
+  __device__ __forceinline__ void add_sums(int o) {
+    others += __shfl_xor_sync(0xffffffffu, others, o);
+    weighted += __shfl_xor_sync(0xffffffffu, weighted, o);
+    ties += __shfl_xor_sync(0xffffffffu, ties, o);
   }
 };
 static_assert(sizeof(State) == 16, "one store");
@@ -99,11 +180,15 @@ struct ScoreParams {
   const int* token_of;
   float* z_target;
   State* part;              // scores: [job][half][row of the tile]; few: [replica][token][part]
-  Key* lists;               // scores: [job][half][entry][row of the tile]; few: [replica][token][part][entry]
-  Key* best;                // a list's first, laid out as part
+  Key* lists;               // in falling order; scores: [job][half][entry][row of the tile]; few: [replica][token][part][entry]
+  float* logits;            // kept: [replica][rows_pad][pitch], and the largest of every 32: [group][replica][rows_pad]
+  float* group_top;
+  int64_t pitch;
+  int* floor;               // [replica][rows_pad]: some list of the row is full of logits from here on (ordered_bits)
   int n_parts;              // few: blocks a replica
   int n_tiles;              // of the vocabulary
-  int list;                 // entries of a list, 0: none
+  int list;                 // entries of a list that count, 0: none
+  int held;                 // entries of a reader's list
   int clusters, most_jobs;  // that run at once; that there is room for
   int chunk, stages;
   Control* control;
@@ -134,55 +219,166 @@ __device__ __forceinline__ int splits_for(const ScoreParams& p, int row_tiles) {
   return (int)(best & 0xfffffu);
 }
 
+constexpr int kNoList = 0, kKeep = -1;             // in the place of a list's length: no alternatives; the logits are kept
+constexpr int kRowGroup = 32;
+
 // ------------------------------------------------------------------------------------------------ lists
-// A reader thread's list of its row's best classes: `size` entries in shared memory, in no order; entry e of all threads lies together.
-struct List {
-  float* value;             // this thread's first entry; the next is kReaderThreads further
-  int* id;
-  int size, used, worst;
-  float least;              // a class has to be above it: the worst entry's logit once the list is full
-  __device__ __forceinline__ void clear() { used = 0; least = -INFINITY; }
-  // Classes come in rising order, so one that equals the worst entry is behind it.
-  __device__ __forceinline__ void add(float z, int v) {
-    const int at = (used < size ? used : worst) * kReaderThreads;
-    value[at] = z;
-    id[at] = v;
-    used += used < size;
-    if (used < size) return;
-    worst = 0;
-    least = value[0];
-#pragma unroll 4
-    for (int e = 1; e < size; ++e) {
-      const float w = value[e * kReaderThreads];
-      if (w < least || (w == least && id[e * kReaderThreads] > id[worst * kReaderThreads])) {
-        least = w;
-        worst = e;
+// The order of floats as that of integers (kNoFloor: that of -inf).
+__device__ __forceinline__ int ordered_bits(float x) {
+  const int u = __float_as_int(x);
+  return u < 0 ? u ^ 0x7fffffff : u;
+}
+__device__ __forceinline__ float from_ordered(int u) { return __int_as_float(u < 0 ? u ^ 0x7fffffff : u); }
+
+// A reader thread's list of its row's best classes, LENGTH of them in falling order, and behind it a buffer of classes on their way into
+// it, both in shared memory (entry e of all threads lies together).  Putting a class into the list where it is found costs a warp as much as if
+// all its rows had found one, and rows find theirs at different columns; so it goes into the buffer, and when some row's buffer is half
+// full all rows put theirs in together: the buffer is sorted and merged with the list, by networks whose places are known to the compiler.
+// (8 x 2048 tokens x 50257 classes, width 1024, without lists 1.16 ms.  With 12 entries, put in one at a time: 1.63 ms when found, 1.45 from the
+// buffer.)
+constexpr uint2 kNothing = {0xff800000u, 0u};      // a logit of -inf
+
+// Brings the `wanted` best of n entries to the front, in order, equal ones by their ids: for the rare rows with equal logits where it matters.
+__device__ __noinline__ void order_exactly(uint2* at, int n, int wanted) {
+  for (int i = 0; i < wanted; ++i) {
+    uint2 best = at[i * kReaderThreads];
+    int place = i;
+    for (int j = i + 1; j < n; ++j) {
+      const uint2 u = at[j * kReaderThreads];
+      const float a = __uint_as_float(u.x), b = __uint_as_float(best.x);
+      if (a > b || (a == b && u.y < best.y)) {
+        best = u;
+        place = j;
       }
     }
-  }
-};
-
-// Adds those of columns v .. v + 15 of a row that belong into its list.  A register cannot be picked by a number, so the columns
-// go through shared memory, each thread's own; threads then take theirs at the same time, each its next one.
-__device__ __forceinline__ void look_through(const float* x, int v, List& list, float* staging) {
-  unsigned found = 0;
-#pragma unroll
-  for (int i = 0; i < kGroup; ++i) found |= (x[i] > list.least ? 1u : 0u) << i;
-  if (!__any_sync(0xffffffffu, found)) return;
-#pragma unroll
-  for (int i = 0; i < kGroup; ++i) staging[32 * i] = x[i];
-  while (__any_sync(0xffffffffu, found)) {
-    if (found) {
-      const int i = __ffs(found) - 1;
-      found &= found - 1;
-      const float z = staging[32 * i];
-      if (z > list.least) list.add(z, v + i);
-    }
+    at[place * kReaderThreads] = at[i * kReaderThreads];
+    at[i * kReaderThreads] = best;
   }
 }
 
+// Puts `waiting` classes of the buffer into the list; returns the logit of entry `list` - 1.  A call, since what it takes in registers and
+// instructions would weigh on the loop that hardly ever comes here.
+template <int LENGTH>
+__device__ __noinline__ float empty_buffer(uint2* at, int waiting, int list) {
+  float z[LENGTH], y[kBuffer];
+  unsigned id[LENGTH], w[kBuffer];
+#pragma unroll
+  for (int e = 0; e < kBuffer; ++e) {
+    const uint2 u = e < waiting ? at[(LENGTH + e) * kReaderThreads] : kNothing;
+    y[e] = __uint_as_float(u.x);
+    w[e] = u.y;
+  }
+#pragma unroll
+  for (int e = 0; e < LENGTH; ++e) {
+    const uint2 u = at[e * kReaderThreads];
+    z[e] = __uint_as_float(u.x);
+    id[e] = u.y;
+  }
+  const auto order = [](float& a, unsigned& i, float& b, unsigned& j) {     // a >= b
+    const bool swap = b > a;
+    const float more = fmaxf(a, b), less = fminf(a, b);
+    const unsigned k = swap ? j : i, l = swap ? i : j;
+    a = more; b = less; i = k; j = l;
+  };
+  // odd-even merge sort of the buffer
+#pragma unroll
+  for (int p = 1; p < kBuffer; p *= 2)
+#pragma unroll
+    for (int k = p; k >= 1; k /= 2)
+#pragma unroll
+      for (int j = k % p; j + k < kBuffer; j += 2 * k)
+#pragma unroll
+        for (int i = 0; i < k; ++i)
+          if (i + j + k < kBuffer && (i + j) / (2 * p) == (i + j + k) / (2 * p)) order(y[i + j], w[i + j], y[i + j + k], w[i + j + k]);
+  // the LENGTH largest of both: the list's last against the buffer's first, and so on; then that (bitonic) sequence into order
+  float out = -INFINITY;                           // the largest that fell out
+#pragma unroll
+  for (int e = 0; e < kBuffer; ++e) {
+    order(z[LENGTH - 1 - e], id[LENGTH - 1 - e], y[e], w[e]);
+    out = fmaxf(out, y[e]);
+  }
+#pragma unroll
+  for (int k = LENGTH / 2; k >= 1; k /= 2)
+#pragma unroll
+    for (int e = 0; e < LENGTH; ++e)
+      if ((e & k) == 0) order(z[e], id[e], z[e + k], id[e + k]);
+  if (__any_sync(0xffffffffu, out == z[LENGTH - 1] && out > -INFINITY)) {
+    for (int e = waiting; e < kBuffer; ++e) at[(LENGTH + e) * kReaderThreads] = kNothing;
+    order_exactly(at, LENGTH + kBuffer, LENGTH);
+  } else {
+#pragma unroll
+    for (int e = 0; e < LENGTH; ++e) at[e * kReaderThreads] = make_uint2(__float_as_uint(z[e]), id[e]);
+  }
+  float last = z[LENGTH - 1];
+#pragma unroll
+  for (int e = 0; e < LENGTH - 1; ++e)
+    if (e == list - 1) last = z[e];
+  return last;
+}
+
+template <int LENGTH>
+struct List {
+  uint2* at;                // this thread's first entry
+  int waiting;              // in the buffer
+  int size;                 // entries that count
+  float above;              // a class has to have a larger logit: the list's last that counts, or what other lists of the row say
+  __device__ __forceinline__ void clear(int row_floor) {
+#pragma unroll
+    for (int e = 0; e < LENGTH; ++e) at[e * kReaderThreads] = kNothing;
+    waiting = 0;
+    above = below(row_floor);
+  }
+  // The largest logit that a class below all of a full list has.  (One that equals the list's last may go before it, by its id.)
+  static __device__ __forceinline__ float below(int row_floor) {
+    return row_floor > kNoFloor ? from_ordered(row_floor == 0 ? -2 : row_floor - 1) : -INFINITY;      // -1 is -0, which equals 0
+  }
+  __device__ __forceinline__ void empty(int* row_floor) {
+    const float last = empty_buffer<LENGTH>(at, waiting, size);
+    waiting = 0;
+    if (last > above) {
+      above = last;
+      atomicMax(row_floor, ordered_bits(above + 0.0f));
+    }
+    above = fmaxf(above, below(__ldcg(row_floor)));
+  }
+  // Columns v .. v + 7 of the row.
+  __device__ __forceinline__ void look_through(const float* x, int v, int* row_floor) {
+    if (__any_sync(0xffffffffu, waiting > kBuffer - kGroup)) empty(row_floor);
+    uint2* to = at + (LENGTH + waiting) * kReaderThreads;
+    const uint2* const from = to;
+#pragma unroll
+    for (int i = 0; i < kGroup; ++i)
+      if (x[i] > above) {
+        *to = make_uint2(__float_as_uint(x[i]), (unsigned)(v + i));
+        to += kReaderThreads;
+      }
+    waiting += (int)(to - from) / kReaderThreads;
+  }
+  // At the run's end: the entries that count are in the order of their keys.
+  __device__ __forceinline__ void finish(int* row_floor) {
+    empty(row_floor);
+    bool equal = false;
+    for (int e = 0; e < min(size, LENGTH - 1); ++e) {
+      const float z = __uint_as_float(at[e * kReaderThreads].x);
+      equal = equal || (z > -INFINITY && z == __uint_as_float(at[(e + 1) * kReaderThreads].x));
+    }
+    if (__any_sync(0xffffffffu, equal)) order_exactly(at, LENGTH, size);
+  }
+};
+template <>
+struct List<kNoList> {
+  uint2* at;
+};
+template <>
+struct List<kKeep> {
+  uint2* at;                // (not used)
+  Rows rows;                // where the warp's rows of logits go
+  uint32_t staging;
+  int64_t group;            // this row's place in a group's maxima
+};
+
 // ------------------------------------------------------------------------------------------------ product
-struct Shared {             // behind the stages, the lists and the staging
+struct Shared {             // behind the stages and the lists
   uint64_t full[kMaxStages], empty[kMaxStages];    // a stage holds its operands; the products have read it
   uint64_t acc_full[2], acc_empty[2];              // an accumulator is complete; its readers are done with it
   uint32_t tmem;
@@ -191,10 +387,12 @@ struct Shared {             // behind the stages, the lists and the staging
   int splits;
 };
 
-constexpr int kStagingBytes = 4 * kGroup * kReaderThreads;
-__host__ __device__ constexpr int list_bytes(int list) { return list ? 8 * list * kReaderThreads + kStagingBytes : 0; }
+constexpr int kStagingBytes = 4096;        // per reader: 32 rows x 128 bytes
+__host__ __device__ constexpr int list_bytes(int held) {
+  return held == kKeep ? kReaders * kStagingBytes : held ? 8 * (held + kBuffer) * kReaderThreads : 0;
+}
 constexpr int kFixedSmem = 1024 + (int)sizeof(Shared);
-static_assert(kFixedSmem + 5 * kStageBytes + list_bytes(kMaxList) <= kMaxSmem, "five stages beside the longest lists");
+static_assert(kFixedSmem + 4 * kStageBytes + list_bytes(kLong) <= kMaxSmem, "four stages beside the longest lists");
 
 struct Run {                // a cluster's job: 128 CTAS tokens of a replica, and tiles from .. to of the vocabulary
   int r, m0, from, to;
@@ -223,62 +421,81 @@ __device__ __forceinline__ bool find_run(const ScoreParams& p, const Shared& sh,
   return false;
 }
 
-// 64 columns of a row, from class v on, into its state and list.
-template <bool LIST>
-__device__ __forceinline__ void take_logits(const ScoreParams& p, float (&x)[2][32], int v, int target, float* z_target, State& s, List& list,
-                                            float* staging) {
-  cut_columns(x, v, p.vocab);
-  const float top = largest(x);
-  if ((unsigned)(target - v) < 64u) {
+// 32 columns of a row, from class v on, into its state and list.
+template <int LENGTH>
+__device__ __forceinline__ void take_logits(const ScoreParams& p, float (&x)[32], int v, int target, int64_t row, State& s, List<LENGTH>& list) {
+  if (v + 32 > p.vocab) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      if (v + i == target) *z_target = x[0][i];
-      if (v + 32 + i == target) *z_target = x[1][i];
+    for (int i = 0; i < 32; ++i)
+      if (v + i >= p.vocab) x[i] = -INFINITY;      // behind the vocabulary's end: nothing of theirs is left in exp
+  }
+  float most[32 / kGroup];
+#pragma unroll
+  for (int g = 0; g < 32 / kGroup; ++g) {
+    most[g] = x[kGroup * g];
+#pragma unroll
+    for (int i = 1; i < kGroup; ++i) most[g] = fmaxf(most[g], x[kGroup * g + i]);
+  }
+  if ((unsigned)(target - v) < 32u) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      if (v + i == target) p.z_target[row] = x[i];
+  }
+  const float top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+  if constexpr (LENGTH > 0) {
+    if (__any_sync(0xffffffffu, top > list.above)) {
+#pragma unroll
+      for (int g = 0; g < 32 / kGroup; ++g)
+        if (__any_sync(0xffffffffu, most[g] > list.above)) list.look_through(x + kGroup * g, v + kGroup * g, p.floor + row);
     }
   }
-  if constexpr (LIST) {
-    if (__any_sync(0xffffffffu, top > list.least)) {
+  if constexpr (LENGTH == kKeep) {
+    const int lane = threadIdx.x & 31;
 #pragma unroll
-      for (int g = 0; g < 64 / kGroup; ++g) look_through(&x[g / 2][kGroup * (g % 2)], v + kGroup * g, list, staging);
-    }
+    for (int k = 0; k < 8; ++k)
+      stage(list.staging, lane, k, make_uint4(__float_as_uint(x[4 * k]), __float_as_uint(x[4 * k + 1]), __float_as_uint(x[4 * k + 2]),
+                                              __float_as_uint(x[4 * k + 3])));
+    write_staged(list.rows, list.staging, lane, 4 * (int64_t)v, 4 * p.pitch);
+    p.group_top[(int64_t)(v / kRowGroup) * p.n_replicas * p.rows_pad + list.group] = top;
   }
   if (__any_sync(0xffffffffu, top >= s.top && top > -INFINITY)) {
     if (top > s.top) s.raise(top);
     const float m = s.top > -INFINITY ? s.top : NAN;       // equal to nothing
     float n = 0.0f;
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        const bool is = x[h][i] == m;
-        n += is ? 1.0f : 0.0f;
-        x[h][i] = is ? -INFINITY : x[h][i];
-      }
+    for (int i = 0; i < 32; ++i) {
+      const bool is = x[i] == m;
+      n += is ? 1.0f : 0.0f;
+      x[i] = is ? -INFINITY : x[i];
+    }
     s.ties += n;
   }
   const float from = s.top > -INFINITY ? s.top : 0.0f;     // nothing finite yet: exp of -inf, not of NaN
   float e[4] = {0.0f, 0.0f, 0.0f, 0.0f}, u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
-#pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      const float d = x[h][i] - from, y = exp2_fast(d * kLog2e);
-      e[i % 4] += y;
-      u[i % 4] = fmaf(y, fmaxf(d, -1e4f), u[i % 4]);       // -inf adds 0, not NaN; what is NaN makes e NaN
-    }
+  for (int i = 0; i < 32; ++i) {
+    const float d = x[i] - from, y = exp2_fast(d * kLog2e);
+    e[i % 4] += y;
+    u[i % 4] = fmaf(y, fmaxf(d, -1e4f), u[i % 4]);         // -inf adds 0, not NaN; what is NaN makes e NaN
+  }
   s.others += (e[0] + e[1]) + (e[2] + e[3]);
   s.weighted += (u[0] + u[1]) + (u[2] + u[3]);
 }
 
 // Tiles of (128 * CTAS) x (128 * CTAS) by a resident CTA (or pair): copies, products and readers each go through the same runs, with a ring
 // of stages and two accumulators between them.  Every wait is bounded.
-template <int CTAS, bool SUMS, bool LIST>
+//
+// The tensor cores cut the sums that they keep instead of rounding them, so a long sum is taken over every kChunk steps: a tile's first
+// chunk stays in one accumulator, the next ones go to the other and are added to it by the readers, in fp32 and rounded.  The next tile starts in the
+// other one, while the readers go through this tile's sums, 32 columns at a time.  (Sums that were added up in the readers' registers left
+// too few for a list: 3.45 ms for 8 x 2048 tokens of width 2048 with 12 entries, against 2.42 without a list.)
+template <int CTAS, int LENGTH>
 __global__ void __launch_bounds__(kScoreThreads, 1) scores_kernel(const __grid_constant__ ScoreParams p) {
   extern __shared__ uint8_t smem_raw[];
   constexpr int kTile = 128 * CTAS, kCols = 64 * CTAS;
   const uint32_t smem = (bulk::smem_addr(smem_raw) + 1023u) & ~1023u;
   uint8_t* const behind = smem_raw + (smem - bulk::smem_addr(smem_raw)) + p.stages * kStageBytes;
-  Shared& sh = *reinterpret_cast<Shared*>(behind + list_bytes(p.list));
+  Shared& sh = *reinterpret_cast<Shared*>(behind + list_bytes(LENGTH));
   volatile int& failed = sh.failed;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = CTAS == 1 ? 0 : cluster_rank();
@@ -362,7 +579,7 @@ __global__ void __launch_bounds__(kScoreThreads, 1) scores_kernel(const __grid_c
     for (int k = kb > p.stages ? kb - p.stages : 0; k < kb && __all_sync(0xffffffffu, !failed); ++k)
       if (!warp_wait(bar(sh.empty[k % p.stages]), (k / p.stages) & 1, p.wait_limit)) failed = 1;
   } else if (warp == 1 && rank == 0) {
-    int s = 0, uses = 0;
+    int s = 0, used[2] = {0, 0}, b = 0;
     uint32_t parity = 0;
     bool go = true;
     const uint64_t a_desc = operand_desc(smem, kMajor), b_desc = operand_desc(smem + kOperandBytes, kMajor);
@@ -373,8 +590,9 @@ __global__ void __launch_bounds__(kScoreThreads, 1) scores_kernel(const __grid_c
         uint32_t acc = 0;
         for (int step = 0, in_chunk = 0; step < steps; ++step) {
           if (in_chunk == 0) {
-            const int b = uses & 1;
-            if (uses >= 2 && !__all_sync(0xffffffffu, wait_cluster(bar(sh.acc_empty[b]), (uses / 2 - 1) & 1, p.wait_limit))) {
+            if (step == p.chunk) b ^= 1;         // behind the tile's first chunk
+            const int uses = b ? used[1] : used[0];
+            if (uses > 0 && !__all_sync(0xffffffffu, wait_cluster(bar(sh.acc_empty[b]), (uses - 1) & 1, 2 * p.wait_limit))) {
               failed = 1;
               go = false;
               break;
@@ -394,9 +612,9 @@ __global__ void __launch_bounds__(kScoreThreads, 1) scores_kernel(const __grid_c
                       in_chunk > 0 || k > 0);
           commit<CTAS>(bar(sh.empty[s]));
           ++in_chunk;
-          if ((SUMS && in_chunk == p.chunk) || step + 1 == steps) {
-            commit<CTAS>(bar(sh.acc_full[uses & 1]));
-            ++uses;
+          if (in_chunk == p.chunk || step + 1 == steps) {
+            commit<CTAS>(bar(sh.acc_full[b]));
+            if (b) ++used[1]; else ++used[0];
             in_chunk = 0;
           }
           if (++s == p.stages) {
@@ -404,72 +622,90 @@ __global__ void __launch_bounds__(kScoreThreads, 1) scores_kernel(const __grid_c
             parity ^= 1;
           }
         }
+        if (steps <= p.chunk) b ^= 1;            // the next tile starts in the accumulator that does not hold this one's sums
         if (__any_sync(0xffffffffu, failed)) go = false;
       }
     }
   } else if (warp >= kFirstReader) {
     const int reader = warp - kFirstReader, quarter = warp & 3, half = reader >> 2;
     const int tile_row = 128 * (int)rank + quarter * 32 + lane, thread = 32 * reader + lane;
-    List list;
-    list.size = p.list;
-    list.value = reinterpret_cast<float*>(behind) + thread;
-    list.id = reinterpret_cast<int*>(behind + 4 * p.list * kReaderThreads) + thread;
-    float* const staging = reinterpret_cast<float*>(behind + 8 * p.list * kReaderThreads) + reader * 32 * kGroup + lane;
-    int uses = 0;
+    List<LENGTH> list;
+    list.at = reinterpret_cast<uint2*>(behind) + thread;
+    int used[2] = {0, 0}, b = 0;
     bool go = true;
+    const uint32_t my_columns = tmem + half * kCols + ((uint32_t)(quarter * 32) << 16);
     for (int job = blockIdx.x / CTAS; go && find_run<CTAS>(p, sh, job, run); job += clusters) {
       const int64_t row = (int64_t)run.r * p.rows_pad + run.m0 + tile_row;
       const int target = p.target[row];
-      float* const z_target = p.z_target + row;
       State s;
       s.clear();
-      list.clear();
+      if constexpr (LENGTH > 0) {
+        list.size = p.list;
+        list.clear(__ldcg(p.floor + row));
+      }
+      if constexpr (LENGTH == kKeep) {
+        list.rows.base = reinterpret_cast<char*>(p.logits);
+        list.rows.offset = row * p.pitch * 4;
+        list.rows.on = __ballot_sync(0xffffffffu, run.m0 + tile_row < sh.count[run.r]);
+        list.staging = bulk::smem_addr(behind) + reader * kStagingBytes;
+        list.group = row;
+      }
       for (int tile = run.from; go && tile < run.to; ++tile) {
-        Columns<SUMS ? CTAS : 0> acc;
-        const auto acc_at = [&] { return tmem + (uses & 1) * 128 * CTAS + half * kCols + ((uint32_t)(quarter * 32) << 16); };
-        const auto acc_done = [&] {
+        const auto acc_done = [&](int b) {
           fence_before_sync();
           __syncwarp();
-          if (lane == 0) arrive_leader(bar(sh.acc_empty[uses & 1]));
-          ++uses;
+          if (lane == 0) arrive_leader(bar(sh.acc_empty[b]));
+          if (b) ++used[1]; else ++used[0];
         };
-        for (int step = 0; step < steps; step += SUMS ? p.chunk : steps) {
-          if (!warp_wait(bar(sh.acc_full[uses & 1]), (uses / 2) & 1, 2 * p.wait_limit)) {
+        const auto acc_wait = [&](int b) {
+          if (!warp_wait(bar(sh.acc_full[b]), (b ? used[1] : used[0]) & 1, 2 * p.wait_limit)) {
             failed = 1;
             go = false;
-            break;
           }
           fence_after_sync();
-          if constexpr (SUMS) {
-            take_columns(acc_at(), acc, step > 0);
-            acc_done();
+          return go;
+        };
+        if (!acc_wait(b)) break;
+        const uint32_t sums = my_columns + b * 128 * CTAS, chunk = my_columns + (b ^ 1) * 128 * CTAS;
+        for (int step = p.chunk; step < steps; step += p.chunk) {
+          if (!acc_wait(b ^ 1)) break;
+          Columns<CTAS> y;                       // taken at once: the products wait for this accumulator
+          take_columns(chunk, y, false);
+          acc_done(b ^ 1);
+#pragma unroll
+          for (int i = 0; i < 4 * CTAS; ++i) {
+            float x[16];
+            tmem_load16(sums + 16 * i, x);
+            tmem_load_wait(x);
+#pragma unroll
+            for (int k = 0; k < 16; ++k) x[k] += y.x[i / 4][i / 2 % 2][16 * (i % 2) + k];
+            tmem_store16(sums + 16 * i, x);
           }
+          tmem_store_wait();
         }
         if (!go) break;
-        Source<CTAS, SUMS> from;
-        from.tmem = acc_at();
-        from.empty = false;
-        if constexpr (SUMS) from.acc = &acc;
-#pragma unroll (SUMS ? CTAS : 1)
-        for (int c = 0; c < kCols; c += 64) {
-          float loaded[2][32];
-          float (&x)[2][32] = from.get(c, loaded);
-          take_logits<LIST>(p, x, tile * kTile + half * kCols + c, target, z_target, s, list, staging);
+#pragma unroll 1
+        for (int c = 0; c < kCols; c += 32) {
+          float x[32];
+          __syncwarp();
+          tmem_load32(sums + c, x);
+          tmem_load_wait(x);
+          take_logits<LENGTH>(p, x, tile * kTile + half * kCols + c, target, row, s, list);
         }
-        if constexpr (!SUMS) acc_done();
+        acc_done(b);
+        b ^= 1;
       }
       if (!go) break;
       const int64_t at = ((int64_t)job * 2 + half) * kTile + tile_row;
       p.part[at] = s;
-      if constexpr (LIST) {
-        Key best = 0;
+      if constexpr (LENGTH > 0) {
+        list.finish(p.floor + row);
         Key* to = p.lists + ((int64_t)job * 2 + half) * p.list * kTile + tile_row;
         for (int e = 0; e < p.list; ++e) {
-          const Key k = e < list.used ? key_of(list.value[e * kReaderThreads], list.id[e * kReaderThreads]) : 0;
-          to[(int64_t)e * kTile] = k;
-          best = max(best, k);
+          const uint2 u = list.at[e * kReaderThreads];
+          const float z = __uint_as_float(u.x);
+          to[(int64_t)e * kTile] = z > -INFINITY ? key_of(z, (int)u.y) : 0;
         }
-        p.best[at] = best;
       }
     }
   }
@@ -488,15 +724,15 @@ __global__ void __launch_bounds__(kScoreThreads, 1) scores_kernel(const __grid_c
 
 // ------------------------------------------------------------------------------------------------ few tokens
 // One or two tokens a replica: the table is read once, so that is what bounds it.  A warp takes a run of the table's rows, three at a
-// time, a lane 8 elements of each per step.  A logit is the same in all lanes then, so the warp keeps one state, and its best classes
-// in order, one in each lane.
-constexpr int kFew = 2, kFewRows = 3;
+// time, a lane 8 elements of each per step.  Every 30 rows (or at the run's end) a lane has one of their logits, and the warp's state and its
+// list, sorted, an entry in each lane, take them in together.
+constexpr int kFew = 2, kFewRows = 3, kFewBatch = 30;
 constexpr int64_t kFewElements = 150000000;      // of all tables, for two tokens: the product is faster beyond
 
 template <int NT>
 __global__ void __launch_bounds__(256, 3) few_scores_kernel(const __grid_constant__ ScoreParams p, const __grid_constant__ PackParams k) {
   __shared__ State s_state[8][NT];
-  __shared__ Key s_key[NT][8 * 32];
+  __shared__ Key s_key[8][32];
   let_next_start();
   wait_for_previous();
   const int r = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -534,13 +770,25 @@ __global__ void __launch_bounds__(256, 3) few_scores_kernel(const __grid_constan
   const __nv_bfloat16* base = p.table + r * p.table_stride;
   State s[NT];
   Key mine[NT];                                    // this lane's entry of the sorted list
-  float least[NT];
+  float held[NT];                                  // this lane's logit of those that wait
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     s[t].clear();
     mine[t] = 0;
-    least[t] = -INFINITY;
+    held[t] = -INFINITY;
   }
+  int first = from;                                // of those that wait
+  const auto take_in = [&](int first) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      s[t].add_warp(held[t]);
+      if (p.list) {
+        const Key key = held[t] > -INFINITY ? key_of(held[t], first + lane) : 0, last = __shfl_sync(0xffffffffu, mine[t], p.list - 1);
+        if (__any_sync(0xffffffffu, key > last)) mine[t] = merged(mine[t], sorted(key));
+      }
+      held[t] = -INFINITY;
+    }
+  };
   for (int v = from; v < to; v += kFewRows) {
     float z[kFewRows][NT];
     const __nv_bfloat16* row[kFewRows];
@@ -577,23 +825,17 @@ __global__ void __launch_bounds__(256, 3) few_scores_kernel(const __grid_constan
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) z[i][t] += __shfl_xor_sync(0xffffffffu, z[i][t], o);
         if (v + i >= to) continue;
-        s[t].add_logit(z[i][t]);
+        if (v + i - first == lane) held[t] = z[i][t];
         if (v + i == target[t] && lane == 0) p.z_target[(int64_t)r * p.rows_pad + t] = z[i][t];
-        if (p.list && z[i][t] > least[t]) {
-          const Key key = key_of(z[i][t], v + i);
-          const int place = __popc(__ballot_sync(0xffffffffu, mine[t] > key));
-          const Key above = __shfl_up_sync(0xffffffffu, mine[t], 1);
-          mine[t] = lane < place ? mine[t] : lane == place ? key : above;
-          const Key last = __shfl_sync(0xffffffffu, mine[t], p.list - 1);
-          least[t] = last ? logit_of(last) : -INFINITY;
-        }
       }
+    if (v + kFewRows - first == kFewBatch || v + kFewRows >= to) {
+      take_in(first);
+      first = v + kFewRows;
+    }
   }
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
+  for (int t = 0; t < NT; ++t)
     if (lane == 0) s_state[warp][t] = s[t];
-    s_key[t][threadIdx.x] = lane < p.list ? mine[t] : 0;
-  }
   __syncthreads();
   if (threadIdx.x < count) {
     State all = s_state[0][threadIdx.x];
@@ -601,50 +843,50 @@ __global__ void __launch_bounds__(256, 3) few_scores_kernel(const __grid_constan
     p.part[((int64_t)r * kFew + threadIdx.x) * p.n_parts + blockIdx.x] = all;
   }
   if (!p.list) return;
-  // the block's list: each of the eight lists' entries finds its place by counting those before it
-  for (int t = 0; t < count; ++t) {
-    const int64_t at = ((int64_t)r * kFew + t) * p.n_parts + blockIdx.x;
-    const Key key = s_key[t][threadIdx.x];
-    const int held = __syncthreads_count(key != 0);
-    int place = 0;
-    if (lane < p.list) {
-      for (int i = 0; i < 8; ++i)
-        for (int e = 0; e < p.list; ++e) place += s_key[t][32 * i + e] > key;
-      if (key && place < p.list) {
-        p.lists[at * p.list + place] = key;
-        if (place == 0) p.best[at] = key;
-      }
-    }
-    if (threadIdx.x >= held && threadIdx.x < p.list) p.lists[at * p.list + threadIdx.x] = 0;
-    if (held == 0 && threadIdx.x == 0) p.best[at] = 0;
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    if (t >= count) break;
+    const Key key = merged_of_warps<8>(mine[t], warp, s_key);
+    if (warp == 0 && lane < p.list) p.lists[(((int64_t)r * kFew + t) * p.n_parts + blockIdx.x) * p.list + lane] = key;
+    __syncthreads();
   }
 }
 
 // ------------------------------------------------------------------------------------------------ joining
-constexpr int kJoinThreads = 256;
-constexpr int kMostParts = 2048;                   // states and lists of a row
+__host__ __device__ constexpr int join_rows(int warps) { return warps == 1 ? 8 : 1; }        // rows a block
+__host__ __device__ constexpr int join_threads(int warps) { return 32 * warps * join_rows(warps); }
+constexpr int kMostCands = 256;                    // candidates of a row; more of them take a longer way
 
-// A block a row.  With L lists of C entries each, the row's C best are in the C lists whose first entries are the largest: those are
-// found by counting, then the C best of their entries, by counting too.
-template <int CTAS>                                // 0: after few_scores_kernel
-__global__ void __launch_bounds__(kJoinThreads) join_scores_kernel(const __grid_constant__ ScoreParams p) {
-  constexpr int kTile = CTAS ? 128 * CTAS : 1;
-  __shared__ State s_state[kJoinThreads / 32];
-  __shared__ Key s_first[kMostParts], s_cand[kMaxList * kMaxList], s_best[kMaxList];
-  __shared__ double s_exact[kMaxList];
-  __shared__ int s_chosen[kMaxList], s_held;
-  const int r = blockIdx.y, row = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+// WARPS warps a row: all of a block where rows are few, one where they are many.  The row's lists (or, KEPT, its groups of 32 logits) hold
+// its C best.  Any C of their entries give a bound that the C best are not below: the C-th of the lists' first entries (of the threads' best
+// of them), or, with few lists, of their first entries, second ones, and so on.  The entries at or above it are hardly more than C; they are
+// collected and sorted.
+template <int CTAS, int WARPS, bool KEPT = false>  // CTAS 0: after few_scores_kernel
+__global__ void __launch_bounds__(join_threads(WARPS)) join_scores_kernel(const __grid_constant__ ScoreParams p) {
+  constexpr int kTile = CTAS ? 128 * CTAS : 1, kRows = join_rows(WARPS), kRowThreads = 32 * WARPS;
+  __shared__ float s_state[WARPS][4], s_head[WARPS][32];
+  __shared__ Key s_key[WARPS][32], s_best[kRows][32], s_cand[kRows][kMostCands];
+  __shared__ int s_list[kRows][kMostCands], s_lists[kRows], s_cands[kRows];
+  __shared__ long long s_exact[kRows][32];         // doubles as integers of the same order
+  const int lane = threadIdx.x & 31, in_block = (threadIdx.x >> 5) / WARPS, warp = (threadIdx.x >> 5) % WARPS, thread = 32 * warp + lane;
+  const int r = blockIdx.y, row = blockIdx.x * kRows + in_block;
+  const auto sync = [] { if constexpr (WARPS == 1) __syncwarp(); else __syncthreads(); };
   let_next_start();
+  if (thread == 0) s_lists[in_block] = s_cands[in_block] = 0;
   wait_for_previous();
-  if (row >= p.count[r]) return;
+  const int64_t at = (int64_t)r * p.rows_pad + row;
+  const int count = p.count[r], splits = CTAS ? p.control->splits : 0;
+  const unsigned status = CTAS ? p.control->status : 0;
+  if (row >= count) return;                        // (all of a row's warps)
+  const int token = p.token_of[at];
+  const float z_target = p.out.logprob.p ? p.z_target[at] : 0.0f;
   // where this row's states and lists are
   int parts = p.n_parts, row_tiles = 0;
   int64_t first_job = 0;
   if constexpr (CTAS) {
-    const int splits = p.control->splits;
     for (int i = 0; i < r; ++i) first_job += (p.count[i] + kTile - 1) / kTile;
     first_job = first_job * splits + row / kTile;
-    row_tiles = (p.count[r] + kTile - 1) / kTile;
+    row_tiles = (count + kTile - 1) / kTile;
     parts = 2 * splits;
   }
   const auto part_at = [&](int l) -> int64_t {
@@ -652,131 +894,224 @@ __global__ void __launch_bounds__(kJoinThreads) join_scores_kernel(const __grid_
     else return ((int64_t)r * kFew + row) * p.n_parts + l;
   };
   const auto entry = [&](int l, int e) -> Key {
-    if constexpr (CTAS) return p.lists[(((first_job + (int64_t)(l >> 1) * row_tiles) * 2 + (l & 1)) * p.list + e) * kTile + row % kTile];
-    else return p.lists[part_at(l) * p.list + e];
+    if constexpr (KEPT) {
+      const float z = p.logits[at * p.pitch + l * kRowGroup + e];
+      return z > -INFINITY ? key_of(z, l * kRowGroup + e) : 0;
+    } else if constexpr (CTAS) {
+      return p.lists[(((first_job + (int64_t)(l >> 1) * row_tiles) * 2 + (l & 1)) * p.list + e) * kTile + row % kTile];
+    } else {
+      return p.lists[part_at(l) * p.list + e];
+    }
+  };
+  const auto logit = [](Key key) { return key ? logit_of(key) : -INFINITY; };
+  const auto first_of = [&](int l) -> float {      // the largest of the list's logits
+    if constexpr (KEPT) return p.group_top[(int64_t)l * p.n_replicas * p.rows_pad + at];
+    else return logit(entry(l, 0));
   };
   State s;
   s.clear();
-  for (int l = threadIdx.x; l < parts; l += kJoinThreads) {
-    s.add(p.part[part_at(l)]);
-    if (p.list) s_first[l] = p.best[part_at(l)];
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) s.add_lane(o);
-  if (lane == 0) s_state[warp] = s;
-  if (threadIdx.x == 0) s_held = 0;
-  __syncthreads();
-  s = s_state[0];
-#pragma unroll
-  for (int w = 1; w < kJoinThreads / 32; ++w) s.add(s_state[w]);
-  const int64_t at = (int64_t)r * p.rows_pad + row;
-  const int token = p.token_of[at];
+  for (int l = thread; l < parts; l += kRowThreads) s.add(p.part[part_at(l)]);
+  s.add_all<WARPS>(warp, s_state);
   // the logarithm of the sum less the maximum's: >= 0
   float rest = logf(s.ties) + log1pf(s.others / s.ties);
-  const bool failed = CTAS && p.control->status != 0;
-  if (failed || !(fabsf(s.top) < INFINITY) || !(rest < INFINITY)) rest = NAN;
+  if (status != 0 || !(fabsf(s.top) < INFINITY) || !(rest < INFINITY)) rest = NAN;
   const ScoreOut& o = p.out;
-  if (threadIdx.x == 0) {
+  if (thread == 0) {
     if (o.lse.p) o.lse.at(r, token) = s.top + rest;
     if (o.entropy.p) o.entropy.at(r, token) = rest - s.weighted / (s.ties + s.others);
-    if (o.logprob.p) o.logprob.at(r, token) = -((s.top - p.z_target[at]) + rest);
+    if (o.logprob.p) o.logprob.at(r, token) = -((s.top - z_target) + rest);
   }
   if (!p.list) return;
   const int list = p.list, n_top = o.n_top;
+  const int64_t out_at = (int64_t)token * n_top;
   if (rest != rest) {
-    if (threadIdx.x < n_top) {
-      o.top_ids.at(r, (int64_t)token * n_top + threadIdx.x) = -1;
-      if (o.top_logprob.p) o.top_logprob.at(r, (int64_t)token * n_top + threadIdx.x) = NAN;
+    if (thread < n_top) {
+      o.top_ids.at(r, out_at + thread) = -1;
+      if (o.top_logprob.p) o.top_logprob.at(r, out_at + thread) = NAN;
     }
     return;
   }
-  int lists = parts;
-  if (parts > list) {
-    for (int l = threadIdx.x; l < parts; l += kJoinThreads) {
-      const Key key = s_first[l];
-      int place = 0;
-      for (int i = 0; i < parts; ++i) place += s_first[i] > key;
-      if (key && place < list) s_chosen[place] = l;
-    }
-    int some = 0;
-    for (int l = threadIdx.x; l < parts; l += kJoinThreads) some += s_first[l] != 0;
-    some = __reduce_add_sync(0xffffffffu, some);
-    if (lane == 0) atomicAdd(&s_held, some);
-    __syncthreads();
-    lists = min(list, s_held);
-  }
-  const int cands = lists * list;
-  if (threadIdx.x < list) s_best[threadIdx.x] = 0;
-  for (int c = threadIdx.x; c < cands; c += kJoinThreads) s_cand[c] = entry(parts > list ? s_chosen[c / list] : c / list, c % list);
-  __syncthreads();
-  for (int c = threadIdx.x; c < cands; c += kJoinThreads) {
-    const Key key = s_cand[c];
-    int place = 0;
-    for (int i = 0; i < cands; ++i) place += s_cand[i] > key;
-    if (key && place < list) s_best[place] = key;
-  }
-  __syncthreads();
-  // their logits in fp64
-  const __nv_bfloat16* h = p.rows + r * p.rows_stride + (p.rows_packed ? row : token) * p.rows_row;
-  for (int e = warp; e < list; e += kJoinThreads / 32) {
-    const Key key = s_best[e];
-    if (!key) continue;
-    const __nv_bfloat16* w = p.table + (p.weight_shared ? 0 : r * p.table_stride) + class_of(key) * p.table_row;
-    double sum = 0.0;
-    if (p.rows_vec) {
-      const int whole = p.width & ~7;
-      for (int c = lane * 8; c < whole; c += 256) {
-        const uint4 a4 = *reinterpret_cast<const uint4*>(h + c), b4 = *reinterpret_cast<const uint4*>(w + c);
-        const uint32_t a[4] = {a4.x, a4.y, a4.z, a4.w}, b[4] = {b4.x, b4.y, b4.z, b4.w};
+  // the bound
+  const int lists = KEPT ? (p.vocab + kRowGroup - 1) / kRowGroup : parts, entries = KEPT ? kRowGroup : list;
+  constexpr int kHeads = 4;                        // lists a thread whose largest logits stay in registers
+  float heads[kHeads], head = -INFINITY;
+  const bool flat = !KEPT && lists * entries <= 8 * kRowThreads;       // few enough to look at all entries
+  if (flat) {
+    if (thread < lists * entries) head = logit(entry(thread % lists, thread / lists));
+  } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {              // a product of two bf16 numbers is an fp32 number
-          sum += (double)(__uint_as_float(a[i] << 16) * __uint_as_float(b[i] << 16));
-          sum += (double)(__uint_as_float(a[i] & 0xffff0000u) * __uint_as_float(b[i] & 0xffff0000u));
+    for (int k = 0; k < kHeads; ++k) {
+      heads[k] = thread + k * kRowThreads < lists ? first_of(thread + k * kRowThreads) : -INFINITY;
+      head = fmaxf(head, heads[k]);
+    }
+#pragma unroll 4
+    for (int l = thread + kHeads * kRowThreads; l < lists; l += kRowThreads) head = fmaxf(head, first_of(l));
+  }
+  head = sorted(head);
+  if constexpr (WARPS > 1) {
+    head = merged_of_warps<WARPS>(head, warp, s_head);
+    if (warp == 0) s_head[0][lane] = head;
+    __syncthreads();
+    head = s_head[0][list - 1];
+  } else {
+    head = __shfl_sync(0xffffffffu, head, list - 1);
+    __syncwarp();                                  // the counters are zero
+  }
+  const Key bound = head > -INFINITY ? key_of(head, -1) : 1;      // of all ids; 1: fewer than C
+  // what is not below it
+  const unsigned before_me = (1u << lane) - 1;
+  int found = 0, cands = 0;                        // of a warp that is alone with its row
+  const auto place_of = [&](bool is, int& mine, int* shared) {       // in a list of the row's; of a warp's threads together
+    const unsigned some = __ballot_sync(0xffffffffu, is);
+    int first = mine;
+    if constexpr (WARPS == 1) {
+      mine += __popc(some);
+    } else if (some) {
+      if (lane == 0) first = atomicAdd(shared, __popc(some));
+      first = __shfl_sync(0xffffffffu, first, 0);
+    }
+    return first + __popc(some & before_me);
+  };
+  const auto collect = [&](Key key) {
+    const int place = place_of(key >= bound, cands, &s_cands[in_block]);
+    if (key >= bound && place < kMostCands) s_cand[in_block][place] = key;
+  };
+  bool all = true;
+  if (flat) {
+#pragma unroll 4
+    for (int c = thread - lane; c < lists * entries; c += kRowThreads)
+      collect(c + lane < lists * entries ? entry((c + lane) % lists, (c + lane) / lists) : 0);
+  } else {
+    const auto look = [&](int l, float largest) {
+      const bool is = l < lists && largest >= head;
+      const int place = place_of(is, found, &s_lists[in_block]);
+      if (is && place < kMostCands) s_list[in_block][place] = l;
+    };
+#pragma unroll
+    for (int k = 0; k < kHeads; ++k) look(thread + k * kRowThreads, heads[k]);
+    for (int l = thread - lane + kHeads * kRowThreads; l < lists; l += kRowThreads) look(l + lane, l + lane < lists ? first_of(l + lane) : -INFINITY);
+    sync();
+    if constexpr (WARPS > 1) found = s_lists[in_block];
+    all = found <= kMostCands;
+    constexpr int kListsAtOnce = WARPS == 1 ? 8 : 2;
+    for (int i = warp; i < min(found, kMostCands); i += kListsAtOnce * WARPS) {
+      Key key[kListsAtOnce];
+#pragma unroll
+      for (int k = 0; k < kListsAtOnce; ++k)
+        key[k] = i + k * WARPS < min(found, kMostCands) && lane < entries ? entry(s_list[in_block][i + k * WARPS], lane) : 0;
+#pragma unroll
+      for (int k = 0; k < kListsAtOnce; ++k) collect(key[k]);
+    }
+  }
+  sync();
+  if constexpr (WARPS > 1) cands = s_cands[in_block];
+  Key mine = 0;
+  if (all && cands <= kMostCands) {
+    for (int c = 32 * warp; c < cands; c += kRowThreads) {
+      const Key key = sorted(c + lane < cands ? s_cand[in_block][c + lane] : 0);
+      mine = mine ? merged(mine, key) : key;
+    }
+  } else {                                         // many equal or nearly equal logits: every list after the other
+    for (int l = warp; l < lists; l += WARPS) {
+      const Key key = lane < entries ? entry(l, lane) : 0, last = __shfl_sync(0xffffffffu, mine, list - 1);
+      if (__any_sync(0xffffffffu, key > last)) mine = merged(mine, sorted(key));
+    }
+  }
+  if (WARPS > 1 && cands > 32) mine = merged_of_warps<WARPS>(mine, warp, s_key);
+  if (warp == 0) s_best[in_block][lane] = mine;
+  sync();
+  // their logits in fp64, kAtOnce classes and kAhead x 256 columns of them at a time, all loads before the first sum
+  const __nv_bfloat16* h = p.rows + r * p.rows_stride + (p.rows_packed ? row : token) * p.rows_row;
+  const __nv_bfloat16* table = p.table + (p.weight_shared ? 0 : r * p.table_stride);
+  constexpr int kAtOnce = WARPS >= 32 ? 1 : WARPS >= 8 ? 2 : 4, kAhead = 3;
+  for (int e0 = warp; e0 < list; e0 += kAtOnce * WARPS) {
+    const __nv_bfloat16* w[kAtOnce];
+    double sum[kAtOnce];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const Key key = e0 + i * WARPS < list ? s_best[in_block][e0 + i * WARPS] : 0;
+      w[i] = table + (key ? class_of(key) : 0) * p.table_row;
+      sum[i] = 0.0;
+    }
+    const int whole = p.rows_vec ? p.width & ~7 : 0;
+    for (int c0 = lane * 8; c0 < whole; c0 += 256 * kAhead) {
+      uint4 a4[kAhead], b4[kAtOnce][kAhead];
+#pragma unroll
+      for (int q = 0; q < kAhead; ++q) {
+        const int c = c0 + 256 * q;
+        if (c >= whole) continue;
+        a4[q] = *reinterpret_cast<const uint4*>(h + c);
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i)
+          if (e0 + i * WARPS < list) b4[i][q] = *reinterpret_cast<const uint4*>(w[i] + c);
+      }
+#pragma unroll
+      for (int q = 0; q < kAhead; ++q) {
+        if (c0 + 256 * q >= whole) continue;
+        const uint32_t a[4] = {a4[q].x, a4[q].y, a4[q].z, a4[q].w};
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+          if (e0 + i * WARPS >= list) continue;
+          const uint32_t b[4] = {b4[i][q].x, b4[i][q].y, b4[i][q].z, b4[i][q].w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {            // a product of two bf16 numbers is an fp32 number
+            sum[i] += (double)(__uint_as_float(a[k] << 16) * __uint_as_float(b[k] << 16));
+            sum[i] += (double)(__uint_as_float(a[k] & 0xffff0000u) * __uint_as_float(b[k] & 0xffff0000u));
+          }
         }
       }
-      if (whole + lane < p.width) sum += (double)(__bfloat162float(h[whole + lane]) * __bfloat162float(w[whole + lane]));
-    } else {
-      for (int c = lane; c < p.width; c += 32) sum += (double)(__bfloat162float(h[c]) * __bfloat162float(w[c]));
     }
+    for (int c = whole + lane; c < p.width; c += 32)
 #pragma unroll
-    for (int i = 16; i > 0; i >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, i);
-    if (lane == 0) s_exact[e] = sum;
+      for (int i = 0; i < kAtOnce; ++i) sum[i] += (double)(__bfloat162float(h[c]) * __bfloat162float(w[i][c]));
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+#pragma unroll
+      for (int k = 16; k > 0; k >>= 1) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], k);
+      const long long u = __double_as_longlong(sum[i] + 0.0);
+      if (lane == 0 && e0 + i * WARPS < list) s_exact[in_block][e0 + i * WARPS] = u < 0 ? u ^ 0x7fffffffffffffffll : u;
+    }
   }
-  __syncthreads();
-  if (threadIdx.x >= list) return;
-  const Key key = s_best[threadIdx.x];
-  int place = threadIdx.x;                         // of an entry that holds nothing
+  sync();
+  if (warp != 0 || lane >= list) return;
+  const Key key = s_best[in_block][lane];
+  int place = lane;                                // of an entry that holds nothing
   if (key) {
-    const double z = s_exact[threadIdx.x];
+    const long long z = s_exact[in_block][lane];
     const int id = class_of(key);
     place = 0;
+#pragma unroll 8
     for (int i = 0; i < list; ++i) {
-      const Key other = s_best[i];
-      place += other && (s_exact[i] > z || (s_exact[i] == z && class_of(other) < id));
+      const Key other = s_best[in_block][i];
+      const long long y = s_exact[in_block][i];
+      place += (other != 0) & ((y > z) | ((y == z) & (class_of(other) < id)));      // (no branch, so that the loads go on)
     }
   }
   if (place < n_top) {
-    o.top_ids.at(r, (int64_t)token * n_top + place) = key ? class_of(key) : -1;
-    if (o.top_logprob.p) o.top_logprob.at(r, (int64_t)token * n_top + place) = key ? -((s.top - logit_of(key)) + rest) : -INFINITY;
+    o.top_ids.at(r, out_at + place) = key ? class_of(key) : -1;
+    if (o.top_logprob.p) o.top_logprob.at(r, out_at + place) = key ? -((s.top - logit_of(key)) + rest) : -INFINITY;
   }
 }
 
 // ------------------------------------------------------------------------------------------------ host side
+constexpr int kSms = 148;        // of a B200, for sizes that must not depend on the device; with another count only times change
+constexpr int64_t kFewRowsToJoin = 2 * kSms, kManyRows = 2048;
+constexpr int64_t kKeepLogits = 64ll << 20;      // 256 MB
+
 // Whether the table's boxes can be copied from where it is.
 bool table_fits(const hdet_token_scores_args* d) {
   return aligned(d->weight, 16) && d->weight_row % 8 == 0 && (d->n_replicas == 1 || d->weight_stride % 8 == 0);
 }
 
-constexpr int kSms = 148;        // of a B200, for sizes that must not depend on the device; with another count only times change
 constexpr int64_t kFewBlocks = kSms * 3;        // blocks of few_scores_kernel that are resident at once
 
 struct Plan {
-  int ctas, tile, list;
+  int ctas, tile, list, held;
   int64_t rows_pad, packed_row, m_tiles, n_tiles;
   bool few, pack_table;
   int64_t n_parts;                // of few_scores_kernel
-  int64_t most_jobs;
-  int64_t off_count, off_target, off_token, off_z, off_part, off_best, off_lists, off_hidden, off_table, total;
+  int64_t most_jobs, pitch;
+  int64_t off_count, off_target, off_token, off_z, off_floor, off_part, off_lists, off_logits, off_groups, off_hidden, off_table, total;
 };
 
 Plan plan_of(const hdet_token_scores_args* d) {
@@ -790,6 +1125,8 @@ Plan plan_of(const hdet_token_scores_args* d) {
   q.m_tiles = q.rows_pad / q.tile;
   q.n_tiles = div_up(V, q.tile);
   q.list = d->n_top ? (int)std::min<int64_t>(d->n_top + kMargin, V) : 0;
+  q.pitch = q.n_tiles * q.tile;
+  q.held = !q.list ? kNoList : R * q.rows_pad * q.pitch <= kKeepLogits ? kKeep : q.list <= kShort ? kShort : kLong;
   q.pack_table = !table_fits(d);
   q.few = T > 0 && T <= kFew && (T == 1 || R * V * D <= kFewElements) && !q.pack_table && D % 8 == 0 && aligned(d->hidden, 16) &&
           d->hidden_row % 8 == 0 && (R == 1 || d->hidden_stride % 8 == 0);
@@ -804,11 +1141,15 @@ Plan plan_of(const hdet_token_scores_args* d) {
   q.off_target = take(4 * R * q.rows_pad);
   q.off_token = take(4 * R * q.rows_pad);
   q.off_z = take(4 * R * q.rows_pad);
+  q.off_floor = take(4 * R * q.rows_pad);
   // room for either kernel's: which one runs depends on the hidden states' address, and the size does not
   const int64_t states = std::max<int64_t>(q.most_jobs * 2 * q.tile, T <= kFew ? R * kFew * q.n_parts : 0);
   q.off_part = take(16 * states);
-  q.off_best = take(q.list ? 8 * states : 0);
-  q.off_lists = take(8 * states * q.list);
+  q.off_lists = take(q.held > 0 || T <= kFew ? 8 * states * q.list : 0);
+  if (q.held == kKeep) {
+    q.off_logits = take(4 * R * q.rows_pad * q.pitch);
+    q.off_groups = take(4 * R * q.rows_pad * (q.pitch / kRowGroup));
+  }
   q.off_hidden = take(2 * R * q.rows_pad * q.packed_row);
   if (q.pack_table) q.off_table = take(2 * (R > 1 && d->weight_stride ? R : 1) * V * q.packed_row);
   q.total = at;
@@ -825,14 +1166,18 @@ int64_t workspace_of(const hdet_token_scores_args* d) {
   return most;
 }
 
-template <int CTAS, bool SUMS>
-auto pick_kernel(bool list) { return list ? scores_kernel<CTAS, SUMS, true> : scores_kernel<CTAS, SUMS, false>; }
+template <int CTAS>
+auto pick_kernel(int held) {
+  return held == kNoList ? scores_kernel<CTAS, kNoList> : held == kKeep ? scores_kernel<CTAS, kKeep> : held == kShort ? scores_kernel<CTAS, kShort> : scores_kernel<CTAS, kLong>;
+}
 
 cudaError_t prepare(int device, int* sms) {
-  const void* kernels[] = {(const void*)scores_kernel<1, false, false>, (const void*)scores_kernel<1, false, true>,
-                           (const void*)scores_kernel<1, true, false>,  (const void*)scores_kernel<1, true, true>,
-                           (const void*)scores_kernel<2, false, false>, (const void*)scores_kernel<2, false, true>,
-                           (const void*)scores_kernel<2, true, false>,  (const void*)scores_kernel<2, true, true>};
+  const void* kernels[] = {
+#define HDET_LENGTHS(ctas)                                                                             \
+  (const void*)scores_kernel<ctas, kNoList>, (const void*)scores_kernel<ctas, kKeep>,                  \
+      (const void*)scores_kernel<ctas, kShort>, (const void*)scores_kernel<ctas, kLong>
+      HDET_LENGTHS(1), HDET_LENGTHS(2)};
+#undef HDET_LENGTHS
   return prepare_device(device, sms, kernels, kMaxSmem);
 }
 
@@ -965,7 +1310,7 @@ int token_scores(const char* who, const hdet_token_scores_args* d, void* workspa
   p.token_of = reinterpret_cast<int*>(ws + q.off_token);
   p.z_target = reinterpret_cast<float*>(ws + q.off_z);
   p.part = reinterpret_cast<State*>(ws + q.off_part);
-  p.best = reinterpret_cast<Key*>(ws + q.off_best);
+  p.floor = reinterpret_cast<int*>(ws + q.off_floor);
   p.lists = reinterpret_cast<Key*>(ws + q.off_lists);
   p.n_parts = (int)q.n_parts;
   p.n_tiles = (int)q.n_tiles;
@@ -981,6 +1326,10 @@ int token_scores(const char* who, const hdet_token_scores_args* d, void* workspa
   p.out.top_logprob = per_token<float>(d->top_logprob, d->top_logprob_stride, many);
   p.out.top_ids = per_token<int>(d->top_ids, d->top_ids_stride, many);
   p.out.n_top = d->n_top;
+  p.logits = reinterpret_cast<float*>(ws + q.off_logits);
+  p.group_top = reinterpret_cast<float*>(ws + q.off_groups);
+  p.pitch = q.pitch;
+  p.out.floor = q.held > 0 && !q.few ? p.floor : nullptr;
 
   PackParams k{};
   k.hidden = static_cast<const __nv_bfloat16*>(d->hidden);
@@ -1001,13 +1350,15 @@ int token_scores(const char* who, const hdet_token_scores_args* d, void* workspa
   p.table_row = d->weight_row;
   p.table_stride = shared_table ? 0 : d->weight_stride;
   const int tables = shared_table ? 1 : d->n_replicas;
-  const dim3 join_grid((unsigned)d->n_tokens, d->n_replicas);
+  const auto join = [&](auto kernel, int warps) {
+    return launch(kernel, dim3((unsigned)div_up(d->n_tokens, join_rows(warps)), d->n_replicas), join_threads(warps), 0, 1, st, p);
+  };
   if (q.few) {
     p.rows = k.hidden; p.rows_stride = k.hidden_stride; p.rows_row = k.hidden_row;
     p.rows_vec = true;
     const dim3 grid((unsigned)q.n_parts, d->n_replicas);
     e = launch(d->n_tokens == 1 ? few_scores_kernel<1> : few_scores_kernel<2>, grid, 256, 0, 1, st, p, k);
-    if (e == cudaSuccess) e = launch(join_scores_kernel<0>, join_grid, kJoinThreads, 0, 1, st, p);
+    if (e == cudaSuccess) e = join(join_scores_kernel<0, 32>, 32);
     return e == cudaSuccess ? HDET_OK : fail_cuda(who, e);
   }
   const int64_t pack_rows = round_up(div_up(d->n_tokens, kPackBlocks), 8);
@@ -1028,14 +1379,22 @@ int token_scores(const char* who, const hdet_token_scores_args* d, void* workspa
     return fail(HDET_ERR_CUDA, who, "the driver refused a tensor map");
   // every cluster that finds a job has one; none has two while another has none
   p.clusters = (int)std::min<int64_t>(sms / q.ctas, (int64_t)d->n_replicas * q.m_tiles * q.n_tiles);
-  const int lists = list_bytes(q.list);
+  const int lists = list_bytes(q.held);
   p.stages = std::min(kMaxStages, (kMaxSmem - kFixedSmem - lists) / kStageBytes);
   const int smem = kFixedSmem + lists + p.stages * kStageBytes;
-  const bool sums = div_up(d->width, kBlockK) > kChunk, list = q.list > 0;
-  const auto kernel = q.ctas == 1 ? (sums ? pick_kernel<1, true>(list) : pick_kernel<1, false>(list))
-                                  : (sums ? pick_kernel<2, true>(list) : pick_kernel<2, false>(list));
+  const auto kernel = q.ctas == 1 ? pick_kernel<1>(q.held) : pick_kernel<2>(q.held);
   e = launch(kernel, dim3((unsigned)(p.clusters * q.ctas)), kScoreThreads, smem, q.ctas, st, p);
-  if (e == cudaSuccess) e = launch(q.ctas == 1 ? join_scores_kernel<1> : join_scores_kernel<2>, join_grid, kJoinThreads, 0, 1, st, p);
+  if (e == cudaSuccess) {
+    const int64_t rows = d->n_replicas * d->n_tokens;
+    const int warps = rows <= kFewRowsToJoin ? 32 : rows < kManyRows ? 8 : 1;
+    const auto of = [&](auto few, auto some, auto many) { return join(warps == 32 ? few : warps == 8 ? some : many, warps); };
+    if (q.held == kKeep)
+      e = q.ctas == 1 ? of(join_scores_kernel<1, 32, true>, join_scores_kernel<1, 8, true>, join_scores_kernel<1, 1, true>)
+                      : of(join_scores_kernel<2, 32, true>, join_scores_kernel<2, 8, true>, join_scores_kernel<2, 1, true>);
+    else
+      e = q.ctas == 1 ? of(join_scores_kernel<1, 32>, join_scores_kernel<1, 8>, join_scores_kernel<1, 1>)
+                      : of(join_scores_kernel<2, 32>, join_scores_kernel<2, 8>, join_scores_kernel<2, 1>);
+  }
   return e == cudaSuccess ? HDET_OK : fail_cuda(who, e);
 }
 

@@ -241,6 +241,17 @@ __device__ __forceinline__ void tmem_load_wait(float (&x)[16]) {
       : "memory");
 }
 
+// 16 consecutive columns of this warp's 32 lanes, written; the wait is for all of this thread's stores.
+__device__ __forceinline__ void tmem_store16(uint32_t tmem, const float (&x)[16]) {
+  const uint32_t* u = reinterpret_cast<const uint32_t*>(x);
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]),
+      "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]), "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15]), "r"(tmem)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

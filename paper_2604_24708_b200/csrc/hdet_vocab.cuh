@@ -133,6 +133,51 @@ __device__ __forceinline__ void cut_columns(float (&x)[2][32], int v, int vocab)
   }
 }
 
+// ------------------------------------------------------------------------------------------------ rows through shared memory
+// One thread per row of the tile; a reader's half of the accumulator's columns passes through registers 64 at a time.
+//
+// A thread's row is contiguous in memory and its warp's 32 rows are not, so values go through shared memory: every thread
+// leaves 128 bytes of its row there (16-byte chunk k at place k ^ (row % 8), so that neither side meets a bank twice), and
+// eight threads at a time write one row's 128 bytes.  Written straight from registers, 16 bytes to each of 32 rows at a
+// time, the same tile took the probs kernel of 16 x 1024 tokens x 50257 (width 768) 1684 us instead of 1115 us.
+
+// Where a warp's 32 rows go: byte offset of each lane's own row, and which rows are written.
+struct Rows {
+  char* base;
+  int64_t offset;
+  unsigned on;
+};
+
+__device__ __forceinline__ void stage(uint32_t at, int lane, int chunk, uint4 v) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + lane * 128 + ((chunk ^ (lane & 7)) << 4)), "r"(v.x), "r"(v.y),
+               "r"(v.z), "r"(v.w)
+               : "memory");
+}
+
+__device__ __forceinline__ uint4 unstage(uint32_t at, int row, int chunk) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "r"(at + row * 128 + ((chunk ^ (row & 7)) << 4))
+               : "memory");
+  return v;
+}
+
+// Staged rows of 128 bytes to memory, from byte `first` of each row on; chunks at or behind `limit` bytes are left out.
+__device__ __forceinline__ void write_staged(const Rows& rows, uint32_t at, int lane, int64_t first, int64_t limit) {
+  __syncwarp();
+  const int chunk = lane & 7;
+  const int64_t byte = first + 16 * chunk;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int row = 4 * i + (lane >> 3);
+    const uint4 v = unstage(at, row, chunk);
+    const int64_t offset = __shfl_sync(0xffffffffu, rows.offset, row);
+    if ((rows.on >> row & 1) && byte < limit) *reinterpret_cast<uint4*>(rows.base + offset + byte) = v;
+  }
+  __syncwarp();
+}
+
 // ------------------------------------------------------------------------------------------------ packing
 struct PackParams {
   const __nv_bfloat16* hidden;
@@ -157,11 +202,14 @@ struct PerToken {
   __device__ __forceinline__ T& at(int r, int64_t t) const { return p[r * stride + t]; }
 };
 
+constexpr int kNoFloor = (int)0x807fffffu;         // -inf, as an integer of the same order
+
 // What hdet_token_scores writes.
 struct ScoreOut {
   PerToken<float> logprob, entropy, lse, top_logprob;   // the last with n_top values a token
   PerToken<int> top_ids;
   int n_top;
+  int* floor;               // where packing leaves kNoFloor for every row, or NULL
   __device__ __forceinline__ void padding(int r, int64_t t) const {
     if (logprob.p) logprob.at(r, t) = 0.0f;
     if (entropy.p) entropy.at(r, t) = 0.0f;
@@ -244,6 +292,9 @@ __global__ void __launch_bounds__(256) pack_kernel(const PackParams p, int rows,
       if (y >= 0) {
         p.target[base + place] = FOR == kPackLoss || p.targets ? y : -1;
         p.token_of[base + place] = mine;
+        if constexpr (FOR == kPackScores) {
+          if (more.floor) more.floor[base + place] = kNoFloor;
+        }
         if constexpr (FOR == kPackGiven) more.norm[base + place] = more.of(r, mine);
       } else if constexpr (FOR == kPackScores) {
         more.padding(r, mine);
@@ -283,7 +334,13 @@ __global__ void __launch_bounds__(256) pack_kernel(const PackParams p, int rows,
   // rows behind the last counted token, up to the tile's end: zeros, since a product sums over them
   const int end = min(p.rows_pad, (all + p.row_tile - 1) / p.row_tile * p.row_tile);
   for (int row = all + (int)blockIdx.x * 8 + warp; row < end; row += (int)gridDim.x * 8) {
-    if (lane == 0) { p.target[base + row] = -1; p.token_of[base + row] = 0; }
+    if (lane == 0) {
+      p.target[base + row] = -1;
+      p.token_of[base + row] = 0;
+      if constexpr (FOR == kPackScores) {
+        if (more.floor) more.floor[base + row] = kNoFloor;
+      }
+    }
     __nv_bfloat16* dst = p.packed + (base + row) * p.packed_row;
     for (int c = lane * 8; c < p.packed_row; c += 256) *reinterpret_cast<uint4*>(dst + c) = make_uint4(0, 0, 0, 0);
   }
