@@ -223,6 +223,7 @@ struct WorkPlan {
   std::vector<TensorDesc> descs;
   std::vector<Tile> tiles;
   std::vector<GradSpan> spans;
+  int span_elems = 0;
   bool shared_grads = true;   // every tensor has one gradient for all replicas
   int64_t n_shared_state = 0;
   int64_t partial_numel = 0;
@@ -326,10 +327,17 @@ int plan_work(const hdet_config* cfg, const hdet_tensor* tensors, int64_t n_tens
     partial_numel += (t.numel + 3) / 4 * 4;
     descs.push_back(d);
     for (int64_t j = 0; j < n_tiles_t; ++j) tiles.push_back(Tile{(int)k, (int)j});
-    for (int64_t off = 0; off < t.numel; off += kSpanElems)
-      out.spans.push_back(GradSpan{off, (int)k, (int)std::min<int64_t>(kSpanElems, t.numel - off)});
     out.shared_grads = out.shared_grads && t.grad_stride == 0;
   }
+
+  // spans of the gradient norm: a CTA reads one replica's, or with the mean all replicas'
+  const int elem_bytes = (int)gsz * (cfg->grad_mode == HDET_GRAD_REPLICA_MEAN ? n : 1);
+  double total_bytes = 0.0;
+  for (int64_t k = 0; k < n_tensors; ++k) total_bytes += (double)tensors[k].numel * (double)gsz * (out.shared_grads ? 1 : n);
+  out.span_elems = span_elems(total_bytes, elem_bytes);
+  for (int64_t k = 0; k < n_tensors; ++k)
+    for (int64_t off = 0; off < tensors[k].numel; off += out.span_elems)
+      out.spans.push_back(GradSpan{off, (int)k, (int)std::min<int64_t>(out.span_elems, tensors[k].numel - off)});
 
   if (n_shared_state != 0 && n_shared_state != n_tensors)
     return fail(nullptr, HDET_ERR_UNSUPPORTED, "hdet_create: state_stride 0 must be used by all tensors or by none");
@@ -379,7 +387,7 @@ int hdet_create(const hdet_config* cfg, const hdet_tensor* tensors, int64_t n_te
       const int n_tiles_k = (int)((tensors[k].numel + kTileElems - 1) / kTileElems);
       run.n_tensors += 1;
       run.n_tiles += n_tiles_k;
-      const int n_spans_k = (int)((tensors[k].numel + kSpanElems - 1) / kSpanElems);
+      const int n_spans_k = (int)((tensors[k].numel + work.span_elems - 1) / work.span_elems);
       run.n_spans += n_spans_k;
       span_cursor += n_spans_k;
       in_run += (double)tensors[k].numel;

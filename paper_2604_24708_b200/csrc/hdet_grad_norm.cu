@@ -1,6 +1,6 @@
 // Global gradient norms over a handle's tensors: n_r = sqrt(sum of g_r^2), for every replica, or for the replicas' mean gradient.
 //
-// Bound by reading the gradients once.  A CTA sums one span (up to kSpanElems elements of one tensor of one replica) and leaves an fp64
+// Bound by reading the gradients once.  A CTA sums one span (consecutive elements of one tensor of one replica) and leaves an fp64
 // partial sum; the CTA that finishes a replica's last span adds the partial sums in a fixed order, so that there is one launch, and the
 // same bits on every run whichever CTA it is.
 #include <cuda_bf16.h>
@@ -13,9 +13,9 @@ namespace {
 constexpr int kNormThreads = 256;
 constexpr int kAhead = 8;              // 16-byte loads of a thread under way
 
-template <typename GradT> struct Packed;      // 16 bytes of gradients
-template <> struct Packed<float> { static constexpr int n = 4; };
-template <> struct Packed<__nv_bfloat16> { static constexpr int n = 8; };
+template <typename GradT> struct Packed;      // 16 bytes of gradients, and what a mean of them is summed in
+template <> struct Packed<float> { static constexpr int n = 4; using Sum = double; };
+template <> struct Packed<__nv_bfloat16> { static constexpr int n = 8; using Sum = float; };
 
 __device__ __forceinline__ void unpack16(const uint4& u, float (&g)[4]) {
   g[0] = __uint_as_float(u.x); g[1] = __uint_as_float(u.y); g[2] = __uint_as_float(u.z); g[3] = __uint_as_float(u.w);
@@ -89,34 +89,57 @@ __device__ __forceinline__ double span_squares(const GradT* p, int len) {
   return acc;
 }
 
-// The same of the mean over n replicas, formed as the update forms it: fp64 sum in the order of the replicas, rounded to fp32 once.
+// The same of the mean over n replicas, summed in their order: fp32 gradients in fp64, as the update does, bf16 ones in fp32, whose rounding is
+// 2^15 times finer than theirs (in fp64 the conversions took 976 us for four of the 350 M list that are read in 440).
 template <typename GradT>
 __device__ __forceinline__ double span_mean_squares(const GradT* p, long long stride, int n, double inv_n, int len) {
+  using Sum = typename Packed<GradT>::Sum;
   constexpr int kN = Packed<GradT>::n;
   const bool wide = (stride * (long long)sizeof(GradT)) % 16 == 0;
   const int head = wide ? min(len, (int)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / (int)sizeof(GradT)) : len;
   const int vecs = (len - head) / kN;
   double acc = 0.0;
-  for (int j = threadIdx.x; j < vecs; j += kNormThreads) {
-    double sum[kN];
+  // kV vectors of kReplicas replicas under way
+  constexpr int kV = 2, kReplicas = 4;
+  for (int j = threadIdx.x; j < vecs; j += kV * kNormThreads) {
+    Sum sum[kV][kN];
 #pragma unroll
-    for (int i = 0; i < kN; ++i) sum[i] = 0.0;
-#pragma unroll 4
-    for (int r = 0; r < n; ++r) {
-      float g[kN];
-      unpack16(__ldcs(reinterpret_cast<const uint4*>(p + r * stride + head) + j), g);
+    for (int v = 0; v < kV; ++v)
 #pragma unroll
-      for (int i = 0; i < kN; ++i) sum[i] += (double)g[i];
+      for (int i = 0; i < kN; ++i) sum[v][i] = 0;
+    const bool second = j + kNormThreads < vecs;
+    for (int r0 = 0; r0 < n; r0 += kReplicas) {
+      uint4 u[kReplicas][kV];
+#pragma unroll
+      for (int r = 0; r < kReplicas; ++r)
+#pragma unroll
+        for (int v = 0; v < kV; ++v) {
+          u[r][v] = make_uint4(0, 0, 0, 0);
+          if (r0 + r < n && (v == 0 || second))
+            u[r][v] = __ldcs(reinterpret_cast<const uint4*>(p + (r0 + r) * stride + head) + j + v * kNormThreads);
+        }
+#pragma unroll
+      for (int r = 0; r < kReplicas; ++r)
+#pragma unroll
+        for (int v = 0; v < kV; ++v) {
+          float g[kN];
+          unpack16(u[r][v], g);
+#pragma unroll
+          for (int i = 0; i < kN; ++i) sum[v][i] += (Sum)g[i];
+        }
     }
-    float g[kN];
 #pragma unroll
-    for (int i = 0; i < kN; ++i) g[i] = (float)(sum[i] * inv_n);
-    acc += squares(g);
+    for (int v = 0; v < kV; ++v) {
+      float g[kN];
+#pragma unroll
+      for (int i = 0; i < kN; ++i) g[i] = (float)(sum[v][i] * (Sum)inv_n);
+      acc += squares(g);
+    }
   }
   const auto single = [&](int e) {
-    double sum = 0.0;
-    for (int r = 0; r < n; ++r) sum += (double)one(p + r * stride + e);
-    const double g = (float)(sum * inv_n);
+    Sum sum = 0;
+    for (int r = 0; r < n; ++r) sum += (Sum)one(p + r * stride + e);
+    const double g = (float)(sum * (Sum)inv_n);
     acc += g * g;
   };
   for (int e = threadIdx.x; e < head; e += kNormThreads) single(e);
