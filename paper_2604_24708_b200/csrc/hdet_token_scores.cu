@@ -908,6 +908,23 @@ __global__ void __launch_bounds__(join_threads(WARPS)) join_scores_kernel(const 
     if constexpr (KEPT) return p.group_top[(int64_t)l * p.n_replicas * p.rows_pad + at];
     else return logit(entry(l, 0));
   };
+  // the lists' largest logits, under way with the states
+  const int list = p.list, n_top = p.out.n_top;
+  const int lists = KEPT ? (p.vocab + kRowGroup - 1) / kRowGroup : parts, entries = KEPT ? kRowGroup : list;
+  constexpr int kHeads = 4;                        // lists a thread whose largest logits stay in registers
+  float heads[kHeads], head = -INFINITY;
+  const bool flat = !KEPT && lists * entries <= 8 * kRowThreads;       // few enough to look at all entries
+  if (flat) {
+    if (p.list && thread < lists * entries) head = logit(entry(thread % lists, thread / lists));
+  } else if (p.list) {
+#pragma unroll
+    for (int k = 0; k < kHeads; ++k) {
+      heads[k] = thread + k * kRowThreads < lists ? first_of(thread + k * kRowThreads) : -INFINITY;
+      head = fmaxf(head, heads[k]);
+    }
+#pragma unroll 4
+    for (int l = thread + kHeads * kRowThreads; l < lists; l += kRowThreads) head = fmaxf(head, first_of(l));
+  }
   State s;
   s.clear();
   for (int l = thread; l < parts; l += kRowThreads) s.add(p.part[part_at(l)]);
@@ -921,8 +938,7 @@ __global__ void __launch_bounds__(join_threads(WARPS)) join_scores_kernel(const 
     if (o.entropy.p) o.entropy.at(r, token) = rest - s.weighted / (s.ties + s.others);
     if (o.logprob.p) o.logprob.at(r, token) = -((s.top - z_target) + rest);
   }
-  if (!p.list) return;
-  const int list = p.list, n_top = o.n_top;
+  if (!list) return;
   const int64_t out_at = (int64_t)token * n_top;
   if (rest != rest) {
     if (thread < n_top) {
@@ -932,21 +948,6 @@ __global__ void __launch_bounds__(join_threads(WARPS)) join_scores_kernel(const 
     return;
   }
   // the bound
-  const int lists = KEPT ? (p.vocab + kRowGroup - 1) / kRowGroup : parts, entries = KEPT ? kRowGroup : list;
-  constexpr int kHeads = 4;                        // lists a thread whose largest logits stay in registers
-  float heads[kHeads], head = -INFINITY;
-  const bool flat = !KEPT && lists * entries <= 8 * kRowThreads;       // few enough to look at all entries
-  if (flat) {
-    if (thread < lists * entries) head = logit(entry(thread % lists, thread / lists));
-  } else {
-#pragma unroll
-    for (int k = 0; k < kHeads; ++k) {
-      heads[k] = thread + k * kRowThreads < lists ? first_of(thread + k * kRowThreads) : -INFINITY;
-      head = fmaxf(head, heads[k]);
-    }
-#pragma unroll 4
-    for (int l = thread + kHeads * kRowThreads; l < lists; l += kRowThreads) head = fmaxf(head, first_of(l));
-  }
   head = sorted(head);
   if constexpr (WARPS > 1) {
     head = merged_of_warps<WARPS>(head, warp, s_head);
@@ -1023,7 +1024,7 @@ __global__ void __launch_bounds__(join_threads(WARPS)) join_scores_kernel(const 
   // their logits in fp64, kAtOnce classes and kAhead x 256 columns of them at a time, all loads before the first sum
   const __nv_bfloat16* h = p.rows + r * p.rows_stride + (p.rows_packed ? row : token) * p.rows_row;
   const __nv_bfloat16* table = p.table + (p.weight_shared ? 0 : r * p.table_stride);
-  constexpr int kAtOnce = WARPS >= 32 ? 1 : WARPS >= 8 ? 2 : 4, kAhead = 3;
+  constexpr int kAtOnce = WARPS >= 32 ? 1 : WARPS > 1 ? 2 : 4, kAhead = 3;
   for (int e0 = warp; e0 < list; e0 += kAtOnce * WARPS) {
     const __nv_bfloat16* w[kAtOnce];
     double sum[kAtOnce];
@@ -1358,7 +1359,7 @@ int token_scores(const char* who, const hdet_token_scores_args* d, void* workspa
     p.rows_vec = true;
     const dim3 grid((unsigned)q.n_parts, d->n_replicas);
     e = launch(d->n_tokens == 1 ? few_scores_kernel<1> : few_scores_kernel<2>, grid, 256, 0, 1, st, p, k);
-    if (e == cudaSuccess) e = join(join_scores_kernel<0, 32>, 32);
+    if (e == cudaSuccess) e = join(join_scores_kernel<0, 16>, 16);
     return e == cudaSuccess ? HDET_OK : fail_cuda(who, e);
   }
   const int64_t pack_rows = round_up(div_up(d->n_tokens, kPackBlocks), 8);
