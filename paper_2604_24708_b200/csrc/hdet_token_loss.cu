@@ -375,14 +375,24 @@ __device__ __forceinline__ void probs_epilogue(const LossParams& p, const Job& j
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int v = v0 + c + 32 * h;
+      if constexpr (PHASE == kGiven) {             // two columns an instruction where there is one for it
+        const uint64_t top = pair_of(-norm.top, -norm.top), scale = pair_of(kLog2e, kLog2e);
+        const uint64_t slope = pair_of(-norm.slope, -norm.slope), inverse = pair_of(-norm.inverse, -norm.inverse);
 #pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        if constexpr (PHASE == kGiven) {           // a logit of -inf: 0, not NaN; one that is NaN stays so
-          const float d = x[h][i] - norm.top;
-          x[h][i] = -exp2_fast(d * kLog2e) * fmaf(norm.slope, fmaxf(d, -1e4f), norm.inverse);
-        } else {
-          x[h][i] = exp_from(x[h][i], norm.top) * norm.inverse;
+        for (int i = 0; i < 32; i += 2) {
+          const uint64_t d = add_pair(pair_of(x[h][i], x[h][i + 1]), top);
+          float a, b;
+          halves_of(mul_pair(d, scale), a, b);
+          a = exp2_fast(a);
+          b = exp2_fast(b);
+          // a logit of -inf: 0, not NaN; one that is NaN stays so
+          float f, g;
+          halves_of(d, f, g);
+          halves_of(mul_pair(pair_of(a, b), fma_pair(slope, pair_of(fmaxf(f, -1e4f), fmaxf(g, -1e4f)), inverse)), x[h][i], x[h][i + 1]);
         }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) x[h][i] = exp_from(x[h][i], norm.top) * norm.inverse;
       }
       if ((unsigned)(target - v) < 32u) {
 #pragma unroll

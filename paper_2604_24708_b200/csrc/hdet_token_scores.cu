@@ -30,6 +30,7 @@ constexpr int kStageBytes = 2 * kOperandBytes;
 // columns each
 constexpr int kScoreThreads = 384, kFirstReader = 4, kReaders = 8, kReaderThreads = 32 * kReaders;
 constexpr int kMaxStages = 6;
+constexpr float kLn2 = 0.69314718055994531f;
 constexpr int kMargin = 4;                 // classes kept beyond n_top: as many could be out of order by the fp32 logits
 constexpr int kMaxList = HDET_MAX_TOP + kMargin;
 constexpr int kShort = 16, kLong = 32;     // a reader's list has one of these lengths
@@ -466,20 +467,39 @@ __device__ __forceinline__ void take_logits(const ScoreParams& p, float (&x)[32]
     for (int i = 0; i < 32; ++i) {
       const bool is = x[i] == m;
       n += is ? 1.0f : 0.0f;
-      x[i] = is ? -INFINITY : x[i];
+      x[i] = is ? -1e38f : x[i];                   // exp of it is 0, and so is 0 times it
     }
     s.ties += n;
   }
   const float from = s.top > -INFINITY ? s.top : 0.0f;     // nothing finite yet: exp of -inf, not of NaN
-  float e[4] = {0.0f, 0.0f, 0.0f, 0.0f}, u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  // Two columns an instruction where there is one for it.  The exponent x log2(e) - M log2(e) has the second product rounded, which is off by
+  // up to 2^-24 of M for all columns: of delta that is a relative error, since the maximum itself is not in it.
+  const uint64_t scale = pair_of(kLog2e, kLog2e), shift = pair_of(-from * kLog2e, -from * kLog2e);
+  uint64_t e2[2] = {0, 0}, u2[2] = {0, 0};
 #pragma unroll
-  for (int i = 0; i < 32; ++i) {
-    const float d = x[i] - from, y = exp2_fast(d * kLog2e);
-    e[i % 4] += y;
-    u[i % 4] = fmaf(y, fmaxf(d, -1e4f), u[i % 4]);         // -inf adds 0, not NaN; what is NaN makes e NaN
+  for (int i = 0; i < 32; i += 2) {
+    const uint64_t d = fma_pair(pair_of(x[i], x[i + 1]), scale, shift);
+    float a, b;
+    halves_of(d, a, b);
+    const uint64_t y = pair_of(exp2_fast(a), exp2_fast(b));
+    e2[i / 2 % 2] = add_pair(e2[i / 2 % 2], y);
+    u2[i / 2 % 2] = fma_pair(y, d, u2[i / 2 % 2]);
   }
-  s.others += (e[0] + e[1]) + (e[2] + e[3]);
-  s.weighted += (u[0] + u[1]) + (u[2] + u[3]);
+  float e, u, more;
+  halves_of(add_pair(e2[0], e2[1]), e, more);
+  e += more;
+  halves_of(add_pair(u2[0], u2[1]), u, more);
+  u += more;
+  if (__any_sync(0xffffffffu, u != u && e == e)) {         // logits of -inf: 0 times them is to be 0, not NaN
+    u = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const float d = fmaf(x[i], kLog2e, -from * kLog2e);
+      u = fmaf(exp2_fast(d), fmaxf(d, -1e38f), u);
+    }
+  }
+  s.others += e;
+  s.weighted = fmaf(u, kLn2, s.weighted);
 }
 
 // Tiles of (128 * CTAS) x (128 * CTAS) by a resident CTA (or pair): copies, products and readers each go through the same runs, with a ring
@@ -687,6 +707,7 @@ __global__ void __launch_bounds__(kScoreThreads, 1) scores_kernel(const __grid_c
 #pragma unroll 1
         for (int c = 0; c < kCols; c += 32) {
           float x[32];
+          if (LENGTH != kKeep && tile * kTile + half * kCols + c >= p.vocab) break;        // (kept: those are -inf)
           __syncwarp();
           tmem_load32(sums + c, x);
           tmem_load_wait(x);
