@@ -662,6 +662,7 @@ __global__ void __launch_bounds__(kScoreThreads, 1) scores_kernel(const __grid_c
       if constexpr (LENGTH > 0) {
         list.size = p.list;
         list.clear(__ldcg(p.floor + row));
+        if (run.m0 + tile_row >= sh.count[run.r]) list.above = INFINITY;      // zeros behind the counted tokens: nothing is looked for
       }
       if constexpr (LENGTH == kKeep) {
         list.rows.base = reinterpret_cast<char*>(p.logits);
@@ -707,7 +708,7 @@ __global__ void __launch_bounds__(kScoreThreads, 1) scores_kernel(const __grid_c
 #pragma unroll 1
         for (int c = 0; c < kCols; c += 32) {
           float x[32];
-          if (LENGTH != kKeep && tile * kTile + half * kCols + c >= p.vocab) break;        // (kept: those are -inf)
+          if (tile * kTile + half * kCols + c >= p.vocab) break;
           __syncwarp();
           tmem_load32(sums + c, x);
           tmem_load_wait(x);
@@ -1028,7 +1029,8 @@ __global__ void __launch_bounds__(join_threads(WARPS)) join_scores_kernel(const 
   sync();
   if constexpr (WARPS > 1) cands = s_cands[in_block];
   Key mine = 0;
-  if (all && cands <= kMostCands) {
+  const bool collected = all && cands <= kMostCands;
+  if (collected) {
     for (int c = 32 * warp; c < cands; c += kRowThreads) {
       const Key key = sorted(c + lane < cands ? s_cand[in_block][c + lane] : 0);
       mine = mine ? merged(mine, key) : key;
@@ -1039,7 +1041,7 @@ __global__ void __launch_bounds__(join_threads(WARPS)) join_scores_kernel(const 
       if (__any_sync(0xffffffffu, key > last)) mine = merged(mine, sorted(key));
     }
   }
-  if (WARPS > 1 && cands > 32) mine = merged_of_warps<WARPS>(mine, warp, s_key);
+  if (WARPS > 1 && (!collected || cands > 32)) mine = merged_of_warps<WARPS>(mine, warp, s_key);
   if (warp == 0) s_best[in_block][lane] = mine;
   sync();
   // their logits in fp64, kAtOnce classes and kAhead x 256 columns of them at a time, all loads before the first sum
