@@ -207,6 +207,9 @@ SHAPES = [      # R, T, V, D, n_top
     (1, 1, 1000, 63, 7), (1, 3, 500, 40, 4), (2, 5, 129, 33, 20), (1, 48, 5000, 256, 8), (1, 128, 2000, 64, 20), (1, 129, 999, 72, 5), (3, 150, 257, 130, 2),
     (2, 200, 4099, 520, 6), (1, 192, 300, 1, 20), (1, 193, 300, 2, 20), (1, 1000, 20, 64, 20), (5, 257, 1, 24, 1), (4, 300, 8200, 64, 16), (16, 256, 1030, 136, 3),
     (1, 300, 3000, 1025, 4), (2, 130, 600, 2048, 20), (1, 20, 700, 1100, 9), (8, 513, 4099, 64, 0), (1, 1, 3000, 64, 0), (1, 700, 65, 640, 0), (1, 2500, 16411, 128, 12),
+    # too many logits to be kept: lists of 16 and of 32, pairs of CTAs and single ones, sums in several chunks, short vocabularies
+    (1, 1400, 50257, 64, 8), (1, 1400, 50257, 72, 20), (4, 400, 50257, 1100, 6), (32, 64, 50257, 32, 12), (3, 190, 130000, 40, 13), (1, 120000, 600, 16, 12),
+    (2, 60000, 700, 8, 20),
 ]
 
 
@@ -257,42 +260,47 @@ def test_padding(T):
         run(h, w, y.int().cuda().contiguous(), 3)
 
 
+SIZES = [(1, 5000), (2, 5000), (30, 5000), (400, 5000), (1400, 50257), (100, 700_000)]      # the last two: too many logits to be kept
+
+
 @pytest.mark.gpu
-@pytest.mark.parametrize("T", [1, 2, 30, 400])
-def test_equal_logits_go_by_their_ids(T):
+@pytest.mark.parametrize("T,V", SIZES)
+@pytest.mark.parametrize("n_top", [3, 20])
+def test_equal_logits_go_by_their_ids(T, V, n_top):
     """Rows of the table that are the same, more of them than a list holds, near and far apart; and a hidden state of zeros."""
     gen = torch.Generator().manual_seed(3)
-    h, w, _ = inputs(1, T, 5000, 72, seed=2, pad=0.0)
+    h, w, _ = inputs(1, T, V, 72, seed=2, pad=0.0)
     for count in (2, 7, 40, 600):
-        at = torch.randperm(5000, generator=gen)[:count]
+        at = torch.randperm(V, generator=gen)[:count]
         w2 = w.clone()
         w2[0, at] = w[0, int(at[0])] * 4
-        run(h, w2, None, 20)
-    run(h, w[:, :1].expand(1, 5000, 72).contiguous(), None, 20)
-    run(torch.zeros_like(h), w, None, 20)
-    steps = (torch.arange(5000, device="cuda") // 37).float().bfloat16()        # falling and rising plateaus
+        run(h, w2, None, n_top)
+    run(h, w[:, :1].expand(1, V, 72).contiguous(), None, n_top)
+    run(torch.zeros_like(h), w, None, n_top)
+    steps = (torch.arange(V, device="cuda") // (V // 135)).float().bfloat16()        # falling and rising plateaus
     for s in (steps, -steps):
         w2 = torch.zeros_like(w)
         w2[0, :, 0] = s
-        run(h.abs(), w2, None, 20)
+        run(h.abs(), w2, None, n_top)
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("T", [1, 2, 30, 400])
-def test_logits_that_fall_and_rise_along_the_table(T):
+@pytest.mark.parametrize("T,V", [(1, 20000), (2, 20000), (30, 20000), (400, 20000), (1400, 50257), (100, 700_000)])
+@pytest.mark.parametrize("n_top", [12, 20])
+def test_logits_that_fall_and_rise_along_the_table(T, V, n_top):
     """A table in falling order fills the lists at once; one in rising order replaces every entry of them, again and again."""
-    h, w, _ = inputs(1, T, 20000, 64, seed=4, pad=0.0)
-    size = torch.linspace(0.0, 3.0, 20000, device="cuda")[:, None]
+    h, w, _ = inputs(1, T, V, 64, seed=4, pad=0.0)
+    size = torch.linspace(0.0, 3.0, V, device="cuda")[:, None]
     for s in (size, size.flip(0)):
         w2 = (w[0].abs().float() * 0.01 + s).bfloat16()[None].contiguous()
-        run(h.abs(), w2, None, 20)
+        run(h.abs(), w2, None, n_top)
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("T", [1, 2, 30, 300])
-def test_values_that_are_not_finite(T):
+@pytest.mark.parametrize("T,V", [(1, 700), (2, 700), (30, 700), (300, 700), (1400, 50257)])
+def test_values_that_are_not_finite(T, V):
     inf, nan = float("inf"), float("nan")
-    V, D = 700, 64
+    D = 64
     _, w, _ = inputs(1, T, V, D, seed=6, pad=0.0)
     h = torch.ones((1, T, D), device="cuda").bfloat16()
     y = torch.zeros((1, T), dtype=torch.int32, device="cuda")
@@ -304,12 +312,13 @@ def test_values_that_are_not_finite(T):
             assert torch.isnan(out[k]).all(), (k, value)
         assert (out["top_ids"] == -1).all()
     # a class with the logit -inf has probability 0: as if the table had none
-    w2, left = w.clone(), [i for i in range(V) if i not in (0, 130, 699)]
-    w2[0, [0, 130, 699], 5] = -inf
+    gone = (0, 130, V - 1)
+    w2, left = w.clone(), torch.tensor([i for i in range(V) if i not in gone], device="cuda")
+    w2[0, list(gone), 5] = -inf
     out, ref = run(h, w2, y, 4, check=False), run(h, w2[:, left].contiguous(), None, 4)
     for k in ("entropy", "lse"):
         assert ((out[k] - ref[k]).abs() <= 2.0 ** -18 * ref[k].abs()).all(), k
-    assert (out["logprob"] == -inf).all() and torch.equal(torch.tensor(left, dtype=torch.int32, device="cuda")[ref["top_ids"].long()], out["top_ids"])
+    assert (out["logprob"] == -inf).all() and torch.equal(left[ref["top_ids"].long()].int(), out["top_ids"])
     # fewer of them than are asked for, and none
     w2[0, 2:, 5] = -inf
     out = run(h, w2, y + 1, 4, check=False)
@@ -327,8 +336,7 @@ def test_values_that_are_not_finite(T):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("T", [1, 2, 130, 520])
-@pytest.mark.parametrize("V,D", [(50257, 64), (4099, 1088)])
+@pytest.mark.parametrize("T,V,D", [(T, V, D) for T in (1, 2, 130, 520) for V, D in ((50257, 64), (4099, 1088))] + [(1400, 50257, 64)])
 def test_likely_tokens_keep_their_relative_precision(T, V, D):
     """Probabilities up to 1 - 1e-12: log probability and entropy are off by no more, relatively, than the logits' errors make them."""
     gen = torch.Generator().manual_seed(7)
@@ -400,7 +408,7 @@ def test_captured_and_on_another_stream(T):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("R,T,V,D", [(1, 40, 2000, 64), (2, 600, 5000, 1088), (3, 300, 4099, 128)])
+@pytest.mark.parametrize("R,T,V,D", [(1, 40, 2000, 64), (2, 600, 5000, 1088), (3, 300, 4099, 128), (1, 1400, 50257, 64)])
 def test_a_wait_that_runs_out_marks_every_token(R, T, V, D):
     h, w, y = inputs(R, T, V, D, seed=11)
     ref = run(h, w, y, 4)
