@@ -12,8 +12,8 @@
 // holds the 1 (with lse and a plain sum a token of probability 1 - 1e-6 was several percent off).
 //
 //   pack     counted tokens move together (padding drops out)
-//   scores   a CTA (or pair) takes 128 (256) tokens and a run of the vocabulary's tiles, one after the other: a reader keeps its row's
-//            state and its list of the best classes over the whole run
+//   scores   a CTA (or pair) takes 128 (256) tokens and a run of the vocabulary, tile by tile: a reader keeps its row's state and its
+//            list of the best classes over the whole run
 //            (or, where all logits together are few, leaves the logits and the largest of every 32)
 //   join     a warp or a block a row: the runs' states and lists become the row's; the best are summed again in fp64 and ordered
 // One or two tokens a replica take a kernel of their own in place of the first two (few).
@@ -187,7 +187,7 @@ struct ScoreParams {
   int64_t pitch;
   int* floor;               // [replica][rows_pad]: some list of the row is full of logits from here on (ordered_bits)
   int n_parts;              // few: blocks a replica
-  int n_tiles;              // of the vocabulary
+  int n_units;              // of unit_of(CTAs) classes
   int list;                 // entries of a list that count, 0: none
   int held;                 // entries of a reader's list
   int clusters, most_jobs;  // that run at once; that there is room for
@@ -203,17 +203,29 @@ struct ScoreParams {
   ScoreOut out;
 };
 
-// How many runs the vocabulary is cut into: every cluster takes equal jobs in turn, so the shortest end has the fewest rounds times tiles
-// a run; a run costs about a tile more than its tiles (its first ones fill the lists), and one state and list a row.  A warp's lanes
-// try different numbers; every warp of the launch finds the same.
+constexpr int kColumns = 32;               // that a reader takes at a time
+// Classes that a run is made of.  A single CTA's tiles end with a box of 64 rows of the table: it is for few tokens, where every row that is
+// copied without need counts (48 tokens x 50257, width 1024: 46.3 us, with 32 classes 48.0).
+__host__ __device__ constexpr int unit_of(int ctas) { return 64 / ctas; }
+
+// How many runs the vocabulary is cut into: every cluster takes equal jobs in turn, so the shortest end has the fewest rounds times the
+// length of a run.  A narrow last tile counts as half of one (its copies of the hidden states are those of a whole one), and a run costs a
+// tile more than its tiles (its start, and filling the lists).  A warp's lanes try different numbers; every warp of the launch finds the same.
+// (Runs of whole tiles: 52.8 us for 3 x 777 tokens x 4099, width 520, which has 17 tiles for 8 runs.)
+template <int CTAS>
 __device__ __forceinline__ int splits_for(const ScoreParams& p, int row_tiles) {
-  const int lane = threadIdx.x & 31, most = min(p.n_tiles, max(1, p.most_jobs / max(1, row_tiles)));
+  constexpr unsigned kTileUnits = 128 * CTAS / unit_of(CTAS);
+  row_tiles = max(1, row_tiles);
+  // many runs at once need no second round to even out; few take up to four
+  const int lane = threadIdx.x & 31, at_once = p.clusters / row_tiles;
+  const int most = min(p.n_units, max(1, min(p.most_jobs / row_tiles, at_once >= 16 ? at_once : 4 * at_once + 4)));
   Key best = ~0ull;
   for (int s = lane + 1; s <= most; s += 32) {
-    const unsigned len = (p.n_tiles + s - 1) / s;
-    if ((unsigned)s != (p.n_tiles + len - 1) / len) continue;            // the same length with fewer runs
-    const Key rounds = ((Key)row_tiles * s + p.clusters - 1) / p.clusters;
-    best = min(best, (rounds * (len + 1)) << 20 | (unsigned)s);
+    const unsigned len = (p.n_units + s - 1) / s;
+    if ((unsigned)s != (p.n_units + len - 1) / len) continue;            // the same length with fewer runs
+    const unsigned rest = len % kTileUnits, tiles = len - rest + (rest ? max(rest, kTileUnits / 2) : 0);
+    const unsigned rounds = ((unsigned)(row_tiles * s) + p.clusters - 1) / p.clusters;
+    best = min(best, ((Key)rounds * (tiles + kTileUnits)) << 20 | (unsigned)s);
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) best = min(best, __shfl_xor_sync(0xffffffffu, best, o));
@@ -395,21 +407,27 @@ __host__ __device__ constexpr int list_bytes(int held) {
 constexpr int kFixedSmem = 1024 + (int)sizeof(Shared);
 static_assert(kFixedSmem + 4 * kStageBytes + list_bytes(kLong) <= kMaxSmem, "four stages beside the longest lists");
 
-struct Run {                // a cluster's job: 128 CTAS tokens of a replica, and tiles from .. to of the vocabulary
+struct Run {                // a cluster's job: 128 CTAS tokens of a replica, and classes from .. to (multiples of unit_of)
   int r, m0, from, to;
 };
+
+// A tile's columns, and the boxes of 64 rows of the table that a CTA copies for its share of them.
+template <int CTAS>
+__device__ __forceinline__ int columns_of(const Run& run, int n0) { return min(128 * CTAS, run.to - n0); }
+template <int CTAS>
+__device__ __forceinline__ int boxes_of(int columns) { return columns > 64 * CTAS ? 2 : 1; }
 
 template <int CTAS>
 __device__ __forceinline__ bool find_run(const ScoreParams& p, const Shared& sh, int job, Run& run) {
   constexpr int kTile = 128 * CTAS;
-  const int splits = sh.splits, len = (p.n_tiles + splits - 1) / splits;
+  const int splits = sh.splits, len = (p.n_units + splits - 1) / splits * unit_of(CTAS);
   // tokens fastest: runs that go on at the same time read the same rows of the table
   for (run.r = 0; run.r < p.n_replicas; ++run.r) {
     const int row_tiles = (sh.count[run.r] + kTile - 1) / kTile;
     if (job < row_tiles * splits) {
       run.m0 = job % row_tiles * kTile;
       run.from = job / row_tiles * len;
-      run.to = min(run.from + len, p.n_tiles);
+      run.to = min(run.from + len, p.n_units * unit_of(CTAS));
       // one value for the warp, so that what is worked out from it is the warp's too
       run.r = __shfl_sync(0xffffffffu, run.r, 0);
       run.m0 = __shfl_sync(0xffffffffu, run.m0, 0);
@@ -543,7 +561,7 @@ __global__ void __launch_bounds__(kScoreThreads, 1) scores_kernel(const __grid_c
   if (warp == 2) {
     const int count = lane < p.n_replicas ? p.count[lane] : 0;
     sh.count[lane] = count;
-    const int splits = splits_for(p, __reduce_add_sync(0xffffffffu, (count + kTile - 1) / kTile));
+    const int splits = splits_for<CTAS>(p, __reduce_add_sync(0xffffffffu, (count + kTile - 1) / kTile));
     if (lane == 0) {
       sh.splits = splits;
       if (blockIdx.x == 0) p.control->splits = splits;
@@ -567,9 +585,9 @@ __global__ void __launch_bounds__(kScoreThreads, 1) scores_kernel(const __grid_c
     bool go = !p.withhold;
     for (int job = blockIdx.x / CTAS; go && find_run<CTAS>(p, sh, job, run); job += clusters) {
       const int table = p.weight_shared ? 0 : run.r;
-      for (int tile = run.from; go && tile < run.to; ++tile) {
-        const int boxes = boxes_for<CTAS>(p.vocab - tile * kTile);
-        const int a_row = run.m0 + 128 * (int)rank, b_row = tile * kTile + 64 * boxes * (int)rank;
+      for (int n0 = run.from; go && n0 < run.to; n0 += kTile) {
+        const int columns = columns_of<CTAS>(run, n0), boxes = boxes_of<CTAS>(columns);
+        const int a_row = run.m0 + 128 * (int)rank, b_row = n0 + columns / CTAS * (int)rank;
         for (int step = 0; step < steps; ++step, ++kb) {
           if (kb >= p.stages && !warp_wait(bar(sh.empty[s]), parity ^ 1, p.wait_limit)) {
             failed = 1;
@@ -605,8 +623,8 @@ __global__ void __launch_bounds__(kScoreThreads, 1) scores_kernel(const __grid_c
     const uint64_t a_desc = operand_desc(smem, kMajor), b_desc = operand_desc(smem + kOperandBytes, kMajor);
     const uint32_t k_step = k_step_bytes(kMajor);
     for (int job = blockIdx.x / CTAS; go && find_run<CTAS>(p, sh, job, run); job += clusters) {
-      for (int tile = run.from; go && tile < run.to; ++tile) {
-        const uint32_t idesc = instruction_desc<CTAS>(64 * CTAS * boxes_for<CTAS>(p.vocab - tile * kTile), kMajor, kMajor);
+      for (int n0 = run.from; go && n0 < run.to; n0 += kTile) {
+        const uint32_t idesc = instruction_desc<CTAS>(columns_of<CTAS>(run, n0), kMajor, kMajor);
         uint32_t acc = 0;
         for (int step = 0, in_chunk = 0; step < steps; ++step) {
           if (in_chunk == 0) {
@@ -671,7 +689,8 @@ __global__ void __launch_bounds__(kScoreThreads, 1) scores_kernel(const __grid_c
         list.staging = bulk::smem_addr(behind) + reader * kStagingBytes;
         list.group = row;
       }
-      for (int tile = run.from; go && tile < run.to; ++tile) {
+      for (int n0 = run.from; go && n0 < run.to; n0 += kTile) {
+        const int columns = columns_of<CTAS>(run, n0) - half * kCols;      // that this reader's half has (or none)
         const auto acc_done = [&](int b) {
           fence_before_sync();
           __syncwarp();
@@ -706,13 +725,12 @@ __global__ void __launch_bounds__(kScoreThreads, 1) scores_kernel(const __grid_c
         }
         if (!go) break;
 #pragma unroll 1
-        for (int c = 0; c < kCols; c += 32) {
+        for (int c = 0; c < min(kCols, columns); c += kColumns) {
           float x[32];
-          if (tile * kTile + half * kCols + c >= p.vocab) break;
           __syncwarp();
           tmem_load32(sums + c, x);
           tmem_load_wait(x);
-          take_logits<LENGTH>(p, x, tile * kTile + half * kCols + c, target, row, s, list);
+          take_logits<LENGTH>(p, x, n0 + half * kCols + c, target, row, s, list);
         }
         acc_done(b);
         b ^= 1;
@@ -1337,7 +1355,7 @@ int token_scores(const char* who, const hdet_token_scores_args* d, void* workspa
   p.floor = reinterpret_cast<int*>(ws + q.off_floor);
   p.lists = reinterpret_cast<Key*>(ws + q.off_lists);
   p.n_parts = (int)q.n_parts;
-  p.n_tiles = (int)q.n_tiles;
+  p.n_units = (int)div_up(d->vocab, unit_of(q.ctas));
   p.list = q.list;
   p.most_jobs = (int)std::min<int64_t>(q.most_jobs, INT32_MAX);
   p.chunk = kChunk;
@@ -1402,7 +1420,7 @@ int token_scores(const char* who, const hdet_token_scores_args* d, void* workspa
       !encode(&p.weight, p.table, d->width, d->vocab, tables, p.table_row, shared_table ? p.table_row * d->vocab : p.table_stride))
     return fail(HDET_ERR_CUDA, who, "the driver refused a tensor map");
   // every cluster that finds a job has one; none has two while another has none
-  p.clusters = (int)std::min<int64_t>(sms / q.ctas, (int64_t)d->n_replicas * q.m_tiles * q.n_tiles);
+  p.clusters = (int)std::min<int64_t>(sms / q.ctas, (int64_t)d->n_replicas * q.m_tiles * p.n_units);
   const int lists = list_bytes(q.held);
   p.stages = std::min(kMaxStages, (kMaxSmem - kFixedSmem - lists) / kStageBytes);
   const int smem = kFixedSmem + lists + p.stages * kStageBytes;
