@@ -329,8 +329,8 @@ HDET_API int hdet_step_device(hdet_handle h, const void* d_step_losses, int32_t 
  * hdet_grad_norm -- the replicas' global gradient norms, n_r = sqrt(sum over all tensors and elements of g_r^2), from the
  * gradients as they lie (hdet_tensor.grad), to d_norms: DEVICE, N values of norm_dtype HDET_DTYPE_F32 or HDET_DTYPE_F64.
  * With grad_mode HDET_GRAD_REPLICA_MEAN, or one gradient for all replicas, all N values are the one norm (of the mean).
- * (Not in the paper.)  A handle that holds a shard of the replica axis
- * measures its own replicas.  Squares are added in fp64 beyond 16 bytes, in a fixed order: the same bits on every run.  The handle
+ * (Not in the paper.)  A mean of fp32 gradients is summed in fp64, of bf16 ones in fp32, and rounded to fp32.  A handle that holds a shard
+ * of the replica axis measures its own replicas.  Squares are added in fp64 beyond 16 bytes, in a fixed order: the same bits on every run.  The handle
  * keeps partial sums and counters, so these launches must be ordered with the handle's others.
  * Errors: INVALID_ARG (NULL, norm_dtype), ALIGN, UNSUPPORTED (handle without tensors), CUDA.
  */

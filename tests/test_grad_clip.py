@@ -133,6 +133,20 @@ def test_norms_of_one_gradient_for_all(n, align, shift, shared, grad):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("grad", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [2, 32])
+def test_norms_of_a_mean_whose_sum_is_out_of_range(n, grad):
+    run = Run(n, (70001, 33, 5), grad, align=1, shift=1, grad_mode=B.HDET_GRAD_REPLICA_MEAN)
+    out = torch.empty(n, dtype=torch.float64, device="cuda")
+    for fill in (3.2e38, 2.0 ** -126, 2.0 ** -133):
+        run.grad.fill_(fill)                    # equal in all replicas: their mean is exact but for one rounding of 1 / n
+        B.hdet_grad_norm(run.h, out, stream=_stream())
+        want = run.gradient(0).double().square().sum().sqrt().expand(n)
+        assert ((out - want).abs() <= (4.5 + 1.0) * 2.0 ** -24 * want).all(), (fill, out[0], want[0])
+    run.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("grad", ["f32", "bf16"])
 def test_norms_of_values_at_the_ends_of_the_range(grad):
     run = Run(2, (70001, 33), grad)
     out = torch.empty(2, dtype=torch.float64, device="cuda")
