@@ -436,6 +436,7 @@ int hdet_create(const hdet_config* cfg, const hdet_tensor* tensors, int64_t n_te
     if (e == cudaSuccess) e = cudaMemset(m.done, 0, 2 * words);
     if (e == cudaSuccess)
       e = prepare_fanout(cfg->optimizer, cfg->grad_dtype, cfg->grad_mode == HDET_GRAD_REPLICA_MEAN, h->shared_state);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);      // zeros and tables are there before any stream's first step
     if (e != cudaSuccess) {
       free_device(h);
       delete h;
