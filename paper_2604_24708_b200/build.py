@@ -85,6 +85,7 @@ def ptxas_table() -> str:
     out = ["| kernel | registers | spill stores (B) | spill loads (B) | stack (B) | static smem (B) |", "|---|---|---|---|---|---|"]
     for (raw, regs, st, ld, stk, smem), nm in zip(rows, dem):
         nm = re.sub(r"hdet::\(anonymous namespace\)::|\(anonymous namespace\)::", "", nm)
+        nm = re.sub(r"\([\w: ]+\)(?=\d)", "", nm)                 # casts of enumerators in template arguments
         nm = re.sub(r"\(hdet::LaunchPlan.*$|\(.*$", "", nm).replace("void ", "")
         out.append(f"| `{nm}` | {regs} | {st} | {ld} | {stk} | {smem} |")
     return "\n".join(out)
