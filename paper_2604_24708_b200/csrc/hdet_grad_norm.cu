@@ -90,15 +90,14 @@ __device__ __forceinline__ double span_squares(const GradT* p, int len) {
 }
 
 // What a sum over replicas takes of one: in fp32 a 32nd, which changes no digit and lets no sum leave the range that the mean is in.
-// to_mean makes the mean of it.  (It is an argument: set up in the function from 1 / n, the compiler's order of the loads took 674 us for four of the 350 M list
-// in place of 493.)
+// to_mean makes the mean of it.
 constexpr float kPart = 32.0f;
 static_assert(HDET_MAX_REPLICAS <= kPart, "a sum of 32nds is at most the largest gradient");
 __device__ __forceinline__ void add_part(double& sum, float g) { sum += (double)g; }
 __device__ __forceinline__ void add_part(float& sum, float g) { sum = fmaf(g, 1.0f / kPart, sum); }
 
 // The same of the mean over n replicas, summed in their order: fp32 gradients in fp64, as the update does, bf16 ones in fp32, whose rounding is
-// 2^15 times finer than theirs (in fp64 the conversions took 976 us for four of the 350 M list).
+// 2^15 times finer than theirs (in fp64 the conversions took 976 us for four of the 350 M list, whose bytes take 440).
 template <typename GradT>
 __device__ __forceinline__ double span_mean_squares(const GradT* p, long long stride, int n, double to_mean, int len) {
   using Sum = typename Packed<GradT>::Sum;
@@ -107,42 +106,30 @@ __device__ __forceinline__ double span_mean_squares(const GradT* p, long long st
   const int head = wide ? min(len, (int)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / (int)sizeof(GradT)) : len;
   const int vecs = (len - head) / kN;
   double acc = 0.0;
-  // kV vectors of kReplicas replicas under way
-  constexpr int kV = 2, kReplicas = 4;
-  for (int j = threadIdx.x; j < vecs; j += kV * kNormThreads) {
-    Sum sum[kV][kN];
-#pragma unroll
-    for (int v = 0; v < kV; ++v)
-#pragma unroll
-      for (int i = 0; i < kN; ++i) sum[v][i] = 0;
-    const bool second = j + kNormThreads < vecs;
+  // 16 bytes of kReplicas replicas under way (of four bf16 gradients of the 350 M list 441 us, of four fp32 ones of the 125 M list 346; with two times 16
+  // bytes and fewer threads at once 493 and 353; with three replicas 483 and 371).
+  constexpr int kReplicas = 4;
+  for (int j = threadIdx.x; j < vecs; j += kNormThreads) {
+    Sum sum[kN] = {};
     for (int r0 = 0; r0 < n; r0 += kReplicas) {
-      uint4 u[kReplicas][kV];
+      uint4 u[kReplicas];
 #pragma unroll
-      for (int r = 0; r < kReplicas; ++r)
+      for (int r = 0; r < kReplicas; ++r) {
+        u[r] = make_uint4(0, 0, 0, 0);
+        if (r0 + r < n) u[r] = __ldcs(reinterpret_cast<const uint4*>(p + (r0 + r) * stride + head) + j);
+      }
 #pragma unroll
-        for (int v = 0; v < kV; ++v) {
-          u[r][v] = make_uint4(0, 0, 0, 0);
-          if (r0 + r < n && (v == 0 || second))
-            u[r][v] = __ldcs(reinterpret_cast<const uint4*>(p + (r0 + r) * stride + head) + j + v * kNormThreads);
-        }
+      for (int r = 0; r < kReplicas; ++r) {
+        float g[kN];
+        unpack16(u[r], g);
 #pragma unroll
-      for (int r = 0; r < kReplicas; ++r)
-#pragma unroll
-        for (int v = 0; v < kV; ++v) {
-          float g[kN];
-          unpack16(u[r][v], g);
-#pragma unroll
-          for (int i = 0; i < kN; ++i) add_part(sum[v][i], g[i]);
-        }
+        for (int i = 0; i < kN; ++i) add_part(sum[i], g[i]);
+      }
     }
+    float g[kN];
 #pragma unroll
-    for (int v = 0; v < kV; ++v) {
-      float g[kN];
-#pragma unroll
-      for (int i = 0; i < kN; ++i) g[i] = (float)(sum[v][i] * (Sum)to_mean);
-      acc += squares(g);
-    }
+    for (int i = 0; i < kN; ++i) g[i] = (float)(sum[i] * (Sum)to_mean);
+    acc += squares(g);
   }
   const auto single = [&](int e) {
     Sum sum = 0;

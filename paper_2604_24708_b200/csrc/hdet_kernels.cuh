@@ -116,7 +116,7 @@ struct GradSpan {
   int tensor, len;
 };
 // A span is what one CTA reads: enough to outweigh starting it (four replicas of the 350 M list, bf16: 472, 432, 405 and 397 us with 32, 64, 128 and 256 KB; the mean
-// of four fp32 gradients of the 125 M list 359, 355 and 377 us with 256, 512 and 1024 KB), less where a list is small, so that every SM has some.
+// of four fp32 gradients of the 125 M list, before its loop was made shorter, 359, 355 and 377 us with 256, 512 and 1024 KB), less where a list is small, so that every SM has some.
 constexpr long long kSpanBytesMin = 16 << 10, kSpanBytesMax = 256 << 10, kSpansWanted = 148 * 8;
 inline int span_elems(double total_bytes, int elem_bytes) {        // elem_bytes: that a CTA reads for each element
   double bytes = total_bytes / (double)kSpansWanted;
