@@ -1245,11 +1245,13 @@ Plan plan_of(const hdet_token_loss_args* d, bool given) {
   q.off_count = take(4 * R);
   q.off_target = take(4 * R * q.rows_pad);
   q.off_token = take(4 * R * q.rows_pad);
-  q.off_z = take(4 * R * q.rows_pad);
   q.off_norm = take(sizeof(RowNorm) * R * q.rows_pad);
-  // room for either kernel's parts: which one runs depends on the hidden states' address, and the size does not
-  q.off_part = take(8 * R * std::max(2 * q.n_tiles, !q.grads && T <= kFew ? few_parts : 0) * q.rows_pad);
-  q.off_loss = take(4 * R * q.rows_pad);
+  if (!given) {
+    q.off_z = take(4 * R * q.rows_pad);
+    // room for either kernel's parts: which one runs depends on the hidden states' address, and the size does not
+    q.off_part = take(8 * R * std::max(2 * q.n_tiles, !q.grads && T <= kFew ? few_parts : 0) * q.rows_pad);
+    q.off_loss = take(4 * R * q.rows_pad);
+  }
   q.off_hidden = take(2 * R * q.rows_pad * q.packed_row);
   if (q.pack_table) q.off_table = take(2 * (d->n_replicas > 1 && d->weight_stride ? R : 1) * V * q.packed_row);
   if (q.grads) {
@@ -1371,10 +1373,12 @@ int token_loss(const char* who, const hdet_token_loss_args* d, const ScoreGiven*
   p.count = reinterpret_cast<int*>(ws + q.off_count);
   p.target = reinterpret_cast<int*>(ws + q.off_target);
   p.token_of = reinterpret_cast<int*>(ws + q.off_token);
-  p.z_target = reinterpret_cast<float*>(ws + q.off_z);
   p.norm = reinterpret_cast<RowNorm*>(ws + q.off_norm);
-  p.part = reinterpret_cast<float2*>(ws + q.off_part);
-  p.row_loss = reinterpret_cast<float*>(ws + q.off_loss);
+  if (!given) {
+    p.z_target = reinterpret_cast<float*>(ws + q.off_z);
+    p.part = reinterpret_cast<float2*>(ws + q.off_part);
+    p.row_loss = reinterpret_cast<float*>(ws + q.off_loss);
+  }
   p.token_loss = static_cast<float*>(d->token_loss);
   p.token_loss_stride = many ? d->token_loss_stride : 0;
   p.loss = d->loss;
