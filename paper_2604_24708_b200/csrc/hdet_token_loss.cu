@@ -22,6 +22,8 @@
 // and for each piece of the vocabulary
 //   probs       Z again; the epilogue writes G
 //   grads       as above; after the last piece, dH's partial sums are joined
+// G from given gradients of log probabilities and entropies takes probs' place (given), and then, for rows with one very likely class,
+//   likely      that class's entry of G, from the sum of the row's others
 // Up to two tokens a replica without gradients take a kernel of their own (few).
 //
 // G is the operand of a bf16 product, so it is rounded to bf16, unscaled, as the last step of its own.  Its relative error, 2^-8 of a
@@ -64,6 +66,11 @@ struct LossParams {
   float2* part;             // [replica][rows_pad][n_parts]: Lse of a part of the row
   int n_parts;
   float* row_loss;          // [replica][rows_pad]
+  // given gradients (NULL without those of entropies): ScoreGiven's, and sums of the certain rows' entries of G but the likely class's
+  const int* certain;
+  int* likely;
+  float* others;            // [half tile][replica of a launch][rows_pad]
+  bool sums_only;           // leaves those sums and nothing of G; `count` is that of the certain rows
   // piece of the vocabulary
   int r0, n_r;              // replicas of this launch
   int v0, v_len, v_pitch;   // first row of the table, rows, pitch of G
@@ -358,13 +365,15 @@ __device__ __forceinline__ void numerators_epilogue(const LossParams& p, const J
   if (target >= v0 && target < v0 + kCols) p.z_target[at] = taken;
 }
 
-// kGiven: G from given gradients of log probabilities and entropies in place of the loss's.
-template <int CTAS, int PHASE, bool SUMS>
+// kGiven: G from given gradients of log probabilities and entropies in place of the loss's.  CERTAIN: of the first `certain` rows the likely
+// class's entry is 0 for now, and the others are summed (in memory beyond 64 of them: a register that lasts is one that the kernel does not have).
+template <int CTAS, int PHASE, bool SUMS, bool CERTAIN>
 __device__ __forceinline__ void probs_epilogue(const LossParams& p, const Job& j, const Source<CTAS, SUMS>& from, int row, int half, bool counted,
-                                               int target, const RowNorm& norm, uint32_t staging, int lane) {
+                                               int certain, int target, const RowNorm& norm, uint32_t staging, int lane) {
   constexpr int kCols = 64 * CTAS;
   target = counted ? target - p.v0 : -1;
   const int v0 = j.n0 + half;
+  const bool some = CERTAIN && __any_sync(0xffffffffu, row < certain);
   Rows rows;
   rows.offset = (((int64_t)(j.r - p.r0) * p.rows_pad + row) * p.v_pitch + v0) * 2;
   rows.on = 0xffffffffu;
@@ -372,6 +381,14 @@ __device__ __forceinline__ void probs_epilogue(const LossParams& p, const Job& j
   for (int c = 0; c < kCols; c += 64) {
     float loaded[2][32];
     float (&x)[2][32] = from.get(c, loaded);
+    if (some && row < certain && largest(x) - norm.top > kLikely) {
+#pragma unroll
+      for (int i = 0; i < 64; ++i)
+        if (v0 + c + i < p.v_len && x[i / 32][i % 32] - norm.top > kLikely) {
+          p.likely[(int64_t)j.r * p.rows_pad + row] = p.v0 + v0 + c + i;
+          x[i / 32][i % 32] = -INFINITY;
+        }
+    }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int v = v0 + c + 32 * h;
@@ -405,6 +422,18 @@ __device__ __forceinline__ void probs_epilogue(const LossParams& p, const Job& j
           if (!counted || v + i >= p.v_len) x[h][i] = 0.0f;
       }
     }
+    if (some) {
+      uint64_t sum[4] = {0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < 64; i += 2) sum[i / 2 % 4] = add_pair(sum[i / 2 % 4], pair_of(x[i / 32][i % 32], x[i / 32][i % 32 + 1]));
+      float a, b;
+      halves_of(add_pair(add_pair(sum[0], sum[1]), add_pair(sum[2], sum[3])), a, b);
+      if (row < certain) {
+        float* to = p.others + ((int64_t)((p.v0 + v0) / kCols) * p.g_group + (j.r - p.r0)) * p.rows_pad + row;
+        *to = c ? *to + (a + b) : a + b;
+      }
+    }
+    if (CERTAIN && p.sums_only) continue;
     // each term goes out, and what it leaves of each value stays in its place for the next
     for (int term = 0; term < p.g_terms; ++term) {
 #pragma unroll
@@ -488,7 +517,7 @@ struct Shared {             // behind the stages and the readers' staging
   alignas(16) Job job[kTileSlots];
   uint32_t tmem;
   int failed;
-  int count[HDET_MAX_REPLICAS];
+  int count[HDET_MAX_REPLICAS], certain[HDET_MAX_REPLICAS];
 };
 
 constexpr int kGemmSmem = 1024 + kStages * kStageBytes + kReaders * kStagingBytes + (int)sizeof(Shared);
@@ -542,7 +571,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
   }
   if (warp == 1) tmem_alloc<CTAS>(bulk::smem_addr(&sh.tmem), 2 * 128 * CTAS);
   wait_for_previous();
-  if (threadIdx.x < p.n_replicas) sh.count[threadIdx.x] = p.count[threadIdx.x];
+  if (threadIdx.x < p.n_replicas) {
+    sh.count[threadIdx.x] = p.count[threadIdx.x];
+    if constexpr (PHASE == kGiven) sh.certain[threadIdx.x] = p.certain ? p.certain[threadIdx.x] : 0;
+  }
   fence_before_sync();
   __syncthreads();
   if constexpr (CTAS == 2) cluster_sync();       // the peer's barriers exist before anything arrives there
@@ -586,7 +618,15 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
   const auto a_mn = [&](const Job& j) { return PHASE == kGrads && j.is_dw; };
   constexpr bool b_mn = PHASE == kGrads;
 
-  if (warp == 0) {
+  // no row is certain: the launch hands its numbers back, and nothing waits
+  bool idle = PHASE == kGiven && p.sums_only;
+  if constexpr (PHASE == kGiven) {
+    if (idle)
+      for (int r = 0; r < p.n_r; ++r) idle = idle && sh.certain[p.r0 + r] == 0;
+  }
+  if (idle) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) atomicAdd(&p.control->ticket, (unsigned)p.jobs);
+  } else if (warp == 0) {
     {
       int kb = 0, s = 0;                         // stages filled so far, the next stage
       uint32_t parity = 0;                       // of the ring's present round
@@ -759,9 +799,14 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
       if constexpr (SUMS) from.acc = &acc;
       if constexpr (PHASE == kStats) stats_epilogue(p, j, from, row, half, target);
       else if constexpr (PHASE == kNumerators) numerators_epilogue(p, j, from, row, half, target, staging, lane);
-      else if constexpr (PHASE == kProbs || PHASE == kGiven)
-        probs_epilogue<CTAS, PHASE>(p, j, from, row, half, row < sh.count[j.r], target, norm, staging, lane);
-      else grads_epilogue(p, j, from, row, half, sh.count[j.r], staging, lane);
+      else if constexpr (PHASE == kProbs || PHASE == kGiven) {
+        // Two forms, since the second's few branches make the first 6 % longer; in the second's place alone where sums leave no registers for both
+        // (1232 bytes spilled).
+        if (PHASE == kGiven && (SUMS || __any_sync(0xffffffffu, row < sh.certain[j.r])))
+          probs_epilogue<CTAS, PHASE, SUMS, PHASE == kGiven>(p, j, from, row, half, row < sh.count[j.r], sh.certain[j.r], target, norm, staging, lane);
+        else
+          probs_epilogue<CTAS, PHASE, SUMS, false>(p, j, from, row, half, row < sh.count[j.r], 0, target, norm, staging, lane);
+      } else grads_epilogue(p, j, from, row, half, sh.count[j.r], staging, lane);
       if constexpr (!SUMS) {
         if (j.k_blocks > 0) acc_done();
       }
@@ -1065,6 +1110,39 @@ __global__ void __launch_bounds__(256) join_hidden_kernel(const __grid_constant_
   }
 }
 
+// After G from given gradients: the likely classes' entries.  32 rows a block, a lane each, whose sums the block's warps share.
+__global__ void __launch_bounds__(1024) likely_kernel(const __grid_constant__ LossParams p) {
+  __shared__ float s_sum[32][33];
+  let_next_start();
+  wait_for_previous();
+  const int r = p.r0 + blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = blockIdx.x * 32 + lane, certain = p.certain[r];
+  if (blockIdx.x * 32 >= certain) return;
+  // below 0: in an earlier piece, or not found
+  const int v = row < certain ? p.likely[(int64_t)r * p.rows_pad + row] - p.v0 : -1;
+  const bool here = v >= 0 && v < p.v_len;
+  const int64_t in_group = (int64_t)blockIdx.y * p.rows_pad + row, all = (int64_t)p.g_group * p.rows_pad;
+  float sum = 0.0f;
+  if (here) {
+#pragma unroll 8
+    for (int i = warp; i < p.n_parts; i += 32) sum += p.others[i * all + in_group];
+  }
+  s_sum[warp][lane] = sum;
+  __syncthreads();
+  sum = s_sum[lane][warp];                         // a warp a row
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  __syncthreads();
+  if (lane == 0) s_sum[0][warp] = sum;
+  __syncthreads();
+  if (warp != 0 || !here) return;
+  float left = -s_sum[0][lane];
+  for (int term = 0; term < p.g_terms; ++term) {
+    const __nv_bfloat16 g = __float2bfloat16_rn(left);
+    p.g[(term * all + in_group) * p.v_pitch + v] = g;
+    left -= __bfloat162float(g);
+  }
+}
+
 // After the gradients for given ones, which have no losses that could tell: if a wait ran out, the gradients' first elements do.
 __global__ void __launch_bounds__(32) poison_grads_kernel(const __grid_constant__ LossParams p) {
   wait_for_previous();
@@ -1169,7 +1247,7 @@ struct Plan {
   int64_t n_pieces, h_len, h_splits;
   bool h_slabs;
   bool pack_table;
-  int64_t off_count, off_target, off_token, off_z, off_norm, off_part, off_loss, off_hidden, off_table, off_g,
+  int64_t off_count, off_target, off_token, off_z, off_norm, off_part, off_loss, off_certain, off_likely, off_others, off_hidden, off_table, off_g,
       off_slabs, total;
 };
 
@@ -1251,6 +1329,10 @@ Plan plan_of(const hdet_token_loss_args* d, bool given) {
     // room for either kernel's parts: which one runs depends on the hidden states' address, and the size does not
     q.off_part = take(8 * R * std::max(2 * q.n_tiles, !q.grads && T <= kFew ? few_parts : 0) * q.rows_pad);
     q.off_loss = take(4 * R * q.rows_pad);
+  } else if (q.grads) {
+    q.off_certain = take(4 * R);
+    q.off_likely = take(4 * R * q.rows_pad);
+    q.off_others = take(4 * q.group * q.rows_pad * 2 * q.n_tiles);
   }
   q.off_hidden = take(2 * R * q.rows_pad * q.packed_row);
   if (q.pack_table) q.off_table = take(2 * (d->n_replicas > 1 && d->weight_stride ? R : 1) * V * q.packed_row);
@@ -1378,6 +1460,10 @@ int token_loss(const char* who, const hdet_token_loss_args* d, const ScoreGiven*
     p.z_target = reinterpret_cast<float*>(ws + q.off_z);
     p.part = reinterpret_cast<float2*>(ws + q.off_part);
     p.row_loss = reinterpret_cast<float*>(ws + q.off_loss);
+  } else if (given->d_entropy.p) {
+    p.certain = reinterpret_cast<int*>(ws + q.off_certain);
+    p.likely = reinterpret_cast<int*>(ws + q.off_likely);
+    p.others = reinterpret_cast<float*>(ws + q.off_others);
   }
   p.token_loss = static_cast<float*>(d->token_loss);
   p.token_loss_stride = many ? d->token_loss_stride : 0;
@@ -1426,6 +1512,8 @@ int token_loss(const char* who, const hdet_token_loss_args* d, const ScoreGiven*
   if (given) {
     ScoreGiven g = *given;
     g.norm = const_cast<RowNorm*>(p.norm);
+    g.certain = const_cast<int*>(p.certain);
+    g.likely = p.likely;
     e = launch(pack_kernel<kPackGiven, ScoreGiven>, pack_grid, 256, 0, 1, st, k, (int)pack_rows, g);
   } else {
     e = launch(pack_kernel<kPackLoss, int>, pack_grid, 256, 0, 1, st, k, (int)pack_rows, 0);
@@ -1468,19 +1556,36 @@ int token_loss(const char* who, const hdet_token_loss_args* d, const ScoreGiven*
     p.h_slabs = q.h_slabs;
     p.h_splits = (int)q.h_splits; p.h_len = (int)q.h_len;
     p.h_tiles_m = (int)q.m_tiles; p.h_tiles_n = p.w_tiles_n = (int)div_up(d->width, q.tile);
+    const auto take_piece = [&](int64_t piece) {
+      p.v0 = (int)(piece * q.piece);
+      p.v_len = (int)(d->vocab - p.v0 < q.piece ? d->vocab - p.v0 : q.piece);
+      p.n_tiles = (int)div_up(p.v_len, q.tile);
+    };
     for (int64_t r0 = 0; r0 < d->n_replicas; r0 += q.group) {
       p.r0 = (int)r0;
       p.n_r = (int)(d->n_replicas - r0 < q.group ? d->n_replicas - r0 : q.group);
+      // The likely classes' entries need the others of the whole vocabulary: with more than one piece, the certain rows' logits are formed once more
+      // (2 x 2048 tokens x 50257 of width 768, fp32 gradients in two pieces, 60 % of the rows certain: 2.15 -> 2.50 ms).
+      if (p.certain && any && q.n_pieces > 1) {
+        p.sums_only = true;
+        p.count = p.certain;
+        for (int64_t piece = 0; e == cudaSuccess && piece < q.n_pieces; ++piece) {
+          take_piece(piece);
+          e = launch_gemm<kGiven>(p, q.ctas, (int64_t)p.n_r * p.m_tiles * p.n_tiles, sms, st);
+        }
+        p.sums_only = false;
+        p.count = k.count;
+        if (e != cudaSuccess) return fail_cuda(who, e);
+      }
       for (int64_t piece = 0; piece < q.n_pieces; ++piece) {
-        p.v0 = (int)(piece * q.piece);
-        p.v_len = (int)(d->vocab - p.v0 < q.piece ? d->vocab - p.v0 : q.piece);
-        p.n_tiles = (int)div_up(p.v_len, q.tile);
+        take_piece(piece);
         p.w_tiles_m = d->d_weight ? p.n_tiles : 0;
         p.h_jobs = d->d_hidden && any ? p.h_splits * p.n_r * p.h_tiles_m * p.h_tiles_n : 0;
         p.h_add = piece > 0;
         const int64_t tiles = (int64_t)p.n_r * p.m_tiles * p.n_tiles;
         if (given) {
           if (any) e = launch_gemm<kGiven>(p, q.ctas, tiles, sms, st);
+          if (e == cudaSuccess && any && p.certain) e = launch(likely_kernel, dim3((unsigned)(q.rows_pad / 32), p.n_r), 1024, 0, 1, st, p);
         } else if (!q.numerators) {
           if (any) e = launch_gemm<kProbs>(p, q.ctas, tiles, sms, st);
         } else {
@@ -1563,7 +1668,7 @@ extern "C" HDET_API int hdet_token_scores_grad(const hdet_token_scores_args* d, 
   const auto per_token = [&](const void* p, int64_t stride) { return PerToken<const float>{static_cast<const float*>(p), many ? stride : 0}; };
   const ScoreGiven given{per_token(d->lse, d->lse_stride), per_token(d->targets ? d->logprob : nullptr, d->logprob_stride),
                          per_token(d->entropy, d->entropy_stride), per_token(d->d_logprob, d->d_logprob_stride),
-                         per_token(d->d_entropy, d->d_entropy_stride), nullptr};
+                         per_token(d->d_entropy, d->d_entropy_stride), nullptr, nullptr, nullptr};
   const hdet_token_loss_args a = loss_args(d);
   return token_loss(who, &a, &given, workspace, workspace_bytes, stream, false);
 }

@@ -223,15 +223,32 @@ struct ScoreOut {
 
 // What hdet_token_scores_grad is given: with a and b the gradients of a token's log probability and entropy H, and lp = z - lse the
 // logarithms of the probabilities p,  G = a (onehot - p) - b p (lp + H).
+//
+// Where one class has nearly all of the probability, its lp and H are both near zero, and lp from fp32 logits and an fp32 lse has none of its digits
+// left: of d_entropy alone such rows' gradients were 5 to 10 % off at 1 - p of 1e-8 to 1e-12, and up to 2e6 times their value where the logits are
+// formed in another order than before.  A row of G adds up to nothing, so that class's entry is less the sum of the others, none of which is
+// near zero in that way.  Rows with an entropy below kCertainEntropy are treated so: they have a class
+// with a probability of at least exp(-0.25) = 0.78.  Where that is the given token nothing is to do, its own logarithm being given.
+constexpr float kCertainEntropy = 0.25f;
+constexpr float kLikely = -0.6931472f;             // a class with a larger lp is that class: no other has more than exp(-1.5)
+
 struct ScoreGiven {
   PerToken<const float> lse, logprob, entropy, d_logprob, d_entropy;
   RowNorm* norm;
-  __device__ __forceinline__ RowNorm of(int r, int64_t t) const {
+  int* certain;             // per replica: so many rows are such rows; they are packed before the others.  NULL without d_entropy
+  int* likely;              // per row: the class, -1 until it is found
+  __device__ __forceinline__ bool is_certain(int r, int64_t t) const {
+    if (!certain) return false;
+    const float b = d_entropy.at(r, t), h = entropy.at(r, t), lp = logprob.p ? logprob.at(r, t) : -INFINITY;
+    return (b != 0.0f) & (h < kCertainEntropy) & !(lp > kLikely);      // (no branch, so that the loads go together)
+  }
+  __device__ __forceinline__ void row(int64_t row, int r, int64_t t) const {
     const float a = d_logprob.p ? d_logprob.at(r, t) : 0.0f, b = d_entropy.p ? d_entropy.at(r, t) : 0.0f;
-    const float h = entropy.p && d_entropy.p ? entropy.at(r, t) : 0.0f, lp = logprob.p ? logprob.at(r, t) : 0.0f;
+    const float h = entropy.p && d_entropy.p ? entropy.at(r, t) : 0.0f, lp = logprob.p ? logprob.at(r, t) : -INFINITY;
     const float p = expf(lp);
     // 1 - p of a likely target from its logarithm, not as a difference
-    return RowNorm{lse.at(r, t), fmaf(b, h, a), -a * expm1f(lp) - (p > 0.0f ? b * p * (lp + h) : 0.0f), b};
+    norm[row] = RowNorm{lse.at(r, t), fmaf(b, h, a), -a * expm1f(lp) - (p > 0.0f ? b * p * (lp + h) : 0.0f), b};
+    if (likely) likely[row] = -1;
   }
 };
 
@@ -256,7 +273,8 @@ __device__ __forceinline__ int target_of(const PackParams& p, int r, int t) {
 // own for the offsets.
 template <PackFor FOR, typename More>
 __global__ void __launch_bounds__(256) pack_kernel(const PackParams p, int rows, const More more) {
-  __shared__ int s_before[8], s_all[8];
+  constexpr bool kTwo = FOR == kPackGiven;         // rows of one kind before those of the other
+  __shared__ int s_before[8], s_all[8], s_before_first[8], s_all_first[8];
   const int r = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int t0 = (int)blockIdx.x * rows, t1 = min(t0 + rows, p.n_tokens);
   let_next_start();
@@ -265,29 +283,58 @@ __global__ void __launch_bounds__(256) pack_kernel(const PackParams p, int rows,
     p.control->done[r] = 0;
     if (r == 0) p.control->status = p.control->ticket = 0;
   }
-  int before = 0, all = 0;
+  const auto is_first = [&](int t) {
+    if constexpr (kTwo) return more.is_certain(r, t);
+    else return false;
+  };
+  int before = 0, all = 0, before_first = 0, all_first = 0;        // counted tokens, and those of the first kind among them
 #pragma unroll 4
   for (int t = threadIdx.x; t < p.n_tokens; t += 256) {
     const int one = target_of(p, r, t) >= 0;
     all += one;
     before += t < t0 ? one : 0;
+    if constexpr (kTwo) {
+      const int first = is_first(t) ? one : 0;
+      all_first += first;
+      before_first += t < t0 ? first : 0;
+    }
   }
   before = __reduce_add_sync(0xffffffffu, before);
   all = __reduce_add_sync(0xffffffffu, all);
   if (lane == 0) { s_before[warp] = before; s_all[warp] = all; }
+  if constexpr (kTwo) {
+    before_first = __reduce_add_sync(0xffffffffu, before_first);
+    all_first = __reduce_add_sync(0xffffffffu, all_first);
+    if (lane == 0) { s_before_first[warp] = before_first; s_all_first[warp] = all_first; }
+  }
   __syncthreads();
-  before = all = 0;
+  before = all = before_first = all_first = 0;
 #pragma unroll
-  for (int w = 0; w < 8; ++w) { before += s_before[w]; all += s_all[w]; }
+  for (int w = 0; w < 8; ++w) {
+    before += s_before[w];
+    all += s_all[w];
+    if constexpr (kTwo) {
+      before_first += s_before_first[w];
+      all_first += s_all_first[w];
+    }
+  }
+  before += all_first - before_first;              // the place of the block's first token of the second kind
   const int64_t base = (int64_t)r * p.rows_pad;
-  if (blockIdx.x == 0 && threadIdx.x == 0) p.count[r] = all;
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    p.count[r] = all;
+    if constexpr (kTwo) {
+      if (more.certain) more.certain[r] = all_first;
+    }
+  }
   // 32 tokens at a time: every warp finds out where they go, and moves every eighth
   for (int first = t0; first < t1; first += 32) {
     const int mine = first + lane;
     const int y = mine < t1 ? target_of(p, r, mine) : -1;
-    const unsigned counted = __ballot_sync(0xffffffffu, y >= 0);
-    const int place = before + __popc(counted & ((1u << lane) - 1));
-    before += __popc(counted);
+    const unsigned counted = __ballot_sync(0xffffffffu, y >= 0), below = (1u << lane) - 1;
+    const unsigned first_kind = kTwo ? __ballot_sync(0xffffffffu, y >= 0 && is_first(mine)) : 0u;
+    const int place = first_kind >> lane & 1 ? before_first + __popc(first_kind & below) : before + __popc(counted & ~first_kind & below);
+    before += __popc(counted & ~first_kind);
+    before_first += __popc(first_kind);
     if (warp == 0 && mine < t1) {
       if (y >= 0) {
         p.target[base + place] = FOR == kPackLoss || p.targets ? y : -1;
@@ -295,7 +342,7 @@ __global__ void __launch_bounds__(256) pack_kernel(const PackParams p, int rows,
         if constexpr (FOR == kPackScores) {
           if (more.floor) more.floor[base + place] = kNoFloor;
         }
-        if constexpr (FOR == kPackGiven) more.norm[base + place] = more.of(r, mine);
+        if constexpr (FOR == kPackGiven) more.row(base + place, r, mine);
       } else if constexpr (FOR == kPackScores) {
         more.padding(r, mine);
       } else if (p.token_loss) {
