@@ -30,7 +30,6 @@ constexpr int kStageBytes = 2 * kOperandBytes;
 // columns each
 constexpr int kScoreThreads = 384, kFirstReader = 4, kReaders = 8, kReaderThreads = 32 * kReaders;
 constexpr int kMaxStages = 6;
-constexpr float kLn2 = 0.69314718055994531f;
 constexpr int kMargin = 4;                 // classes kept beyond n_top: as many could be out of order by the fp32 logits
 constexpr int kMaxList = HDET_MAX_TOP + kMargin;
 constexpr int kShort = 16, kLong = 32;     // a reader's list has one of these lengths
@@ -104,7 +103,7 @@ struct State {
   __device__ __forceinline__ void raise(float to) {
     const float d = top - to, f = exp_from(top, to), all = ties + others;
     if (all != 0.0f) {                     // (not for the first value, where top is -inf)
-      weighted = f * fmaf(all, d, weighted);
+      weighted = f * fmaf(all, fmaxf(d, -1e4f), weighted);           // (where f is 0, so is that, however far apart the two are)
       others = f * all;
     }
     top = to;
@@ -480,25 +479,26 @@ __device__ __forceinline__ void take_logits(const ScoreParams& p, float (&x)[32]
   if (__any_sync(0xffffffffu, top >= s.top && top > -INFINITY)) {
     if (top > s.top) s.raise(top);
     const float m = s.top > -INFINITY ? s.top : NAN;       // equal to nothing
+    const float gone = m > -1e37f ? -1e38f : -INFINITY;    // exp of it is 0, and so is 0 times it (-inf: below)
     float n = 0.0f;
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
       const bool is = x[i] == m;
       n += is ? 1.0f : 0.0f;
-      x[i] = is ? -1e38f : x[i];                   // exp of it is 0, and so is 0 times it
+      x[i] = is ? gone : x[i];
     }
     s.ties += n;
   }
   const float from = s.top > -INFINITY ? s.top : 0.0f;     // nothing finite yet: exp of -inf, not of NaN
-  // Two columns an instruction where there is one for it.  The exponent x log2(e) - M log2(e) has the second product rounded, which is off by
-  // up to 2^-24 of M for all columns: of delta that is a relative error, since the maximum itself is not in it.
-  const uint64_t scale = pair_of(kLog2e, kLog2e), shift = pair_of(-from * kLog2e, -from * kLog2e);
+  // Two columns an instruction where there is one for it.  The subtraction comes first, as in the loss: in one fma with M log2(e) the rounding of that
+  // product is an error of delta that grows with the logits (1e-4 at 2000), and at the ends of the range it is no number.
+  const uint64_t scale = pair_of(kLog2e, kLog2e), top2 = pair_of(-from, -from);
   uint64_t e2[2] = {0, 0}, u2[2] = {0, 0};
 #pragma unroll
   for (int i = 0; i < 32; i += 2) {
-    const uint64_t d = fma_pair(pair_of(x[i], x[i + 1]), scale, shift);
+    const uint64_t d = add_pair(pair_of(x[i], x[i + 1]), top2);
     float a, b;
-    halves_of(d, a, b);
+    halves_of(mul_pair(d, scale), a, b);
     const uint64_t y = pair_of(exp2_fast(a), exp2_fast(b));
     e2[i / 2 % 2] = add_pair(e2[i / 2 % 2], y);
     u2[i / 2 % 2] = fma_pair(y, d, u2[i / 2 % 2]);
@@ -508,16 +508,16 @@ __device__ __forceinline__ void take_logits(const ScoreParams& p, float (&x)[32]
   e += more;
   halves_of(add_pair(u2[0], u2[1]), u, more);
   u += more;
-  if (__any_sync(0xffffffffu, u != u && e == e)) {         // logits of -inf: 0 times them is to be 0, not NaN
+  if (__any_sync(0xffffffffu, u != u && e == e)) {         // differences of -inf: 0 times them is to be 0, not NaN
     u = 0.0f;
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
-      const float d = fmaf(x[i], kLog2e, -from * kLog2e);
-      u = fmaf(exp2_fast(d), fmaxf(d, -1e38f), u);
+      const float d = x[i] - from;
+      u = fmaf(exp2_fast(d * kLog2e), fmaxf(d, -1e4f), u);
     }
   }
   s.others += e;
-  s.weighted = fmaf(u, kLn2, s.weighted);
+  s.weighted += u;
 }
 
 // Tiles of (128 * CTAS) x (128 * CTAS) by a resident CTA (or pair): copies, products and readers each go through the same runs, with a ring
