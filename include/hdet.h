@@ -22,7 +22,7 @@
  *   hdet_grad_norm / hdet_set_clip   the replicas' global gradient norms; steps with clipped gradients
  *   hdet_plan_tiles        host-only view of the work plan (tests, tools)
  *   hdet_selftest_bounded_wait   makes a kernel's bounded wait run out, to show the timeout status
- *   hdet_selftest_token_loss_wait   the same in the token loss
+ *   hdet_selftest_token_loss_wait, _token_scores_wait, _token_scores_grad_wait   the same in the token loss, the scores and their gradient
  * and where the replicas' models meet their vocabulary (no handle needed):
  *   hdet_embed / hdet_embed_grad   embedding lookup with scaling, and the table's gradient
  *   hdet_token_loss                softmax cross entropy against the table, one mean per replica (the losses that
@@ -658,6 +658,13 @@ HDET_API int hdet_token_scores_grad(const hdet_token_scores_args* d, void* works
  * Errors: as hdet_token_scores, plus UNSUPPORTED (no kernel of this call waits).
  */
 HDET_API int hdet_selftest_token_scores_wait(const hdet_token_scores_args* d, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * hdet_selftest_token_scores_grad_wait -- (a diagnostic, too.)  hdet_token_scores_grad with waits of about 2 ms and tiles withheld, so that
+ * the waits for them run out: the first element of every replica's gradients becomes NaN.
+ * Errors: as hdet_token_scores_grad.
+ */
+HDET_API int hdet_selftest_token_scores_grad_wait(const hdet_token_scores_args* d, void* workspace, int64_t workspace_bytes, void* stream);
 
 /* hdet_last_error -- text of the last failure on h (when h is NULL: of the last failed call
  * that has no handle, hdet_create, hdet_converge_static or a call of the vocabulary ends, on this thread).  The pointer stays valid until the next call on that handle. */

@@ -181,7 +181,7 @@ def _load() -> C.CDLL:
         f.argtypes = [C.c_void_p, C.POINTER(C.c_int64)]
         f.restype = C.c_int
     for f in (lib.hdet_token_loss, lib.hdet_selftest_token_loss_wait, lib.hdet_token_scores, lib.hdet_token_scores_grad,
-              lib.hdet_selftest_token_scores_wait):
+              lib.hdet_selftest_token_scores_wait, lib.hdet_selftest_token_scores_grad_wait):
         f.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]
         f.restype = C.c_int
     for f in ("hdet_create", "hdet_set_schedule", "hdet_step", "hdet_converge", "hdet_autolr_update",
@@ -688,6 +688,16 @@ def hdet_token_scores_grad(hidden, weight, targets, workspace, lse, logprob=None
     status = _lib.hdet_token_scores_grad(a, ptr, size, stream)
     if status:
         _check(status, None)
+
+
+def hdet_selftest_token_scores_grad_wait(hidden, weight, targets, workspace, lse, logprob=None, entropy=None, d_logprob=None, d_entropy=None,
+                                         d_hidden=None, d_weight=None, accumulate: bool = False, piece_bytes: int = 0, stream: int = 0) -> None:
+    """hdet_token_scores_grad whose kernels' waits run out after some milliseconds: the first element of every replica's gradients is NaN."""
+    n = _scores_replicas(hidden, weight, targets, d_hidden, d_weight)
+    a = _token_scores_args(hidden, weight, targets, n, logprob, entropy, lse, d_logprob=d_logprob, d_entropy=d_entropy, d_hidden=d_hidden,
+                           d_weight=d_weight, accumulate=accumulate, piece_bytes=piece_bytes, read=True)
+    ptr, size = _workspace(workspace, hidden.get_device())
+    _check(_lib.hdet_selftest_token_scores_grad_wait(a, ptr, size, stream), None)
 
 
 def _workspace(workspace, device: int):

@@ -93,7 +93,7 @@ struct LossParams {
   int chunk;                // steps of 64 that the tensor core sums before a reader takes them over
   unsigned first_ticket;    // Control::ticket when it starts
   long long wait_limit;     // of every wait, in cycles; twice that where one waits for whole tiles
-  bool withhold;            // hands no tile over, so that the waits for it run out (hdet_selftest_token_loss_wait)
+  bool withhold;            // hands no tile over, so that the waits for it run out (hdet_selftest_token_loss_wait, _token_scores_grad_wait)
 };
 
 __device__ __forceinline__ void poison_loss(const LossParams& p) {
@@ -1659,8 +1659,9 @@ extern "C" HDET_API int hdet_token_scores_grad_workspace(const hdet_token_scores
   return HDET_OK;
 }
 
-extern "C" HDET_API int hdet_token_scores_grad(const hdet_token_scores_args* d, void* workspace, int64_t workspace_bytes, void* stream) {
-  const char* who = "hdet_token_scores_grad";
+namespace {
+
+int token_scores_grad(const char* who, const hdet_token_scores_args* d, void* workspace, int64_t workspace_bytes, void* stream, bool selftest) {
   TraceRange trace(who);
   if (const int rc = check_token_scores(who, d, true)) return rc;
   if (const int rc = check_token_scores_pointers(who, d, true)) return rc;
@@ -1670,5 +1671,15 @@ extern "C" HDET_API int hdet_token_scores_grad(const hdet_token_scores_args* d, 
                          per_token(d->entropy, d->entropy_stride), per_token(d->d_logprob, d->d_logprob_stride),
                          per_token(d->d_entropy, d->d_entropy_stride), nullptr, nullptr, nullptr};
   const hdet_token_loss_args a = loss_args(d);
-  return token_loss(who, &a, &given, workspace, workspace_bytes, stream, false);
+  return token_loss(who, &a, &given, workspace, workspace_bytes, stream, selftest);
+}
+
+}  // namespace
+
+extern "C" HDET_API int hdet_token_scores_grad(const hdet_token_scores_args* d, void* workspace, int64_t workspace_bytes, void* stream) {
+  return token_scores_grad("hdet_token_scores_grad", d, workspace, workspace_bytes, stream, false);
+}
+
+extern "C" HDET_API int hdet_selftest_token_scores_grad_wait(const hdet_token_scores_args* d, void* workspace, int64_t workspace_bytes, void* stream) {
+  return token_scores_grad("hdet_selftest_token_scores_grad_wait", d, workspace, workspace_bytes, stream, true);
 }
