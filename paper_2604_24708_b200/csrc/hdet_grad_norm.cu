@@ -34,13 +34,17 @@ __device__ __forceinline__ float one(const __nv_bfloat16* p) {
 }
 
 // Squares are added in fp32 over 16 bytes and in fp64 from there on.  Where an fp32 square could leave its range (gradients above 1e15
-// or, all of them, below 1e-15) those 16 bytes are taken in fp64.
+// or, all of them, below 1e-15) those 16 bytes are taken in fp64, but for zeros: a table's rows without tokens are full of them.
 template <int kN>
 __device__ __forceinline__ double squares(const float (&g)[kN]) {
   float s = 0.0f;
 #pragma unroll
   for (int i = 0; i < kN; ++i) s = fmaf(g[i], g[i], s);
   if (s >= 1e-30f && s <= 1e30f) return (double)s;
+  unsigned bits = 0;
+#pragma unroll
+  for (int i = 0; i < kN; ++i) bits |= __float_as_uint(g[i]);
+  if (bits << 1 == 0) return 0.0;                  // (-0, too)
   double d = 0.0;
 #pragma unroll
   for (int i = 0; i < kN; ++i) d += (double)g[i] * (double)g[i];
