@@ -43,10 +43,9 @@ class TiedTable:
                                                     piece_bytes=piece_bytes))
             if scores and d_hidden is not None:
                 need.append(B.hdet_token_scores_grad_workspace(rows, self.weight, tokens, d_hidden=d_hidden, d_weight=self.grad, piece_bytes=piece_bytes))
-        if scores:
-            # fewer alternatives can need more: with short lists more of the logits are kept
-            need += [B.hdet_token_scores_workspace(rows, self.weight, tokens, n_top=k) for k in range(min(n_top, vocab) + 1)]
         self.n_top = min(n_top, vocab) if scores else -1
+        if scores:                       # fewer alternatives need no more
+            need.append(B.hdet_token_scores_workspace(rows, self.weight, tokens, n_top=self.n_top))
         # the calls follow one another on one stream, so they share one workspace
         self.workspace = torch.empty((max(need),), dtype=torch.uint8, device=dev)
         self.refresh()
