@@ -74,13 +74,15 @@ class TiedTable:
         B.hdet_token_scores(hidden, self.weight, targets, self.workspace, logprob=logprob, entropy=entropy, lse=lse, top_ids=top_ids,
                             top_logprob=top_logprob, stream=self._stream())
 
-    def scores_grad(self, hidden, targets, lse, d_hidden, logprob=None, entropy=None, d_logprob=None, d_entropy=None) -> None:
+    def scores_grad(self, hidden, targets, lse, d_hidden, logprob=None, entropy=None, d_logprob=None, d_entropy=None,
+                    accumulate: bool = False) -> None:
         """The gradients of a loss of log probabilities and entropies, given its own with respect to those and what ``scores`` left:
-        ``d_hidden`` (bfloat16 or float32), and the table's to the arena, over what was there."""
+        ``d_hidden`` (bfloat16 or float32), and the table's to the arena, over what was there or, with ``accumulate``, added to it."""
         if self.n_top < 0:
             raise ValueError("build the table with scores=True")
         B.hdet_token_scores_grad(hidden, self.weight, targets, self.workspace, lse, logprob=logprob, entropy=entropy, d_logprob=d_logprob,
-                                 d_entropy=d_entropy, d_hidden=d_hidden, d_weight=self.grad, piece_bytes=self.piece_bytes, stream=self._stream())
+                                 d_entropy=d_entropy, d_hidden=d_hidden, d_weight=self.grad, accumulate=accumulate, piece_bytes=self.piece_bytes,
+                                 stream=self._stream())
 
     def embed_grad(self, tokens, d_out) -> None:
         """Adds the lookup's gradient to the table's in the arena; call it after ``loss`` or ``scores_grad``.  (A bf16 gradient is rounded by each.)"""
