@@ -256,7 +256,7 @@ def hdet_create(cfg: hdet_config, tensors: Sequence[hdet_tensor]) -> C.c_void_p:
     h = C.c_void_p()
     status = _lib.hdet_create(C.byref(cfg), arr, len(tensors), C.byref(h))
     _check(status, None)
-    h.n_replicas = int(cfg.n_replicas)
+    h.n_replicas, h.device = int(cfg.n_replicas), int(cfg.device)
     return h
 
 
@@ -340,9 +340,9 @@ def hdet_selftest_bounded_wait(h, stream: int = 0) -> None:
 
 
 def _norms(h, norms):
-    """(pointer, dtype code) of a contiguous CUDA tensor of N float32 or float64 norms."""
-    if not norms.is_cuda or norms.shape != (h.n_replicas,) or not norms.is_contiguous():
-        raise ValueError("norms must be a contiguous CUDA tensor with one value per replica")
+    """(pointer, dtype code) of a contiguous tensor of N float32 or float64 norms on the handle's device."""
+    if not norms.is_cuda or norms.get_device() != h.device or norms.shape != (h.n_replicas,) or not norms.is_contiguous():
+        raise ValueError("norms must be a contiguous tensor on the handle's CUDA device with one value per replica")
     return norms.data_ptr(), _dtype_code[norms.dtype]
 
 
