@@ -86,7 +86,9 @@ int fail(hdet_ctx* h, int code, const std::string& msg) {
   return code;
 }
 
+// The call's own error, which does not stay behind: launches ask the runtime for its last one.
 int fail_cuda(hdet_ctx* h, const char* what, cudaError_t e) {
+  cudaGetLastError();
   return fail(h, HDET_ERR_CUDA, std::string(what) + ": " + cudaGetErrorString(e));
 }
 

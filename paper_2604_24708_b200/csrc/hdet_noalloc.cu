@@ -160,6 +160,7 @@ extern "C" HDET_API int hdet_converge_static(const hdet_tensor* tensors, int64_t
     return fail(HDET_ERR_UNSUPPORTED, "hdet_converge_static: the stream is being captured; this call copies its tables "
                                       "from temporary host memory and refuses to be recorded");
   if (e != cudaSuccess) {
+    cudaGetLastError();        // the error does not stay behind for the next call
     char msg[200];
     snprintf(msg, sizeof msg, "hdet_converge_static: %s", cudaGetErrorString(e));
     return fail(HDET_ERR_CUDA, msg);
