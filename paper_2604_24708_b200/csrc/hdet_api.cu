@@ -4,6 +4,7 @@
 #include <cmath>
 #include <cstdio>
 #include <cstring>
+#include <exception>
 #include <new>
 #include <string>
 #include <vector>
@@ -355,9 +356,30 @@ void set_handleless_error(const char* msg) { g_create_error = msg ? msg : ""; }
 
 extern "C" {
 
+// Host memory that is not there for the tables of a list is an error of the call, not an exception out of it.
+static int out_of_memory(const char* who) noexcept {
+  try {
+    return fail(nullptr, HDET_ERR_INVALID_ARG, std::string(who) + ": out of host memory");
+  } catch (...) {
+    return HDET_ERR_INVALID_ARG;
+  }
+}
+
+static int create(const hdet_config* cfg, const hdet_tensor* tensors, int64_t n_tensors, hdet_handle* out, hdet_ctx*& h);
+
 int hdet_create(const hdet_config* cfg, const hdet_tensor* tensors, int64_t n_tensors, hdet_handle* out) {
   TraceRange trace("hdet_create");
   if (out) *out = nullptr;
+  hdet_ctx* h = nullptr;
+  try {
+    return create(cfg, tensors, n_tensors, out, h);
+  } catch (const std::exception&) {      // only while nothing is allocated on the device
+    delete h;
+    return out_of_memory("hdet_create");
+  }
+}
+
+static int create(const hdet_config* cfg, const hdet_tensor* tensors, int64_t n_tensors, hdet_handle* out, hdet_ctx*& h) {
   if (!cfg || !out) return fail(nullptr, HDET_ERR_INVALID_ARG, "hdet_create: cfg and out must not be NULL");
   WorkPlan work;
   if (const int rc = plan_work(cfg, tensors, n_tensors, work)) return rc;
@@ -368,8 +390,8 @@ int hdet_create(const hdet_config* cfg, const hdet_tensor* tensors, int64_t n_te
   const bool sharded = cfg->n_replicas_global != 0;
   const int n_global = sharded ? cfg->n_replicas_global : n;
 
-  hdet_ctx* h = new (std::nothrow) hdet_ctx();
-  if (!h) return fail(nullptr, HDET_ERR_INVALID_ARG, "hdet_create: out of host memory");
+  h = new (std::nothrow) hdet_ctx();
+  if (!h) return out_of_memory("hdet_create");
   h->cfg = *cfg;
   h->n_tensors = n_tensors;
   h->n_tiles = (int)tiles.size();
@@ -442,6 +464,7 @@ int hdet_create(const hdet_config* cfg, const hdet_tensor* tensors, int64_t n_te
     if (e != cudaSuccess) {
       free_device(h);
       delete h;
+      h = nullptr;
       return fail_cuda(nullptr, "hdet_create", e);
     }
     // One CTA per tile, handed out by the hardware scheduler as SMs free up.  Measured on B200: a
@@ -459,7 +482,11 @@ int hdet_plan_tiles(const hdet_config* cfg, const hdet_tensor* tensors, int64_t 
                     int64_t* partial_offsets) {
   if (!cfg || !n_tiles) return fail(nullptr, HDET_ERR_INVALID_ARG, "hdet_plan_tiles: cfg and n_tiles must not be NULL");
   WorkPlan work;
-  if (const int rc = plan_work(cfg, tensors, n_tensors, work)) return rc;
+  try {
+    if (const int rc = plan_work(cfg, tensors, n_tensors, work)) return rc;
+  } catch (const std::exception&) {
+    return out_of_memory("hdet_plan_tiles");
+  }
   *n_tiles = (int64_t)work.tiles.size();
   if (tile_tensor && tile_index) {
     if (capacity < *n_tiles) return fail(nullptr, HDET_ERR_INVALID_ARG, "hdet_plan_tiles: capacity is smaller than the tile count");
