@@ -644,6 +644,7 @@ HDET_API int hdet_token_scores(const hdet_token_scores_args* d, void* workspace,
  * fp32 gradients), as in hdet_token_loss, and the rounding and overlap rules of its gradients hold.  What is there at padding does not count.
  * In a row with an entropy below 0.25 the likely class's entry of G is less the sum of the others (a row of G adds up to 0), so that rows
  * that are nearly certain keep the relative precision of their gradients; it needs entropies with theirs, as hdet_token_scores leaves them.
+ * p is formed with the fp32 lse, so that half a step of lse is a relative error of p.
  * If a bounded wait inside a kernel runs out, the first element of every replica's gradients is NaN and the rest undefined.
  * hdet_token_scores_grad_workspace: as hdet_token_loss_workspace.
  * Errors: INVALID_ARG (NULL where one is needed, no gradient asked for, sizes, strides or dtypes out of range, workspace NULL or too

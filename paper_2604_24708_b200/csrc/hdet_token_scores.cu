@@ -527,8 +527,8 @@ __device__ __forceinline__ void take_logits(const ScoreParams& p, float (&x)[32]
 // chunk stays in one accumulator, the next ones go to the other and are added to it by the readers, in fp32 and rounded.  The next tile starts in the
 // other one, while the readers go through this tile's sums, 32 columns at a time.  (Sums that were added up in the readers' registers left
 // too few for a list: 3.45 ms for 8 x 2048 tokens of width 2048 with 12 entries, against 2.42 without a list.)
-// Bound by the tensor cores at the power limit where there are many tokens, and by its readers beside them where alternatives are wanted: tensor cores
-// active 59 % of the cycles with 1024 tokens x 50257 of width 1024 and kept logits (101 us), 54 % with 8 x 512 tokens and lists (419 us).
+// Bound by its readers beside the tensor cores, which are active 60 % of the cycles with 1024 tokens x 50257 of width 1024 and kept logits (99 us), 54 % with
+// 8 x 512 tokens and lists (424 us); 8 x 2048 tokens without alternatives take 1.31 ms, 0.83 of the sustained rate of a plain product.
 template <int CTAS, int LENGTH>
 __global__ void __launch_bounds__(kScoreThreads, 1) scores_kernel(const __grid_constant__ ScoreParams p) {
   extern __shared__ uint8_t smem_raw[];
@@ -1146,8 +1146,9 @@ constexpr int kSms = 148;        // of a B200, for sizes that must not depend on
 // (3 x 777 tokens of a vocabulary of 4099, width 520: 56 us for the call with a warp a row, 70 with 8.)
 constexpr int64_t kFewRowsToJoin = 2 * kSms, kManyRows = 2048;
 // Logits that are kept for the join to look through, in place of lists that are held while they are formed: writing and reading them is 8 bytes
-// each, lists cost a start and the merges of a run, which are dear where runs are short.  (1024 tokens x 50257 of width 1024, 8 alternatives,
-// 51 M logits: 153 us kept, 179 with lists; 2048 tokens, 103 M: 307 and 279.)
+// each, lists cost a start and the merges of a run, which are dear where runs are short.  (1024 tokens x 50257 of width 1024, 51 M logits: 146 us
+// kept and 173 with lists for 8 alternatives, 165 and 273 for 20; 2048 tokens, 103 M: 260 and 245 for 8, 274 and 266 for 12, but 284 and 346 for 13, 310 and 398
+// for 20: for more than 12 alternatives, whose lists are longer, this is too low; 8 x 2048 tokens, 823 M: 2095 and 1450 for 8, 2218 and 1867 for 20.)
 constexpr int64_t kKeepLogits = 64ll << 20;      // 256 MB
 
 // Whether the table's boxes can be copied from where it is.
